@@ -17,8 +17,8 @@
  *     neither frees nor keeps it beyond the call.  Pointers without the suffix are
  *     host pointers.  `stream` is a cudaStream_t passed as void* (NULL = default).
  *   - Hot calls (draft_entropy, verify, update_thresholds, vanilla_verify, greedy_verify,
- *     gen_only_update, get_thresholds, reset) only enqueue kernels on `stream`: they never allocate,
- *     free or synchronise.  create/destroy/state_export/state_import/status do.
+ *     gen_only_update, token_logprob, token_logprob_grad, policy_loss, preference_loss, get_thresholds,
+ *     reset) only enqueue kernels on `stream`: they never allocate, free or synchronise.  create/destroy/state_export/state_import/status do.
  *   - Logits are row-major with contiguous vocabulary; strides are in ELEMENTS.
  *     bf16 or fp32 as fixed at create time.  Rows may start at any multiple of their element
  *     size; they are copied by the aligned 16-byte granules that hold them, so that up to 14
@@ -55,7 +55,7 @@ extern "C" {
 #define ADASD_ERR_ALIGN (-2)     /* a pointer is not aligned to its element type (4 bytes for float /
                                     int32 arrays, 2 or 4 for logits); nothing is launched */
 #define ADASD_ERR_SHAPE (-3)     /* a size, stride or window is out of range */
-#define ADASD_ERR_DTYPE (-4)     /* unknown dtype / rule */
+#define ADASD_ERR_DTYPE (-4)     /* unknown dtype / rule, or a rule the call does not work with */
 #define ADASD_ERR_CAPACITY (-5)  /* size beyond a stated maximum */
 #define ADASD_ERR_CUDA (-7)      /* a CUDA runtime call failed */
 #define ADASD_ERR_DEVICE (-9)    /* the calling thread's current device is not the context's device */
@@ -293,6 +293,123 @@ int adasd_vanilla_verify_static(int32_t B, int32_t V, int32_t Kmax, int32_t dtyp
                                 const float* u_resample_dev, int32_t* accept_len_dev,
                                 int32_t* next_token_dev, float* alpha_out_dev,
                                 uint32_t* status_out_dev, void* stream);
+
+/*
+ * ---- Scoring and training on given tokens ---------------------------------------------------
+ *
+ * What a user does with generated sequences next: log-probs of their tokens, and losses made of
+ * them with the gradient with respect to the logits.  (The paper has no counterpart.  Tokens
+ * that adaptive verification accepts are not distributed as the target's samples, so that
+ * training on them needs the ratio of the two models' probabilities.)
+ *
+ * The four calls below take rows of logits [n_rows, V] at row_stride elements (V, element type
+ * and device are the context's; n_rows up to 2^27, 0 included: arrays of no entries may be NULL)
+ * and the token of each row:
+ *   l_r = ln softmax(z_r / T)[token_r],  H_r = entropy of softmax(z_r / T), T the temperature of
+ * adasd_set_warpers, as sampled tokens have it.  With top-k or top-p on, all four return
+ * ADASD_ERR_DTYPE: a cut distribution has no gradient at the tokens it leaves out.
+ *   - A row whose token is outside [0, V) is LEFT OUT (prompt, padding): its logits are not read,
+ *     its outputs are 0 and its row of a gradient is zeros.
+ *   - A row with a NaN, a +inf or no finite logit sets ADASD_STATUS_NAN; its outputs, every total it
+ *     enters and its row of a gradient are NaN.  A logit of -inf has probability 0 and gradient 0; as
+ *     the token's own logit it gives l = -inf, and losses what their formulas give.
+ *   - grad_logits_dev (element type of the logits, row r at r * grad_row_stride) receives dL/dz; each
+ *     element of the n_rows rows is written, what lies between rows is left as it was.  It may be
+ *     the logits themselves (same address and stride): every row is read before it is
+ *     overwritten.  Any other overlap of the two is refused (ADASD_ERR_SHAPE).
+ *   - Gradients are correctly rounded to within a unit or so of the element type; sums,
+ *     statistics and losses are held in 32 bits or more.  Results do not vary from run to run.
+ *   - These calls keep nothing in the context but the status word, so that calls of one context
+ *     may overlap on several streams, as long as their arguments do not.
+ */
+
+/* l, entropy and log-sum-exp (of z / T) of every row; each output [n_rows], entropy and lse nullable. */
+int adasd_token_logprob(adasd_ctx* ctx, const void* logits_dev, int64_t row_stride,
+                        const int32_t* tokens_dev, int32_t n_rows, float* logp_out_dev,
+                        float* entropy_out_dev, float* lse_out_dev, void* stream);
+
+/*
+ * Backward pass of adasd_token_logprob: dL/dz from grad_logp_dev [n_rows] = dL/dl and
+ * grad_entropy_dev [n_rows] = dL/dH (nullable: 0):
+ *   dL/dz_v = (dL/dl (1[v = token] - p_v) - dL/dH p_v (ln p_v + H)) / T
+ * A row for which both are 0 counts as left out.
+ */
+int adasd_token_logprob_grad(adasd_ctx* ctx, const void* logits_dev, int64_t row_stride,
+                             const int32_t* tokens_dev, int32_t n_rows, const float* grad_logp_dev,
+                             const float* grad_entropy_dev, void* grad_logits_dev,
+                             int64_t grad_row_stride, void* stream);
+
+typedef struct {
+    float clip_low, clip_high; /* the ratio is clipped to [1 - clip_low, 1 + clip_high]; both >= 0, clip_low <= 1 */
+    float kl_coef;             /* >= 0 */
+    float entropy_coef;        /* of the entropy bonus */
+    float scale;               /* factor of every loss term, as 1 / accumulation steps */
+} adasd_policy_options;
+
+/*
+ * Clipped policy loss with a KL term and an entropy bonus, and its gradient.  Per row, with advantage A:
+ *   rho = exp(l - old_logp),   r = ref_logp - l
+ *   L   = -min(rho A, clip(rho) A) + kl_coef (e^r - r - 1) - entropy_coef H
+ *   row_loss = scale weight L;  the total is the sum of the row losses
+ *   old_logp_dev   [n_rows] log-probs under the model that drew the tokens (nullable: rho = 1, the
+ *                  gradient of the policy's own samples)
+ *   ref_logp_dev   [n_rows] log-probs under a reference model (nullable when kl_coef is 0)
+ *   weight_dev     [n_rows] (nullable: 1), as 1 / rows counted, or 1 / (sequences * length).  A row of
+ *                  weight 0 counts as left out.
+ *   options        host struct
+ *   row_loss_out_dev [n_rows]; loss_out_dev [1], logp_out_dev, entropy_out_dev [n_rows], nullable;
+ *   kl_out_dev     [n_rows] e^r - r - 1, nullable (needs ref_logp_dev)
+ *   grad_logits_dev  nullable: the loss alone
+ * The branch of the minimum that holds gives the gradient; where both are equal, that of rho A.  An
+ * advantage of 0 adds nothing whatever the ratio.
+ */
+int adasd_policy_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_stride,
+                      const int32_t* tokens_dev, int32_t n_rows, const float* advantage_dev,
+                      const float* old_logp_dev, const float* ref_logp_dev, const float* weight_dev,
+                      const adasd_policy_options* options, float* row_loss_out_dev,
+                      float* loss_out_dev, float* logp_out_dev, float* entropy_out_dev,
+                      float* kl_out_dev, void* grad_logits_dev, int64_t grad_row_stride,
+                      void* stream);
+
+#define ADASD_PREF_SIGMOID 0 /* -(1 - s) ln sigma(u) - s ln sigma(-u), u = beta D - margin, s = label_smoothing */
+#define ADASD_PREF_SQUARED 1 /* (D - margin - 1 / (2 beta))^2 */
+#define ADASD_PREF_HINGE 2   /* max(0, 1 - (beta D - margin)) */
+
+typedef struct {
+    int32_t rule;          /* ADASD_PREF_* */
+    int32_t average;       /* 1: a sequence's log-prob is the mean over its rows that count, 0: the sum */
+    float beta;            /* > 0 */
+    float margin;
+    float label_smoothing; /* in [0, 1/2]; 0 with the other rules */
+    float scale;           /* factor of every pair's loss, as 1 / pairs */
+} adasd_preference_options;
+
+/* Bytes of scratch of adasd_preference_loss for a row. */
+#define ADASD_PREF_SCRATCH_PER_ROW 16
+
+/*
+ * Preference loss of n_pairs pairs of sequences, and its gradient.  Sequences are packed: rows
+ * seq_start[s] .. seq_start[s + 1] - 1 are sequence s, s = 0 .. 2 n_pairs - 1; pair i is the chosen sequence
+ * i and the rejected one n_pairs + i.  l_s = sum (or mean) of its rows' l over the rows that are not
+ * left out (0 if there are none), D = (l_chosen - ref_chosen) - (l_rejected - ref_rejected).
+ *   seq_start_dev  [2 n_pairs + 1] non-decreasing, within [0, n_rows] (values outside are clamped).
+ *                  Rows of no sequence (ahead of the first, behind the last) are not read and
+ *                  their rows of the gradient are left as they were.
+ *   ref_logp_dev   [2 n_pairs] l_s under the reference model (nullable: 0)
+ *   pair_weight_dev [n_pairs] (nullable: 1); a pair of weight 0 has loss 0 and a gradient of zeros,
+ *                  whatever its rows hold
+ *   options        host struct
+ *   scratch_dev    ADASD_PREF_SCRATCH_PER_ROW * n_rows bytes, 16-byte aligned, contents of no meaning
+ *                  between calls
+ *   seq_logp_out_dev [2 n_pairs] l_s;  pair_loss_out_dev [n_pairs] scale weight loss;  loss_out_dev [1] their
+ *                  sum, nullable;  grad_logits_dev nullable: the loss alone
+ */
+int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_stride,
+                          const int32_t* tokens_dev, int32_t n_rows, const int32_t* seq_start_dev,
+                          int32_t n_pairs, const float* ref_logp_dev, const float* pair_weight_dev,
+                          const adasd_preference_options* options, void* scratch_dev,
+                          float* seq_logp_out_dev, float* pair_loss_out_dev, float* loss_out_dev,
+                          void* grad_logits_dev, int64_t grad_row_stride, void* stream);
 
 /* Copies T_G and the list sizes |L_E^R|, |L_D^A|, |L_D^R| to caller arrays [B] (each nullable). */
 int adasd_get_thresholds(adasd_ctx* ctx, float* T_G_dev, int32_t* nE_dev, int32_t* nA_dev,

@@ -18,6 +18,8 @@ ADASD_BF16, ADASD_FP32 = 0, 1
 ADASD_FUSE_UPDATE = 1
 ADASD_KMAX_LIMIT = 32
 STATUS_CAPACITY, STATUS_TIMEOUT, STATUS_NAN = 1, 2, 4
+PREF_SIGMOID, PREF_SQUARED, PREF_HINGE = 0, 1, 2
+PREF_SCRATCH_PER_ROW = 16
 ERR_NULL, ERR_ALIGN, ERR_SHAPE, ERR_DTYPE, ERR_CAPACITY, ERR_CUDA, ERR_DEVICE = -1, -2, -3, -4, -5, -7, -9
 
 
@@ -38,6 +40,15 @@ class RoundRecord(C.Structure):
     """Host struct of device array addresses (``adasd_round_record``)."""
     _fields_ = [(n, C.c_void_p) for n in ("H_d", "H_t", "lse_d", "lse_t", "jsd", "dist", "p_acc",
                                           "y", "draft_len", "accept_len", "rejected")]
+
+
+class PolicyOptions(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("clip_low", "clip_high", "kl_coef", "entropy_coef", "scale")]
+
+
+class PreferenceOptions(C.Structure):
+    _fields_ = [("rule", C.c_int32), ("average", C.c_int32), ("beta", C.c_float), ("margin", C.c_float),
+                ("label_smoothing", C.c_float), ("scale", C.c_float)]
 
 
 def library_path() -> str:
@@ -67,6 +78,11 @@ def lib() -> C.CDLL:
         "adasd_greedy_verify": [P, P, I64, I64, P, P, P, P, P, P],
         "adasd_gen_only_update": [P, P, P, P, P],
         "adasd_selftest_expired_wait": [P, P, I64, I32, P, P, P, P],
+        "adasd_token_logprob": [P, P, I64, P, I32, P, P, P, P],
+        "adasd_token_logprob_grad": [P, P, I64, P, I32, P, P, P, I64, P],
+        "adasd_policy_loss": [P, P, I64, P, I32, P, P, P, P, C.POINTER(PolicyOptions), P, P, P, P, P, P, I64, P],
+        "adasd_preference_loss": [P, P, I64, P, I32, P, I32, P, P, C.POINTER(PreferenceOptions), P, P, P, P, P,
+                                  I64, P],
         "adasd_set_warpers": [P, C.c_float, I32, C.c_float],
         "adasd_get_thresholds": [P, P, P, P, P, P],
         "adasd_state_export": [P, I32, P, C.POINTER(C.c_size_t)],
@@ -169,6 +185,37 @@ def adasd_selftest_expired_wait(ctx, logits_dev, row_stride, row, u_dev, H_out_d
                                              stream)
 
 
+def adasd_token_logprob(ctx, logits_dev, row_stride, tokens_dev, n_rows, logp_out_dev, entropy_out_dev, lse_out_dev,
+                        stream) -> int:
+    return lib().adasd_token_logprob(ctx, logits_dev, row_stride, tokens_dev, n_rows, logp_out_dev, entropy_out_dev,
+                                     lse_out_dev, stream)
+
+
+def adasd_token_logprob_grad(ctx, logits_dev, row_stride, tokens_dev, n_rows, grad_logp_dev, grad_entropy_dev,
+                             grad_logits_dev, grad_row_stride, stream) -> int:
+    return lib().adasd_token_logprob_grad(ctx, logits_dev, row_stride, tokens_dev, n_rows, grad_logp_dev,
+                                          grad_entropy_dev, grad_logits_dev, grad_row_stride, stream)
+
+
+def adasd_policy_loss(ctx, logits_dev, row_stride, tokens_dev, n_rows, advantage_dev, old_logp_dev, ref_logp_dev,
+                      weight_dev, options, row_loss_out_dev, loss_out_dev, logp_out_dev, entropy_out_dev, kl_out_dev,
+                      grad_logits_dev, grad_row_stride, stream) -> int:
+    return lib().adasd_policy_loss(ctx, logits_dev, row_stride, tokens_dev, n_rows, advantage_dev, old_logp_dev,
+                                   ref_logp_dev, weight_dev, C.byref(options) if options is not None else None,
+                                   row_loss_out_dev, loss_out_dev, logp_out_dev, entropy_out_dev, kl_out_dev,
+                                   grad_logits_dev, grad_row_stride, stream)
+
+
+def adasd_preference_loss(ctx, logits_dev, row_stride, tokens_dev, n_rows, seq_start_dev, n_pairs, ref_logp_dev,
+                          pair_weight_dev, options, scratch_dev, seq_logp_out_dev, pair_loss_out_dev, loss_out_dev,
+                          grad_logits_dev, grad_row_stride, stream) -> int:
+    return lib().adasd_preference_loss(ctx, logits_dev, row_stride, tokens_dev, n_rows, seq_start_dev, n_pairs,
+                                       ref_logp_dev, pair_weight_dev,
+                                       C.byref(options) if options is not None else None, scratch_dev,
+                                       seq_logp_out_dev, pair_loss_out_dev, loss_out_dev, grad_logits_dev,
+                                       grad_row_stride, stream)
+
+
 def adasd_get_thresholds(ctx, T_G_dev, nE_dev, nA_dev, nR_dev, stream) -> int:
     return lib().adasd_get_thresholds(ctx, T_G_dev, nE_dev, nA_dev, nR_dev, stream)
 
@@ -217,6 +264,9 @@ class Context:
         L = lib()
         self._draft_entropy, self._verify = L.adasd_draft_entropy, L.adasd_verify
         self._vanilla_verify, self._greedy_verify = L.adasd_vanilla_verify, L.adasd_greedy_verify
+        self._token_logprob, self._token_logprob_grad = L.adasd_token_logprob, L.adasd_token_logprob_grad
+        self._policy_loss, self._preference_loss = L.adasd_policy_loss, L.adasd_preference_loss
+        self._logit_dtype = torch.bfloat16 if dtype == ADASD_BF16 else torch.float32
         self._raw_stream = torch._C._cuda_getCurrentRawStream
         self._rec = None                           # the last record's addresses and their struct
 
@@ -332,6 +382,102 @@ class Context:
     def set_warpers(self, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0) -> None:
         self._check(adasd_set_warpers(self.handle, float(temperature), int(top_k), float(top_p)),
                     "adasd_set_warpers")
+
+    # ---- scoring and training on given tokens: rows of logits [n, V], their tokens [n] ----------------
+
+    def _rows(self, where: str, logits, tokens, grad=None) -> int:
+        """The number of rows, after the checks that addresses alone do not allow."""
+        n = logits.shape[0] if logits.dim() == 2 else -1
+        for t in (logits,) if grad is None else (logits, grad):
+            if t.dim() != 2 or t.shape[0] != n or t.shape[1] != self.V or (t.stride(1) != 1 and self.V > 1):
+                raise AdasdError(ERR_SHAPE, where)
+            if t.dtype is not self._logit_dtype:
+                raise AdasdError(ERR_DTYPE, where)
+            if t.device != self.device:
+                raise AdasdError(ERR_DEVICE, where)
+        self._arrays(where, self.torch.int32, n, tokens)
+        return n
+
+    def _arrays(self, where: str, dtype, n: int, *arrays) -> None:
+        """Contiguous device arrays of at least n entries (each may be None)."""
+        for t in arrays:
+            if t is None:
+                continue
+            if t.dtype is not dtype:
+                raise AdasdError(ERR_DTYPE, where)
+            if t.numel() < n or not t.is_contiguous():
+                raise AdasdError(ERR_SHAPE, where)
+            if t.device != self.device:
+                raise AdasdError(ERR_DEVICE, where)
+
+    def _row_stride(self, t) -> int:
+        return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), self.V)   # (of a single row it says nothing)
+
+    def token_logprob(self, logits, tokens, logp_out, entropy_out=None, lse_out=None) -> None:
+        n = self._rows("adasd_token_logprob", logits, tokens)
+        self._arrays("adasd_token_logprob", self.torch.float32, n, logp_out, entropy_out, lse_out)
+        rc = self._token_logprob(self.handle, logits.data_ptr(), self._row_stride(logits), tokens.data_ptr(), n,
+                                 logp_out.data_ptr(), None if entropy_out is None else entropy_out.data_ptr(),
+                                 None if lse_out is None else lse_out.data_ptr(), self._raw_stream(self.device.index))
+        if rc:
+            raise AdasdError(rc, "adasd_token_logprob")
+
+    def token_logprob_grad(self, logits, tokens, grad_logp, grad_out, grad_entropy=None) -> None:
+        n = self._rows("adasd_token_logprob_grad", logits, tokens, grad_out)
+        self._arrays("adasd_token_logprob_grad", self.torch.float32, n, grad_logp, grad_entropy)
+        rc = self._token_logprob_grad(self.handle, logits.data_ptr(), self._row_stride(logits), tokens.data_ptr(), n,
+                                      grad_logp.data_ptr(), None if grad_entropy is None else grad_entropy.data_ptr(),
+                                      grad_out.data_ptr(), self._row_stride(grad_out),
+                                      self._raw_stream(self.device.index))
+        if rc:
+            raise AdasdError(rc, "adasd_token_logprob_grad")
+
+    def policy_loss(self, logits, tokens, advantage, row_loss_out, old_logp=None, ref_logp=None, weight=None,
+                    clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0,
+                    scale: float = 1.0, loss_out=None, logp_out=None, entropy_out=None, kl_out=None,
+                    grad_out=None) -> None:
+        where = "adasd_policy_loss"
+        n = self._rows(where, logits, tokens, grad_out)
+        self._arrays(where, self.torch.float32, n, advantage, row_loss_out, old_logp, ref_logp, weight, logp_out,
+                     entropy_out, kl_out)
+        self._arrays(where, self.torch.float32, 1, loss_out)
+        rc = self._policy_loss(self.handle, logits.data_ptr(), self._row_stride(logits), tokens.data_ptr(), n,
+                               advantage.data_ptr(), _ptr(old_logp), _ptr(ref_logp), _ptr(weight),
+                               C.byref(PolicyOptions(clip_low, clip_high, kl_coef, entropy_coef, scale)),
+                               row_loss_out.data_ptr(), _ptr(loss_out), _ptr(logp_out), _ptr(entropy_out), _ptr(kl_out),
+                               _ptr(grad_out), 0 if grad_out is None else self._row_stride(grad_out),
+                               self._raw_stream(self.device.index))
+        if rc:
+            raise AdasdError(rc, where)
+
+    def preference_loss(self, logits, tokens, seq_start, pair_loss_out, seq_logp_out, scratch, ref_logp=None,
+                        pair_weight=None, rule: str = "sigmoid", beta: float = 0.1, margin: float = 0.0,
+                        label_smoothing: float = 0.0, average: bool = False, scale: float = 1.0, loss_out=None,
+                        grad_out=None) -> None:
+        """rule: "sigmoid", "squared" or "hinge"; scratch: a device tensor of PREF_SCRATCH_PER_ROW bytes a row."""
+        where = "adasd_preference_loss"
+        n, f32 = self._rows(where, logits, tokens, grad_out), self.torch.float32
+        if seq_start.numel() % 2 == 0:
+            raise AdasdError(ERR_SHAPE, where)
+        pairs = seq_start.numel() // 2
+        self._arrays(where, self.torch.int32, 1, seq_start)
+        self._arrays(where, f32, 2 * pairs, seq_logp_out, ref_logp)
+        self._arrays(where, f32, pairs, pair_loss_out, pair_weight)
+        self._arrays(where, f32, 1, loss_out)
+        self._arrays(where, scratch.dtype, -(-PREF_SCRATCH_PER_ROW * n // scratch.element_size()), scratch)
+        if rule not in ("sigmoid", "squared", "hinge"):
+            raise AdasdError(ERR_DTYPE, where)
+        rule_id = PREF_SIGMOID if rule == "sigmoid" else PREF_SQUARED if rule == "squared" else PREF_HINGE
+        rc = self._preference_loss(self.handle, logits.data_ptr(), self._row_stride(logits), tokens.data_ptr(), n,
+                                   seq_start.data_ptr(), pairs, _ptr(ref_logp), _ptr(pair_weight),
+                                   C.byref(PreferenceOptions(rule_id, 1 if average else 0, beta, margin,
+                                                             label_smoothing, scale)),
+                                   scratch.data_ptr(), seq_logp_out.data_ptr(), pair_loss_out.data_ptr(),
+                                   _ptr(loss_out), _ptr(grad_out),
+                                   0 if grad_out is None else self._row_stride(grad_out),
+                                   self._raw_stream(self.device.index))
+        if rc:
+            raise AdasdError(rc, where)
 
     def get_thresholds(self):
         """(T_G, nE, nA, nR) as new device tensors."""

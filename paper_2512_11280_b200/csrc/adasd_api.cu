@@ -11,6 +11,7 @@
 #include <new>
 #include <type_traits>
 
+#include "adasd_launch.cuh"
 #include "adasd_rows.cuh"
 #include "adasd_cluster.cuh"
 #include "adasd_spec.cuh"
@@ -20,6 +21,7 @@
 #include "adasd_stream.cuh"
 #include "adasd_topk.cuh"
 #include "adasd_modes.cuh"
+#include "adasd_score_types.cuh"
 
 using namespace adasd;
 
@@ -59,12 +61,6 @@ struct adasd_ctx {
 };
 
 namespace {
-
-#define CUDA_TRY(expr)                         \
-    do {                                       \
-        cudaError_t e__ = (expr);              \
-        if (e__ != cudaSuccess) return ADASD_ERR_CUDA; \
-    } while (0)
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -283,34 +279,6 @@ cudaError_t stream_prepare_it() {
 }
 template <typename T, bool ALIGNED>
 cudaError_t stream_prepare(int it) { return it == 8 ? stream_prepare_it<T, ALIGNED, 8>() : stream_prepare_it<T, ALIGNED, 2>(); }
-
-// early: launch with programmatic stream serialisation: the kernel may become resident while the one ahead of
-// it is still running (it waits before it reads what that one wrote).  cs: CTAs per cluster; 0: the kernel
-// uses no cluster.  (A kernel that uses cluster-scope instructions gets the attribute even for clusters of one.)
-template <typename K, typename... Args>
-int launch_kernel(bool early, K kernel, int grid, int threads, int smem, int cs, cudaStream_t stream, const Args&... args) {
-    cudaLaunchConfig_t lc;
-    memset(&lc, 0, sizeof(lc));
-    lc.gridDim = dim3((unsigned)grid, 1, 1);
-    lc.blockDim = dim3((unsigned)threads, 1, 1);
-    lc.dynamicSmemBytes = (size_t)smem;
-    lc.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = early ? 1 : 0;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)cs;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    lc.attrs = attr;
-    lc.numAttrs = cs > 0 ? 2 : 1;
-    CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, args...));
-    return ADASD_OK;
-}
-template <typename K, typename... Args>
-int launch_pdl(K kernel, int grid, int threads, int smem, int cs, cudaStream_t stream, const Args&... args) {
-    return launch_kernel(true, kernel, grid, threads, smem, cs, stream, args...);
-}
 
 template <typename T, bool ALIGNED, int IT>
 int launch_stream_it(adasd_ctx* c, const StreamParams& p, int op, cudaStream_t stream) {
@@ -1038,6 +1006,162 @@ int adasd_gen_only_update(adasd_ctx* ctx, const float* H_draft_dev, const int32_
     return ADASD_OK;
 }
 
+// ---- scoring and training on given tokens -----------------------------------------------
+
+// Rows of logits and tokens, and the gradient's rows (nullable), of the calls below.
+static int check_rows(const adasd_ctx* ctx, const void* z, int64_t row_stride, const int32_t* tokens, int32_t n_rows, const void* grad,
+                      int64_t grad_row_stride) {
+    if (n_rows > 0 && (!z || !tokens)) return ADASD_ERR_NULL;
+    if (int rc = check_device(ctx)) return rc;
+    if (ctx->cuts_on()) return ADASD_ERR_DTYPE;
+    const int64_t es = (int64_t)elt_size(ctx->cfg.dtype), V = ctx->cfg.V;
+    if (!aligned_to(z, (size_t)es) || !aligned_to(grad, (size_t)es) || !aligned4({tokens})) return ADASD_ERR_ALIGN;
+    // (2^27 rows: a launch has a CTA or more a row; strides: byte offsets stay within 64 bits)
+    if (n_rows < 0 || n_rows > (1 << 27) || row_stride < V || row_stride > (int64_t)1 << 33) return ADASD_ERR_SHAPE;
+    if (!grad) return ADASD_OK;
+    if (grad_row_stride < V || grad_row_stride > (int64_t)1 << 33) return ADASD_ERR_SHAPE;
+    if (n_rows > 0 && !(grad == z && grad_row_stride == row_stride)) {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(z), b = reinterpret_cast<uintptr_t>(grad);
+        const uintptr_t na = (uintptr_t)(((int64_t)(n_rows - 1) * row_stride + V) * es);
+        const uintptr_t nb = (uintptr_t)(((int64_t)(n_rows - 1) * grad_row_stride + V) * es);
+        if (a < b + nb && b < a + na) return ADASD_ERR_SHAPE;
+    }
+    return ADASD_OK;
+}
+static ScoreParams score_params(const adasd_ctx* ctx, int32_t op, const void* z, int64_t row_stride, const int32_t* tokens, int32_t n_rows) {
+    ScoreParams p;
+    memset(&p, 0, sizeof(p));
+    p.op = op;
+    p.z = z;
+    p.row_stride = row_stride;
+    p.tok = tokens;
+    p.n_rows = n_rows;
+    p.V = ctx->cfg.V;
+    p.temperature = ctx->temperature;
+    p.c1 = kLog2e / ctx->temperature;
+    p.status = ctx->st.status;
+    return p;
+}
+
+int adasd_token_logprob(adasd_ctx* ctx, const void* logits_dev, int64_t row_stride, const int32_t* tokens_dev, int32_t n_rows,
+                        float* logp_out_dev, float* entropy_out_dev, float* lse_out_dev, void* stream) {
+    if (!ctx || (n_rows > 0 && !logp_out_dev)) return ADASD_ERR_NULL;
+    if (int rc = check_rows(ctx, logits_dev, row_stride, tokens_dev, n_rows, nullptr, 0)) return rc;
+    if (!aligned4({logp_out_dev, entropy_out_dev, lse_out_dev})) return ADASD_ERR_ALIGN;
+    if (n_rows == 0) return ADASD_OK;
+    ScoreParams p = score_params(ctx, SCORE_LOGPROB, logits_dev, row_stride, tokens_dev, n_rows);
+    p.logp = logp_out_dev;
+    p.H = entropy_out_dev;
+    p.lse = lse_out_dev;
+    return launch_score(p, ctx->cfg.dtype, entropy_out_dev != nullptr, ctx->sm_count, (cudaStream_t)stream);
+}
+
+int adasd_token_logprob_grad(adasd_ctx* ctx, const void* logits_dev, int64_t row_stride, const int32_t* tokens_dev, int32_t n_rows,
+                             const float* grad_logp_dev, const float* grad_entropy_dev, void* grad_logits_dev, int64_t grad_row_stride,
+                             void* stream) {
+    if (!ctx || (n_rows > 0 && (!grad_logp_dev || !grad_logits_dev))) return ADASD_ERR_NULL;
+    if (int rc = check_rows(ctx, logits_dev, row_stride, tokens_dev, n_rows, grad_logits_dev, grad_row_stride)) return rc;
+    if (!aligned4({grad_logp_dev, grad_entropy_dev})) return ADASD_ERR_ALIGN;
+    if (n_rows == 0) return ADASD_OK;
+    ScoreParams p = score_params(ctx, SCORE_GIVEN, logits_dev, row_stride, tokens_dev, n_rows);
+    p.g_logp = grad_logp_dev;
+    p.g_H = grad_entropy_dev;
+    p.grad = grad_logits_dev;
+    p.g_stride = grad_row_stride;
+    return launch_score(p, ctx->cfg.dtype, grad_entropy_dev != nullptr, ctx->sm_count, (cudaStream_t)stream);
+}
+
+int adasd_policy_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_stride, const int32_t* tokens_dev, int32_t n_rows,
+                      const float* advantage_dev, const float* old_logp_dev, const float* ref_logp_dev, const float* weight_dev,
+                      const adasd_policy_options* options, float* row_loss_out_dev, float* loss_out_dev, float* logp_out_dev,
+                      float* entropy_out_dev, float* kl_out_dev, void* grad_logits_dev, int64_t grad_row_stride, void* stream) {
+    if (!ctx || !options || (n_rows > 0 && (!advantage_dev || !row_loss_out_dev))) return ADASD_ERR_NULL;
+    const adasd_policy_options& o = *options;
+    if (!(o.clip_low >= 0.f) || o.clip_low > 1.f || !(o.clip_high >= 0.f) || !(o.kl_coef >= 0.f) || !std::isfinite(o.clip_high) ||
+        !std::isfinite(o.kl_coef) || !std::isfinite(o.entropy_coef) || !std::isfinite(o.scale))
+        return ADASD_ERR_SHAPE;
+    if (n_rows > 0 && !ref_logp_dev && (o.kl_coef != 0.f || kl_out_dev)) return ADASD_ERR_NULL;
+    if (int rc = check_rows(ctx, logits_dev, row_stride, tokens_dev, n_rows, grad_logits_dev, grad_row_stride)) return rc;
+    if (!aligned4({advantage_dev, old_logp_dev, ref_logp_dev, weight_dev, row_loss_out_dev, loss_out_dev, logp_out_dev, entropy_out_dev,
+                   kl_out_dev}))
+        return ADASD_ERR_ALIGN;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (n_rows > 0) {
+        ScoreParams p = score_params(ctx, SCORE_POLICY, logits_dev, row_stride, tokens_dev, n_rows);
+        p.adv = advantage_dev;
+        p.old_logp = old_logp_dev;
+        p.ref_logp = o.kl_coef != 0.f || kl_out_dev ? ref_logp_dev : nullptr;
+        p.weight = weight_dev;
+        p.clip_low = o.clip_low;
+        p.clip_high = o.clip_high;
+        p.kl_coef = o.kl_coef;
+        p.ent_coef = o.entropy_coef;
+        p.scale = o.scale;
+        p.row_loss = row_loss_out_dev;
+        p.logp = logp_out_dev;
+        p.H = entropy_out_dev;
+        p.kl = kl_out_dev;
+        p.grad = grad_logits_dev;
+        p.g_stride = grad_row_stride;
+        if (int rc = launch_score(p, ctx->cfg.dtype, entropy_out_dev || o.entropy_coef != 0.f, ctx->sm_count, st)) return rc;
+    }
+    return loss_out_dev ? launch_total(row_loss_out_dev, n_rows, loss_out_dev, st) : ADASD_OK;
+}
+
+int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_stride, const int32_t* tokens_dev, int32_t n_rows,
+                          const int32_t* seq_start_dev, int32_t n_pairs, const float* ref_logp_dev, const float* pair_weight_dev,
+                          const adasd_preference_options* options, void* scratch_dev, float* seq_logp_out_dev, float* pair_loss_out_dev,
+                          float* loss_out_dev, void* grad_logits_dev, int64_t grad_row_stride, void* stream) {
+    if (!ctx || !options || (n_rows > 0 && !scratch_dev)) return ADASD_ERR_NULL;
+    if (n_pairs > 0 && (!seq_start_dev || !seq_logp_out_dev || !pair_loss_out_dev)) return ADASD_ERR_NULL;
+    const adasd_preference_options& o = *options;
+    if (o.rule < ADASD_PREF_SIGMOID || o.rule > ADASD_PREF_HINGE || o.average < 0 || o.average > 1) return ADASD_ERR_DTYPE;
+    if (!(o.beta > 0.f) || !std::isfinite(o.beta) || !std::isfinite(o.margin) || !std::isfinite(o.scale) || !(o.label_smoothing >= 0.f) ||
+        o.label_smoothing > 0.5f || (o.label_smoothing != 0.f && o.rule != ADASD_PREF_SIGMOID))
+        return ADASD_ERR_SHAPE;
+    if (n_pairs < 0 || n_pairs > (1 << 27)) return ADASD_ERR_SHAPE;
+    if (int rc = check_rows(ctx, logits_dev, row_stride, tokens_dev, n_rows, grad_logits_dev, grad_row_stride)) return rc;
+    if (!aligned16(scratch_dev) || !aligned4({seq_start_dev, ref_logp_dev, pair_weight_dev, seq_logp_out_dev, pair_loss_out_dev, loss_out_dev}))
+        return ADASD_ERR_ALIGN;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (n_pairs > 0) {
+        ScoreParams s = score_params(ctx, SCORE_PREF, logits_dev, row_stride, tokens_dev, n_rows);
+        s.seq_start = seq_start_dev;
+        s.n_seqs = 2 * n_pairs;
+        s.pref = static_cast<PrefRow*>(scratch_dev);
+        if (n_rows > 0)
+            if (int rc = launch_score(s, ctx->cfg.dtype, false, ctx->sm_count, st)) return rc;
+        PrefParams p;
+        memset(&p, 0, sizeof(p));
+        p.z = logits_dev;
+        p.row_stride = row_stride;
+        p.tok = tokens_dev;
+        p.grad = grad_logits_dev;
+        p.g_stride = grad_row_stride;
+        p.n_rows = n_rows;
+        p.V = s.V;
+        p.n_pairs = n_pairs;
+        p.temperature = s.temperature;
+        p.c1 = s.c1;
+        p.seq_start = seq_start_dev;
+        p.ref_logp = ref_logp_dev;
+        p.pair_weight = pair_weight_dev;
+        p.rule = o.rule;
+        p.average = o.average;
+        p.beta = o.beta;
+        p.margin = o.margin;
+        p.label_smoothing = o.label_smoothing;
+        p.scale = o.scale;
+        p.pref = s.pref;
+        p.seq_logp = seq_logp_out_dev;
+        p.pair_loss = pair_loss_out_dev;
+        if (int rc = launch_pref_pairs(p, st)) return rc;
+        if (grad_logits_dev && n_rows > 0)
+            if (int rc = launch_pref_grad(p, ctx->cfg.dtype, st)) return rc;
+    }
+    return loss_out_dev ? launch_total(pair_loss_out_dev, n_pairs, loss_out_dev, st) : ADASD_OK;
+}
+
 int adasd_set_warpers(adasd_ctx* ctx, float temperature, int32_t top_k, float top_p) {
     if (!ctx) return ADASD_ERR_NULL;
     if (!(temperature > 0.f) || !std::isfinite(temperature)) return ADASD_ERR_SHAPE;
@@ -1236,7 +1360,7 @@ const char* adasd_strerror(int code) {
         case ADASD_ERR_NULL: return "a required pointer is NULL";
         case ADASD_ERR_ALIGN: return "a pointer is not aligned to its element type";
         case ADASD_ERR_SHAPE: return "size, stride or window out of range";
-        case ADASD_ERR_DTYPE: return "unknown dtype or rule";
+        case ADASD_ERR_DTYPE: return "unknown dtype or rule, or one the call does not work with";
         case ADASD_ERR_CAPACITY: return "size beyond a stated maximum";
         case ADASD_ERR_CUDA: return "a CUDA runtime call failed";
         case ADASD_ERR_DEVICE: return "the current device is not the context's device";

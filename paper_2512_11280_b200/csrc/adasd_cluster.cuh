@@ -4,8 +4,6 @@
 #pragma once
 
 #include "adasd_device.cuh"
-#include "adasd_rows.cuh"
-#include "adasd_tail.cuh"
 
 namespace adasd {
 

@@ -22,6 +22,7 @@
 #pragma once
 
 #include "adasd_async.cuh"
+#include "adasd_rows.cuh"
 
 namespace adasd {
 

@@ -1,0 +1,487 @@
+// Scoring and losses of given tokens for sm_100a: log-probs and entropies of rows of logits, and the gradients
+// with respect to the logits of losses made of them.
+//
+// A row z, the token x that stands there, T the temperature, m the largest logit, S = sum 2^((z - m) log2 e / T):
+//   l = (z_x - m) / T - ln S,   p_v = 2^((z_v - m) log2 e / T) / S,   H = ln S - (1/S) sum p'_v ln p'_v  (p' = S p)
+//   dL/dz_v = (dL/dl (1[v = x] - p_v) - dL/dH p_v (ln p_v + H)) / T
+// dL/dl and dL/dH hang on the row's own l and H alone (policy loss) or are given, so one launch reads a row, forms
+// its statistics and writes its gradient.  In a preference loss they hang on all rows of a pair: score_kernel leaves
+// the statistics, pref_pair_kernel forms the pairs' losses, pref_grad_kernel reads the rows again.
+//
+// score_kernel gives a row to a cluster of CTAs; a thread loads its 16-byte units into registers, and they stay
+// there between the sums and the gradient, so that a row crosses the memory once each way.  The warps' statistics go
+// to every CTA of the cluster (one barrier) and are folded by each warp in the same order.
+#pragma once
+
+#include "adasd_async.cuh"
+#include "adasd_score_types.cuh"
+
+namespace adasd {
+
+constexpr int kScMaxCluster = 8;
+constexpr float kLowT = -16384.f;          // 2^t = 0 from here down; keeps 0 * (-inf) out of the sums
+
+// A row's units of 16 bytes, aligned in the memory of the array that decides: the gradient's row where one is written
+// (so that whole units are stored at once), else the logits'.  Unit u holds elements u N - m0 .. u N - m0 + N - 1; logits that
+// lie elsewhere relative to 16 bytes are put together from two granules.
+template <typename T, bool ALIGNED>
+struct RowUnits {
+    using U = Unit<T>;
+    static constexpr int N = U::N;
+    const uint4* src;                      // granule that unit 0 starts in
+    int m0, sh;                            // elements before the row in unit 0; elements of src's granule before unit 0
+    int glo, ghi;                          // granules that hold elements of the row
+    int V, NU;
+
+    __device__ __forceinline__ RowUnits(const T* z, const T* frame, int V_) : V(V_) {
+        const unsigned long long a = reinterpret_cast<unsigned long long>(z);
+        if (ALIGNED) {
+            src = reinterpret_cast<const uint4*>(z);
+            m0 = sh = glo = 0;
+            NU = ghi = (V + N - 1) / N;
+        } else {
+            m0 = (int)((reinterpret_cast<unsigned long long>(frame) & 15ull) / sizeof(T));
+            NU = (int)(((long long)m0 + V + N - 1) / N);
+            const unsigned long long s = a - (unsigned long long)m0 * sizeof(T), b = s & ~15ull;
+            src = reinterpret_cast<const uint4*>(b);
+            sh = (int)((s & 15ull) / sizeof(T));
+            glo = (int)(((a & ~15ull) - b) >> 4);
+            ghi = (int)((a + (unsigned long long)V * sizeof(T) + 15ull - b) >> 4);
+        }
+    }
+    // elements outside the row read as -inf
+    __device__ __forceinline__ uint4 load(int u) const {
+        uint4 w;
+        if (ALIGNED) {
+            w = __ldcs(src + u);
+            if (u == NU - 1) U::mask(w, 0, V - u * N);
+            return w;
+        }
+        w = u >= glo && u < ghi ? __ldcs(src + u) : U::none4();
+        if (sh) w = U::realign(w, u + 1 < ghi ? __ldcg(src + u + 1) : U::none4(), sh);
+        if (u == 0 || u == NU - 1) U::mask(w, u == 0 ? m0 : 0, min((long long)N, (long long)V + m0 - (long long)u * N));
+        return w;
+    }
+    // elements of unit u that belong to the row: [lo, hi)
+    __device__ __forceinline__ void bounds(int u, int& lo, int& hi) const {
+        const long long e0 = (long long)u * N - (ALIGNED ? 0 : m0);
+        lo = e0 < 0 ? (int)-e0 : 0;
+        hi = e0 + N > V ? (int)(V - e0) : N;
+    }
+    __device__ __forceinline__ int unit_of(int v) const { return (int)(((long long)v + (ALIGNED ? 0 : m0)) / N); }
+    // unit u of row g
+    __device__ __forceinline__ void store(T* g, int u, const uint4& w) const {
+        T* const at = g + ((long long)u * N - (ALIGNED ? 0 : m0));
+        int lo, hi;
+        bounds(u, lo, hi);
+        if (hi - lo == N) {
+            __stcs(reinterpret_cast<uint4*>(at), w);
+        } else {
+            const uint32_t* q = &w.x;
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (j >= lo && j < hi) {
+                    if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(at)[j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
+                    else reinterpret_cast<uint32_t*>(at)[j] = q[j];
+                }
+        }
+    }
+};
+
+__device__ __forceinline__ uint4 pack16(const float2 (&v)[4]) {
+    uint32_t r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r[j]) : "f"(v[j].y), "f"(v[j].x));
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+__device__ __forceinline__ uint4 pack16(const float2 (&v)[2]) {
+    return make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
+}
+__device__ __forceinline__ void put(__nv_bfloat16* at, float v) { *at = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void put(float* at, float v) { *at = v; }
+
+// dL/dz of a unit.  q = log2 p_v; the value is p_v (b + a q), a = -dL/dH ln 2 / T, b = -(dL/dl + dL/dH H) / T.
+struct GradConsts {
+    float2 nm2, L2, nl2, a2, b2;           // -m, log2 e / T, -log2 S, a, b
+};
+template <typename T, bool ENT>
+__device__ __forceinline__ uint4 grad_unit(const uint4& w, const GradConsts& c) {
+    using U = Unit<T>;
+    float2 z[U::N / 2];
+    U::unpack_raw(w, z);
+#pragma unroll
+    for (int j = 0; j < U::N / 2; ++j) {
+        float2 q = __ffma2_rn(__fadd2_rn(z[j], c.nm2), c.L2, c.nl2);
+        if (ENT) q = make_float2(fmaxf(q.x, kLowT), fmaxf(q.y, kLowT));
+        const float2 e = make_float2(ex2(q.x), ex2(q.y));
+        z[j] = __fmul2_rn(e, ENT ? __ffma2_rn(q, c.a2, c.b2) : c.b2);
+    }
+    return pack16(z);
+}
+// ... and of the token's own element, which has dL/dl / T on top
+template <typename T, bool ENT>
+__device__ __forceinline__ void grad_token(T* g, int x, float zx, float m, float lg2S, float c1, float a, float b, float top) {
+    float q = fmaf(zx - m, c1, -lg2S);
+    if (ENT) q = fmaxf(q, kLowT);
+    put(g + x, fmaf(ex2(q), ENT ? fmaf(q, a, b) : b, top));
+}
+
+// What a row's loss asks of its gradient.
+struct RowCoefs {
+    double dl, dH;
+};
+
+// Loss terms of a row from its l and H, in 64 bits (once a row): a ratio e^(l - l_old) and a total of terms of either
+// sign show a rounding of l, whose size is that of the logits.
+__device__ __forceinline__ RowCoefs row_coefs(const ScoreParams& p, int row, double l, double H, bool write) {
+    RowCoefs r{0.0, 0.0};
+    if (p.op == SCORE_GIVEN) {
+        r.dl = (double)__ldcg(p.g_logp + row);
+        r.dH = p.g_H ? (double)__ldcg(p.g_H + row) : 0.0;
+        if (l != l) r.dl = l;
+    } else if (p.op == SCORE_POLICY) {
+        const double A = (double)__ldcg(p.adv + row);
+        const double w = (double)p.scale * (p.weight ? (double)__ldcg(p.weight + row) : 1.0);
+        const double ratio = p.old_logp ? exp(l - (double)__ldcg(p.old_logp + row)) : l == l ? 1.0 : l;
+        double loss = 0.0, k3 = 0.0;
+        if (A != 0.0) {                    // (0 times an overflowed ratio is no term either)
+            const double lo = 1.0 - (double)p.clip_low, hi = 1.0 + (double)p.clip_high;
+            const double s1 = ratio * A, s2 = (ratio < lo ? lo : ratio > hi ? hi : ratio) * A;
+            loss = s1 <= s2 ? -s1 : s2 == s2 ? -s2 : s1;
+            if (!(s1 > s2)) r.dl = -s1;
+        } else if (l != l) {
+            r.dl = loss = l;
+        }
+        if (p.ref_logp) {
+            const double d = (double)__ldcg(p.ref_logp + row) - l, e = expm1(d);
+            k3 = e < INFINITY ? e - d : e;
+            if (p.kl_coef != 0.f) {
+                loss += (double)p.kl_coef * k3;
+                r.dl -= (double)p.kl_coef * e;
+            }
+        }
+        if (p.ent_coef != 0.f) {
+            loss -= (double)p.ent_coef * H;
+            r.dH = -(double)p.ent_coef;
+        }
+        r.dl *= w;
+        r.dH *= w;
+        if (write) {
+            p.row_loss[row] = (float)(w * loss);
+            if (p.kl) p.kl[row] = (float)k3;
+        }
+    }
+    return r;
+}
+
+// ALIGNED: rows of logits and gradient start on 16-byte boundaries.  NW warps a CTA, UPT units a thread.  HOLD: a CTA's units
+// fit its registers; else (rows longer than the cluster holds) they are taken in turn and read again for the gradient.
+// GRAD: a gradient is written.  ENT: the entropy or its gradient is wanted.
+template <typename T, bool ALIGNED, int NW, int UPT, bool HOLD, bool GRAD, bool ENT>
+__global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_constant__ ScoreParams p) {
+    using U = Unit<T>;
+    constexpr int N = U::N, NT = NW * 32;
+    const float floor_v = N == 8 ? ADASD_FLOOR_BF : kFloor;
+    __shared__ float4 part[kScMaxCluster * NW];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int CS = p.cs, row = (int)(blockIdx.x / (unsigned)CS), rank = (int)(blockIdx.x - (unsigned)row * (unsigned)CS);
+    cg::cluster_group cluster = cg::this_cluster();
+    pdl_wait();
+    pdl_trigger();
+
+    const T* const z = reinterpret_cast<const T*>(p.z) + (long long)row * p.row_stride;
+    T* const g = GRAD ? reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride : nullptr;
+    const RowUnits<T, ALIGNED> ru(z, GRAD ? g : z, p.V);
+    const int u0 = min(rank * p.per_cta, ru.NU), u1 = min(u0 + p.per_cta, ru.NU);
+    const int x = __ldcg(p.tok + row);
+    // (the same in every CTA of the cluster)
+    bool out = x < 0 || x >= p.V;
+    if (p.op == SCORE_POLICY && p.weight) out = out || __ldcg(p.weight + row) == 0.f;
+    if (p.op == SCORE_GIVEN) out = out || (__ldcg(p.g_logp + row) == 0.f && (!p.g_H || __ldcg(p.g_H + row) == 0.f));
+    int kind = 1;
+    if (!GRAD && p.op == SCORE_PREF) {
+        const int first = max(0, __ldcg(p.seq_start)), end = min(p.n_rows, __ldcg(p.seq_start + p.n_seqs));
+        kind = row < first || row >= end ? -1 : out ? 0 : 1;
+        out = kind != 1;
+    }
+    if (out) {
+        if (GRAD)
+            for (int u = u0 + (int)threadIdx.x; u < u1; u += NT) ru.store(g, u, make_uint4(0u, 0u, 0u, 0u));
+        if (rank == 0 && threadIdx.x == 0) {
+            if (p.logp) p.logp[row] = 0.f;
+            if (p.H) p.H[row] = 0.f;
+            if (p.lse) p.lse[row] = 0.f;
+            if (p.row_loss) p.row_loss[row] = 0.f;
+            if (p.kl) p.kl[row] = 0.f;
+            if (!GRAD && p.op == SCORE_PREF) p.pref[row] = PrefRow{0.f, 0.f, 0.f, kind};
+        }
+        return;
+    }
+    if (CS > 1) cluster.barrier_arrive();           // (waited for before the first remote store: that CTA has started)
+    const float zx = to_f32(z[x]);
+
+    // ---- sums -----------------------------------------------------------------------------
+    const float c1 = p.c1;
+    const float2 L2 = pair2(c1);
+    float m = -INFINITY;
+    float2 S2 = make_float2(0.f, 0.f), T2 = make_float2(0.f, 0.f);
+    uint32_t bad = 0u;
+    uint4 w[UPT];
+    for (int base = u0; base < u1; base += NT * UPT) {
+#pragma unroll
+        for (int k = 0; k < UPT; ++k) {
+            const int u = base + k * NT + (int)threadIdx.x;
+            w[k] = u < u1 ? ru.load(u) : U::none4();
+        }
+        typename U::Max mx = U::max0();
+#pragma unroll
+        for (int k = 0; k < UPT; ++k) U::max_add(mx, w[k]);
+        const float t = warp_max_f32(U::max_val(mx, bad));
+        if (t == INFINITY) bad = 1u;
+        if (t > m) {
+            const float d = fmaxf((m - t) * c1, kLowT), f = ex2(d);
+            if (ENT) {
+                T2.x = f * fmaf(d, S2.x, T2.x);
+                T2.y = f * fmaf(d, S2.y, T2.y);
+            }
+            S2.x *= f;
+            S2.y *= f;
+            m = t;
+        }
+        const float2 nm2 = pair2(m > -INFINITY ? -m : 0.f);
+#pragma unroll
+        for (int k = 0; k < UPT; ++k) {
+            if (base + k * NT < u1) {
+                float2 v[N / 2];
+                U::unpack_raw(w[k], v);
+#pragma unroll
+                for (int j = 0; j < N / 2; ++j) {
+                    float2 q = __fmul2_rn(__fadd2_rn(v[j], nm2), L2);
+                    if (ENT) q = make_float2(fmaxf(q.x, kLowT), fmaxf(q.y, kLowT));
+                    const float2 e = make_float2(ex2(q.x), ex2(q.y));
+                    S2 = __fadd2_rn(S2, e);
+                    if (ENT) T2 = __ffma2_rn(e, q, T2);
+                }
+            }
+        }
+    }
+    bad = __any_sync(0xFFFFFFFFu, bad) ? 1u : 0u;
+    const float4 mine = make_float4(m, warp_sum(S2.x + S2.y), ENT ? warp_sum(T2.x + T2.y) : 0.f, __uint_as_float(bad));
+    if (CS > 1) {
+        cluster.barrier_wait();
+        if (lane < CS) *cluster.map_shared_rank(part + rank * NW + warp, lane) = mine;
+        cluster.sync();
+    } else {
+        if (lane == 0) part[warp] = mine;
+        __syncthreads();
+    }
+    if (!GRAD && (rank != 0 || warp != 0)) return;
+
+    // ---- the row's totals, by every warp in the same order ----------------------------------
+    constexpr int PL = kScMaxCluster * NW > 32 ? 2 : 1;          // partials of a lane
+    float4 q[PL];
+    float M = -INFINITY;
+    uint32_t any = 0u;
+#pragma unroll
+    for (int k = 0; k < PL; ++k) {
+        q[k] = lane + 32 * k < CS * NW ? part[lane + 32 * k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        M = fmaxf(M, q[k].x);
+        any |= __float_as_uint(q[k].w);
+    }
+    M = warp_max_f32(M);
+    const bool none = __any_sync(0xFFFFFFFFu, any) || !(M > floor_v);
+    float S = 0.f, Ts = 0.f;
+#pragma unroll
+    for (int k = 0; k < PL; ++k) {
+        const float d = fmaxf((q[k].x - M) * c1, kLowT), f = ex2(d);
+        S = fmaf(f, q[k].y, S);
+        if (ENT) Ts = fmaf(f, fmaf(d, q[k].y, q[k].z), Ts);
+    }
+    S = warp_sum(S);
+    if (ENT) Ts = warp_sum(Ts);
+    if (none) S = NAN;
+
+    const bool writer = rank == 0 && threadIdx.x == 0;
+    if (!GRAD && p.op == SCORE_PREF) {
+        if (writer) {
+            p.pref[row] = PrefRow{M, S, zx - M, 1};
+            if (none) atomicOr(p.status, ADASD_STATUS_NAN);
+        }
+        return;
+    }
+    const double lnS = log((double)S), iT = 1.0 / (double)p.temperature;
+    const double l = ((double)zx - (double)M) * iT - lnS;
+    const double H = ENT ? lnS - 0.69314718055994530942 * ((double)Ts / (double)S) : 0.0;
+    const RowCoefs r = row_coefs(p, row, l, H, writer);
+    if (writer) {
+        if (p.logp) p.logp[row] = (float)l;
+        if (p.H) p.H[row] = (float)H;
+        if (p.lse) p.lse[row] = (float)((double)M * iT + lnS);
+        if (none) atomicOr(p.status, ADASD_STATUS_NAN);
+    }
+    if (!GRAD) return;
+
+    // ---- gradient ---------------------------------------------------------------------------
+    const float top = (float)(r.dl * iT);
+    GradConsts c;
+    const float a = ENT ? (float)(-0.69314718055994530942 * r.dH * iT) : 0.f, b = (float)((-r.dl - r.dH * H) * iT);
+    const float lg2S = (float)(lnS * 1.4426950408889634074);
+    c.nm2 = pair2(-M);
+    c.L2 = L2;
+    c.nl2 = pair2(-lg2S);
+    c.a2 = pair2(a);
+    c.b2 = pair2(b);
+    const bool zero = r.dl == 0.0 && r.dH == 0.0;
+    const int ux = ru.unit_of(x);
+    for (int base = u0; base < u1; base += NT * UPT) {
+#pragma unroll
+        for (int k = 0; k < UPT; ++k) {
+            const int u = base + k * NT + (int)threadIdx.x;
+            if (u < u1) {
+                const uint4 v = HOLD || zero ? w[k] : ru.load(u);
+                ru.store(g, u, zero ? make_uint4(0u, 0u, 0u, 0u) : grad_unit<T, ENT>(v, c));
+                if (u == ux && !zero) grad_token<T, ENT>(g, x, zx, M, lg2S, c1, a, b, top);
+            }
+        }
+        if (HOLD) break;
+    }
+}
+
+// ---- preference loss -----------------------------------------------------------------------
+
+template <int NT>
+__device__ __forceinline__ double block_sum_f64(double v, double* s) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    v = warp_sum_f64(v);
+    __syncthreads();
+    if (lane == 0) s[warp] = v;
+    __syncthreads();
+    double t = 0.0;
+#pragma unroll
+    for (int k = 0; k < NT / 32; ++k) t += s[k];
+    return t;
+}
+
+// Sum of n terms in a fixed order.
+constexpr int kTotThreads = 512;
+__global__ void __launch_bounds__(kTotThreads) total_kernel(const float* terms, int n, float* out) {
+    __shared__ double s[kTotThreads / 32];
+    pdl_wait();
+    pdl_trigger();
+    double v = 0.0;
+    for (int k = threadIdx.x; k < n; k += kTotThreads) v += (double)__ldcg(terms + k);
+    v = block_sum_f64<kTotThreads>(v, s);
+    if (threadIdx.x == 0) *out = (float)v;
+}
+
+// A pair: log-probs of its two sequences, its loss, and dL/dl of its rows.
+constexpr int kPairThreads = 256;
+__global__ void __launch_bounds__(kPairThreads) pref_pair_kernel(const __grid_constant__ PrefParams p) {
+    __shared__ double s[kPairThreads / 32];
+    pdl_wait();
+    pdl_trigger();
+    const int P = p.n_pairs, i = blockIdx.x;
+    const double iT = 1.0 / (double)p.temperature;
+    double l[2];
+    int first[2], end[2];
+    double count[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int q = i + k * P;
+        first[k] = min(max(__ldcg(p.seq_start + q), 0), p.n_rows);
+        end[k] = min(max(__ldcg(p.seq_start + q + 1), first[k]), p.n_rows);
+        double t = 0.0, n = 0.0;
+        for (int r = first[k] + (int)threadIdx.x; r < end[k]; r += kPairThreads) {
+            const float4 e = __ldcg(reinterpret_cast<const float4*>(p.pref + r));
+            if (__float_as_int(e.w) == 1) {
+                t += (double)e.z * iT - log((double)e.y);
+                n += 1.0;
+            }
+        }
+        l[k] = block_sum_f64<kPairThreads>(t, s);
+        count[k] = block_sum_f64<kPairThreads>(n, s);
+        if (p.average && count[k] > 0.0) l[k] /= count[k];
+    }
+    const double w = (double)p.scale * (p.pair_weight ? (double)__ldcg(p.pair_weight + i) : 1.0);
+    const double D = p.ref_logp ? (l[0] - (double)__ldcg(p.ref_logp + i)) - (l[1] - (double)__ldcg(p.ref_logp + P + i)) : l[0] - l[1];
+    const double beta = (double)p.beta, margin = (double)p.margin;
+    double loss, dD;
+    if (p.rule == ADASD_PREF_SIGMOID) {
+        // -(1 - e) ln sigma(u) - e ln sigma(-u) = max(-u, 0) + ln(1 + e^-|u|) + e u
+        const double u = beta * D - margin, ls = (double)p.label_smoothing, t = exp(-fabs(u));
+        loss = (u < 0.0 ? -u : u == u ? 0.0 : u) + log1p(t) + (ls != 0.0 ? ls * u : 0.0);
+        dD = beta * (ls - (u >= 0.0 ? t / (1.0 + t) : 1.0 / (1.0 + t)));
+    } else if (p.rule == ADASD_PREF_SQUARED) {
+        const double u = D - margin - 0.5 / beta;
+        loss = u * u;
+        dD = 2.0 * u;
+    } else {
+        const double u = 1.0 - (beta * D - margin);
+        loss = u > 0.0 ? u : u == u ? 0.0 : u;
+        dD = u > 0.0 ? -beta : u == u ? 0.0 : u;
+    }
+    const bool off = w == 0.0;
+    if (threadIdx.x == 0) {
+        p.seq_logp[i] = (float)l[0];
+        p.seq_logp[i + P] = (float)l[1];
+        p.pair_loss[i] = off ? 0.f : (float)(w * loss);
+    }
+    if (!p.grad) return;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        double d = off ? 0.0 : (k ? -w : w) * dD;
+        if (p.average && count[k] > 0.0) d /= count[k];
+        const float df = (float)d;
+        for (int r = first[k] + (int)threadIdx.x; r < end[k]; r += kPairThreads) p.pref[r].dz = df;
+    }
+}
+
+// Gradient of rows whose statistics and dL/dl are known: dL/dz_v = dL/dl (1[v = x] - p_v) / T.  From the last row to the
+// first: what the L2 still holds of score_kernel's reads is read first.
+constexpr int kPgThreads = 256, kPgUnits = 8;
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(kPgThreads) pref_grad_kernel(const __grid_constant__ PrefParams p) {
+    using U = Unit<T>;
+    const int back = (int)(blockIdx.x / (unsigned)p.segs), seg = (int)(blockIdx.x - (unsigned)back * (unsigned)p.segs);
+    const int row = p.n_rows - 1 - back;
+    pdl_wait();
+    pdl_trigger();
+    const float4 e = __ldcg(reinterpret_cast<const float4*>(p.pref + row));
+    const int kind = __float_as_int(e.w);
+    if (kind < 0) return;
+    const T* const z = reinterpret_cast<const T*>(p.z) + (long long)row * p.row_stride;
+    T* const g = reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride;
+    const RowUnits<T, ALIGNED> ru(z, g, p.V);
+    const int u0 = min(seg * p.per_cta, ru.NU), u1 = min(u0 + p.per_cta, ru.NU);
+    if (kind == 0 || e.z == 0.f) {
+        for (int u = u0 + (int)threadIdx.x; u < u1; u += kPgThreads) ru.store(g, u, make_uint4(0u, 0u, 0u, 0u));
+        return;
+    }
+    const int x = __ldcg(p.tok + row), ux = ru.unit_of(x);
+    uint4 w[kPgUnits];
+#pragma unroll
+    for (int k = 0; k < kPgUnits; ++k) {
+        const int u = u0 + k * kPgThreads + (int)threadIdx.x;
+        w[k] = u < u1 ? ru.load(u) : U::none4();
+    }
+    float zx = 0.f;
+    if (ux >= u0 && ux < u1) zx = to_f32(z[x]);      // (of its CTA alone: another may have written its gradient there)
+    __syncthreads();
+    const float iT = 1.f / p.temperature, top = e.z * iT, lg2S = log2f(e.y);
+    GradConsts c;
+    c.nm2 = pair2(-e.x);
+    c.L2 = pair2(p.c1);
+    c.nl2 = pair2(-lg2S);
+    c.a2 = pair2(0.f);
+    c.b2 = pair2(-top);
+#pragma unroll
+    for (int k = 0; k < kPgUnits; ++k) {
+        const int u = u0 + k * kPgThreads + (int)threadIdx.x;
+        if (u < u1) {
+            ru.store(g, u, grad_unit<T, false>(w[k], c));
+            if (u == ux) grad_token<T, false>(g, x, zx, e.x, lg2S, p.c1, 0.f, -top, top);
+        }
+    }
+}
+
+}  // namespace adasd

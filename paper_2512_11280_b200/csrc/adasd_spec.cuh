@@ -41,6 +41,7 @@
 #pragma once
 
 #include "adasd_async.cuh"
+#include "adasd_rows.cuh"
 
 namespace adasd {
 
