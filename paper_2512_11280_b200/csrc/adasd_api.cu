@@ -1037,7 +1037,7 @@ static ScoreParams score_params(const adasd_ctx* ctx, int32_t op, const void* z,
     p.tok = tokens;
     p.n_rows = n_rows;
     p.V = ctx->cfg.V;
-    p.temperature = ctx->temperature;
+    p.inv_temp = 1.0 / (double)ctx->temperature;
     p.c1 = kLog2e / ctx->temperature;
     p.status = ctx->st.status;
     return p;
@@ -1141,7 +1141,7 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
         p.n_rows = n_rows;
         p.V = s.V;
         p.n_pairs = n_pairs;
-        p.temperature = s.temperature;
+        p.temperature = ctx->temperature;
         p.c1 = s.c1;
         p.seq_start = seq_start_dev;
         p.ref_logp = ref_logp_dev;

@@ -1,8 +1,9 @@
 // Launches of the scoring and loss kernels (adasd_score.cuh).
 #include "adasd_launch.cuh"
-#include "adasd_score.cuh"
+#include "adasd_score_stream.cuh"
 
 #include <algorithm>
+#include <atomic>
 
 namespace adasd {
 namespace {
@@ -26,10 +27,77 @@ int launch(const ScoreParams& p, bool ent, cudaStream_t stream) {
     return ent ? launch<T, ALIGNED, NW, UPT, HOLD, false, true>(p, stream) : launch<T, ALIGNED, NW, UPT, HOLD, false, false>(p, stream);
 }
 
+template <typename K>
+int resident_clusters(K kern, int threads, int smem, int cs) {
+    cudaLaunchConfig_t lc;
+    memset(&lc, 0, sizeof(lc));
+    lc.gridDim = dim3((unsigned)cs, 1, 1);
+    lc.blockDim = dim3((unsigned)threads, 1, 1);
+    lc.dynamicSmemBytes = (size_t)smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cs;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &lc) != cudaSuccess) {
+        cudaGetLastError();
+        return 0;
+    }
+    return n;
+}
+// Clusters of a kernel that are resident at once, asked for once per device, kernel and cluster size.
+template <typename T, bool ALIGNED, int NW, bool GRAD, bool ENT>
+int stream_clusters(int cs) {
+    constexpr int kDevices = 64;
+    static std::atomic<int> known[kDevices][kScMaxCluster + 1];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return 0;
+    int n = known[dev][cs].load(std::memory_order_acquire);
+    if (n == 0) {
+        const auto kern = score_stream_kernel<T, ALIGNED, NW, GRAD, ENT>;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NW * kSsStage) != cudaSuccess) {
+            cudaGetLastError();
+            return 0;
+        }
+        n = resident_clusters(kern, NW * 32, NW * kSsStage, cs);
+        known[dev][cs].store(n, std::memory_order_release);
+    }
+    return n;
+}
+// ADASD_ERR_SHAPE: not a launch for score_stream_kernel (rows too long, or too few of them).
+template <typename T, bool ALIGNED, int NW, bool GRAD, bool ENT>
+int launch_stream_t(ScoreParams p, int cs, int per_warp, cudaStream_t stream) {
+    const int ncl = stream_clusters<T, ALIGNED, NW, GRAD, ENT>(cs);
+    if (p.n_rows <= ncl || ncl == 0) return ADASD_ERR_SHAPE;
+    p.cs = cs;
+    p.per_cta = per_warp;
+    return launch_pdl(score_stream_kernel<T, ALIGNED, NW, GRAD, ENT>, ncl * cs, NW * 32, NW * kSsStage, cs, stream, p);
+}
+template <typename T, bool ALIGNED, int NW>
+int launch_stream_n(const ScoreParams& p, bool ent, int cs, int per_warp, cudaStream_t stream) {
+    if (p.grad) return ent ? launch_stream_t<T, ALIGNED, NW, true, true>(p, cs, per_warp, stream) : launch_stream_t<T, ALIGNED, NW, true, false>(p, cs, per_warp, stream);
+    return ent ? launch_stream_t<T, ALIGNED, NW, false, true>(p, cs, per_warp, stream) : launch_stream_t<T, ALIGNED, NW, false, false>(p, cs, per_warp, stream);
+}
+template <typename T, bool ALIGNED>
+int launch_stream(const ScoreParams& p, bool ent, int NU, cudaStream_t stream) {
+    constexpr int W = kSsUPT * 32;
+    const int warps = (NU + W - 1) / W;
+    if (warps == 1) return launch_stream_n<T, ALIGNED, 1>(p, ent, 1, NU, stream);
+    if (warps == 2) return launch_stream_n<T, ALIGNED, 2>(p, ent, 1, (NU + 1) / 2, stream);
+    if (warps <= 4) return launch_stream_n<T, ALIGNED, 4>(p, ent, 1, (NU + 3) / 4, stream);
+    const int cs = (warps + 7) / 8;
+    if (cs > kScMaxCluster) return ADASD_ERR_SHAPE;
+    return launch_stream_n<T, ALIGNED, 8>(p, ent, cs, (NU + 8 * cs - 1) / (8 * cs), stream);
+}
+
 constexpr int kScNW = 8, kScUnits = kScNW * 32;      // CTAs of 8 warps; units of a CTA and unit a thread
 
 template <typename T, bool ALIGNED>
 int launch(ScoreParams p, bool ent, int NU, int sms, cudaStream_t stream) {
+    if (const int rc = launch_stream<T, ALIGNED>(p, ent, NU, stream); rc != ADASD_ERR_SHAPE) return rc;
     if (NU <= 2 * 32 * 4) {
         p.cs = 1;
         p.per_cta = NU;

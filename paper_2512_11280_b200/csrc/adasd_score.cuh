@@ -126,51 +126,187 @@ __device__ __forceinline__ void grad_token(T* g, int x, float zx, float m, float
     put(g + x, fmaf(ex2(q), ENT ? fmaf(q, a, b) : b, top));
 }
 
-// What a row's loss asks of its gradient.
-struct RowCoefs {
-    double dl, dH;
+// Inputs of a row's loss.
+struct RowIn {
+    float adv, old, ref, w;                // SCORE_GIVEN: dL/dl, dL/dH in the first two
 };
-
-// Loss terms of a row from its l and H, in 64 bits (once a row): a ratio e^(l - l_old) and a total of terms of either
-// sign show a rounding of l, whose size is that of the logits.
-__device__ __forceinline__ RowCoefs row_coefs(const ScoreParams& p, int row, double l, double H, bool write) {
-    RowCoefs r{0.0, 0.0};
+__device__ __forceinline__ RowIn row_in(const ScoreParams& p, int row) {
+    RowIn r{0.f, 0.f, 0.f, 1.f};
     if (p.op == SCORE_GIVEN) {
-        r.dl = (double)__ldcg(p.g_logp + row);
-        r.dH = p.g_H ? (double)__ldcg(p.g_H + row) : 0.0;
-        if (l != l) r.dl = l;
+        r.adv = __ldcg(p.g_logp + row);
+        if (p.g_H) r.old = __ldcg(p.g_H + row);
     } else if (p.op == SCORE_POLICY) {
-        const double A = (double)__ldcg(p.adv + row);
-        const double w = (double)p.scale * (p.weight ? (double)__ldcg(p.weight + row) : 1.0);
-        const double ratio = p.old_logp ? exp(l - (double)__ldcg(p.old_logp + row)) : l == l ? 1.0 : l;
-        double loss = 0.0, k3 = 0.0;
-        if (A != 0.0) {                    // (0 times an overflowed ratio is no term either)
-            const double lo = 1.0 - (double)p.clip_low, hi = 1.0 + (double)p.clip_high;
-            const double s1 = ratio * A, s2 = (ratio < lo ? lo : ratio > hi ? hi : ratio) * A;
-            loss = s1 <= s2 ? -s1 : s2 == s2 ? -s2 : s1;
-            if (!(s1 > s2)) r.dl = -s1;
-        } else if (l != l) {
-            r.dl = loss = l;
-        }
-        if (p.ref_logp) {
-            const double d = (double)__ldcg(p.ref_logp + row) - l, e = expm1(d);
-            k3 = e < INFINITY ? e - d : e;
-            if (p.kl_coef != 0.f) {
-                loss += (double)p.kl_coef * k3;
-                r.dl -= (double)p.kl_coef * e;
-            }
-        }
-        if (p.ent_coef != 0.f) {
-            loss -= (double)p.ent_coef * H;
-            r.dH = -(double)p.ent_coef;
-        }
-        r.dl *= w;
-        r.dH *= w;
-        if (write) {
-            p.row_loss[row] = (float)(w * loss);
-            if (p.kl) p.kl[row] = (float)k3;
+        r.adv = __ldcg(p.adv + row);
+        if (p.old_logp) r.old = __ldcg(p.old_logp + row);
+        if (p.ref_logp) r.ref = __ldcg(p.ref_logp + row);
+        if (p.weight) r.w = __ldcg(p.weight + row);
+    }
+    return r;
+}
+// Whether a row is left out.
+__device__ __forceinline__ bool row_out(const ScoreParams& p, int row, int x) {
+    bool out = x < 0 || x >= p.V;
+    if (p.op == SCORE_POLICY && p.weight) out = out || __ldcg(p.weight + row) == 0.f;
+    if (p.op == SCORE_GIVEN) out = out || (__ldcg(p.g_logp + row) == 0.f && (!p.g_H || __ldcg(p.g_H + row) == 0.f));
+    return out;
+}
+
+// Terms of the policy loss and its derivatives, without the weight.  F: float for the gradient's coefficients, double for what
+// is reported (KL estimates of 1e-3 and less, totals of terms of either sign).  The differences of log-probs come as such:
+// rounded after they are formed.
+template <typename F>
+__device__ __forceinline__ void policy_terms(const ScoreParams& p, const RowIn& in, F l_old, F ref_l, F H, F& loss, F& k3, F& dl, F& dH) {
+    const F A = (F)in.adv, ratio = p.old_logp ? exp(l_old) : l_old == l_old ? (F)1 : l_old;
+    loss = dl = dH = k3 = (F)0;
+    if (A != (F)0) {                       // (0 times an overflowed ratio is no term either)
+        const F lo = (F)1 - (F)p.clip_low, hi = (F)1 + (F)p.clip_high;
+        const F s1 = ratio * A, s2 = (ratio < lo ? lo : ratio > hi ? hi : ratio) * A;
+        loss = s1 <= s2 ? -s1 : s2 == s2 ? -s2 : s1;
+        if (!(s1 > s2)) dl = -s1;
+    } else if (ratio != ratio) {
+        loss = dl = ratio;
+    }
+    if (p.ref_logp) {
+        const F e = expm1(ref_l);
+        k3 = e < (F)INFINITY ? e - ref_l : e;
+        if (p.kl_coef != 0.f) {
+            loss += (F)p.kl_coef * k3;
+            dl -= (F)p.kl_coef * e;
         }
     }
+    if (p.ent_coef != 0.f) {
+        loss -= (F)p.ent_coef * H;
+        dH = -(F)p.ent_coef;
+    }
+}
+
+// Statistics of a row: largest logit, S, T = sum 2^t t, the token's logit.
+struct RowStats {
+    float M, S, Ts, zx;
+};
+
+// dL/dl and dL/dH.  lnS: its logarithm in 32 bits, which is as good as S.
+__device__ __forceinline__ float2 row_coefs(const ScoreParams& p, const RowIn& in, const RowStats& s, float lnS, float H) {
+    const double l = ((double)s.zx - (double)s.M) * p.inv_temp - (double)lnS;
+    if (p.op == SCORE_GIVEN) return make_float2(l == l ? in.adv : (float)l, in.old);
+    float loss, k3, dl, dH;
+    policy_terms<float>(p, in, (float)(l - (double)in.old), (float)((double)in.ref - l), H, loss, k3, dl, dH);
+    const float w = p.scale * in.w;
+    return make_float2(w * dl, w * dH);
+}
+
+// What a row reports, by one thread, in 64 bits.
+__device__ __forceinline__ void row_report(const ScoreParams& p, int row, const RowIn& in, const RowStats& s) {
+    if (s.S != s.S) atomicOr(p.status, ADASD_STATUS_NAN);
+    if (p.op == SCORE_PREF) {
+        p.pref[row] = PrefRow{s.M, s.S, s.zx - s.M, 1};
+        return;
+    }
+    if (p.op == SCORE_GIVEN) return;
+    const double lnS = log((double)s.S), l = ((double)s.zx - (double)s.M) * p.inv_temp - lnS;
+    const double H = lnS - 0.69314718055994530942 * ((double)s.Ts / (double)s.S);
+    if (p.logp) p.logp[row] = (float)l;
+    if (p.H) p.H[row] = (float)H;
+    if (p.lse) p.lse[row] = (float)((double)s.M * p.inv_temp + lnS);
+    if (p.op == SCORE_POLICY) {
+        double loss, k3, dl, dH;
+        policy_terms<double>(p, in, l - (double)in.old, (double)in.ref - l, H, loss, k3, dl, dH);
+        p.row_loss[row] = (float)((double)p.scale * (double)in.w * loss);
+        if (p.kl) p.kl[row] = (float)k3;
+    }
+}
+// ... and one that is left out.  kind: -1 in no sequence (SCORE_PREF)
+__device__ __forceinline__ void row_report_out(const ScoreParams& p, int row, int kind) {
+    if (p.logp) p.logp[row] = 0.f;
+    if (p.H) p.H[row] = 0.f;
+    if (p.lse) p.lse[row] = 0.f;
+    if (p.row_loss) p.row_loss[row] = 0.f;
+    if (p.kl) p.kl[row] = 0.f;
+    if (p.op == SCORE_PREF) p.pref[row] = PrefRow{0.f, 0.f, 0.f, kind};
+}
+// kind of a row of SCORE_PREF (-1: in no sequence), 0 left out, 1 counted
+__device__ __forceinline__ int row_kind(const ScoreParams& p, int row, int x) {
+    if (p.op == SCORE_PREF) {
+        const int first = max(0, __ldcg(p.seq_start)), end = min(p.n_rows, __ldcg(p.seq_start + p.n_seqs));
+        if (row < first || row >= end) return -1;
+    }
+    return row_out(p, row, x) ? 0 : 1;
+}
+
+// Totals of a row from its warps' partials {m, S, T, bad}, by a whole warp, in the same order in every warp.
+template <int MOST>
+__device__ __forceinline__ RowStats fold_partials(const float4* part, int n, float c1, float floor_v, float zx) {
+    constexpr int PL = MOST > 32 ? 2 : 1;  // partials of a lane
+    const int lane = threadIdx.x & 31;
+    float4 q[PL];
+    RowStats r;
+    r.M = -INFINITY;
+    r.zx = zx;
+    uint32_t any = 0u;
+#pragma unroll
+    for (int k = 0; k < PL; ++k) {
+        q[k] = lane + 32 * k < n ? part[lane + 32 * k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        r.M = fmaxf(r.M, q[k].x);
+        any |= __float_as_uint(q[k].w);
+    }
+    r.M = warp_max_f32(r.M);
+    const bool none = __any_sync(0xFFFFFFFFu, any) || !(r.M > floor_v);
+    r.S = r.Ts = 0.f;
+#pragma unroll
+    for (int k = 0; k < PL; ++k) {
+        const float d = fmaxf((q[k].x - r.M) * c1, kLowT), f = ex2(d);
+        r.S = fmaf(f, q[k].y, r.S);
+        r.Ts = fmaf(f, fmaf(d, q[k].y, q[k].z), r.Ts);
+    }
+    r.S = warp_sum(r.S);
+    r.Ts = warp_sum(r.Ts);
+    if (none) r.S = NAN;
+    return r;
+}
+
+// Sums of a warp's units, held in registers: adds 2^t (and 2^t t) under the maximum m to S2 (T2).  used(k): whether unit k of the
+// lanes can hold anything (warp-uniform).
+template <typename T, bool ENT, int UPT, typename F>
+__device__ __forceinline__ void sum_units(const uint4 (&w)[UPT], float m, float2 L2, float2& S2, float2& T2, F used) {
+    using U = Unit<T>;
+    const float2 nm2 = pair2(m > -INFINITY ? -m : 0.f);
+#pragma unroll
+    for (int k = 0; k < UPT; ++k) {
+        if (used(k)) {
+            float2 v[U::N / 2];
+            U::unpack_raw(w[k], v);
+#pragma unroll
+            for (int j = 0; j < U::N / 2; ++j) {
+                float2 q = __fmul2_rn(__fadd2_rn(v[j], nm2), L2);
+                if (ENT) q = make_float2(fmaxf(q.x, kLowT), fmaxf(q.y, kLowT));
+                const float2 e = make_float2(ex2(q.x), ex2(q.y));
+                S2 = __fadd2_rn(S2, e);
+                if (ENT) T2 = __ffma2_rn(e, q, T2);
+            }
+        }
+    }
+}
+
+// What the gradient of a row takes: its constants, and the token's own element.
+struct RowGrad {
+    GradConsts c;
+    float a, b, top, lg2S;
+    bool zero;
+};
+__device__ __forceinline__ RowGrad row_grad(const ScoreParams& p, const RowIn& in, const RowStats& s, float2 L2, bool ent) {
+    RowGrad r;
+    const float lnS = logf(s.S), H = ent ? lnS - kLn2 * (s.Ts / s.S) : 0.f, iT = (float)p.inv_temp;
+    const float2 d = row_coefs(p, in, s, lnS, H);
+    r.zero = d.x == 0.f && d.y == 0.f;
+    r.top = d.x * iT;
+    r.a = ent ? -kLn2 * d.y * iT : 0.f;
+    r.b = (ent ? fmaf(-d.y, H, -d.x) : -d.x) * iT;
+    r.lg2S = log2f(s.S);
+    r.c.nm2 = pair2(-s.M);
+    r.c.L2 = L2;
+    r.c.nl2 = pair2(-r.lg2S);
+    r.c.a2 = pair2(r.a);
+    r.c.b2 = pair2(r.b);
     return r;
 }
 
@@ -193,32 +329,16 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
     T* const g = GRAD ? reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride : nullptr;
     const RowUnits<T, ALIGNED> ru(z, GRAD ? g : z, p.V);
     const int u0 = min(rank * p.per_cta, ru.NU), u1 = min(u0 + p.per_cta, ru.NU);
-    const int x = __ldcg(p.tok + row);
-    // (the same in every CTA of the cluster)
-    bool out = x < 0 || x >= p.V;
-    if (p.op == SCORE_POLICY && p.weight) out = out || __ldcg(p.weight + row) == 0.f;
-    if (p.op == SCORE_GIVEN) out = out || (__ldcg(p.g_logp + row) == 0.f && (!p.g_H || __ldcg(p.g_H + row) == 0.f));
-    int kind = 1;
-    if (!GRAD && p.op == SCORE_PREF) {
-        const int first = max(0, __ldcg(p.seq_start)), end = min(p.n_rows, __ldcg(p.seq_start + p.n_seqs));
-        kind = row < first || row >= end ? -1 : out ? 0 : 1;
-        out = kind != 1;
-    }
-    if (out) {
+    const int x = __ldcg(p.tok + row), kind = row_kind(p, row, x);       // (the same in every CTA of the cluster)
+    if (kind != 1) {
         if (GRAD)
             for (int u = u0 + (int)threadIdx.x; u < u1; u += NT) ru.store(g, u, make_uint4(0u, 0u, 0u, 0u));
-        if (rank == 0 && threadIdx.x == 0) {
-            if (p.logp) p.logp[row] = 0.f;
-            if (p.H) p.H[row] = 0.f;
-            if (p.lse) p.lse[row] = 0.f;
-            if (p.row_loss) p.row_loss[row] = 0.f;
-            if (p.kl) p.kl[row] = 0.f;
-            if (!GRAD && p.op == SCORE_PREF) p.pref[row] = PrefRow{0.f, 0.f, 0.f, kind};
-        }
+        if (rank == 0 && threadIdx.x == 0) row_report_out(p, row, kind);
         return;
     }
     if (CS > 1) cluster.barrier_arrive();           // (waited for before the first remote store: that CTA has started)
     const float zx = to_f32(z[x]);
+    const RowIn in = row_in(p, row);
 
     // ---- sums -----------------------------------------------------------------------------
     const float c1 = p.c1;
@@ -248,22 +368,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
             S2.y *= f;
             m = t;
         }
-        const float2 nm2 = pair2(m > -INFINITY ? -m : 0.f);
-#pragma unroll
-        for (int k = 0; k < UPT; ++k) {
-            if (base + k * NT < u1) {
-                float2 v[N / 2];
-                U::unpack_raw(w[k], v);
-#pragma unroll
-                for (int j = 0; j < N / 2; ++j) {
-                    float2 q = __fmul2_rn(__fadd2_rn(v[j], nm2), L2);
-                    if (ENT) q = make_float2(fmaxf(q.x, kLowT), fmaxf(q.y, kLowT));
-                    const float2 e = make_float2(ex2(q.x), ex2(q.y));
-                    S2 = __fadd2_rn(S2, e);
-                    if (ENT) T2 = __ffma2_rn(e, q, T2);
-                }
-            }
-        }
+        sum_units<T, ENT, UPT>(w, m, L2, S2, T2, [&](int k) { return base + k * NT < u1; });
     }
     bad = __any_sync(0xFFFFFFFFu, bad) ? 1u : 0u;
     const float4 mine = make_float4(m, warp_sum(S2.x + S2.y), ENT ? warp_sum(T2.x + T2.y) : 0.f, __uint_as_float(bad));
@@ -276,75 +381,26 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
         __syncthreads();
     }
     if (!GRAD && (rank != 0 || warp != 0)) return;
-
-    // ---- the row's totals, by every warp in the same order ----------------------------------
-    constexpr int PL = kScMaxCluster * NW > 32 ? 2 : 1;          // partials of a lane
-    float4 q[PL];
-    float M = -INFINITY;
-    uint32_t any = 0u;
-#pragma unroll
-    for (int k = 0; k < PL; ++k) {
-        q[k] = lane + 32 * k < CS * NW ? part[lane + 32 * k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-        M = fmaxf(M, q[k].x);
-        any |= __float_as_uint(q[k].w);
-    }
-    M = warp_max_f32(M);
-    const bool none = __any_sync(0xFFFFFFFFu, any) || !(M > floor_v);
-    float S = 0.f, Ts = 0.f;
-#pragma unroll
-    for (int k = 0; k < PL; ++k) {
-        const float d = fmaxf((q[k].x - M) * c1, kLowT), f = ex2(d);
-        S = fmaf(f, q[k].y, S);
-        if (ENT) Ts = fmaf(f, fmaf(d, q[k].y, q[k].z), Ts);
-    }
-    S = warp_sum(S);
-    if (ENT) Ts = warp_sum(Ts);
-    if (none) S = NAN;
-
-    const bool writer = rank == 0 && threadIdx.x == 0;
-    if (!GRAD && p.op == SCORE_PREF) {
-        if (writer) {
-            p.pref[row] = PrefRow{M, S, zx - M, 1};
-            if (none) atomicOr(p.status, ADASD_STATUS_NAN);
-        }
-        return;
-    }
-    const double lnS = log((double)S), iT = 1.0 / (double)p.temperature;
-    const double l = ((double)zx - (double)M) * iT - lnS;
-    const double H = ENT ? lnS - 0.69314718055994530942 * ((double)Ts / (double)S) : 0.0;
-    const RowCoefs r = row_coefs(p, row, l, H, writer);
-    if (writer) {
-        if (p.logp) p.logp[row] = (float)l;
-        if (p.H) p.H[row] = (float)H;
-        if (p.lse) p.lse[row] = (float)((double)M * iT + lnS);
-        if (none) atomicOr(p.status, ADASD_STATUS_NAN);
-    }
-    if (!GRAD) return;
+    const RowStats st = fold_partials<kScMaxCluster * NW>(part, CS * NW, c1, floor_v, zx);
 
     // ---- gradient ---------------------------------------------------------------------------
-    const float top = (float)(r.dl * iT);
-    GradConsts c;
-    const float a = ENT ? (float)(-0.69314718055994530942 * r.dH * iT) : 0.f, b = (float)((-r.dl - r.dH * H) * iT);
-    const float lg2S = (float)(lnS * 1.4426950408889634074);
-    c.nm2 = pair2(-M);
-    c.L2 = L2;
-    c.nl2 = pair2(-lg2S);
-    c.a2 = pair2(a);
-    c.b2 = pair2(b);
-    const bool zero = r.dl == 0.0 && r.dH == 0.0;
-    const int ux = ru.unit_of(x);
-    for (int base = u0; base < u1; base += NT * UPT) {
+    if (GRAD) {
+        const RowGrad r = row_grad(p, in, st, L2, ENT);
+        const int ux = ru.unit_of(x);
+        for (int base = u0; base < u1; base += NT * UPT) {
 #pragma unroll
-        for (int k = 0; k < UPT; ++k) {
-            const int u = base + k * NT + (int)threadIdx.x;
-            if (u < u1) {
-                const uint4 v = HOLD || zero ? w[k] : ru.load(u);
-                ru.store(g, u, zero ? make_uint4(0u, 0u, 0u, 0u) : grad_unit<T, ENT>(v, c));
-                if (u == ux && !zero) grad_token<T, ENT>(g, x, zx, M, lg2S, c1, a, b, top);
+            for (int k = 0; k < UPT; ++k) {
+                const int u = base + k * NT + (int)threadIdx.x;
+                if (u < u1) {
+                    const uint4 v = HOLD || r.zero ? w[k] : ru.load(u);
+                    ru.store(g, u, r.zero ? make_uint4(0u, 0u, 0u, 0u) : grad_unit<T, ENT>(v, r.c));
+                    if (u == ux && !r.zero) grad_token<T, ENT>(g, x, zx, st.M, r.lg2S, c1, r.a, r.b, r.top);
+                }
             }
+            if (HOLD) break;
         }
-        if (HOLD) break;
     }
+    if (rank == 0 && threadIdx.x == 0) row_report(p, row, in, st);
 }
 
 // ---- preference loss -----------------------------------------------------------------------

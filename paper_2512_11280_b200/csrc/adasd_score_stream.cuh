@@ -1,0 +1,211 @@
+// score_kernel for launches of many rows (same rows, same outputs): a cluster takes row after row, and while a row is summed
+// and its gradient formed from the registers that hold it, the next one is on its way into shared memory.
+//
+// A warp owns a stretch of units of every row: it asks for it with one bulk copy, takes it into registers when it has landed,
+// and asks for the next row's at once, so that an SM has up to 128 KB of loads under way whatever its warps are at.  The warps'
+// statistics go to every CTA of the cluster with stores that count their bytes on a barrier there; a warp waits for nothing else.
+#pragma once
+
+#include "adasd_score.cuh"
+
+namespace adasd {
+
+constexpr int kSsUPT = 16;                                   // units a lane holds
+constexpr int kSsStage = (kSsUPT * 32 + 1) * 16;             // a warp's stretch (+ one unit: rows off 16-byte boundaries)
+
+struct __align__(16) RowHist {
+    RowStats s;
+    int32_t row, pad[3];
+};
+
+// The rows a cluster has to do, 32 at a time: lane j holds row first + (wi + j) clusters.  Rows left out are set aside.
+struct RowWindow {
+    int wi, row, x;
+    unsigned todo, zero;                                     // lanes with rows to do, with gradient rows to zero
+};
+
+template <typename T, bool ALIGNED, int NW, bool GRAD, bool ENT>
+__global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __grid_constant__ ScoreParams p) {
+    using U = Unit<T>;
+    constexpr int N = U::N, UPT = kSsUPT;
+    const float floor_v = N == 8 ? ADASD_FLOOR_BF : kFloor;
+    extern __shared__ __align__(128) unsigned char dyn_smem[];
+    __shared__ float4 part[2][kScMaxCluster * NW];
+    __shared__ unsigned long long full_s[NW], got_s[2];
+    __shared__ RowHist hist[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int CS = p.cs, ncl = (int)(gridDim.x / (unsigned)CS), cl = (int)(blockIdx.x / (unsigned)CS);
+    const int rank = (int)(blockIdx.x - (unsigned)cl * (unsigned)CS);
+    const bool keeper = rank == 0 && warp == 0;              // the warp that reports
+    uint64_t* const full = reinterpret_cast<uint64_t*>(&full_s[warp]);
+    unsigned char* const stage = dyn_smem + warp * kSsStage;
+    cg::cluster_group cluster = cg::this_cluster();
+    if (lane == 0) {
+        mbar_init(full, 1);
+        if (warp == 0) {
+            mbar_init(reinterpret_cast<uint64_t*>(&got_s[0]), 1);
+            mbar_init(reinterpret_cast<uint64_t*>(&got_s[1]), 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (CS > 1) cluster.sync();
+    else __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+
+    const int ua = (rank * NW + warp) * p.per_cta, ub = ua + p.per_cta;          // (per_cta: units of a WARP here)
+    auto units = [&](int row) {
+        const T* const z = reinterpret_cast<const T*>(p.z) + (long long)row * p.row_stride;
+        return RowUnits<T, ALIGNED>(z, GRAD ? reinterpret_cast<const T*>(p.grad) + (long long)row * p.g_stride : z, p.V);
+    };
+    RowWindow win;
+    auto open = [&](int wi) {
+        win.wi = wi;
+        const long long r = (long long)cl + (long long)(wi + lane) * ncl;
+        int kind = -2;
+        if (r < p.n_rows) {
+            win.row = (int)r;
+            win.x = __ldcg(p.tok + r);
+            kind = row_kind(p, (int)r, win.x);
+            if (keeper && kind != 1) row_report_out(p, (int)r, kind);
+        }
+        win.todo = __ballot_sync(0xFFFFFFFFu, kind == 1);
+        win.zero = GRAD ? __ballot_sync(0xFFFFFFFFu, kind == 0) : 0u;
+    };
+    auto zero_row = [&]() {                                  // one row set aside
+        const int j = __ffs(win.zero) - 1, row = __shfl_sync(0xFFFFFFFFu, win.row, j);
+        win.zero &= win.zero - 1;
+        const RowUnits<T, ALIGNED> ru = units(row);
+        T* const g = reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride;
+        for (int u = ua + lane; u < min(ub, ru.NU); u += 32) ru.store(g, u, make_uint4(0u, 0u, 0u, 0u));
+    };
+    int row = -1, x = 0;                                     // the row asked for; -1: none left
+    auto next = [&]() {
+        while (!win.todo) {
+            while (GRAD && win.zero) zero_row();
+            row = -1;
+            if ((long long)cl + (long long)(win.wi + 32) * ncl >= p.n_rows) return;
+            open(win.wi + 32);
+        }
+        const int j = __ffs(win.todo) - 1;
+        win.todo &= win.todo - 1;
+        row = __shfl_sync(0xFFFFFFFFu, win.row, j);
+        x = __shfl_sync(0xFFFFFFFFu, win.x, j);
+    };
+    auto ask = [&]() {                                       // its stretch: granules from unit ua's first on that hold elements
+        if (lane == 0) {
+            const RowUnits<T, ALIGNED> ru = units(row);
+            const int g0 = max(ua, ru.glo), g1 = min(min(ub, ru.NU) + (!ALIGNED && ru.sh ? 1 : 0), ru.ghi);
+            const uint32_t bytes = (uint32_t)max(g1 - g0, 0) * 16u;
+            mbar_expect_tx(full, bytes);
+            if (bytes) bulk_g2s(stage + (g0 - ua) * 16, ru.src + g0, bytes, full);
+        }
+    };
+    bool alive = true, asked = false;                        // (no more copies once a wait has run out; one under way is waited for)
+    open(0);
+    next();
+    if (row >= 0) {
+        ask();
+        asked = true;
+    }
+
+    const float c1 = p.c1;
+    const float2 L2 = pair2(c1);
+    uint32_t ph = 0u;
+    int done = 0;
+    while (row >= 0) {
+        const int my_row = row, my_x = x, par = done & 1;
+        const RowUnits<T, ALIGNED> ru = units(my_row);
+        const int un = min(ub, ru.NU);
+        const float zx = to_f32((reinterpret_cast<const T*>(p.z) + (long long)my_row * p.row_stride)[my_x]);
+        RowIn in;
+        if (GRAD) in = row_in(p, my_row);
+        uint64_t* const got = reinterpret_cast<uint64_t*>(&got_s[par]);
+        if (CS > 1 && warp == 0 && lane == 0) mbar_expect_tx(got, (uint32_t)(CS * NW) * 16u);
+        if (asked) {
+            const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(full, ph));
+            if (!ok && lane == 0) atomicOr(p.status, ADASD_STATUS_TIMEOUT);
+            alive = alive && ok;
+        }
+        ph ^= 1u;
+        uint32_t bad = alive ? 0u : 1u;
+        uint4 w[UPT];
+        typename U::Max mx = U::max0();
+#pragma unroll
+        for (int k = 0; k < UPT; ++k) {
+            const int u = ua + k * 32 + lane;
+            w[k] = U::none4();
+            if (u < un) {
+                const unsigned char* const at = stage + (k * 32 + lane) * 16;
+                if (ALIGNED) {
+                    w[k] = *reinterpret_cast<const uint4*>(at);
+                    if (u == ru.NU - 1) U::mask(w[k], 0, ru.V - u * N);
+                } else {
+                    if (u >= ru.glo && u < ru.ghi) w[k] = *reinterpret_cast<const uint4*>(at);
+                    if (ru.sh) w[k] = U::realign(w[k], u + 1 < ru.ghi ? *reinterpret_cast<const uint4*>(at + 16) : U::none4(), ru.sh);
+                    if (u == 0 || u == ru.NU - 1)
+                        U::mask(w[k], u == 0 ? ru.m0 : 0, (int)min((long long)N, (long long)ru.V + ru.m0 - (long long)u * N));
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < UPT; ++k) U::max_add(mx, w[k]);
+        const float m = warp_max_f32(U::max_val(mx, bad));   // (every lane's loads from the stage have ended)
+        if (m == INFINITY) bad = 1u;
+        next();
+        asked = row >= 0 && alive;
+        if (asked) ask();
+        float2 S2 = make_float2(0.f, 0.f), T2 = make_float2(0.f, 0.f);
+        sum_units<T, ENT, UPT>(w, m, L2, S2, T2, [&](int k) { return ua + k * 32 < un; });
+        // (with the token's logit: every warp has read it before any warp can overwrite it with its gradient)
+        bad = __any_sync(0xFFFFFFFFu, bad != 0u || zx != zx) ? 1u : 0u;
+        const float4 mine = make_float4(m, warp_sum(S2.x + S2.y), ENT ? warp_sum(T2.x + T2.y) : 0.f, __uint_as_float(bad));
+        if (CS > 1) {
+            if (lane < CS) st_async_v4(mapa_u32(&part[par][rank * NW + warp], lane), mine, mapa_u32(got, lane));
+            if (alive) {
+                alive = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(got, (uint32_t)(done >> 1) & 1u));
+                if (!alive && lane == 0) atomicOr(p.status, ADASD_STATUS_TIMEOUT);
+            }
+        } else if (NW > 1) {
+            if (lane == 0) part[par][warp] = mine;
+            __syncthreads();
+        }
+        RowStats st;
+        if (NW == 1 && CS == 1) {
+            st.M = m;
+            st.S = bad || !(m > floor_v) ? NAN : mine.y;
+            st.Ts = mine.z;
+            st.zx = zx;
+        } else {
+            st = fold_partials<kScMaxCluster * NW>(part[par], CS * NW, c1, floor_v, zx);
+        }
+        if (!alive) st.S = NAN;
+        if (GRAD) {
+            const RowGrad r = row_grad(p, in, st, L2, ENT);
+            T* const g = reinterpret_cast<T*>(p.grad) + (long long)my_row * p.g_stride;
+            const int ux = ru.unit_of(my_x);
+#pragma unroll
+            for (int k = 0; k < UPT; ++k) {
+                const int u = ua + k * 32 + lane;
+                if (u < un) {
+                    ru.store(g, u, r.zero ? make_uint4(0u, 0u, 0u, 0u) : grad_unit<T, ENT>(w[k], r.c));
+                    if (u == ux && !r.zero) grad_token<T, ENT>(g, my_x, zx, st.M, r.lg2S, c1, r.a, r.b, r.top);
+                }
+            }
+        }
+        if (keeper && lane == 0) {
+            RowHist& h = hist[done & 31];
+            h.s = st;
+            h.row = my_row;
+        }
+        ++done;
+        if (keeper && ((done & 31) == 0 || row < 0)) {       // 32 rows' reports, a lane each
+            __syncwarp();
+            if (lane < ((done - 1) & 31) + 1) row_report(p, hist[lane].row, row_in(p, hist[lane].row), hist[lane].s);
+            __syncwarp();
+        }
+    }
+    if (CS > 1) cluster.sync();                              // (nobody leaves while a warp's partials are on their way to it)
+}
+
+}  // namespace adasd

@@ -30,7 +30,8 @@ struct ScoreParams {
     long long g_stride;
     int32_t n_rows, V, op;
     int32_t cs, per_cta;                           // CTAs per row; 16-byte units of a CTA
-    float temperature, c1;                         // c1: log2 e / temperature
+    float c1;                                      // log2 e / temperature
+    double inv_temp;
     uint32_t* status;
     float* logp;                                   // [n_rows] outputs, nullable
     float* H;
