@@ -8,23 +8,26 @@
 namespace adasd {
 namespace {
 
-inline bool aligned_rows(const void* base, long long stride, int dtype) {
-    return (reinterpret_cast<uintptr_t>(base) & 15u) == 0 && (stride * (dtype == ADASD_BF16 ? 2 : 4)) % 16 == 0;
+inline int unit_elements(int dtype) { return dtype == ADASD_BF16 ? 8 : 4; }
+// Rows that start on 16-byte boundaries and end on one.
+inline bool whole_rows(const void* base, long long stride, int V, int dtype) {
+    const int N = unit_elements(dtype);
+    return (reinterpret_cast<uintptr_t>(base) & 15u) == 0 && stride % N == 0 && V % N == 0;
 }
 // Units of a row, at most.
-inline int row_units(int V, int dtype, bool aligned) {
-    const int N = dtype == ADASD_BF16 ? 8 : 4;
-    return (int)(((long long)V + (aligned ? N - 1 : 2 * N - 2)) / N);
+inline int row_units(int V, int dtype, bool whole) {
+    const int N = unit_elements(dtype);
+    return (int)(((long long)V + (whole ? 0 : 2 * N - 2)) / N);
 }
 
-template <typename T, bool ALIGNED, int NW, int UPT, bool HOLD, bool GRAD, bool ENT>
+template <typename T, bool WHOLE, int NW, int UPT, bool HOLD, bool GRAD, bool ENT>
 int launch(const ScoreParams& p, cudaStream_t stream) {
-    return launch_pdl(score_kernel<T, ALIGNED, NW, UPT, HOLD, GRAD, ENT>, p.n_rows * p.cs, NW * 32, 0, p.cs, stream, p);
+    return launch_pdl(score_kernel<T, WHOLE, NW, UPT, HOLD, GRAD, ENT>, p.n_rows * p.cs, NW * 32, 0, p.cs, stream, p);
 }
-template <typename T, bool ALIGNED, int NW, int UPT, bool HOLD>
+template <typename T, bool WHOLE, int NW, int UPT, bool HOLD>
 int launch(const ScoreParams& p, bool ent, cudaStream_t stream) {
-    if (p.grad) return ent ? launch<T, ALIGNED, NW, UPT, HOLD, true, true>(p, stream) : launch<T, ALIGNED, NW, UPT, HOLD, true, false>(p, stream);
-    return ent ? launch<T, ALIGNED, NW, UPT, HOLD, false, true>(p, stream) : launch<T, ALIGNED, NW, UPT, HOLD, false, false>(p, stream);
+    if (p.grad) return ent ? launch<T, WHOLE, NW, UPT, HOLD, true, true>(p, stream) : launch<T, WHOLE, NW, UPT, HOLD, true, false>(p, stream);
+    return ent ? launch<T, WHOLE, NW, UPT, HOLD, false, true>(p, stream) : launch<T, WHOLE, NW, UPT, HOLD, false, false>(p, stream);
 }
 
 template <typename K>
@@ -49,7 +52,7 @@ int resident_clusters(K kern, int threads, int smem, int cs) {
     return n;
 }
 // Clusters of a kernel that are resident at once, asked for once per device, kernel and cluster size.
-template <typename T, bool ALIGNED, int NW, bool GRAD, bool ENT>
+template <typename T, bool WHOLE, int NW, bool GRAD, bool ENT>
 int stream_clusters(int cs) {
     constexpr int kDevices = 64;
     static std::atomic<int> known[kDevices][kScMaxCluster + 1];
@@ -57,7 +60,7 @@ int stream_clusters(int cs) {
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return 0;
     int n = known[dev][cs].load(std::memory_order_acquire);
     if (n == 0) {
-        const auto kern = score_stream_kernel<T, ALIGNED, NW, GRAD, ENT>;
+        const auto kern = score_stream_kernel<T, WHOLE, NW, GRAD, ENT>;
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NW * kSsStage) != cudaSuccess) {
             cudaGetLastError();
             return 0;
@@ -68,59 +71,59 @@ int stream_clusters(int cs) {
     return n;
 }
 // ADASD_ERR_SHAPE: not a launch for score_stream_kernel (rows too long, or too few of them).
-template <typename T, bool ALIGNED, int NW, bool GRAD, bool ENT>
+template <typename T, bool WHOLE, int NW, bool GRAD, bool ENT>
 int launch_stream_t(ScoreParams p, int cs, int per_warp, cudaStream_t stream) {
-    const int ncl = stream_clusters<T, ALIGNED, NW, GRAD, ENT>(cs);
+    const int ncl = stream_clusters<T, WHOLE, NW, GRAD, ENT>(cs);
     if (p.n_rows <= ncl || ncl == 0) return ADASD_ERR_SHAPE;
     p.cs = cs;
     p.per_cta = per_warp;
-    return launch_pdl(score_stream_kernel<T, ALIGNED, NW, GRAD, ENT>, ncl * cs, NW * 32, NW * kSsStage, cs, stream, p);
+    return launch_pdl(score_stream_kernel<T, WHOLE, NW, GRAD, ENT>, ncl * cs, NW * 32, NW * kSsStage, cs, stream, p);
 }
-template <typename T, bool ALIGNED, int NW>
+template <typename T, bool WHOLE, int NW>
 int launch_stream_n(const ScoreParams& p, bool ent, int cs, int per_warp, cudaStream_t stream) {
-    if (p.grad) return ent ? launch_stream_t<T, ALIGNED, NW, true, true>(p, cs, per_warp, stream) : launch_stream_t<T, ALIGNED, NW, true, false>(p, cs, per_warp, stream);
-    return ent ? launch_stream_t<T, ALIGNED, NW, false, true>(p, cs, per_warp, stream) : launch_stream_t<T, ALIGNED, NW, false, false>(p, cs, per_warp, stream);
+    if (p.grad) return ent ? launch_stream_t<T, WHOLE, NW, true, true>(p, cs, per_warp, stream) : launch_stream_t<T, WHOLE, NW, true, false>(p, cs, per_warp, stream);
+    return ent ? launch_stream_t<T, WHOLE, NW, false, true>(p, cs, per_warp, stream) : launch_stream_t<T, WHOLE, NW, false, false>(p, cs, per_warp, stream);
 }
-template <typename T, bool ALIGNED>
+template <typename T, bool WHOLE>
 int launch_stream(const ScoreParams& p, bool ent, int NU, cudaStream_t stream) {
     constexpr int W = kSsUPT * 32;
     const int warps = (NU + W - 1) / W;
-    if (warps == 1) return launch_stream_n<T, ALIGNED, 1>(p, ent, 1, NU, stream);
-    if (warps == 2) return launch_stream_n<T, ALIGNED, 2>(p, ent, 1, (NU + 1) / 2, stream);
-    if (warps <= 4) return launch_stream_n<T, ALIGNED, 4>(p, ent, 1, (NU + 3) / 4, stream);
+    if (warps == 1) return launch_stream_n<T, WHOLE, 1>(p, ent, 1, NU, stream);
+    if (warps == 2) return launch_stream_n<T, WHOLE, 2>(p, ent, 1, (NU + 1) / 2, stream);
+    if (warps <= 4) return launch_stream_n<T, WHOLE, 4>(p, ent, 1, (NU + 3) / 4, stream);
     const int cs = (warps + 7) / 8;
     if (cs > kScMaxCluster) return ADASD_ERR_SHAPE;
-    return launch_stream_n<T, ALIGNED, 8>(p, ent, cs, (NU + 8 * cs - 1) / (8 * cs), stream);
+    return launch_stream_n<T, WHOLE, 8>(p, ent, cs, (NU + 8 * cs - 1) / (8 * cs), stream);
 }
 
 constexpr int kScNW = 8, kScUnits = kScNW * 32;      // CTAs of 8 warps; units of a CTA and unit a thread
 
-template <typename T, bool ALIGNED>
+template <typename T, bool WHOLE>
 int launch(ScoreParams p, bool ent, int NU, int sms, cudaStream_t stream) {
-    if (const int rc = launch_stream<T, ALIGNED>(p, ent, NU, stream); rc != ADASD_ERR_SHAPE) return rc;
+    if (const int rc = launch_stream<T, WHOLE>(p, ent, NU, stream); rc != ADASD_ERR_SHAPE) return rc;
     if (NU <= 2 * 32 * 4) {
         p.cs = 1;
         p.per_cta = NU;
-        return launch<T, ALIGNED, 2, 4, true>(p, ent, stream);
+        return launch<T, WHOLE, 2, 4, true>(p, ent, stream);
     }
     int cs = std::min(kScMaxCluster, (NU + kScUnits * 16 - 1) / (kScUnits * 16));
     while (cs < kScMaxCluster && (long long)p.n_rows * cs < 2LL * sms && NU > cs * kScUnits) cs = std::min(2 * cs, kScMaxCluster);
     p.cs = cs;
     p.per_cta = (NU + cs - 1) / cs;
-    if (p.per_cta <= kScUnits * 4) return launch<T, ALIGNED, kScNW, 4, true>(p, ent, stream);
-    if (p.per_cta <= kScUnits * 8) return launch<T, ALIGNED, kScNW, 8, true>(p, ent, stream);
-    if (p.per_cta <= kScUnits * 16) return launch<T, ALIGNED, kScNW, 16, true>(p, ent, stream);
-    return launch<T, ALIGNED, kScNW, 16, false>(p, ent, stream);
+    if (p.per_cta <= kScUnits * 4) return launch<T, WHOLE, kScNW, 4, true>(p, ent, stream);
+    if (p.per_cta <= kScUnits * 8) return launch<T, WHOLE, kScNW, 8, true>(p, ent, stream);
+    if (p.per_cta <= kScUnits * 16) return launch<T, WHOLE, kScNW, 16, true>(p, ent, stream);
+    return launch<T, WHOLE, kScNW, 16, false>(p, ent, stream);
 }
 
 }  // namespace
 
 int launch_score(ScoreParams p, int dtype, bool entropy, int sm_count, cudaStream_t stream) {
-    const bool al = aligned_rows(p.z, p.row_stride, dtype) && (!p.grad || aligned_rows(p.grad, p.g_stride, dtype));
-    const int NU = row_units(p.V, dtype, al);
+    const bool whole = whole_rows(p.z, p.row_stride, p.V, dtype) && (!p.grad || whole_rows(p.grad, p.g_stride, p.V, dtype));
+    const int NU = row_units(p.V, dtype, whole);
     if (dtype == ADASD_BF16)
-        return al ? launch<__nv_bfloat16, true>(p, entropy, NU, sm_count, stream) : launch<__nv_bfloat16, false>(p, entropy, NU, sm_count, stream);
-    return al ? launch<float, true>(p, entropy, NU, sm_count, stream) : launch<float, false>(p, entropy, NU, sm_count, stream);
+        return whole ? launch<__nv_bfloat16, true>(p, entropy, NU, sm_count, stream) : launch<__nv_bfloat16, false>(p, entropy, NU, sm_count, stream);
+    return whole ? launch<float, true>(p, entropy, NU, sm_count, stream) : launch<float, false>(p, entropy, NU, sm_count, stream);
 }
 
 int launch_pref_pairs(const PrefParams& p, cudaStream_t stream) {
@@ -128,16 +131,16 @@ int launch_pref_pairs(const PrefParams& p, cudaStream_t stream) {
 }
 
 int launch_pref_grad(PrefParams p, int dtype, cudaStream_t stream) {
-    const bool al = aligned_rows(p.z, p.row_stride, dtype) && aligned_rows(p.grad, p.g_stride, dtype);
-    const int NU = row_units(p.V, dtype, al);
+    const bool whole = whole_rows(p.z, p.row_stride, p.V, dtype) && whole_rows(p.grad, p.g_stride, p.V, dtype);
+    const int NU = row_units(p.V, dtype, whole);
     p.segs = (NU + kPgThreads * kPgUnits - 1) / (kPgThreads * kPgUnits);
     p.per_cta = (NU + p.segs - 1) / p.segs;
     if ((long long)p.n_rows * p.segs > 0x7FFFFFFFLL) return ADASD_ERR_SHAPE;
     const int grid = p.n_rows * p.segs;
     if (dtype == ADASD_BF16)
-        return al ? launch_pdl(pref_grad_kernel<__nv_bfloat16, true>, grid, kPgThreads, 0, 0, stream, p)
+        return whole ? launch_pdl(pref_grad_kernel<__nv_bfloat16, true>, grid, kPgThreads, 0, 0, stream, p)
                   : launch_pdl(pref_grad_kernel<__nv_bfloat16, false>, grid, kPgThreads, 0, 0, stream, p);
-    return al ? launch_pdl(pref_grad_kernel<float, true>, grid, kPgThreads, 0, 0, stream, p)
+    return whole ? launch_pdl(pref_grad_kernel<float, true>, grid, kPgThreads, 0, 0, stream, p)
               : launch_pdl(pref_grad_kernel<float, false>, grid, kPgThreads, 0, 0, stream, p);
 }
 

@@ -16,6 +16,8 @@
 #include "adasd_async.cuh"
 #include "adasd_score_types.cuh"
 
+#include <type_traits>
+
 namespace adasd {
 
 constexpr int kScMaxCluster = 8;
@@ -23,8 +25,9 @@ constexpr float kLowT = -16384.f;          // 2^t = 0 from here down; keeps 0 * 
 
 // A row's units of 16 bytes, aligned in the memory of the array that decides: the gradient's row where one is written
 // (so that whole units are stored at once), else the logits'.  Unit u holds elements u N - m0 .. u N - m0 + N - 1; logits that
-// lie elsewhere relative to 16 bytes are put together from two granules.
-template <typename T, bool ALIGNED>
+// lie elsewhere relative to 16 bytes are put together from two granules.  WHOLE: rows start on 16-byte boundaries and V is
+// a multiple of N, so that no unit needs a look at its ends.
+template <typename T, bool WHOLE>
 struct RowUnits {
     using U = Unit<T>;
     static constexpr int N = U::N;
@@ -35,10 +38,10 @@ struct RowUnits {
 
     __device__ __forceinline__ RowUnits(const T* z, const T* frame, int V_) : V(V_) {
         const unsigned long long a = reinterpret_cast<unsigned long long>(z);
-        if (ALIGNED) {
+        if (WHOLE) {
             src = reinterpret_cast<const uint4*>(z);
             m0 = sh = glo = 0;
-            NU = ghi = (V + N - 1) / N;
+            NU = ghi = V / N;
         } else {
             m0 = (int)((reinterpret_cast<unsigned long long>(frame) & 15ull) / sizeof(T));
             NU = (int)(((long long)m0 + V + N - 1) / N);
@@ -49,41 +52,35 @@ struct RowUnits {
             ghi = (int)((a + (unsigned long long)V * sizeof(T) + 15ull - b) >> 4);
         }
     }
-    // elements outside the row read as -inf
-    __device__ __forceinline__ uint4 load(int u) const {
-        uint4 w;
-        if (ALIGNED) {
-            w = __ldcs(src + u);
-            if (u == NU - 1) U::mask(w, 0, V - u * N);
-            return w;
-        }
-        w = u >= glo && u < ghi ? __ldcs(src + u) : U::none4();
-        if (sh) w = U::realign(w, u + 1 < ghi ? __ldcg(src + u + 1) : U::none4(), sh);
-        if (u == 0 || u == NU - 1) U::mask(w, u == 0 ? m0 : 0, min((long long)N, (long long)V + m0 - (long long)u * N));
+    // unit u from its granule and the next (get(g): granule g of those that hold elements); elements outside the row: -inf
+    template <typename F>
+    __device__ __forceinline__ uint4 unit(int u, F get) const {
+        if (WHOLE) return get(u);
+        uint4 w = u >= glo && u < ghi ? get(u) : U::none4();
+        if (sh) w = U::realign(w, u + 1 < ghi ? get(u + 1) : U::none4(), sh);
+        if (u == 0 || u == NU - 1) U::mask(w, u == 0 ? m0 : 0, (int)min((long long)N, (long long)V + m0 - (long long)u * N));
         return w;
     }
-    // elements of unit u that belong to the row: [lo, hi)
-    __device__ __forceinline__ void bounds(int u, int& lo, int& hi) const {
-        const long long e0 = (long long)u * N - (ALIGNED ? 0 : m0);
-        lo = e0 < 0 ? (int)-e0 : 0;
-        hi = e0 + N > V ? (int)(V - e0) : N;
+    __device__ __forceinline__ uint4 load(int u) const {
+        return unit(u, [&](int g) { return __ldcg(src + g); });
     }
-    __device__ __forceinline__ int unit_of(int v) const { return (int)(((long long)v + (ALIGNED ? 0 : m0)) / N); }
-    // unit u of row g
+    __device__ __forceinline__ int unit_of(int v) const { return (int)(((long long)v + (WHOLE ? 0 : m0)) / N); }
+    // where unit 0 of row g would start
+    __device__ __forceinline__ uint4* frame(T* g) const { return reinterpret_cast<uint4*>(g - (WHOLE ? 0 : m0)); }
     __device__ __forceinline__ void store(T* g, int u, const uint4& w) const {
-        T* const at = g + ((long long)u * N - (ALIGNED ? 0 : m0));
-        int lo, hi;
-        bounds(u, lo, hi);
-        if (hi - lo == N) {
-            __stcs(reinterpret_cast<uint4*>(at), w);
-        } else {
-            const uint32_t* q = &w.x;
+        if (WHOLE || (u != NU - 1 && (u != 0 || m0 == 0))) __stcs(frame(g) + u, w);
+        else store_ends(g, u, w, m0, V);
+    }
+    // the first or the last unit: the elements that belong to the row
+    static __device__ __noinline__ void store_ends(T* g, int u, uint4 w, int m0, int V) {
+        const uint32_t q[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (j >= lo && j < hi) {
-                    if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(at)[j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
-                    else reinterpret_cast<uint32_t*>(at)[j] = q[j];
-                }
+        for (int j = 0; j < N; ++j) {
+            const long long e = (long long)u * N - m0 + j;
+            if (e >= 0 && e < V) {
+                if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(g)[e] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
+                else reinterpret_cast<uint32_t*>(g)[e] = q[j];
+            }
         }
     }
 };
@@ -100,30 +97,38 @@ __device__ __forceinline__ uint4 pack16(const float2 (&v)[2]) {
 __device__ __forceinline__ void put(__nv_bfloat16* at, float v) { *at = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void put(float* at, float v) { *at = v; }
 
-// dL/dz of a unit.  q = log2 p_v; the value is p_v (b + a q), a = -dL/dH ln 2 / T, b = -(dL/dl + dL/dH H) / T.
-struct GradConsts {
-    float2 nm2, L2, nl2, a2, b2;           // -m, log2 e / T, -log2 S, a, b
+// Exponents.  t = (z - m) log2 e / T is formed as fma(z, c1, -s) with s = fl(m c1), one rounding, good however large the
+// logits' common offset; what s is off by is taken back from the sums (at t_m = fma(m, c1, -s), the exponent that the
+// largest logit gets instead of 0).  BIG: offsets or 1 / T so large that t_m is off by whole powers of two: (z - m) c1.
+constexpr float kBigShift = 1e7f;
+struct Shift {
+    float2 L2, ns2, nm2;                   // c1; -s; -m
 };
-template <typename T, bool ENT>
+template <typename T, bool BIG>
+__device__ __forceinline__ void exponents(const uint4& w, const Shift& c, float2 (&q)[Unit<T>::N / 2]) {
+    Unit<T>::unpack_raw(w, q);
+#pragma unroll
+    for (int j = 0; j < Unit<T>::N / 2; ++j)
+        q[j] = BIG ? __fmul2_rn(__fadd2_rn(q[j], c.nm2), c.L2) : __ffma2_rn(q[j], c.L2, c.ns2);
+}
+
+// dL/dz of a unit: 2^q (b + a q).
+struct GradConsts {
+    Shift s;
+    float2 a2, b2;
+};
+template <typename T, bool ENT, bool BIG>
 __device__ __forceinline__ uint4 grad_unit(const uint4& w, const GradConsts& c) {
     using U = Unit<T>;
-    float2 z[U::N / 2];
-    U::unpack_raw(w, z);
+    float2 q[U::N / 2];
+    exponents<T, BIG>(w, c.s, q);
 #pragma unroll
     for (int j = 0; j < U::N / 2; ++j) {
-        float2 q = __ffma2_rn(__fadd2_rn(z[j], c.nm2), c.L2, c.nl2);
-        if (ENT) q = make_float2(fmaxf(q.x, kLowT), fmaxf(q.y, kLowT));
-        const float2 e = make_float2(ex2(q.x), ex2(q.y));
-        z[j] = __fmul2_rn(e, ENT ? __ffma2_rn(q, c.a2, c.b2) : c.b2);
+        if (ENT) q[j] = make_float2(fmaxf(q[j].x, kLowT), fmaxf(q[j].y, kLowT));
+        const float2 e = make_float2(ex2(q[j].x), ex2(q[j].y));
+        q[j] = __fmul2_rn(e, ENT ? __ffma2_rn(q[j], c.a2, c.b2) : c.b2);
     }
-    return pack16(z);
-}
-// ... and of the token's own element, which has dL/dl / T on top
-template <typename T, bool ENT>
-__device__ __forceinline__ void grad_token(T* g, int x, float zx, float m, float lg2S, float c1, float a, float b, float top) {
-    float q = fmaf(zx - m, c1, -lg2S);
-    if (ENT) q = fmaxf(q, kLowT);
-    put(g + x, fmaf(ex2(q), ENT ? fmaf(q, a, b) : b, top));
+    return pack16(q);
 }
 
 // Inputs of a row's loss.
@@ -264,56 +269,92 @@ __device__ __forceinline__ RowStats fold_partials(const float4* part, int n, flo
     return r;
 }
 
-// Sums of a warp's units, held in registers: adds 2^t (and 2^t t) under the maximum m to S2 (T2).  used(k): whether unit k of the
-// lanes can hold anything (warp-uniform).
-template <typename T, bool ENT, int UPT, typename F>
-__device__ __forceinline__ void sum_units(const uint4 (&w)[UPT], float m, float2 L2, float2& S2, float2& T2, F used) {
+// Sums of a warp's units, held in registers, under their largest logit m: {m, S, T}.  Units come in groups of four; used(k):
+// whether group k can hold anything (warp-uniform).
+template <typename T, bool ENT, bool BIG, int UPT, typename F>
+__device__ __forceinline__ float2 sum_units_t(const uint4 (&w)[UPT], const Shift& c, F used) {
     using U = Unit<T>;
-    const float2 nm2 = pair2(m > -INFINITY ? -m : 0.f);
+    float2 S2 = make_float2(0.f, 0.f), T2 = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < UPT; ++k) {
+    for (int k = 0; k < UPT; k += 4) {
         if (used(k)) {
-            float2 v[U::N / 2];
-            U::unpack_raw(w[k], v);
 #pragma unroll
-            for (int j = 0; j < U::N / 2; ++j) {
-                float2 q = __fmul2_rn(__fadd2_rn(v[j], nm2), L2);
-                if (ENT) q = make_float2(fmaxf(q.x, kLowT), fmaxf(q.y, kLowT));
-                const float2 e = make_float2(ex2(q.x), ex2(q.y));
-                S2 = __fadd2_rn(S2, e);
-                if (ENT) T2 = __ffma2_rn(e, q, T2);
+            for (int i = k; i < k + 4; ++i) {
+                float2 q[U::N / 2];
+                exponents<T, BIG>(w[i], c, q);
+#pragma unroll
+                for (int j = 0; j < U::N / 2; ++j) {
+                    if (ENT) q[j] = make_float2(fmaxf(q[j].x, kLowT), fmaxf(q[j].y, kLowT));
+                    const float2 e = make_float2(ex2(q[j].x), ex2(q[j].y));
+                    S2 = __fadd2_rn(S2, e);
+                    if (ENT) T2 = __ffma2_rn(e, q[j], T2);
+                }
             }
         }
     }
+    return make_float2(S2.x + S2.y, T2.x + T2.y);
+}
+template <typename T, bool ENT, int UPT, typename F>
+__device__ __forceinline__ float2 sum_units(const uint4 (&w)[UPT], float m, float c1, float2 L2, F used) {
+    Shift c;
+    c.L2 = L2;
+    const float mm = m > -INFINITY ? m : 0.f, s = mm * c1;
+    if (!(fabsf(s) < kBigShift)) {
+        c.ns2 = c.nm2 = pair2(-mm);
+        float2 r = sum_units_t<T, ENT, true, UPT>(w, c, used);
+        r.x = warp_sum(r.x);
+        if (ENT) r.y = warp_sum(r.y);
+        return r;
+    }
+    c.ns2 = c.nm2 = pair2(-s);
+    float2 r = sum_units_t<T, ENT, false, UPT>(w, c, used);
+    r.x = warp_sum(r.x);
+    if (ENT) r.y = warp_sum(r.y);
+    const float tm = fmaf(mm, c1, -s), em = ex2(tm);
+    if (ENT) r.y = (r.y - __fmul_rn(tm, r.x)) / em;
+    r.x /= em;
+    return r;
 }
 
 // What the gradient of a row takes: its constants, and the token's own element.
 struct RowGrad {
     GradConsts c;
-    float a, b, top, lg2S;
-    bool zero;
+    float a, b, top;
+    bool zero, big;
 };
-__device__ __forceinline__ RowGrad row_grad(const ScoreParams& p, const RowIn& in, const RowStats& s, float2 L2, bool ent) {
+// dL/dz_v = p_v (b + a log2 p_v) = 2^t / S (b + a (t - log2 S)), t = (z_v - M) c1
+__device__ __forceinline__ void grad_consts(RowGrad& r, const RowStats& s, float c1, float2 L2, float a, float b) {
+    const float rS = 1.f / s.S, h = s.M * c1;
+    r.a = a * rS;
+    r.b = fmaf(-a, log2f(s.S), b) * rS;
+    r.big = !(fabsf(h) < kBigShift);
+    r.c.s.L2 = L2;
+    // t = fma(z, c1, -h) + x, x = h - M c1 exactly: 2^x goes to the constants
+    const float x = r.big ? 0.f : -fmaf(s.M, c1, -h), f = ex2(x);
+    r.c.s.ns2 = r.c.s.nm2 = pair2(r.big ? -s.M : -h);
+    r.c.a2 = pair2(f * r.a);
+    r.c.b2 = pair2(f * fmaf(r.a, x, r.b));
+}
+// The token's own element has dL/dl / T on top.
+template <typename T, bool ENT>
+__device__ __forceinline__ void grad_token(T* g, int x, float zx, float m, float c1, const RowGrad& r) {
+    float t = (zx - m) * c1;
+    if (ENT) t = fmaxf(t, kLowT);
+    put(g + x, fmaf(ex2(t), ENT ? fmaf(t, r.a, r.b) : r.b, r.top));
+}
+__device__ __forceinline__ RowGrad row_grad(const ScoreParams& p, const RowIn& in, const RowStats& s, float c1, float2 L2, bool ent) {
     RowGrad r;
     const float lnS = logf(s.S), H = ent ? lnS - kLn2 * (s.Ts / s.S) : 0.f, iT = (float)p.inv_temp;
     const float2 d = row_coefs(p, in, s, lnS, H);
     r.zero = d.x == 0.f && d.y == 0.f;
     r.top = d.x * iT;
-    r.a = ent ? -kLn2 * d.y * iT : 0.f;
-    r.b = (ent ? fmaf(-d.y, H, -d.x) : -d.x) * iT;
-    r.lg2S = log2f(s.S);
-    r.c.nm2 = pair2(-s.M);
-    r.c.L2 = L2;
-    r.c.nl2 = pair2(-r.lg2S);
-    r.c.a2 = pair2(r.a);
-    r.c.b2 = pair2(r.b);
+    grad_consts(r, s, c1, L2, ent ? -kLn2 * d.y * iT : 0.f, (ent ? fmaf(-d.y, H, -d.x) : -d.x) * iT);
     return r;
 }
-
-// ALIGNED: rows of logits and gradient start on 16-byte boundaries.  NW warps a CTA, UPT units a thread.  HOLD: a CTA's units
+// WHOLE: as RowUnits.  NW warps a CTA, UPT units a thread.  HOLD: a CTA's units
 // fit its registers; else (rows longer than the cluster holds) they are taken in turn and read again for the gradient.
 // GRAD: a gradient is written.  ENT: the entropy or its gradient is wanted.
-template <typename T, bool ALIGNED, int NW, int UPT, bool HOLD, bool GRAD, bool ENT>
+template <typename T, bool WHOLE, int NW, int UPT, bool HOLD, bool GRAD, bool ENT>
 __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_constant__ ScoreParams p) {
     using U = Unit<T>;
     constexpr int N = U::N, NT = NW * 32;
@@ -327,7 +368,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
 
     const T* const z = reinterpret_cast<const T*>(p.z) + (long long)row * p.row_stride;
     T* const g = GRAD ? reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride : nullptr;
-    const RowUnits<T, ALIGNED> ru(z, GRAD ? g : z, p.V);
+    const RowUnits<T, WHOLE> ru(z, GRAD ? g : z, p.V);
     const int u0 = min(rank * p.per_cta, ru.NU), u1 = min(u0 + p.per_cta, ru.NU);
     const int x = __ldcg(p.tok + row), kind = row_kind(p, row, x);       // (the same in every CTA of the cluster)
     if (kind != 1) {
@@ -343,8 +384,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
     // ---- sums -----------------------------------------------------------------------------
     const float c1 = p.c1;
     const float2 L2 = pair2(c1);
-    float m = -INFINITY;
-    float2 S2 = make_float2(0.f, 0.f), T2 = make_float2(0.f, 0.f);
+    float m = -INFINITY, S = 0.f, Ts = 0.f;
     uint32_t bad = 0u;
     uint4 w[UPT];
     for (int base = u0; base < u1; base += NT * UPT) {
@@ -358,20 +398,21 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
         for (int k = 0; k < UPT; ++k) U::max_add(mx, w[k]);
         const float t = warp_max_f32(U::max_val(mx, bad));
         if (t == INFINITY) bad = 1u;
-        if (t > m) {
-            const float d = fmaxf((m - t) * c1, kLowT), f = ex2(d);
-            if (ENT) {
-                T2.x = f * fmaf(d, S2.x, T2.x);
-                T2.y = f * fmaf(d, S2.y, T2.y);
-            }
-            S2.x *= f;
-            S2.y *= f;
+        const float2 r = sum_units<T, ENT, UPT>(w, t, c1, L2, [&](int k) { return base + k * NT < u1; });
+        if (HOLD) {
             m = t;
+            S = r.x;
+            Ts = r.y;
+        } else {                                    // fold it into what came before
+            const float n = fmaxf(m, t), d0 = m > -INFINITY ? fmaxf((m - n) * c1, kLowT) : kLowT, d1 = t > -INFINITY ? fmaxf((t - n) * c1, kLowT) : kLowT;
+            const float f0 = ex2(d0), f1 = ex2(d1);
+            Ts = f0 * fmaf(d0, S, Ts) + f1 * fmaf(d1, r.x, r.y);
+            S = f0 * S + f1 * r.x;
+            m = n;
         }
-        sum_units<T, ENT, UPT>(w, m, L2, S2, T2, [&](int k) { return base + k * NT < u1; });
     }
     bad = __any_sync(0xFFFFFFFFu, bad) ? 1u : 0u;
-    const float4 mine = make_float4(m, warp_sum(S2.x + S2.y), ENT ? warp_sum(T2.x + T2.y) : 0.f, __uint_as_float(bad));
+    const float4 mine = make_float4(m, S, Ts, __uint_as_float(bad));
     if (CS > 1) {
         cluster.barrier_wait();
         if (lane < CS) *cluster.map_shared_rank(part + rank * NW + warp, lane) = mine;
@@ -385,7 +426,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
 
     // ---- gradient ---------------------------------------------------------------------------
     if (GRAD) {
-        const RowGrad r = row_grad(p, in, st, L2, ENT);
+        const RowGrad r = row_grad(p, in, st, c1, L2, ENT);
         const int ux = ru.unit_of(x);
         for (int base = u0; base < u1; base += NT * UPT) {
 #pragma unroll
@@ -393,8 +434,8 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
                 const int u = base + k * NT + (int)threadIdx.x;
                 if (u < u1) {
                     const uint4 v = HOLD || r.zero ? w[k] : ru.load(u);
-                    ru.store(g, u, r.zero ? make_uint4(0u, 0u, 0u, 0u) : grad_unit<T, ENT>(v, r.c));
-                    if (u == ux && !r.zero) grad_token<T, ENT>(g, x, zx, st.M, r.lg2S, c1, r.a, r.b, r.top);
+                    ru.store(g, u, r.zero ? make_uint4(0u, 0u, 0u, 0u) : r.big ? grad_unit<T, ENT, true>(v, r.c) : grad_unit<T, ENT, false>(v, r.c));
+                    if (u == ux && !r.zero) grad_token<T, ENT>(g, x, zx, st.M, c1, r);
                 }
             }
             if (HOLD) break;
@@ -495,7 +536,7 @@ __global__ void __launch_bounds__(kPairThreads) pref_pair_kernel(const __grid_co
 // Gradient of rows whose statistics and dL/dl are known: dL/dz_v = dL/dl (1[v = x] - p_v) / T.  From the last row to the
 // first: what the L2 still holds of score_kernel's reads is read first.
 constexpr int kPgThreads = 256, kPgUnits = 8;
-template <typename T, bool ALIGNED>
+template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kPgThreads) pref_grad_kernel(const __grid_constant__ PrefParams p) {
     using U = Unit<T>;
     const int back = (int)(blockIdx.x / (unsigned)p.segs), seg = (int)(blockIdx.x - (unsigned)back * (unsigned)p.segs);
@@ -507,7 +548,7 @@ __global__ void __launch_bounds__(kPgThreads) pref_grad_kernel(const __grid_cons
     if (kind < 0) return;
     const T* const z = reinterpret_cast<const T*>(p.z) + (long long)row * p.row_stride;
     T* const g = reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride;
-    const RowUnits<T, ALIGNED> ru(z, g, p.V);
+    const RowUnits<T, WHOLE> ru(z, g, p.V);
     const int u0 = min(seg * p.per_cta, ru.NU), u1 = min(u0 + p.per_cta, ru.NU);
     if (kind == 0 || e.z == 0.f) {
         for (int u = u0 + (int)threadIdx.x; u < u1; u += kPgThreads) ru.store(g, u, make_uint4(0u, 0u, 0u, 0u));
@@ -523,21 +564,20 @@ __global__ void __launch_bounds__(kPgThreads) pref_grad_kernel(const __grid_cons
     float zx = 0.f;
     if (ux >= u0 && ux < u1) zx = to_f32(z[x]);      // (of its CTA alone: another may have written its gradient there)
     __syncthreads();
-    const float iT = 1.f / p.temperature, top = e.z * iT, lg2S = log2f(e.y);
-    GradConsts c;
-    c.nm2 = pair2(-e.x);
-    c.L2 = pair2(p.c1);
-    c.nl2 = pair2(-lg2S);
-    c.a2 = pair2(0.f);
-    c.b2 = pair2(-top);
+    RowGrad r;
+    const RowStats st{e.x, e.y, 0.f, zx};
+    r.top = e.z / p.temperature;
+    grad_consts(r, st, p.c1, pair2(p.c1), 0.f, -r.top);
+    auto write = [&](auto big) {
 #pragma unroll
-    for (int k = 0; k < kPgUnits; ++k) {
-        const int u = u0 + k * kPgThreads + (int)threadIdx.x;
-        if (u < u1) {
-            ru.store(g, u, grad_unit<T, false>(w[k], c));
-            if (u == ux) grad_token<T, false>(g, x, zx, e.x, lg2S, p.c1, 0.f, -top, top);
+        for (int k = 0; k < kPgUnits; ++k) {
+            const int u = u0 + k * kPgThreads + (int)threadIdx.x;
+            if (u < u1) ru.store(g, u, grad_unit<T, false, decltype(big)::value>(w[k], r.c));
         }
-    }
+    };
+    if (r.big) write(std::true_type{});
+    else write(std::false_type{});
+    if (ux >= u0 && ux < u1 && threadIdx.x == (unsigned)(ux - u0) % kPgThreads) grad_token<T, false>(g, x, zx, e.x, p.c1, r);
 }
 
 }  // namespace adasd

@@ -24,7 +24,7 @@ struct RowWindow {
     unsigned todo, zero;                                     // lanes with rows to do, with gradient rows to zero
 };
 
-template <typename T, bool ALIGNED, int NW, bool GRAD, bool ENT>
+template <typename T, bool WHOLE, int NW, bool GRAD, bool ENT>
 __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __grid_constant__ ScoreParams p) {
     using U = Unit<T>;
     constexpr int N = U::N, UPT = kSsUPT;
@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
     const int ua = (rank * NW + warp) * p.per_cta, ub = ua + p.per_cta;          // (per_cta: units of a WARP here)
     auto units = [&](int row) {
         const T* const z = reinterpret_cast<const T*>(p.z) + (long long)row * p.row_stride;
-        return RowUnits<T, ALIGNED>(z, GRAD ? reinterpret_cast<const T*>(p.grad) + (long long)row * p.g_stride : z, p.V);
+        return RowUnits<T, WHOLE>(z, GRAD ? reinterpret_cast<const T*>(p.grad) + (long long)row * p.g_stride : z, p.V);
     };
     RowWindow win;
     auto open = [&](int wi) {
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
     auto zero_row = [&]() {                                  // one row set aside
         const int j = __ffs(win.zero) - 1, row = __shfl_sync(0xFFFFFFFFu, win.row, j);
         win.zero &= win.zero - 1;
-        const RowUnits<T, ALIGNED> ru = units(row);
+        const RowUnits<T, WHOLE> ru = units(row);
         T* const g = reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride;
         for (int u = ua + lane; u < min(ub, ru.NU); u += 32) ru.store(g, u, make_uint4(0u, 0u, 0u, 0u));
     };
@@ -94,8 +94,8 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
     };
     auto ask = [&]() {                                       // its stretch: granules from unit ua's first on that hold elements
         if (lane == 0) {
-            const RowUnits<T, ALIGNED> ru = units(row);
-            const int g0 = max(ua, ru.glo), g1 = min(min(ub, ru.NU) + (!ALIGNED && ru.sh ? 1 : 0), ru.ghi);
+            const RowUnits<T, WHOLE> ru = units(row);
+            const int g0 = max(ua, ru.glo), g1 = min(min(ub, ru.NU) + (!WHOLE && ru.sh ? 1 : 0), ru.ghi);
             const uint32_t bytes = (uint32_t)max(g1 - g0, 0) * 16u;
             mbar_expect_tx(full, bytes);
             if (bytes) bulk_g2s(stage + (g0 - ua) * 16, ru.src + g0, bytes, full);
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
     int done = 0;
     while (row >= 0) {
         const int my_row = row, my_x = x, par = done & 1;
-        const RowUnits<T, ALIGNED> ru = units(my_row);
+        const RowUnits<T, WHOLE> ru = units(my_row);
         const int un = min(ub, ru.NU);
         const float zx = to_f32((reinterpret_cast<const T*>(p.z) + (long long)my_row * p.row_stride)[my_x]);
         RowIn in;
@@ -134,19 +134,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
 #pragma unroll
         for (int k = 0; k < UPT; ++k) {
             const int u = ua + k * 32 + lane;
-            w[k] = U::none4();
-            if (u < un) {
-                const unsigned char* const at = stage + (k * 32 + lane) * 16;
-                if (ALIGNED) {
-                    w[k] = *reinterpret_cast<const uint4*>(at);
-                    if (u == ru.NU - 1) U::mask(w[k], 0, ru.V - u * N);
-                } else {
-                    if (u >= ru.glo && u < ru.ghi) w[k] = *reinterpret_cast<const uint4*>(at);
-                    if (ru.sh) w[k] = U::realign(w[k], u + 1 < ru.ghi ? *reinterpret_cast<const uint4*>(at + 16) : U::none4(), ru.sh);
-                    if (u == 0 || u == ru.NU - 1)
-                        U::mask(w[k], u == 0 ? ru.m0 : 0, (int)min((long long)N, (long long)ru.V + ru.m0 - (long long)u * N));
-                }
-            }
+            w[k] = u < un ? ru.unit(u, [&](int g) { return *reinterpret_cast<const uint4*>(stage + (g - ua) * 16); }) : U::none4();
         }
 #pragma unroll
         for (int k = 0; k < UPT; ++k) U::max_add(mx, w[k]);
@@ -155,11 +143,10 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         next();
         asked = row >= 0 && alive;
         if (asked) ask();
-        float2 S2 = make_float2(0.f, 0.f), T2 = make_float2(0.f, 0.f);
-        sum_units<T, ENT, UPT>(w, m, L2, S2, T2, [&](int k) { return ua + k * 32 < un; });
+        const float2 sums = sum_units<T, ENT, UPT>(w, m, c1, L2, [&](int k) { return ua + k * 32 < un; });
         // (with the token's logit: every warp has read it before any warp can overwrite it with its gradient)
         bad = __any_sync(0xFFFFFFFFu, bad != 0u || zx != zx) ? 1u : 0u;
-        const float4 mine = make_float4(m, warp_sum(S2.x + S2.y), ENT ? warp_sum(T2.x + T2.y) : 0.f, __uint_as_float(bad));
+        const float4 mine = make_float4(m, sums.x, sums.y, __uint_as_float(bad));
         if (CS > 1) {
             if (lane < CS) st_async_v4(mapa_u32(&part[par][rank * NW + warp], lane), mine, mapa_u32(got, lane));
             if (alive) {
@@ -181,16 +168,28 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         }
         if (!alive) st.S = NAN;
         if (GRAD) {
-            const RowGrad r = row_grad(p, in, st, L2, ENT);
+            const RowGrad r = row_grad(p, in, st, c1, L2, ENT);
             T* const g = reinterpret_cast<T*>(p.grad) + (long long)my_row * p.g_stride;
-            const int ux = ru.unit_of(my_x);
+            auto write = [&](auto big) {
 #pragma unroll
-            for (int k = 0; k < UPT; ++k) {
-                const int u = ua + k * 32 + lane;
-                if (u < un) {
-                    ru.store(g, u, r.zero ? make_uint4(0u, 0u, 0u, 0u) : grad_unit<T, ENT>(w[k], r.c));
-                    if (u == ux && !r.zero) grad_token<T, ENT>(g, my_x, zx, st.M, r.lg2S, c1, r.a, r.b, r.top);
+                for (int k = 0; k < UPT; k += 4) {
+                    if (ua + k * 32 < un) {
+#pragma unroll
+                        for (int i = k; i < k + 4; ++i) {
+                            const int u = ua + i * 32 + lane;
+                            const uint4 v = grad_unit<T, ENT, decltype(big)::value>(w[i], r.c);
+                            if (u < un) ru.store(g, u, v);
+                        }
+                    }
                 }
+            };
+            if (r.zero) {
+                for (int u = ua + lane; u < un; u += 32) ru.store(g, u, make_uint4(0u, 0u, 0u, 0u));
+            } else {
+                if (r.big) write(std::true_type{});
+                else write(std::false_type{});
+                const int o = ru.unit_of(my_x) - ua;          // the lane that wrote the token's element writes it again
+                if (o >= 0 && o < un - ua && lane == (o & 31)) grad_token<T, ENT>(g, my_x, zx, st.M, c1, r);
             }
         }
         if (keeper && lane == 0) {
