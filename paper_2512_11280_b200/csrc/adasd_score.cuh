@@ -238,24 +238,23 @@ __device__ __forceinline__ int row_kind(const ScoreParams& p, int row, int x) {
     return row_out(p, row, x) ? 0 : 1;
 }
 
-// Totals of a row from its warps' partials {m, S, T, bad}, by a whole warp, in the same order in every warp.
-template <int MOST>
-__device__ __forceinline__ RowStats fold_partials(const float4* part, int n, float c1, float floor_v, float zx) {
+// Totals of a row from its warps' partials {m, S (NaN: unusable), T, the token's logit or -inf}, by a whole warp, in the same
+// order in every warp.  get(k): partial k of n.
+template <int MOST, typename F>
+__device__ __forceinline__ RowStats fold_partials(F get, int n, float c1, float floor_v) {
     constexpr int PL = MOST > 32 ? 2 : 1;  // partials of a lane
     const int lane = threadIdx.x & 31;
     float4 q[PL];
     RowStats r;
-    r.M = -INFINITY;
-    r.zx = zx;
-    uint32_t any = 0u;
+    r.M = r.zx = -INFINITY;
 #pragma unroll
     for (int k = 0; k < PL; ++k) {
-        q[k] = lane + 32 * k < n ? part[lane + 32 * k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        q[k] = lane + 32 * k < n ? get(lane + 32 * k) : make_float4(-INFINITY, 0.f, 0.f, -INFINITY);
         r.M = fmaxf(r.M, q[k].x);
-        any |= __float_as_uint(q[k].w);
+        r.zx = fmaxf(r.zx, q[k].w);
     }
     r.M = warp_max_f32(r.M);
-    const bool none = __any_sync(0xFFFFFFFFu, any) || !(r.M > floor_v);
+    r.zx = warp_max_f32(r.zx);
     r.S = r.Ts = 0.f;
 #pragma unroll
     for (int k = 0; k < PL; ++k) {
@@ -265,7 +264,7 @@ __device__ __forceinline__ RowStats fold_partials(const float4* part, int n, flo
     }
     r.S = warp_sum(r.S);
     r.Ts = warp_sum(r.Ts);
-    if (none) r.S = NAN;
+    if (!(r.M > floor_v)) r.S = NAN;
     return r;
 }
 
@@ -411,8 +410,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
             m = n;
         }
     }
-    bad = __any_sync(0xFFFFFFFFu, bad) ? 1u : 0u;
-    const float4 mine = make_float4(m, S, Ts, __uint_as_float(bad));
+    const float4 mine = make_float4(m, __any_sync(0xFFFFFFFFu, bad) ? NAN : S, Ts, zx);
     if (CS > 1) {
         cluster.barrier_wait();
         if (lane < CS) *cluster.map_shared_rank(part + rank * NW + warp, lane) = mine;
@@ -422,7 +420,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
         __syncthreads();
     }
     if (!GRAD && (rank != 0 || warp != 0)) return;
-    const RowStats st = fold_partials<kScMaxCluster * NW>(part, CS * NW, c1, floor_v, zx);
+    const RowStats st = fold_partials<kScMaxCluster * NW>([&](int k) { return part[k]; }, CS * NW, c1, floor_v);
 
     // ---- gradient ---------------------------------------------------------------------------
     if (GRAD) {

@@ -13,6 +13,8 @@ namespace adasd {
 constexpr int kSsUPT = 16;                                   // units a lane holds
 constexpr int kSsStage = (kSsUPT * 32 + 1) * 16;             // a warp's stretch (+ one unit: rows off 16-byte boundaries)
 
+// What a warp keeps of 32 rows: inputs of their losses, until they are used (GRAD); its partials and the rows, until they are
+// folded (forward pass); the rows' statistics, until they are reported (GRAD, one warp of a cluster).
 struct __align__(16) RowHist {
     RowStats s;
     int32_t row, pad[3];
@@ -30,9 +32,11 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
     constexpr int N = U::N, UPT = kSsUPT;
     const float floor_v = N == 8 ? ADASD_FLOOR_BF : kFloor;
     extern __shared__ __align__(128) unsigned char dyn_smem[];
-    __shared__ float4 part[2][kScMaxCluster * NW];
+    __shared__ float4 part[2][GRAD ? kScMaxCluster * NW : 1];
     __shared__ unsigned long long full_s[NW], got_s[2];
-    __shared__ RowHist hist[32];
+    __shared__ RowHist hist[GRAD ? 32 : 1];
+    __shared__ float4 keep[NW][32];                          // GRAD: RowIn of the window's rows; else the partials of 32 rows
+    __shared__ int2 rows_s[GRAD ? 1 : 32];                   // ... and which rows, with their tokens
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int CS = p.cs, ncl = (int)(gridDim.x / (unsigned)CS), cl = (int)(blockIdx.x / (unsigned)CS);
     const int rank = (int)(blockIdx.x - (unsigned)cl * (unsigned)CS);
@@ -69,6 +73,13 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
             kind = row_kind(p, (int)r, win.x);
             if (keeper && kind != 1) row_report_out(p, (int)r, kind);
         }
+        if (GRAD) {
+            RowIn in{0.f, 0.f, 0.f, 0.f};
+            if (kind == 1) in = row_in(p, (int)r);
+            __syncwarp();
+            keep[warp][lane] = make_float4(in.adv, in.old, in.ref, in.w);
+            __syncwarp();
+        }
         win.todo = __ballot_sync(0xFFFFFFFFu, kind == 1);
         win.zero = GRAD ? __ballot_sync(0xFFFFFFFFu, kind == 0) : 0u;
     };
@@ -80,6 +91,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         for (int u = ua + lane; u < min(ub, ru.NU); u += 32) ru.store(g, u, make_uint4(0u, 0u, 0u, 0u));
     };
     int row = -1, x = 0;                                     // the row asked for; -1: none left
+    float4 inputs;                                           // of its loss
     auto next = [&]() {
         while (!win.todo) {
             while (GRAD && win.zero) zero_row();
@@ -91,6 +103,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         win.todo &= win.todo - 1;
         row = __shfl_sync(0xFFFFFFFFu, win.row, j);
         x = __shfl_sync(0xFFFFFFFFu, win.x, j);
+        if (GRAD) inputs = keep[warp][j];
     };
     auto ask = [&]() {                                       // its stretch: granules from unit ua's first on that hold elements
         if (lane == 0) {
@@ -117,11 +130,9 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         const int my_row = row, my_x = x, par = done & 1;
         const RowUnits<T, WHOLE> ru = units(my_row);
         const int un = min(ub, ru.NU);
-        const float zx = to_f32((reinterpret_cast<const T*>(p.z) + (long long)my_row * p.row_stride)[my_x]);
-        RowIn in;
-        if (GRAD) in = row_in(p, my_row);
+        const RowIn in{inputs.x, inputs.y, inputs.z, inputs.w};
         uint64_t* const got = reinterpret_cast<uint64_t*>(&got_s[par]);
-        if (CS > 1 && warp == 0 && lane == 0) mbar_expect_tx(got, (uint32_t)(CS * NW) * 16u);
+        if (GRAD && CS > 1 && warp == 0 && lane == 0) mbar_expect_tx(got, (uint32_t)(CS * NW) * 16u);
         if (asked) {
             const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(full, ph));
             if (!ok && lane == 0) atomicOr(p.status, ADASD_STATUS_TIMEOUT);
@@ -138,15 +149,48 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         }
 #pragma unroll
         for (int k = 0; k < UPT; ++k) U::max_add(mx, w[k]);
-        const float m = warp_max_f32(U::max_val(mx, bad));   // (every lane's loads from the stage have ended)
+        // the token's logit, if it is in this stretch
+        const int ox = ru.unit_of(my_x) - ua;
+        float zx = -INFINITY;
+        if (ox >= 0 && ox < un - ua) {
+            const int e = my_x - ((ua + ox) * N - ru.m0) + ru.sh;           // (of the two granules that hold its unit)
+            zx = to_f32(*reinterpret_cast<const T*>(stage + ox * 16 + e * (int)sizeof(T)));
+        }
+        if (zx != zx) bad = 1u;
+        const float m = warp_max_f32(fmaxf(U::max_val(mx, bad), zx));       // (every lane's loads from the stage have ended)
         if (m == INFINITY) bad = 1u;
         next();
         asked = row >= 0 && alive;
         if (asked) ask();
         const float2 sums = sum_units<T, ENT, UPT>(w, m, c1, L2, [&](int k) { return ua + k * 32 < un; });
-        // (with the token's logit: every warp has read it before any warp can overwrite it with its gradient)
-        bad = __any_sync(0xFFFFFFFFu, bad != 0u || zx != zx) ? 1u : 0u;
-        const float4 mine = make_float4(m, sums.x, sums.y, __uint_as_float(bad));
+        const float4 mine = make_float4(m, __any_sync(0xFFFFFFFFu, bad) ? NAN : sums.x, sums.y, zx);
+        if (!GRAD) {
+            // forward pass: nothing waits for the totals; 32 rows are folded and reported at a time, by all warps of the cluster
+            if (lane == 0) {
+                keep[warp][done & 31] = mine;
+                if (warp == 0) rows_s[done & 31] = make_int2(my_row, my_x);
+            }
+            ++done;
+            if ((done & 31) == 0 || row < 0) {
+                const int n = ((done - 1) & 31) + 1;
+                if (CS > 1) cluster.sync();
+                else __syncthreads();
+                RowStats st;
+                int cnt = 0, which = 0;
+                for (int j = rank * NW + warp; j < n; j += CS * NW, ++cnt) {
+                    const RowStats f = fold_partials<kScMaxCluster * NW>(
+                        [&](int k) { return *cluster.map_shared_rank(&keep[k % NW][j], k / NW); }, CS * NW, c1, floor_v);
+                    if (lane == cnt) {
+                        st = f;
+                        which = j;
+                    }
+                }
+                if (lane < cnt) row_report(p, rows_s[which].x, row_in(p, rows_s[which].x), st);
+                if (CS > 1) cluster.sync();
+                else __syncthreads();
+            }
+            continue;
+        }
         if (CS > 1) {
             if (lane < CS) st_async_v4(mapa_u32(&part[par][rank * NW + warp], lane), mine, mapa_u32(got, lane));
             if (alive) {
@@ -160,11 +204,11 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         RowStats st;
         if (NW == 1 && CS == 1) {
             st.M = m;
-            st.S = bad || !(m > floor_v) ? NAN : mine.y;
+            st.S = m > floor_v ? mine.y : NAN;
             st.Ts = mine.z;
             st.zx = zx;
         } else {
-            st = fold_partials<kScMaxCluster * NW>(part[par], CS * NW, c1, floor_v, zx);
+            st = fold_partials<kScMaxCluster * NW>([&](int k) { return part[par][k]; }, CS * NW, c1, floor_v);
         }
         if (!alive) st.S = NAN;
         if (GRAD) {
@@ -188,8 +232,8 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
             } else {
                 if (r.big) write(std::true_type{});
                 else write(std::false_type{});
-                const int o = ru.unit_of(my_x) - ua;          // the lane that wrote the token's element writes it again
-                if (o >= 0 && o < un - ua && lane == (o & 31)) grad_token<T, ENT>(g, my_x, zx, st.M, c1, r);
+                // (the lane that wrote the token's element writes it again)
+                if (ox >= 0 && ox < un - ua && lane == (ox & 31)) grad_token<T, ENT>(g, my_x, zx, st.M, c1, r);
             }
         }
         if (keeper && lane == 0) {
@@ -204,7 +248,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
             __syncwarp();
         }
     }
-    if (CS > 1) cluster.sync();                              // (nobody leaves while a warp's partials are on their way to it)
+    if (GRAD && CS > 1) cluster.sync();                      // (nobody leaves while a warp's partials are on their way to it)
 }
 
 }  // namespace adasd
