@@ -20,6 +20,7 @@ ADASD_KMAX_LIMIT = 32
 STATUS_CAPACITY, STATUS_TIMEOUT, STATUS_NAN = 1, 2, 4
 PREF_SIGMOID, PREF_SQUARED, PREF_HINGE = 0, 1, 2
 PREF_SCRATCH_PER_ROW = 16
+_PREF_RULES = {"sigmoid": PREF_SIGMOID, "squared": PREF_SQUARED, "hinge": PREF_HINGE}
 ERR_NULL, ERR_ALIGN, ERR_SHAPE, ERR_DTYPE, ERR_CAPACITY, ERR_CUDA, ERR_DEVICE = -1, -2, -3, -4, -5, -7, -9
 
 
@@ -267,6 +268,7 @@ class Context:
         self._token_logprob, self._token_logprob_grad = L.adasd_token_logprob, L.adasd_token_logprob_grad
         self._policy_loss, self._preference_loss = L.adasd_policy_loss, L.adasd_preference_loss
         self._logit_dtype = torch.bfloat16 if dtype == ADASD_BF16 else torch.float32
+        self._i32, self._f32, self._index = torch.int32, torch.float32, self.device.index
         self._raw_stream = torch._C._cuda_getCurrentRawStream
         self._rec = None                           # the last record's addresses and their struct
 
@@ -384,69 +386,70 @@ class Context:
                     "adasd_set_warpers")
 
     # ---- scoring and training on given tokens: rows of logits [n, V], their tokens [n] ----------------
+    # (Every check is a call into torch of 60 to 100 ns, and a launch takes about as long as ten of them on the host: the
+    # checks are kept to one pass over the arguments.)
 
-    def _rows(self, where: str, logits, tokens, grad=None) -> int:
-        """The number of rows, after the checks that addresses alone do not allow."""
-        n = logits.shape[0] if logits.dim() == 2 else -1
-        for t in (logits,) if grad is None else (logits, grad):
-            if t.dim() != 2 or t.shape[0] != n or t.shape[1] != self.V or (t.stride(1) != 1 and self.V > 1):
-                raise AdasdError(ERR_SHAPE, where)
-            if t.dtype is not self._logit_dtype:
-                raise AdasdError(ERR_DTYPE, where)
-            if t.device != self.device:
-                raise AdasdError(ERR_DEVICE, where)
-        self._arrays(where, self.torch.int32, n, tokens)
-        return n
+    def _rows(self, where: str, logits):
+        """(address, row stride, rows) of logits, after the checks that addresses alone do not allow."""
+        if logits.dtype is not self._logit_dtype:
+            raise AdasdError(ERR_DTYPE, where)
+        if logits.get_device() != self._index:
+            raise AdasdError(ERR_DEVICE, where)
+        shape, strides, V = logits.shape, logits.stride(), self.V
+        if len(shape) != 2 or shape[1] != V or (strides[1] != 1 and V > 1):
+            raise AdasdError(ERR_SHAPE, where)
+        n, stride = shape[0], strides[0]
+        return logits.data_ptr(), stride if n > 1 or stride > V else V, n      # (the stride of a single row says nothing)
 
-    def _arrays(self, where: str, dtype, n: int, *arrays) -> None:
-        """Contiguous device arrays of at least n entries (each may be None)."""
+    def _arrays(self, where: str, dtype, n: int, arrays) -> list:
+        """Addresses of contiguous device arrays of at least n entries; None for None."""
+        index, got = self._index, []
         for t in arrays:
             if t is None:
-                continue
-            if t.dtype is not dtype:
-                raise AdasdError(ERR_DTYPE, where)
-            if t.numel() < n or not t.is_contiguous():
-                raise AdasdError(ERR_SHAPE, where)
-            if t.device != self.device:
-                raise AdasdError(ERR_DEVICE, where)
-
-    def _row_stride(self, t) -> int:
-        return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), self.V)   # (of a single row it says nothing)
+                got.append(None)
+            elif t.dtype is dtype and t.get_device() == index and t.numel() >= n and t.is_contiguous():
+                got.append(t.data_ptr())
+            else:
+                raise AdasdError(ERR_DTYPE if t.dtype is not dtype else ERR_DEVICE if t.get_device() != index else ERR_SHAPE,
+                                 where)
+        return got
 
     def token_logprob(self, logits, tokens, logp_out, entropy_out=None, lse_out=None) -> None:
-        n = self._rows("adasd_token_logprob", logits, tokens)
-        self._arrays("adasd_token_logprob", self.torch.float32, n, logp_out, entropy_out, lse_out)
-        rc = self._token_logprob(self.handle, logits.data_ptr(), self._row_stride(logits), tokens.data_ptr(), n,
-                                 logp_out.data_ptr(), None if entropy_out is None else entropy_out.data_ptr(),
-                                 None if lse_out is None else lse_out.data_ptr(), self._raw_stream(self.device.index))
+        z, stride, n = self._rows("adasd_token_logprob", logits)
+        tok, = self._arrays("adasd_token_logprob", self._i32, n, (tokens,))
+        lp, ent, lse = self._arrays("adasd_token_logprob", self._f32, n, (logp_out, entropy_out, lse_out))
+        rc = self._token_logprob(self.handle, z, stride, tok, n, lp, ent, lse, self._raw_stream(self._index))
         if rc:
             raise AdasdError(rc, "adasd_token_logprob")
 
     def token_logprob_grad(self, logits, tokens, grad_logp, grad_out, grad_entropy=None) -> None:
-        n = self._rows("adasd_token_logprob_grad", logits, tokens, grad_out)
-        self._arrays("adasd_token_logprob_grad", self.torch.float32, n, grad_logp, grad_entropy)
-        rc = self._token_logprob_grad(self.handle, logits.data_ptr(), self._row_stride(logits), tokens.data_ptr(), n,
-                                      grad_logp.data_ptr(), None if grad_entropy is None else grad_entropy.data_ptr(),
-                                      grad_out.data_ptr(), self._row_stride(grad_out),
-                                      self._raw_stream(self.device.index))
+        where = "adasd_token_logprob_grad"
+        (z, stride, n), (g, g_stride, n_out) = self._rows(where, logits), self._rows(where, grad_out)
+        if n_out != n:
+            raise AdasdError(ERR_SHAPE, where)
+        tok, = self._arrays(where, self._i32, n, (tokens,))
+        dl, dH = self._arrays(where, self._f32, n, (grad_logp, grad_entropy))
+        rc = self._token_logprob_grad(self.handle, z, stride, tok, n, dl, dH, g, g_stride, self._raw_stream(self._index))
         if rc:
-            raise AdasdError(rc, "adasd_token_logprob_grad")
+            raise AdasdError(rc, where)
 
     def policy_loss(self, logits, tokens, advantage, row_loss_out, old_logp=None, ref_logp=None, weight=None,
                     clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0,
                     scale: float = 1.0, loss_out=None, logp_out=None, entropy_out=None, kl_out=None,
                     grad_out=None) -> None:
         where = "adasd_policy_loss"
-        n = self._rows(where, logits, tokens, grad_out)
-        self._arrays(where, self.torch.float32, n, advantage, row_loss_out, old_logp, ref_logp, weight, logp_out,
-                     entropy_out, kl_out)
-        self._arrays(where, self.torch.float32, 1, loss_out)
-        rc = self._policy_loss(self.handle, logits.data_ptr(), self._row_stride(logits), tokens.data_ptr(), n,
-                               advantage.data_ptr(), _ptr(old_logp), _ptr(ref_logp), _ptr(weight),
-                               C.byref(PolicyOptions(clip_low, clip_high, kl_coef, entropy_coef, scale)),
-                               row_loss_out.data_ptr(), _ptr(loss_out), _ptr(logp_out), _ptr(entropy_out), _ptr(kl_out),
-                               _ptr(grad_out), 0 if grad_out is None else self._row_stride(grad_out),
-                               self._raw_stream(self.device.index))
+        (z, stride, n), g, g_stride = self._rows(where, logits), None, 0
+        if grad_out is not None:
+            g, g_stride, n_out = self._rows(where, grad_out)
+            if n_out != n:
+                raise AdasdError(ERR_SHAPE, where)
+        tok, = self._arrays(where, self._i32, n, (tokens,))
+        adv, rl, old, ref, w, lp, ent, kl = self._arrays(where, self._f32, n, (advantage, row_loss_out, old_logp, ref_logp,
+                                                                              weight, logp_out, entropy_out, kl_out))
+        total, = self._arrays(where, self._f32, 1, (loss_out,))
+        rc = self._policy_loss(self.handle, z, stride, tok, n, adv, old, ref, w,
+                               PolicyOptions(clip_low, clip_high, kl_coef, entropy_coef, scale), rl, total, lp, ent, kl,
+                               g, g_stride, self._raw_stream(self._index))
         if rc:
             raise AdasdError(rc, where)
 
@@ -456,26 +459,27 @@ class Context:
                         grad_out=None) -> None:
         """rule: "sigmoid", "squared" or "hinge"; scratch: a device tensor of PREF_SCRATCH_PER_ROW bytes a row."""
         where = "adasd_preference_loss"
-        n, f32 = self._rows(where, logits, tokens, grad_out), self.torch.float32
-        if seq_start.numel() % 2 == 0:
+        (z, stride, n), g, g_stride = self._rows(where, logits), None, 0
+        if grad_out is not None:
+            g, g_stride, n_out = self._rows(where, grad_out)
+            if n_out != n:
+                raise AdasdError(ERR_SHAPE, where)
+        starts = seq_start.numel()
+        pairs = starts // 2
+        if starts % 2 == 0:
             raise AdasdError(ERR_SHAPE, where)
-        pairs = seq_start.numel() // 2
-        self._arrays(where, self.torch.int32, 1, seq_start)
-        self._arrays(where, f32, 2 * pairs, seq_logp_out, ref_logp)
-        self._arrays(where, f32, pairs, pair_loss_out, pair_weight)
-        self._arrays(where, f32, 1, loss_out)
-        self._arrays(where, scratch.dtype, -(-PREF_SCRATCH_PER_ROW * n // scratch.element_size()), scratch)
-        if rule not in ("sigmoid", "squared", "hinge"):
+        if rule not in _PREF_RULES:
             raise AdasdError(ERR_DTYPE, where)
-        rule_id = PREF_SIGMOID if rule == "sigmoid" else PREF_SQUARED if rule == "squared" else PREF_HINGE
-        rc = self._preference_loss(self.handle, logits.data_ptr(), self._row_stride(logits), tokens.data_ptr(), n,
-                                   seq_start.data_ptr(), pairs, _ptr(ref_logp), _ptr(pair_weight),
-                                   C.byref(PreferenceOptions(rule_id, 1 if average else 0, beta, margin,
-                                                             label_smoothing, scale)),
-                                   scratch.data_ptr(), seq_logp_out.data_ptr(), pair_loss_out.data_ptr(),
-                                   _ptr(loss_out), _ptr(grad_out),
-                                   0 if grad_out is None else self._row_stride(grad_out),
-                                   self._raw_stream(self.device.index))
+        tok, = self._arrays(where, self._i32, n, (tokens,))
+        start, = self._arrays(where, self._i32, 1, (seq_start,))
+        seq, ref = self._arrays(where, self._f32, 2 * pairs, (seq_logp_out, ref_logp))
+        pl, pw = self._arrays(where, self._f32, pairs, (pair_loss_out, pair_weight))
+        total, = self._arrays(where, self._f32, 1, (loss_out,))
+        sc, = self._arrays(where, scratch.dtype, -(-PREF_SCRATCH_PER_ROW * n // scratch.element_size()), (scratch,))
+        rc = self._preference_loss(self.handle, z, stride, tok, n, start, pairs, ref, pw,
+                                   PreferenceOptions(_PREF_RULES[rule], 1 if average else 0, beta, margin, label_smoothing,
+                                                     scale),
+                                   sc, seq, pl, total, g, g_stride, self._raw_stream(self._index))
         if rc:
             raise AdasdError(rc, where)
 

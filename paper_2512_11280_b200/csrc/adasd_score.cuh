@@ -67,20 +67,34 @@ struct RowUnits {
     __device__ __forceinline__ int unit_of(int v) const { return (int)(((long long)v + (WHOLE ? 0 : m0)) / N); }
     // where unit 0 of row g would start
     __device__ __forceinline__ uint4* frame(T* g) const { return reinterpret_cast<uint4*>(g - (WHOLE ? 0 : m0)); }
-    __device__ __forceinline__ void store(T* g, int u, const uint4& w) const {
-        if (WHOLE || (u != NU - 1 && (u != 0 || m0 == 0))) __stcs(frame(g) + u, w);
-        else store_ends(g, u, w, m0, V);
+    // units that lie in the row from end to end: [whole_lo, whole_hi)
+    __device__ __forceinline__ int whole_lo() const { return WHOLE || m0 == 0 ? 0 : 1; }
+    __device__ __forceinline__ int whole_hi() const { return WHOLE || (m0 + V) % N == 0 ? NU : NU - 1; }
+    // for the gradient alone: unit u whose elements outside the row hold anything (the nearest granules that may be read)
+    __device__ __forceinline__ uint4 load_any(int u) const {
+        if (WHOLE) return __ldcg(src + u);
+        uint4 w = __ldcg(src + min(max(u, glo), ghi - 1));
+        if (sh) w = U::realign(w, __ldcg(src + min(max(u + 1, glo), ghi - 1)), sh);
+        return w;
     }
-    // the first or the last unit: the elements that belong to the row
-    static __device__ __noinline__ void store_ends(T* g, int u, uint4 w, int m0, int V) {
-        const uint32_t q[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const long long e = (long long)u * N - m0 + j;
-            if (e >= 0 && e < V) {
-                if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(g)[e] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
-                else reinterpret_cast<uint32_t*>(g)[e] = q[j];
-            }
+    // unit u of row g where it is the row's first or last and not whole: its elements, one a lane (by a whole warp)
+    __device__ __forceinline__ void store_end(T* g, int u, const uint4& w) const {
+        const int j = threadIdx.x & 31;
+        const long long e = (long long)u * N - m0 + j;
+        const uint32_t q = j * (int)sizeof(T) < 8 ? (j * (int)sizeof(T) < 4 ? w.x : w.y) : (j * (int)sizeof(T) < 12 ? w.z : w.w);
+        if (j < N && e >= 0 && e < V) {
+            if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(g)[e] = (uint16_t)(q >> (16 * (j & 1)));
+            else reinterpret_cast<uint32_t*>(g)[e] = q;
+        }
+    }
+    // ... and units of zeros, [u0, u1) by the threads t, t + n, .. of a group of whole warps
+    __device__ __forceinline__ void store_zeros(T* g, int u0, int u1, int t, int n) const {
+        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+        const int lo = max(u0, whole_lo()), hi = min(u1, whole_hi());
+        for (int u = lo + t; u < hi; u += n) __stcs(frame(g) + u, zero);
+        if (!WHOLE && t < 32) {
+            if (u0 < u1 && u0 < whole_lo()) store_end(g, 0, zero);
+            if (u0 < u1 && u1 > whole_hi() && NU - 1 >= whole_lo()) store_end(g, NU - 1, zero);
         }
     }
 };
@@ -350,6 +364,19 @@ __device__ __forceinline__ RowGrad row_grad(const ScoreParams& p, const RowIn& i
     grad_consts(r, s, c1, L2, ent ? -kLn2 * d.y * iT : 0.f, (ent ? fmaf(-d.y, H, -d.x) : -d.x) * iT);
     return r;
 }
+// ... by the thread that wrote it: of the NT that dealt units [u0, u1) among themselves, whole ones lo .. hi - 1; the ends' by
+// the first warp
+template <typename T, bool ENT, int NT>
+__device__ __forceinline__ void grad_token_by(T* g, int x, int ux, int u0, int u1, int lo, int hi, float zx, float m, float c1,
+                                              const RowGrad& r) {
+    if (ux < u0 || ux >= u1) return;
+    const unsigned t = ux >= lo && ux < hi ? (unsigned)(ux - u0) % NT : 0u;
+    if ((threadIdx.x >> 5) == (t >> 5)) {
+        __syncwarp();
+        if (threadIdx.x == t) grad_token<T, ENT>(g, x, zx, m, c1, r);
+    }
+}
+
 // WHOLE: as RowUnits.  NW warps a CTA, UPT units a thread.  HOLD: a CTA's units
 // fit its registers; else (rows longer than the cluster holds) they are taken in turn and read again for the gradient.
 // GRAD: a gradient is written.  ENT: the entropy or its gradient is wanted.
@@ -372,7 +399,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
     const int x = __ldcg(p.tok + row), kind = row_kind(p, row, x);       // (the same in every CTA of the cluster)
     if (kind != 1) {
         if (GRAD)
-            for (int u = u0 + (int)threadIdx.x; u < u1; u += NT) ru.store(g, u, make_uint4(0u, 0u, 0u, 0u));
+            ru.store_zeros(g, u0, u1, (int)threadIdx.x, NT);
         if (rank == 0 && threadIdx.x == 0) row_report_out(p, row, kind);
         return;
     }
@@ -425,18 +452,30 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
     // ---- gradient ---------------------------------------------------------------------------
     if (GRAD) {
         const RowGrad r = row_grad(p, in, st, c1, L2, ENT);
-        const int ux = ru.unit_of(x);
-        for (int base = u0; base < u1; base += NT * UPT) {
-#pragma unroll
-            for (int k = 0; k < UPT; ++k) {
-                const int u = base + k * NT + (int)threadIdx.x;
-                if (u < u1) {
-                    const uint4 v = HOLD || r.zero ? w[k] : ru.load(u);
-                    ru.store(g, u, r.zero ? make_uint4(0u, 0u, 0u, 0u) : r.big ? grad_unit<T, ENT, true>(v, r.c) : grad_unit<T, ENT, false>(v, r.c));
-                    if (u == ux && !r.zero) grad_token<T, ENT>(g, x, zx, st.M, c1, r);
+        if (r.zero) {
+            ru.store_zeros(g, u0, u1, (int)threadIdx.x, NT);
+        } else {
+            const int lo = max(u0, ru.whole_lo()), hi = min(u1, ru.whole_hi());
+            auto write = [&](auto big) {
+                constexpr bool BIG = decltype(big)::value;
+                // (the ends first: what follows may overwrite the logits they are made of)
+                if (!WHOLE && warp == 0 && u0 < u1) {
+                    if (u0 < ru.whole_lo()) ru.store_end(g, 0, grad_unit<T, ENT, BIG>(ru.load_any(0), r.c));
+                    if (u1 > ru.whole_hi() && ru.NU - 1 >= ru.whole_lo()) ru.store_end(g, ru.NU - 1, grad_unit<T, ENT, BIG>(ru.load_any(ru.NU - 1), r.c));
                 }
-            }
-            if (HOLD) break;
+                for (int base = u0; base < u1; base += NT * UPT) {
+#pragma unroll
+                    for (int k = 0; k < UPT; ++k) {
+                        const int u = base + k * NT + (int)threadIdx.x;
+                        if (u >= lo && u < hi) __stcs(ru.frame(g) + u, grad_unit<T, ENT, BIG>(HOLD ? w[k] : ru.load_any(u), r.c));
+                    }
+                    if (HOLD) break;
+                }
+            };
+            if (r.big) write(std::true_type{});
+            else write(std::false_type{});
+            const int ux = ru.unit_of(x);
+            grad_token_by<T, ENT, NT>(g, x, ux, u0, u1, lo, hi, zx, st.M, c1, r);
         }
     }
     if (rank == 0 && threadIdx.x == 0) row_report(p, row, in, st);
@@ -549,16 +588,17 @@ __global__ void __launch_bounds__(kPgThreads) pref_grad_kernel(const __grid_cons
     const RowUnits<T, WHOLE> ru(z, g, p.V);
     const int u0 = min(seg * p.per_cta, ru.NU), u1 = min(u0 + p.per_cta, ru.NU);
     if (kind == 0 || e.z == 0.f) {
-        for (int u = u0 + (int)threadIdx.x; u < u1; u += kPgThreads) ru.store(g, u, make_uint4(0u, 0u, 0u, 0u));
+        ru.store_zeros(g, u0, u1, (int)threadIdx.x, kPgThreads);
         return;
     }
     const int x = __ldcg(p.tok + row), ux = ru.unit_of(x);
-    uint4 w[kPgUnits];
+    uint4 w[kPgUnits], first, last;
 #pragma unroll
-    for (int k = 0; k < kPgUnits; ++k) {
-        const int u = u0 + k * kPgThreads + (int)threadIdx.x;
-        w[k] = u < u1 ? ru.load(u) : U::none4();
-    }
+    for (int k = 0; k < kPgUnits; ++k) w[k] = ru.load_any(min(u0 + k * kPgThreads + (int)threadIdx.x, u1 - 1));
+    const int lo = max(u0, ru.whole_lo()), hi = min(u1, ru.whole_hi());
+    const bool has_first = !WHOLE && u0 < ru.whole_lo(), has_last = !WHOLE && u1 > ru.whole_hi() && ru.NU - 1 >= ru.whole_lo();
+    if (has_first) first = ru.load_any(0);
+    if (has_last) last = ru.load_any(ru.NU - 1);
     float zx = 0.f;
     if (ux >= u0 && ux < u1) zx = to_f32(z[x]);      // (of its CTA alone: another may have written its gradient there)
     __syncthreads();
@@ -567,15 +607,20 @@ __global__ void __launch_bounds__(kPgThreads) pref_grad_kernel(const __grid_cons
     r.top = e.z / p.temperature;
     grad_consts(r, st, p.c1, pair2(p.c1), 0.f, -r.top);
     auto write = [&](auto big) {
+        constexpr bool BIG = decltype(big)::value;
 #pragma unroll
         for (int k = 0; k < kPgUnits; ++k) {
             const int u = u0 + k * kPgThreads + (int)threadIdx.x;
-            if (u < u1) ru.store(g, u, grad_unit<T, false, decltype(big)::value>(w[k], r.c));
+            if (u >= lo && u < hi) __stcs(ru.frame(g) + u, grad_unit<T, false, BIG>(w[k], r.c));
+        }
+        if (threadIdx.x < 32) {
+            if (has_first) ru.store_end(g, 0, grad_unit<T, false, BIG>(first, r.c));
+            if (has_last) ru.store_end(g, ru.NU - 1, grad_unit<T, false, BIG>(last, r.c));
         }
     };
     if (r.big) write(std::true_type{});
     else write(std::false_type{});
-    if (ux >= u0 && ux < u1 && threadIdx.x == (unsigned)(ux - u0) % kPgThreads) grad_token<T, false>(g, x, zx, e.x, p.c1, r);
+    grad_token_by<T, false, kPgThreads>(g, x, ux, u0, u1, lo, hi, zx, e.x, p.c1, r);
 }
 
 }  // namespace adasd

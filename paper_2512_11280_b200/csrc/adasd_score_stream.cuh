@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         win.zero &= win.zero - 1;
         const RowUnits<T, WHOLE> ru = units(row);
         T* const g = reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride;
-        for (int u = ua + lane; u < min(ub, ru.NU); u += 32) ru.store(g, u, make_uint4(0u, 0u, 0u, 0u));
+        ru.store_zeros(g, ua, min(ub, ru.NU), lane, 32);
     };
     int row = -1, x = 0;                                     // the row asked for; -1: none left
     float4 inputs;                                           // of its loss
@@ -140,27 +140,47 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         }
         ph ^= 1u;
         uint32_t bad = alive ? 0u : 1u;
-        uint4 w[UPT];
+        // Off 16-byte boundaries: what the row's first and last granules hold of its neighbours becomes -inf, in the stage.  Element
+        // e of the row is element e + off of the granules.
+        const int off = WHOLE ? 0 : ru.m0 + ru.sh;
+        const bool ends = !WHOLE && ua < un && (ua == 0 || un == ru.NU);
+        if (ends) {
+            T* const s = reinterpret_cast<T*>(stage) - (long long)ua * N;
+            const long long after = (long long)off + ru.V + lane;
+            if (ua == 0 && lane < off) put(s + lane, -INFINITY);
+            if (un == ru.NU && after < (long long)(ru.NU + 1) * N) put(s + after, -INFINITY);
+            __syncwarp();
+        }
+        auto held = [&](int u) {                             // unit u, with the granules around it in the stage
+            const uint4* const at = reinterpret_cast<const uint4*>(stage) + (u - ua);
+            return WHOLE || ru.sh == 0 ? *at : U::realign(at[0], at[1], ru.sh);
+        };
+        uint4 w[UPT], last;
         typename U::Max mx = U::max0();
 #pragma unroll
         for (int k = 0; k < UPT; ++k) {
             const int u = ua + k * 32 + lane;
-            w[k] = u < un ? ru.unit(u, [&](int g) { return *reinterpret_cast<const uint4*>(stage + (g - ua) * 16); }) : U::none4();
+            w[k] = u < un ? held(u) : U::none4();
         }
+        const bool has_last = GRAD && !WHOLE && ua < un && un > ru.whole_hi() && ru.NU - 1 >= ru.whole_lo();
+        if (has_last) last = held(ru.NU - 1);
 #pragma unroll
         for (int k = 0; k < UPT; ++k) U::max_add(mx, w[k]);
         // the token's logit, if it is in this stretch
         const int ox = ru.unit_of(my_x) - ua;
         float zx = -INFINITY;
         if (ox >= 0 && ox < un - ua) {
-            const int e = my_x - ((ua + ox) * N - ru.m0) + ru.sh;           // (of the two granules that hold its unit)
-            zx = to_f32(*reinterpret_cast<const T*>(stage + ox * 16 + e * (int)sizeof(T)));
+            zx = to_f32(*(reinterpret_cast<const T*>(stage) + (my_x + (long long)off - (long long)ua * N)));
         }
         if (zx != zx) bad = 1u;
         const float m = warp_max_f32(fmaxf(U::max_val(mx, bad), zx));       // (every lane's loads from the stage have ended)
         if (m == INFINITY) bad = 1u;
         next();
         asked = row >= 0 && alive;
+        if (ends) {                                          // (the copy comes after what was written to the stage)
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+        }
         if (asked) ask();
         const float2 sums = sum_units<T, ENT, UPT>(w, m, c1, L2, [&](int k) { return ua + k * 32 < un; });
         const float4 mine = make_float4(m, __any_sync(0xFFFFFFFFu, bad) ? NAN : sums.x, sums.y, zx);
@@ -214,25 +234,34 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         if (GRAD) {
             const RowGrad r = row_grad(p, in, st, c1, L2, ENT);
             T* const g = reinterpret_cast<T*>(p.grad) + (long long)my_row * p.g_stride;
+            const int lo = max(ua, ru.whole_lo()), hi = min(un, ru.whole_hi());
             auto write = [&](auto big) {
+                constexpr bool BIG = decltype(big)::value;
 #pragma unroll
                 for (int k = 0; k < UPT; k += 4) {
                     if (ua + k * 32 < un) {
 #pragma unroll
                         for (int i = k; i < k + 4; ++i) {
                             const int u = ua + i * 32 + lane;
-                            const uint4 v = grad_unit<T, ENT, decltype(big)::value>(w[i], r.c);
-                            if (u < un) ru.store(g, u, v);
+                            const uint4 v = grad_unit<T, ENT, BIG>(w[i], r.c);
+                            if ((WHOLE || i > 0 || u >= lo) && u < hi) __stcs(ru.frame(g) + u, v);
                         }
                     }
                 }
+                if (!WHOLE && ua == 0 && ua < un && ru.whole_lo() > 0) {
+                    const uint4 f = make_uint4(__shfl_sync(0xFFFFFFFFu, w[0].x, 0), __shfl_sync(0xFFFFFFFFu, w[0].y, 0),
+                                               __shfl_sync(0xFFFFFFFFu, w[0].z, 0), __shfl_sync(0xFFFFFFFFu, w[0].w, 0));
+                    ru.store_end(g, 0, grad_unit<T, ENT, BIG>(f, r.c));
+                }
+                if (has_last) ru.store_end(g, ru.NU - 1, grad_unit<T, ENT, BIG>(last, r.c));
             };
             if (r.zero) {
-                for (int u = ua + lane; u < un; u += 32) ru.store(g, u, make_uint4(0u, 0u, 0u, 0u));
+                ru.store_zeros(g, ua, un, lane, 32);
             } else {
                 if (r.big) write(std::true_type{});
                 else write(std::false_type{});
-                // (the lane that wrote the token's element writes it again)
+                // the token's own element, by a lane of the warp that wrote it
+                __syncwarp();
                 if (ox >= 0 && ox < un - ua && lane == (ox & 31)) grad_token<T, ENT>(g, my_x, zx, st.M, c1, r);
             }
         }
