@@ -1,6 +1,6 @@
 // Launches of the scoring and loss kernels (adasd_score.cuh).
 #include "adasd_launch.cuh"
-#include "adasd_score_stream.cuh"
+#include "adasd_score_deep.cuh"
 
 #include <algorithm>
 #include <atomic>
@@ -84,6 +84,32 @@ int launch_stream_n(const ScoreParams& p, bool ent, int cs, int per_warp, cudaSt
     if (p.grad) return ent ? launch_stream_t<T, WHOLE, NW, true, true>(p, cs, per_warp, stream) : launch_stream_t<T, WHOLE, NW, true, false>(p, cs, per_warp, stream);
     return ent ? launch_stream_t<T, WHOLE, NW, false, true>(p, cs, per_warp, stream) : launch_stream_t<T, WHOLE, NW, false, false>(p, cs, per_warp, stream);
 }
+template <typename T, bool WHOLE, bool ENT>
+int launch_deep_t(ScoreParams p, int cs, int per_warp, cudaStream_t stream) {
+    static std::atomic<int> known[64][kScMaxCluster + 1];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return ADASD_ERR_SHAPE;
+    int ncl = known[dev][cs].load(std::memory_order_acquire);
+    const auto kern = score_deep_kernel<T, WHOLE, ENT>;
+    if (ncl == 0) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSdSmem) != cudaSuccess) {
+            cudaGetLastError();
+            return ADASD_ERR_SHAPE;
+        }
+        ncl = resident_clusters(kern, kSdThreads, kSdSmem, cs);
+        known[dev][cs].store(ncl, std::memory_order_release);
+    }
+    if (p.n_rows <= 2 * ncl || ncl == 0) return ADASD_ERR_SHAPE;
+    p.cs = cs;
+    p.per_cta = per_warp;
+    return launch_pdl(kern, ncl * cs, kSdThreads, kSdSmem, cs, stream, p);
+}
+template <typename T, bool WHOLE>
+int launch_deep(const ScoreParams& p, bool ent, int NU, cudaStream_t stream) {
+    const int its = (NU + 31) / 32, cs = (NU + kSdUnits - 1) / kSdUnits, per = (its + cs - 1) / cs * 32;
+    if (!p.grad || cs > kScMaxCluster || NU < 2048) return ADASD_ERR_SHAPE;
+    return ent ? launch_deep_t<T, WHOLE, true>(p, cs, per, stream) : launch_deep_t<T, WHOLE, false>(p, cs, per, stream);
+}
 template <typename T, bool WHOLE>
 int launch_stream(const ScoreParams& p, bool ent, int NU, cudaStream_t stream) {
     constexpr int W = kSsUPT * 32;
@@ -100,6 +126,7 @@ constexpr int kScNW = 8, kScUnits = kScNW * 32;      // CTAs of 8 warps; units o
 
 template <typename T, bool WHOLE>
 int launch(ScoreParams p, bool ent, int NU, int sms, cudaStream_t stream) {
+    if (const int rc = launch_deep<T, WHOLE>(p, ent, NU, stream); rc != ADASD_ERR_SHAPE) return rc;
     if (const int rc = launch_stream<T, WHOLE>(p, ent, NU, stream); rc != ADASD_ERR_SHAPE) return rc;
     if (NU <= 2 * 32 * 4) {
         p.cs = 1;

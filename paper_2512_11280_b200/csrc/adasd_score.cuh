@@ -115,15 +115,21 @@ __device__ __forceinline__ void put(float* at, float v) { *at = v; }
 // logits' common offset; what s is off by is taken back from the sums (at t_m = fma(m, c1, -s), the exponent that the
 // largest logit gets instead of 0).  BIG: offsets or 1 / T so large that t_m is off by whole powers of two: (z - m) c1.
 constexpr float kBigShift = 1e7f;
+__device__ __forceinline__ bool big_shift(float m, float c1) { return !(fabsf(m * c1) < kBigShift) || !(c1 < kBigShift); }
 struct Shift {
     float2 L2, ns2, nm2;                   // c1; -s; -m
 };
-template <typename T, bool BIG>
+// ENT: the exponents are factors too and have to be finite: logits of -inf (of bf16 rows: two at a time) or exponents are clamped.
+template <typename T, bool ENT, bool BIG>
 __device__ __forceinline__ void exponents(const uint4& w, const Shift& c, float2 (&q)[Unit<T>::N / 2]) {
-    Unit<T>::unpack_raw(w, q);
+    constexpr bool CLAMP = ENT && !BIG;
+    if (CLAMP && sizeof(T) == 2) Unit<T>::unpack(w, q);
+    else Unit<T>::unpack_raw(w, q);
 #pragma unroll
-    for (int j = 0; j < Unit<T>::N / 2; ++j)
+    for (int j = 0; j < Unit<T>::N / 2; ++j) {
         q[j] = BIG ? __fmul2_rn(__fadd2_rn(q[j], c.nm2), c.L2) : __ffma2_rn(q[j], c.L2, c.ns2);
+        if (ENT && !(CLAMP && sizeof(T) == 2)) q[j] = make_float2(fmaxf(q[j].x, kLowT), fmaxf(q[j].y, kLowT));
+    }
 }
 
 // dL/dz of a unit: 2^q (b + a q).
@@ -135,10 +141,9 @@ template <typename T, bool ENT, bool BIG>
 __device__ __forceinline__ uint4 grad_unit(const uint4& w, const GradConsts& c) {
     using U = Unit<T>;
     float2 q[U::N / 2];
-    exponents<T, BIG>(w, c.s, q);
+    exponents<T, ENT, BIG>(w, c.s, q);
 #pragma unroll
     for (int j = 0; j < U::N / 2; ++j) {
-        if (ENT) q[j] = make_float2(fmaxf(q[j].x, kLowT), fmaxf(q[j].y, kLowT));
         const float2 e = make_float2(ex2(q[j].x), ex2(q[j].y));
         q[j] = __fmul2_rn(e, ENT ? __ffma2_rn(q[j], c.a2, c.b2) : c.b2);
     }
@@ -256,7 +261,7 @@ __device__ __forceinline__ int row_kind(const ScoreParams& p, int row, int x) {
 // order in every warp.  get(k): partial k of n.
 template <int MOST, typename F>
 __device__ __forceinline__ RowStats fold_partials(F get, int n, float c1, float floor_v) {
-    constexpr int PL = MOST > 32 ? 2 : 1;  // partials of a lane
+    constexpr int PL = (MOST + 31) / 32;      // partials of a lane
     const int lane = threadIdx.x & 31;
     float4 q[PL];
     RowStats r;
@@ -282,51 +287,53 @@ __device__ __forceinline__ RowStats fold_partials(F get, int n, float c1, float 
     return r;
 }
 
-// Sums of a warp's units, held in registers, under their largest logit m: {m, S, T}.  Units come in groups of four; used(k):
-// whether group k can hold anything (warp-uniform).
-template <typename T, bool ENT, bool BIG, int UPT, typename F>
-__device__ __forceinline__ float2 sum_units_t(const uint4 (&w)[UPT], const Shift& c, F used) {
-    using U = Unit<T>;
-    float2 S2 = make_float2(0.f, 0.f), T2 = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int k = 0; k < UPT; k += 4) {
-        if (used(k)) {
-#pragma unroll
-            for (int i = k; i < k + 4; ++i) {
-                float2 q[U::N / 2];
-                exponents<T, BIG>(w[i], c, q);
-#pragma unroll
-                for (int j = 0; j < U::N / 2; ++j) {
-                    if (ENT) q[j] = make_float2(fmaxf(q[j].x, kLowT), fmaxf(q[j].y, kLowT));
-                    const float2 e = make_float2(ex2(q[j].x), ex2(q[j].y));
-                    S2 = __fadd2_rn(S2, e);
-                    if (ENT) T2 = __ffma2_rn(e, q[j], T2);
-                }
-            }
-        }
-    }
-    return make_float2(S2.x + S2.y, T2.x + T2.y);
-}
-template <typename T, bool ENT, int UPT, typename F>
-__device__ __forceinline__ float2 sum_units(const uint4 (&w)[UPT], float m, float c1, float2 L2, F used) {
+// Sums of a warp's units under their largest logit m: what sum_units returns is {S, T} of the whole warp.
+__device__ __forceinline__ bool sum_big(float m, float c1) { return m > -INFINITY && big_shift(m, c1); }
+__device__ __forceinline__ Shift sum_shift(float m, float c1, float2 L2) {
     Shift c;
     c.L2 = L2;
-    const float mm = m > -INFINITY ? m : 0.f, s = mm * c1;
-    if (!(fabsf(s) < kBigShift)) {
-        c.ns2 = c.nm2 = pair2(-mm);
-        float2 r = sum_units_t<T, ENT, true, UPT>(w, c, used);
-        r.x = warp_sum(r.x);
-        if (ENT) r.y = warp_sum(r.y);
-        return r;
+    const float mm = m > -INFINITY ? m : 0.f;
+    c.ns2 = c.nm2 = pair2(sum_big(m, c1) ? -mm : -(mm * c1));
+    return c;
+}
+template <typename T, bool ENT, bool BIG>
+__device__ __forceinline__ void add_unit(const uint4& w, const Shift& c, float2& S2, float2& T2) {
+    using U = Unit<T>;
+    float2 q[U::N / 2];
+    exponents<T, ENT, BIG>(w, c, q);
+#pragma unroll
+    for (int j = 0; j < U::N / 2; ++j) {
+        const float2 e = make_float2(ex2(q[j].x), ex2(q[j].y));
+        S2 = __fadd2_rn(S2, e);
+        if (ENT) T2 = __ffma2_rn(e, q[j], T2);
     }
-    c.ns2 = c.nm2 = pair2(-s);
-    float2 r = sum_units_t<T, ENT, false, UPT>(w, c, used);
-    r.x = warp_sum(r.x);
-    if (ENT) r.y = warp_sum(r.y);
-    const float tm = fmaf(mm, c1, -s), em = ex2(tm);
+}
+template <bool ENT>
+__device__ __forceinline__ float2 finish_sums(float2 S2, float2 T2, float m, float c1) {
+    float2 r = make_float2(warp_sum(S2.x + S2.y), ENT ? warp_sum(T2.x + T2.y) : 0.f);
+    if (sum_big(m, c1)) return r;
+    const float mm = m > -INFINITY ? m : 0.f, tm = fmaf(mm, c1, -(mm * c1)), em = ex2(tm);
     if (ENT) r.y = (r.y - __fmul_rn(tm, r.x)) / em;
     r.x /= em;
     return r;
+}
+// Units held in registers, in groups of four; used(k): whether group k can hold anything (warp-uniform).
+template <typename T, bool ENT, int UPT, typename F>
+__device__ __forceinline__ float2 sum_units(const uint4 (&w)[UPT], float m, float c1, float2 L2, F used) {
+    const Shift c = sum_shift(m, c1, L2);
+    float2 S2 = make_float2(0.f, 0.f), T2 = make_float2(0.f, 0.f);
+    auto all = [&](auto big) {
+#pragma unroll
+        for (int k = 0; k < UPT; k += 4) {
+            if (used(k)) {
+#pragma unroll
+                for (int i = k; i < k + 4; ++i) add_unit<T, ENT, decltype(big)::value>(w[i], c, S2, T2);
+            }
+        }
+    };
+    if (sum_big(m, c1)) all(std::true_type{});
+    else all(std::false_type{});
+    return finish_sums<ENT>(S2, T2, m, c1);
 }
 
 // What the gradient of a row takes: its constants, and the token's own element.
@@ -340,7 +347,7 @@ __device__ __forceinline__ void grad_consts(RowGrad& r, const RowStats& s, float
     const float rS = 1.f / s.S, h = s.M * c1;
     r.a = a * rS;
     r.b = fmaf(-a, log2f(s.S), b) * rS;
-    r.big = !(fabsf(h) < kBigShift);
+    r.big = big_shift(s.M, c1);
     r.c.s.L2 = L2;
     // t = fma(z, c1, -h) + x, x = h - M c1 exactly: 2^x goes to the constants
     const float x = r.big ? 0.f : -fmaf(s.M, c1, -h), f = ex2(x);

@@ -26,6 +26,83 @@ struct RowWindow {
     unsigned todo, zero;                                     // lanes with rows to do, with gradient rows to zero
 };
 
+// A warp's stretch [ua, un) of a row in its stage: granule ua first.  Element e of the row is element e + off of the granules.
+template <typename T, bool WHOLE>
+struct RowStage {
+    using U = Unit<T>;
+    static constexpr int N = U::N;
+    unsigned char* at;
+    const RowUnits<T, WHOLE>& ru;
+    int ua, un, off;
+    __device__ __forceinline__ RowStage(unsigned char* at_, const RowUnits<T, WHOLE>& ru_, int ua_, int un_)
+        : at(at_), ru(ru_), ua(ua_), un(un_), off(WHOLE ? 0 : ru_.m0 + ru_.sh) {}
+    __device__ __forceinline__ bool ends() const { return !WHOLE && ua < un && (ua == 0 || un == ru.NU); }
+    // what the row's first and last granules hold of its neighbours becomes -inf
+    __device__ __forceinline__ void clean() const {
+        if (!ends()) return;
+        const int lane = threadIdx.x & 31;
+        T* const s = reinterpret_cast<T*>(at) - (long long)ua * N;
+        const long long after = (long long)off + ru.V + lane;
+        if (ua == 0 && lane < off) put(s + lane, -INFINITY);
+        if (un == ru.NU && after < (long long)(ru.NU + 1) * N) put(s + after, -INFINITY);
+        __syncwarp();
+    }
+    __device__ __forceinline__ uint4 held(int u) const {
+        const uint4* const g = reinterpret_cast<const uint4*>(at) + (u - ua);
+        return WHOLE || ru.sh == 0 ? *g : U::realign(g[0], g[1], ru.sh);
+    }
+    __device__ __forceinline__ bool owns(int x) const {
+        const int u = ru.unit_of(x);
+        return u >= ua && u < un;
+    }
+    __device__ __forceinline__ float token(int x) const {
+        return to_f32(*(reinterpret_cast<const T*>(at) + (x + (long long)off - (long long)ua * N)));
+    }
+    // before another copy is asked for: after what every lane has read and written here
+    __device__ __forceinline__ void release() const {
+        if (ends()) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+    }
+};
+
+// Gradient of a warp's stretch, from its registers.  last: the row's last unit where it is not whole and in this stretch.
+template <typename T, bool WHOLE, bool ENT, int UPT>
+__device__ __forceinline__ void write_row(T* g, const uint4 (&w)[UPT], const uint4& last, bool has_last, const RowUnits<T, WHOLE>& ru, int ua,
+                                          int un, int x, const RowGrad& r, const RowStats& st, float c1) {
+    const int lane = threadIdx.x & 31;
+    if (r.zero) {
+        ru.store_zeros(g, ua, un, lane, 32);
+        return;
+    }
+    const int lo = max(ua, ru.whole_lo()), hi = min(un, ru.whole_hi());
+    auto write = [&](auto big) {
+        constexpr bool BIG = decltype(big)::value;
+#pragma unroll
+        for (int k = 0; k < UPT; k += 4) {
+            if (ua + k * 32 < un) {
+#pragma unroll
+                for (int i = k; i < (k + 4 < UPT ? k + 4 : UPT); ++i) {
+                    const int u = ua + i * 32 + lane;
+                    const uint4 v = grad_unit<T, ENT, BIG>(w[i], r.c);
+                    if ((WHOLE || i > 0 || u >= lo) && u < hi) __stcs(ru.frame(g) + u, v);
+                }
+            }
+        }
+        if (!WHOLE && ua == 0 && ua < un && ru.whole_lo() > 0) {
+            const uint4 f = make_uint4(__shfl_sync(0xFFFFFFFFu, w[0].x, 0), __shfl_sync(0xFFFFFFFFu, w[0].y, 0),
+                                       __shfl_sync(0xFFFFFFFFu, w[0].z, 0), __shfl_sync(0xFFFFFFFFu, w[0].w, 0));
+            ru.store_end(g, 0, grad_unit<T, ENT, BIG>(f, r.c));
+        }
+        if (has_last) ru.store_end(g, ru.NU - 1, grad_unit<T, ENT, BIG>(last, r.c));
+    };
+    if (r.big) write(std::true_type{});
+    else write(std::false_type{});
+    // the token's own element, by a lane of the warp that wrote it
+    __syncwarp();
+    const int ox = ru.unit_of(x) - ua;
+    if (ox >= 0 && ox < un - ua && lane == (ox & 31)) grad_token<T, ENT>(g, x, st.zx, st.M, c1, r);
+}
+
 template <typename T, bool WHOLE, int NW, bool GRAD, bool ENT>
 __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __grid_constant__ ScoreParams p) {
     using U = Unit<T>;
@@ -140,47 +217,26 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         }
         ph ^= 1u;
         uint32_t bad = alive ? 0u : 1u;
-        // Off 16-byte boundaries: what the row's first and last granules hold of its neighbours becomes -inf, in the stage.  Element
-        // e of the row is element e + off of the granules.
-        const int off = WHOLE ? 0 : ru.m0 + ru.sh;
-        const bool ends = !WHOLE && ua < un && (ua == 0 || un == ru.NU);
-        if (ends) {
-            T* const s = reinterpret_cast<T*>(stage) - (long long)ua * N;
-            const long long after = (long long)off + ru.V + lane;
-            if (ua == 0 && lane < off) put(s + lane, -INFINITY);
-            if (un == ru.NU && after < (long long)(ru.NU + 1) * N) put(s + after, -INFINITY);
-            __syncwarp();
-        }
-        auto held = [&](int u) {                             // unit u, with the granules around it in the stage
-            const uint4* const at = reinterpret_cast<const uint4*>(stage) + (u - ua);
-            return WHOLE || ru.sh == 0 ? *at : U::realign(at[0], at[1], ru.sh);
-        };
+        const RowStage<T, WHOLE> rs(stage, ru, ua, un);
+        rs.clean();
         uint4 w[UPT], last;
         typename U::Max mx = U::max0();
 #pragma unroll
         for (int k = 0; k < UPT; ++k) {
             const int u = ua + k * 32 + lane;
-            w[k] = u < un ? held(u) : U::none4();
+            w[k] = u < un ? rs.held(u) : U::none4();
         }
         const bool has_last = GRAD && !WHOLE && ua < un && un > ru.whole_hi() && ru.NU - 1 >= ru.whole_lo();
-        if (has_last) last = held(ru.NU - 1);
+        if (has_last) last = rs.held(ru.NU - 1);
 #pragma unroll
         for (int k = 0; k < UPT; ++k) U::max_add(mx, w[k]);
-        // the token's logit, if it is in this stretch
-        const int ox = ru.unit_of(my_x) - ua;
-        float zx = -INFINITY;
-        if (ox >= 0 && ox < un - ua) {
-            zx = to_f32(*(reinterpret_cast<const T*>(stage) + (my_x + (long long)off - (long long)ua * N)));
-        }
+        const float zx = rs.owns(my_x) ? rs.token(my_x) : -INFINITY;
         if (zx != zx) bad = 1u;
         const float m = warp_max_f32(fmaxf(U::max_val(mx, bad), zx));       // (every lane's loads from the stage have ended)
         if (m == INFINITY) bad = 1u;
         next();
         asked = row >= 0 && alive;
-        if (ends) {                                          // (the copy comes after what was written to the stage)
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-        }
+        rs.release();
         if (asked) ask();
         const float2 sums = sum_units<T, ENT, UPT>(w, m, c1, L2, [&](int k) { return ua + k * 32 < un; });
         const float4 mine = make_float4(m, __any_sync(0xFFFFFFFFu, bad) ? NAN : sums.x, sums.y, zx);
@@ -234,36 +290,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         if (GRAD) {
             const RowGrad r = row_grad(p, in, st, c1, L2, ENT);
             T* const g = reinterpret_cast<T*>(p.grad) + (long long)my_row * p.g_stride;
-            const int lo = max(ua, ru.whole_lo()), hi = min(un, ru.whole_hi());
-            auto write = [&](auto big) {
-                constexpr bool BIG = decltype(big)::value;
-#pragma unroll
-                for (int k = 0; k < UPT; k += 4) {
-                    if (ua + k * 32 < un) {
-#pragma unroll
-                        for (int i = k; i < k + 4; ++i) {
-                            const int u = ua + i * 32 + lane;
-                            const uint4 v = grad_unit<T, ENT, BIG>(w[i], r.c);
-                            if ((WHOLE || i > 0 || u >= lo) && u < hi) __stcs(ru.frame(g) + u, v);
-                        }
-                    }
-                }
-                if (!WHOLE && ua == 0 && ua < un && ru.whole_lo() > 0) {
-                    const uint4 f = make_uint4(__shfl_sync(0xFFFFFFFFu, w[0].x, 0), __shfl_sync(0xFFFFFFFFu, w[0].y, 0),
-                                               __shfl_sync(0xFFFFFFFFu, w[0].z, 0), __shfl_sync(0xFFFFFFFFu, w[0].w, 0));
-                    ru.store_end(g, 0, grad_unit<T, ENT, BIG>(f, r.c));
-                }
-                if (has_last) ru.store_end(g, ru.NU - 1, grad_unit<T, ENT, BIG>(last, r.c));
-            };
-            if (r.zero) {
-                ru.store_zeros(g, ua, un, lane, 32);
-            } else {
-                if (r.big) write(std::true_type{});
-                else write(std::false_type{});
-                // the token's own element, by a lane of the warp that wrote it
-                __syncwarp();
-                if (ox >= 0 && ox < un - ua && lane == (ox & 31)) grad_token<T, ENT>(g, my_x, zx, st.M, c1, r);
-            }
+            write_row<T, WHOLE, ENT, UPT>(g, w, last, has_last, ru, ua, un, my_x, r, st, c1);
         }
         if (keeper && lane == 0) {
             RowHist& h = hist[done & 31];

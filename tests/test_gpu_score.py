@@ -55,7 +55,7 @@ def out(torch, n, k=1, fill=-7.0):
 # One unit, edges of units, of a CTA of 2 warps (256 units), of a thread's 4, 8, 16 units, of a cluster; rows longer than a cluster
 # holds (fp32 131072, bf16 262144 logits)
 SIZES = [(1, 1), (3, 2), (2, 7), (5, 8), (4, 9), (1, 1000), (6, 2047), (3, 2056), (2, 4099), (300, 8200), (1, 32000), (300, 32000),
-         (3, 50257), (2, 128256), (90, 128256), (2, 151936)]
+         (310, 33003), (3, 50257), (2, 128256), (90, 128256), (2, 151936)]
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
