@@ -1,6 +1,7 @@
 // Launches of the scoring and loss kernels (adasd_score.cuh).
 #include "adasd_launch.cuh"
 #include "adasd_score_deep.cuh"
+#include "adasd_score_forward.cuh"
 
 #include <algorithm>
 #include <atomic>
@@ -9,25 +10,17 @@ namespace adasd {
 namespace {
 
 inline int unit_elements(int dtype) { return dtype == ADASD_BF16 ? 8 : 4; }
-// Rows that start on 16-byte boundaries and end on one.
-inline bool whole_rows(const void* base, long long stride, int V, int dtype) {
+// How rows of logits, and of a gradient (null: none), lie relative to 16-byte boundaries.
+inline Layout layout_of(const void* z, long long stride, const void* g, long long g_stride, int V, int dtype) {
     const int N = unit_elements(dtype);
-    return (reinterpret_cast<uintptr_t>(base) & 15u) == 0 && stride % N == 0 && V % N == 0;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(z) & 15u, b = g ? reinterpret_cast<uintptr_t>(g) & 15u : a;
+    if (g && (a != b || (stride - g_stride) % N != 0)) return ROWS_ANY;
+    return a == 0 && stride % N == 0 && V % N == 0 ? ROWS_WHOLE : ROWS_SAME;
 }
 // Units of a row, at most.
-inline int row_units(int V, int dtype, bool whole) {
+inline int row_units(int V, int dtype, Layout layout) {
     const int N = unit_elements(dtype);
-    return (int)(((long long)V + (whole ? 0 : 2 * N - 2)) / N);
-}
-
-template <typename T, bool WHOLE, int NW, int UPT, bool HOLD, bool GRAD, bool ENT>
-int launch(const ScoreParams& p, cudaStream_t stream) {
-    return launch_pdl(score_kernel<T, WHOLE, NW, UPT, HOLD, GRAD, ENT>, p.n_rows * p.cs, NW * 32, 0, p.cs, stream, p);
-}
-template <typename T, bool WHOLE, int NW, int UPT, bool HOLD>
-int launch(const ScoreParams& p, bool ent, cudaStream_t stream) {
-    if (p.grad) return ent ? launch<T, WHOLE, NW, UPT, HOLD, true, true>(p, stream) : launch<T, WHOLE, NW, UPT, HOLD, true, false>(p, stream);
-    return ent ? launch<T, WHOLE, NW, UPT, HOLD, false, true>(p, stream) : launch<T, WHOLE, NW, UPT, HOLD, false, false>(p, stream);
+    return (int)(((long long)V + (layout == ROWS_WHOLE ? 0 : 2 * N - 2)) / N);
 }
 
 template <typename K>
@@ -45,112 +38,124 @@ int resident_clusters(K kern, int threads, int smem, int cs) {
     lc.attrs = attr;
     lc.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, kern, &lc) != cudaSuccess) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kern, &lc) != cudaSuccess) {
         cudaGetLastError();
         return 0;
     }
     return n;
 }
-// Clusters of a kernel that are resident at once, asked for once per device, kernel and cluster size.
-template <typename T, bool WHOLE, int NW, bool GRAD, bool ENT>
-int stream_clusters(int cs) {
-    constexpr int kDevices = 64;
-    static std::atomic<int> known[kDevices][kScMaxCluster + 1];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return 0;
-    int n = known[dev][cs].load(std::memory_order_acquire);
-    if (n == 0) {
-        const auto kern = score_stream_kernel<T, WHOLE, NW, GRAD, ENT>;
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NW * kSsStage) != cudaSuccess) {
-            cudaGetLastError();
-            return 0;
+// Clusters of a persistent kernel that are resident at once, asked for once per device and cluster size (0: not usable).
+struct Resident {
+    std::atomic<int> known[64][kScMaxCluster + 1];           // (0: not asked yet)
+    template <typename K>
+    int operator()(K kern, int threads, int smem, int cs) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+        int n = known[dev][cs].load(std::memory_order_acquire);
+        if (n == 0) {
+            n = resident_clusters(kern, threads, smem, cs);
+            known[dev][cs].store(n > 0 ? n : -1, std::memory_order_release);
         }
-        n = resident_clusters(kern, NW * 32, NW * kSsStage, cs);
-        known[dev][cs].store(n, std::memory_order_release);
+        return std::max(n, 0);
     }
-    return n;
-}
-// ADASD_ERR_SHAPE: not a launch for score_stream_kernel (rows too long, or too few of them).
-template <typename T, bool WHOLE, int NW, bool GRAD, bool ENT>
-int launch_stream_t(ScoreParams p, int cs, int per_warp, cudaStream_t stream) {
-    const int ncl = stream_clusters<T, WHOLE, NW, GRAD, ENT>(cs);
-    if (p.n_rows <= ncl || ncl == 0) return ADASD_ERR_SHAPE;
+};
+// A launch of a persistent kernel, a row a cluster at a time; kNotTaken unless there are more rows than `waves` for each cluster.
+constexpr int kNotTaken = 1;
+template <typename K>
+int launch_rows(Resident& resident, K kern, ScoreParams p, int threads, int smem, int cs, int per, int waves, cudaStream_t stream) {
+    const long long ncl = resident(kern, threads, smem, cs);
+    if (ncl == 0 || p.n_rows <= waves * ncl) return kNotTaken;
     p.cs = cs;
-    p.per_cta = per_warp;
-    return launch_pdl(score_stream_kernel<T, WHOLE, NW, GRAD, ENT>, ncl * cs, NW * 32, NW * kSsStage, cs, stream, p);
+    p.per_cta = per;
+    return launch_pdl(kern, (int)ncl * cs, threads, smem, cs, stream, p);
 }
-template <typename T, bool WHOLE, int NW>
-int launch_stream_n(const ScoreParams& p, bool ent, int cs, int per_warp, cudaStream_t stream) {
-    if (p.grad) return ent ? launch_stream_t<T, WHOLE, NW, true, true>(p, cs, per_warp, stream) : launch_stream_t<T, WHOLE, NW, true, false>(p, cs, per_warp, stream);
-    return ent ? launch_stream_t<T, WHOLE, NW, false, true>(p, cs, per_warp, stream) : launch_stream_t<T, WHOLE, NW, false, false>(p, cs, per_warp, stream);
+template <typename T, int L, int NW, bool ENT>
+int launch_forward(const ScoreParams& p, int cs, int per, cudaStream_t stream) {
+    static Resident r;
+    return launch_rows(r, score_forward_kernel<T, L, NW, ENT>, p, NW * 32, NW * 2 * kSfStage, cs, per, 1, stream);
 }
-template <typename T, bool WHOLE, bool ENT>
-int launch_deep_t(ScoreParams p, int cs, int per_warp, cudaStream_t stream) {
-    static std::atomic<int> known[64][kScMaxCluster + 1];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return ADASD_ERR_SHAPE;
-    int ncl = known[dev][cs].load(std::memory_order_acquire);
-    const auto kern = score_deep_kernel<T, WHOLE, ENT>;
-    if (ncl == 0) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSdSmem) != cudaSuccess) {
-            cudaGetLastError();
-            return ADASD_ERR_SHAPE;
-        }
-        ncl = resident_clusters(kern, kSdThreads, kSdSmem, cs);
-        known[dev][cs].store(ncl, std::memory_order_release);
+template <typename T, int L, int NW, bool ENT>
+int launch_stream(const ScoreParams& p, int cs, int per, cudaStream_t stream) {
+    static Resident r;
+    return launch_rows(r, score_stream_kernel<T, L, NW, ENT>, p, NW * 32, NW * kSsStage, cs, per, 1, stream);
+}
+template <typename T, int L, bool ENT>
+int launch_deep(const ScoreParams& p, int cs, int per, cudaStream_t stream) {
+    static Resident r;
+    return launch_rows(r, score_deep_kernel<T, L, ENT>, p, kSdThreads, kSdSmem, cs, per, 2, stream);
+}
+// Many rows.
+template <typename T, int L, bool ENT>
+int launch_many(const ScoreParams& p, int NU, cudaStream_t stream) {
+    const int its = (NU + 31) / 32;
+    if (p.grad && NU >= 2048) {
+        const int cs = (NU + kSdUnits - 1) / kSdUnits;
+        if (cs <= kScMaxCluster)
+            if (const int rc = launch_deep<T, L, ENT>(p, cs, (its + cs - 1) / cs * 32, stream); rc != kNotTaken) return rc;
     }
-    if (p.n_rows <= 2 * ncl || ncl == 0) return ADASD_ERR_SHAPE;
-    p.cs = cs;
-    p.per_cta = per_warp;
-    return launch_pdl(kern, ncl * cs, kSdThreads, kSdSmem, cs, stream, p);
-}
-template <typename T, bool WHOLE>
-int launch_deep(const ScoreParams& p, bool ent, int NU, cudaStream_t stream) {
-    const int its = (NU + 31) / 32, cs = (NU + kSdUnits - 1) / kSdUnits, per = (its + cs - 1) / cs * 32;
-    if (!p.grad || cs > kScMaxCluster || NU < 2048) return ADASD_ERR_SHAPE;
-    return ent ? launch_deep_t<T, WHOLE, true>(p, cs, per, stream) : launch_deep_t<T, WHOLE, false>(p, cs, per, stream);
-}
-template <typename T, bool WHOLE>
-int launch_stream(const ScoreParams& p, bool ent, int NU, cudaStream_t stream) {
-    constexpr int W = kSsUPT * 32;
-    const int warps = (NU + W - 1) / W;
-    if (warps == 1) return launch_stream_n<T, WHOLE, 1>(p, ent, 1, NU, stream);
-    if (warps == 2) return launch_stream_n<T, WHOLE, 2>(p, ent, 1, (NU + 1) / 2, stream);
-    if (warps <= 4) return launch_stream_n<T, WHOLE, 4>(p, ent, 1, (NU + 3) / 4, stream);
-    const int cs = (warps + 7) / 8;
-    if (cs > kScMaxCluster) return ADASD_ERR_SHAPE;
-    return launch_stream_n<T, WHOLE, 8>(p, ent, cs, (NU + 8 * cs - 1) / (8 * cs), stream);
+    static_assert(kSfWarpUnits == kSsUPT * 32, "either kernel's warps take as many units");
+    const int warps = (NU + kSfWarpUnits - 1) / kSfWarpUnits;
+    auto launch = [&](auto nw, int cs) -> int {
+        constexpr int NW = decltype(nw)::value;
+        const int per = (NU + NW * cs - 1) / (NW * cs);
+        return p.grad ? launch_stream<T, L, NW, ENT>(p, cs, per, stream) : launch_forward<T, L, NW, ENT>(p, cs, per, stream);
+    };
+    if (warps == 1) return launch(std::integral_constant<int, 1>{}, 1);
+    if (warps == 2) return launch(std::integral_constant<int, 2>{}, 1);
+    if (warps <= 4) return launch(std::integral_constant<int, 4>{}, 1);
+    if (warps <= 8 * kScMaxCluster) return launch(std::integral_constant<int, 8>{}, (warps + 7) / 8);
+    return kNotTaken;
 }
 
-constexpr int kScNW = 8, kScUnits = kScNW * 32;      // CTAs of 8 warps; units of a CTA and unit a thread
+constexpr int kScNW = 8, kScUnits = kScNW * 32;      // score_kernel: CTAs of 8 warps; units of a CTA and unit a thread
 
-template <typename T, bool WHOLE>
-int launch(ScoreParams p, bool ent, int NU, int sms, cudaStream_t stream) {
-    if (const int rc = launch_deep<T, WHOLE>(p, ent, NU, stream); rc != ADASD_ERR_SHAPE) return rc;
-    if (const int rc = launch_stream<T, WHOLE>(p, ent, NU, stream); rc != ADASD_ERR_SHAPE) return rc;
+template <typename T, int L, bool GRAD, bool ENT>
+int launch_few(ScoreParams p, int NU, int sms, cudaStream_t stream) {
+    auto go = [&](auto kern, int threads) { return launch_pdl(kern, p.n_rows * p.cs, threads, 0, p.cs, stream, p); };
     if (NU <= 2 * 32 * 4) {
         p.cs = 1;
         p.per_cta = NU;
-        return launch<T, WHOLE, 2, 4, true>(p, ent, stream);
+        return go(score_kernel<T, L, 2, 4, true, GRAD, ENT>, 64);
     }
     int cs = std::min(kScMaxCluster, (NU + kScUnits * 16 - 1) / (kScUnits * 16));
     while (cs < kScMaxCluster && (long long)p.n_rows * cs < 2LL * sms && NU > cs * kScUnits) cs = std::min(2 * cs, kScMaxCluster);
     p.cs = cs;
     p.per_cta = (NU + cs - 1) / cs;
-    if (p.per_cta <= kScUnits * 4) return launch<T, WHOLE, kScNW, 4, true>(p, ent, stream);
-    if (p.per_cta <= kScUnits * 8) return launch<T, WHOLE, kScNW, 8, true>(p, ent, stream);
-    if (p.per_cta <= kScUnits * 16) return launch<T, WHOLE, kScNW, 16, true>(p, ent, stream);
-    return launch<T, WHOLE, kScNW, 16, false>(p, ent, stream);
+    if (p.per_cta <= kScUnits * 4) return go(score_kernel<T, L, kScNW, 4, true, GRAD, ENT>, kScNW * 32);
+    if (p.per_cta <= kScUnits * 8) return go(score_kernel<T, L, kScNW, 8, true, GRAD, ENT>, kScNW * 32);
+    if (p.per_cta <= kScUnits * 16) return go(score_kernel<T, L, kScNW, 16, true, GRAD, ENT>, kScNW * 32);
+    return go(score_kernel<T, L, kScNW, 16, false, GRAD, ENT>, kScNW * 32);
+}
+template <typename T, int L, bool ENT>
+int launch(const ScoreParams& p, int NU, int sms, cudaStream_t stream) {
+    if constexpr (L != ROWS_ANY)
+        if (const int rc = launch_many<T, L, ENT>(p, NU, stream); rc != kNotTaken) return rc;
+    if (p.grad) return launch_few<T, L, true, ENT>(p, NU, sms, stream);
+    if constexpr (L != ROWS_ANY) return launch_few<T, L, false, ENT>(p, NU, sms, stream);
+    return ADASD_ERR_SHAPE;                          // (without a gradient no row lies across granules)
+}
+template <typename T, bool ENT>
+int launch(const ScoreParams& p, int layout, int NU, int sms, cudaStream_t stream) {
+    if (layout == ROWS_WHOLE) return launch<T, ROWS_WHOLE, ENT>(p, NU, sms, stream);
+    if (layout == ROWS_SAME) return launch<T, ROWS_SAME, ENT>(p, NU, sms, stream);
+    return launch<T, ROWS_ANY, ENT>(p, NU, sms, stream);
+}
+template <typename T>
+int launch_grad(const PrefParams& p, int layout, int grid, cudaStream_t stream) {
+    if (layout == ROWS_WHOLE) return launch_pdl(pref_grad_kernel<T, ROWS_WHOLE>, grid, kPgThreads, 0, 0, stream, p);
+    if (layout == ROWS_SAME) return launch_pdl(pref_grad_kernel<T, ROWS_SAME>, grid, kPgThreads, 0, 0, stream, p);
+    return launch_pdl(pref_grad_kernel<T, ROWS_ANY>, grid, kPgThreads, 0, 0, stream, p);
 }
 
 }  // namespace
 
-int launch_score(ScoreParams p, int dtype, bool entropy, int sm_count, cudaStream_t stream) {
-    const bool whole = whole_rows(p.z, p.row_stride, p.V, dtype) && (!p.grad || whole_rows(p.grad, p.g_stride, p.V, dtype));
-    const int NU = row_units(p.V, dtype, whole);
+int launch_score(const ScoreParams& p, int dtype, bool entropy, int sm_count, cudaStream_t stream) {
+    const Layout layout = layout_of(p.z, p.row_stride, p.grad, p.g_stride, p.V, dtype);
+    const int NU = row_units(p.V, dtype, layout);
     if (dtype == ADASD_BF16)
-        return whole ? launch<__nv_bfloat16, true>(p, entropy, NU, sm_count, stream) : launch<__nv_bfloat16, false>(p, entropy, NU, sm_count, stream);
-    return whole ? launch<float, true>(p, entropy, NU, sm_count, stream) : launch<float, false>(p, entropy, NU, sm_count, stream);
+        return entropy ? launch<__nv_bfloat16, true>(p, layout, NU, sm_count, stream) : launch<__nv_bfloat16, false>(p, layout, NU, sm_count, stream);
+    return entropy ? launch<float, true>(p, layout, NU, sm_count, stream) : launch<float, false>(p, layout, NU, sm_count, stream);
 }
 
 int launch_pref_pairs(const PrefParams& p, cudaStream_t stream) {
@@ -158,17 +163,12 @@ int launch_pref_pairs(const PrefParams& p, cudaStream_t stream) {
 }
 
 int launch_pref_grad(PrefParams p, int dtype, cudaStream_t stream) {
-    const bool whole = whole_rows(p.z, p.row_stride, p.V, dtype) && whole_rows(p.grad, p.g_stride, p.V, dtype);
-    const int NU = row_units(p.V, dtype, whole);
+    const Layout layout = layout_of(p.z, p.row_stride, p.grad, p.g_stride, p.V, dtype);
+    const int NU = row_units(p.V, dtype, layout);
     p.segs = (NU + kPgThreads * kPgUnits - 1) / (kPgThreads * kPgUnits);
     p.per_cta = (NU + p.segs - 1) / p.segs;
     if ((long long)p.n_rows * p.segs > 0x7FFFFFFFLL) return ADASD_ERR_SHAPE;
-    const int grid = p.n_rows * p.segs;
-    if (dtype == ADASD_BF16)
-        return whole ? launch_pdl(pref_grad_kernel<__nv_bfloat16, true>, grid, kPgThreads, 0, 0, stream, p)
-                  : launch_pdl(pref_grad_kernel<__nv_bfloat16, false>, grid, kPgThreads, 0, 0, stream, p);
-    return whole ? launch_pdl(pref_grad_kernel<float, true>, grid, kPgThreads, 0, 0, stream, p)
-              : launch_pdl(pref_grad_kernel<float, false>, grid, kPgThreads, 0, 0, stream, p);
+    return dtype == ADASD_BF16 ? launch_grad<__nv_bfloat16>(p, layout, p.n_rows * p.segs, stream) : launch_grad<float>(p, layout, p.n_rows * p.segs, stream);
 }
 
 int launch_total(const float* terms, int n, float* out, cudaStream_t stream) {

@@ -25,12 +25,14 @@ constexpr float kLowT = -16384.f;          // 2^t = 0 from here down; keeps 0 * 
 
 // A row's units of 16 bytes, aligned in the memory of the array that decides: the gradient's row where one is written
 // (so that whole units are stored at once), else the logits'.  Unit u holds elements u N - m0 .. u N - m0 + N - 1; logits that
-// lie elsewhere relative to 16 bytes are put together from two granules.  WHOLE: rows start on 16-byte boundaries and V is
-// a multiple of N, so that no unit needs a look at its ends.
-template <typename T, bool WHOLE>
+// lie elsewhere relative to 16 bytes are put together from two granules (ROWS_ANY).  ROWS_SAME: no row does.  ROWS_WHOLE: rows start
+// on 16-byte boundaries and V is a multiple of N, so that no unit needs a look at its ends.
+enum Layout : int { ROWS_WHOLE, ROWS_SAME, ROWS_ANY };
+template <typename T, int L>
 struct RowUnits {
     using U = Unit<T>;
     static constexpr int N = U::N;
+    static constexpr bool WHOLE = L == ROWS_WHOLE;
     const uint4* src;                      // granule that unit 0 starts in
     int m0, sh;                            // elements before the row in unit 0; elements of src's granule before unit 0
     int glo, ghi;                          // granules that hold elements of the row
@@ -47,7 +49,7 @@ struct RowUnits {
             NU = (int)(((long long)m0 + V + N - 1) / N);
             const unsigned long long s = a - (unsigned long long)m0 * sizeof(T), b = s & ~15ull;
             src = reinterpret_cast<const uint4*>(b);
-            sh = (int)((s & 15ull) / sizeof(T));
+            sh = L == ROWS_ANY ? (int)((s & 15ull) / sizeof(T)) : 0;
             glo = (int)(((a & ~15ull) - b) >> 4);
             ghi = (int)((a + (unsigned long long)V * sizeof(T) + 15ull - b) >> 4);
         }
@@ -57,7 +59,7 @@ struct RowUnits {
     __device__ __forceinline__ uint4 unit(int u, F get) const {
         if (WHOLE) return get(u);
         uint4 w = u >= glo && u < ghi ? get(u) : U::none4();
-        if (sh) w = U::realign(w, u + 1 < ghi ? get(u + 1) : U::none4(), sh);
+        if (L == ROWS_ANY && sh) w = U::realign(w, u + 1 < ghi ? get(u + 1) : U::none4(), sh);
         if (u == 0 || u == NU - 1) U::mask(w, u == 0 ? m0 : 0, (int)min((long long)N, (long long)V + m0 - (long long)u * N));
         return w;
     }
@@ -74,7 +76,7 @@ struct RowUnits {
     __device__ __forceinline__ uint4 load_any(int u) const {
         if (WHOLE) return __ldcg(src + u);
         uint4 w = __ldcg(src + min(max(u, glo), ghi - 1));
-        if (sh) w = U::realign(w, __ldcg(src + min(max(u + 1, glo), ghi - 1)), sh);
+        if (L == ROWS_ANY && sh) w = U::realign(w, __ldcg(src + min(max(u + 1, glo), ghi - 1)), sh);
         return w;
     }
     // unit u of row g where it is the row's first or last and not whole: its elements, one a lane (by a whole warp)
@@ -317,6 +319,14 @@ __device__ __forceinline__ float2 finish_sums(float2 S2, float2 T2, float m, flo
     r.x /= em;
     return r;
 }
+// Adds sums {S, T} = r under the largest logit t to those under m.
+__device__ __forceinline__ void fold_sums(float& m, float& S, float& Ts, float t, float2 r, float c1) {
+    const float n = fmaxf(m, t), d0 = m > -INFINITY ? fmaxf((m - n) * c1, kLowT) : kLowT, d1 = t > -INFINITY ? fmaxf((t - n) * c1, kLowT) : kLowT;
+    const float f0 = ex2(d0), f1 = ex2(d1);
+    Ts = f0 * fmaf(d0, S, Ts) + f1 * fmaf(d1, r.x, r.y);
+    S = f0 * S + f1 * r.x;
+    m = n;
+}
 // Units held in registers, in groups of four; used(k): whether group k can hold anything (warp-uniform).
 template <typename T, bool ENT, int UPT, typename F>
 __device__ __forceinline__ float2 sum_units(const uint4 (&w)[UPT], float m, float c1, float2 L2, F used) {
@@ -384,13 +394,14 @@ __device__ __forceinline__ void grad_token_by(T* g, int x, int ux, int u0, int u
     }
 }
 
-// WHOLE: as RowUnits.  NW warps a CTA, UPT units a thread.  HOLD: a CTA's units
+// L: as RowUnits.  NW warps a CTA, UPT units a thread.  HOLD: a CTA's units
 // fit its registers; else (rows longer than the cluster holds) they are taken in turn and read again for the gradient.
 // GRAD: a gradient is written.  ENT: the entropy or its gradient is wanted.
-template <typename T, bool WHOLE, int NW, int UPT, bool HOLD, bool GRAD, bool ENT>
+template <typename T, int L, int NW, int UPT, bool HOLD, bool GRAD, bool ENT>
 __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_constant__ ScoreParams p) {
     using U = Unit<T>;
     constexpr int N = U::N, NT = NW * 32;
+    constexpr bool WHOLE = L == ROWS_WHOLE;
     const float floor_v = N == 8 ? ADASD_FLOOR_BF : kFloor;
     __shared__ float4 part[kScMaxCluster * NW];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -401,7 +412,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
 
     const T* const z = reinterpret_cast<const T*>(p.z) + (long long)row * p.row_stride;
     T* const g = GRAD ? reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride : nullptr;
-    const RowUnits<T, WHOLE> ru(z, GRAD ? g : z, p.V);
+    const RowUnits<T, L> ru(z, GRAD ? g : z, p.V);
     const int u0 = min(rank * p.per_cta, ru.NU), u1 = min(u0 + p.per_cta, ru.NU);
     const int x = __ldcg(p.tok + row), kind = row_kind(p, row, x);       // (the same in every CTA of the cluster)
     if (kind != 1) {
@@ -436,12 +447,8 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_kernel(const __grid_co
             m = t;
             S = r.x;
             Ts = r.y;
-        } else {                                    // fold it into what came before
-            const float n = fmaxf(m, t), d0 = m > -INFINITY ? fmaxf((m - n) * c1, kLowT) : kLowT, d1 = t > -INFINITY ? fmaxf((t - n) * c1, kLowT) : kLowT;
-            const float f0 = ex2(d0), f1 = ex2(d1);
-            Ts = f0 * fmaf(d0, S, Ts) + f1 * fmaf(d1, r.x, r.y);
-            S = f0 * S + f1 * r.x;
-            m = n;
+        } else {
+            fold_sums(m, S, Ts, t, r, c1);
         }
     }
     const float4 mine = make_float4(m, __any_sync(0xFFFFFFFFu, bad) ? NAN : S, Ts, zx);
@@ -580,9 +587,9 @@ __global__ void __launch_bounds__(kPairThreads) pref_pair_kernel(const __grid_co
 // Gradient of rows whose statistics and dL/dl are known: dL/dz_v = dL/dl (1[v = x] - p_v) / T.  From the last row to the
 // first: what the L2 still holds of score_kernel's reads is read first.
 constexpr int kPgThreads = 256, kPgUnits = 8;
-template <typename T, bool WHOLE>
+template <typename T, int L>
 __global__ void __launch_bounds__(kPgThreads) pref_grad_kernel(const __grid_constant__ PrefParams p) {
-    using U = Unit<T>;
+    constexpr bool WHOLE = L == ROWS_WHOLE;
     const int back = (int)(blockIdx.x / (unsigned)p.segs), seg = (int)(blockIdx.x - (unsigned)back * (unsigned)p.segs);
     const int row = p.n_rows - 1 - back;
     pdl_wait();
@@ -592,7 +599,7 @@ __global__ void __launch_bounds__(kPgThreads) pref_grad_kernel(const __grid_cons
     if (kind < 0) return;
     const T* const z = reinterpret_cast<const T*>(p.z) + (long long)row * p.row_stride;
     T* const g = reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride;
-    const RowUnits<T, WHOLE> ru(z, g, p.V);
+    const RowUnits<T, L> ru(z, g, p.V);
     const int u0 = min(seg * p.per_cta, ru.NU), u1 = min(u0 + p.per_cta, ru.NU);
     if (kind == 0 || e.z == 0.f) {
         ru.store_zeros(g, u0, u1, (int)threadIdx.x, kPgThreads);

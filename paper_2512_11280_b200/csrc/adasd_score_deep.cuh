@@ -31,26 +31,11 @@ struct __align__(16) DeepCoef {
     int32_t zero, big, pad[2];
 };
 
-// f(k) for k < n of UPT, four at a time without a branch between them (n: warp-uniform).
-template <int UPT, typename F>
-__device__ __forceinline__ void for_units(int n, F f) {
-#pragma unroll
-    for (int k = 0; k < UPT; k += 4) {
-        if (k + 4 <= UPT && n >= k + 4) {
-#pragma unroll
-            for (int i = k; i < (k + 4 < UPT ? k + 4 : UPT); ++i) f(i);
-        } else {
-#pragma unroll
-            for (int i = k; i < (k + 4 < UPT ? k + 4 : UPT); ++i)
-                if (i < n) f(i);
-        }
-    }
-}
-
-template <typename T, bool WHOLE, bool ENT>
+template <typename T, int L, bool ENT>
 __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_constant__ ScoreParams p) {
     using U = Unit<T>;
     constexpr int N = U::N, UPT = kSdUPT, NW = kSdNW;
+    constexpr bool WHOLE = L == ROWS_WHOLE;
     const float floor_v = N == 8 ? ADASD_FLOOR_BF : kFloor;
     extern __shared__ __align__(128) unsigned char dyn_smem[];
     // Four rows' worth: a worker sends the partials of row n once it has the constants of row n - 2, for which every
@@ -58,6 +43,7 @@ __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_
     __shared__ float4 part[4][kScMaxCluster * NW];
     __shared__ DeepItem items[4];
     __shared__ DeepCoef coefs[4];
+    __shared__ RowHist hist[32];
     __shared__ unsigned long long full_s[2], empty_s[2], got_s[4], ready_s[4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int CS = p.cs, ncl = (int)(gridDim.x / (unsigned)CS), cl = (int)(blockIdx.x / (unsigned)CS);
@@ -65,6 +51,7 @@ __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_
     auto bar = [](unsigned long long& b) { return reinterpret_cast<uint64_t*>(&b); };
     cg::cluster_group cluster = cg::this_cluster();
     if (threadIdx.x == 0) {
+        items[3].row = 0;
         for (int k = 0; k < 2; ++k) {
             mbar_init(bar(full_s[k]), 1);
             mbar_init(bar(empty_s[k]), NW);
@@ -84,7 +71,7 @@ __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_
 
     const int ua = rank * p.per_cta;                         // the CTA's stretch: units [ua, ua + per_cta), a multiple of 32
     auto units = [&](int row) {
-        return RowUnits<T, WHOLE>(reinterpret_cast<const T*>(p.z) + (long long)row * p.row_stride,
+        return RowUnits<T, L>(reinterpret_cast<const T*>(p.z) + (long long)row * p.row_stride,
                                   reinterpret_cast<const T*>(p.grad) + (long long)row * p.g_stride, p.V);
     };
     const float c1 = p.c1;
@@ -135,8 +122,8 @@ __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_
                 items[n & 3] = it;
                 uint64_t* const f = bar(full_s[n & 1]);
                 if (it.kind == 1) {
-                    const RowUnits<T, WHOLE> ru = units(it.row);
-                    const int g0 = max(ua, ru.glo), g1 = min(min(ua + p.per_cta, ru.NU) + (!WHOLE && ru.sh ? 1 : 0), ru.ghi);
+                    const RowUnits<T, L> ru = units(it.row);
+                    const int g0 = max(ua, ru.glo), g1 = min(min(ua + p.per_cta, ru.NU), ru.ghi);
                     const uint32_t bytes = (uint32_t)max(g1 - g0, 0) * 16u;
                     mbar_expect_tx(f, bytes);
                     if (bytes) bulk_g2s(dyn_smem + (n & 1) * kSdStage + (g0 - ua) * 16, ru.src + g0, bytes, f);
@@ -178,9 +165,14 @@ __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_
                 c.big = r.big;
                 coefs[n & 3] = c;
                 mbar_arrive_cta(bar(ready_s[n & 3]));
-                if (rank == 0) row_report(p, it.row, in, st);
+                hist[n & 31].s = st;
+                hist[n & 31].row = it.row;
             }
             __syncwarp();
+            if (rank == 0 && ((n & 31) == 31 || items[(n + 1) & 3].kind < 0)) {          // 32 rows' reports, a lane each
+                if (lane <= (n & 31)) row_report(p, hist[lane].row, row_in(p, hist[lane].row), hist[lane].s);
+                __syncwarp();
+            }
         }
         for (int n = posted - 1; n <= posted; ++n) mbar_wait_bounded(bar(full_s[n & 1]), (uint32_t)(n >> 1) & 1u);   // (no copy outlives the CTA)
     } else {
@@ -190,12 +182,12 @@ __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_
         // ... k = 0 .. count_of(un) - 1, un: end of the CTA's stretch
         auto count_of = [&](int un) { return max(0, (un - ua - warp * 32 + NW * 32 - 1) / (NW * 32)); };
         auto sum_row = [&](const DeepItem& it, int n) {
-            const RowUnits<T, WHOLE> ru = units(it.row);
+            const RowUnits<T, L> ru = units(it.row);
             const int un = min(ua + p.per_cta, ru.NU);
-            const RowStage<T, WHOLE> st(dyn_smem + (n & 1) * kSdStage, ru, ua, un);
+            const RowStage<T, L> st(dyn_smem + (n & 1) * kSdStage, ru, ua, un);
             uint32_t bad = 0u;
-            // the ends of the row, by the worker that reads them
-            if (!WHOLE && ua < un && ((ua == 0 && warp == 0) || (un == ru.NU && ((un - 1 - ua) >> 5) % NW == warp))) st.clean();
+            // The ends of the row, by the worker that reads them.  (A row that starts elsewhere may have had a unit more.)
+            if (!WHOLE && ua < un && ((ua == 0 && warp == 0) || (un == ru.NU && ((un - 1 - ua) >> 5) % NW == warp))) st.clean(1);
             typename U::Max mx = U::max0();
             const int nk = count_of(un);
             for_units<UPT>(nk, [&](int k) { U::max_add(mx, st.held(unit_at(k))); });
@@ -216,33 +208,35 @@ __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_
             const float4 mine = make_float4(m, __any_sync(0xFFFFFFFFu, bad) ? NAN : sums.x, sums.y, zx);
             if (lane < CS) st_async_v4(mapa_u32(&part[n & 3][rank * NW + warp], lane), mine, mapa_u32(bar(got_s[n & 3]), lane));
         };
-        wait(full_s[0], 0u);
-        if (alive && items[0].kind == 1) sum_row(items[0], 0);
-        for (int n = 0; alive; ++n) {
+        // n = -1: nothing to write yet
+        for (int n = -1; alive; ++n) {
             const int row = items[n & 3].row, x = items[n & 3].x;
-            for (int k = items[n & 3].zeros; k > 0; --k) {
-                const RowUnits<T, WHOLE> ru = units(row - k * ncl);
-                ru.store_zeros(reinterpret_cast<T*>(p.grad) + (long long)(row - k * ncl) * p.g_stride, ua, min(ua + p.per_cta, ru.NU), (int)threadIdx.x, NW * 32);
-            }
-            if (items[n & 3].kind < 0) break;
-            const RowUnits<T, WHOLE> ru = units(row);
+            const RowUnits<T, L> ru = units(max(row, 0));
             const int un = min(ua + p.per_cta, ru.NU), nk = count_of(un);
             uint4 w[UPT], last;
             const bool has_last = !WHOLE && ua < un && un > ru.whole_hi() && ru.NU - 1 >= ru.whole_lo() && ((un - 1 - ua) >> 5) % NW == warp;
-            const RowStage<T, WHOLE> st(dyn_smem + (n & 1) * kSdStage, ru, ua, un);
-            uint32_t v = 0u;
-            for_units<UPT>(nk, [&](int k) {
-                w[k] = st.held(unit_at(k));
-                v |= w[k].x;
-            });
-            if (has_last) last = st.held(ru.NU - 1);
-            __reduce_or_sync(0xFFFFFFFFu, v);            // (the loads have ended)
-            if (!WHOLE) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cta(bar(empty_s[n & 1]));
+            if (n >= 0) {
+                for (int k = items[n & 3].zeros; k > 0; --k) {
+                    const RowUnits<T, L> rz = units(row - k * ncl);
+                    rz.store_zeros(reinterpret_cast<T*>(p.grad) + (long long)(row - k * ncl) * p.g_stride, ua, min(ua + p.per_cta, rz.NU), (int)threadIdx.x, NW * 32);
+                }
+                if (items[n & 3].kind < 0) break;
+                const RowStage<T, L> st(dyn_smem + (n & 1) * kSdStage, ru, ua, un);
+                uint32_t v = 0u;
+                for_units<UPT>(nk, [&](int k) {
+                    w[k] = st.held(unit_at(k));
+                    v |= w[k].x;
+                });
+                if (has_last) last = st.held(ru.NU - 1);
+                __reduce_or_sync(0xFFFFFFFFu, v);            // (the loads have ended)
+                if (!WHOLE) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cta(bar(empty_s[n & 1]));
+            }
             wait(full_s[(n + 1) & 1], (uint32_t)((n + 1) >> 1) & 1u);
             if (!alive) break;
             if (items[(n + 1) & 3].kind == 1) sum_row(items[(n + 1) & 3], n + 1);
+            if (n < 0) continue;
             T* const g = reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride;
             wait(ready_s[n & 3], (uint32_t)(n >> 2) & 1u);
             if (!alive) break;

@@ -1,5 +1,6 @@
-// score_kernel for launches of many rows (same rows, same outputs): a cluster takes row after row, and while a row is summed
-// and its gradient formed from the registers that hold it, the next one is on its way into shared memory.
+// Losses with a gradient on many rows (same outputs as score_kernel), where rows are short or too long for score_deep_kernel: a
+// cluster takes row after row, and while a row is summed and its gradient formed from the registers that hold it, the next
+// one is on its way into shared memory.
 //
 // A warp owns a stretch of units of every row: it asks for it with one bulk copy, takes it into registers when it has landed,
 // and asks for the next row's at once, so that an SM has up to 128 KB of loads under way whatever its warps are at.  The warps'
@@ -11,14 +12,29 @@
 namespace adasd {
 
 constexpr int kSsUPT = 16;                                   // units a lane holds
-constexpr int kSsStage = (kSsUPT * 32 + 1) * 16;             // a warp's stretch (+ one unit: rows off 16-byte boundaries)
+constexpr int kSsStage = kSsUPT * 32 * 16;                   // a warp's stretch
 
-// What a warp keeps of 32 rows: inputs of their losses, until they are used (GRAD); its partials and the rows, until they are
-// folded (forward pass); the rows' statistics, until they are reported (GRAD, one warp of a cluster).
+// Statistics of a row until it is reported, 32 at a time.
 struct __align__(16) RowHist {
     RowStats s;
     int32_t row, pad[3];
 };
+
+// f(k) for k < n of UPT, four at a time without a branch between them (n: warp-uniform).
+template <int UPT, typename F>
+__device__ __forceinline__ void for_units(int n, F f) {
+#pragma unroll
+    for (int k = 0; k < UPT; k += 4) {
+        if (k + 4 <= UPT && n >= k + 4) {
+#pragma unroll
+            for (int i = k; i < (k + 4 < UPT ? k + 4 : UPT); ++i) f(i);
+        } else {
+#pragma unroll
+            for (int i = k; i < (k + 4 < UPT ? k + 4 : UPT); ++i)
+                if (i < n) f(i);
+        }
+    }
+}
 
 // The rows a cluster has to do, 32 at a time: lane j holds row first + (wi + j) clusters.  Rows left out are set aside.
 struct RowWindow {
@@ -27,29 +43,31 @@ struct RowWindow {
 };
 
 // A warp's stretch [ua, un) of a row in its stage: granule ua first.  Element e of the row is element e + off of the granules.
-template <typename T, bool WHOLE>
+template <typename T, int L>
 struct RowStage {
     using U = Unit<T>;
     static constexpr int N = U::N;
+    static constexpr bool WHOLE = L == ROWS_WHOLE;
     unsigned char* at;
-    const RowUnits<T, WHOLE>& ru;
+    const RowUnits<T, L>& ru;
     int ua, un, off;
-    __device__ __forceinline__ RowStage(unsigned char* at_, const RowUnits<T, WHOLE>& ru_, int ua_, int un_)
+    __device__ __forceinline__ RowStage(unsigned char* at_, const RowUnits<T, L>& ru_, int ua_, int un_)
         : at(at_), ru(ru_), ua(ua_), un(un_), off(WHOLE ? 0 : ru_.m0 + ru_.sh) {}
     __device__ __forceinline__ bool ends() const { return !WHOLE && ua < un && (ua == 0 || un == ru.NU); }
-    // what the row's first and last granules hold of its neighbours becomes -inf
-    __device__ __forceinline__ void clean() const {
+    // what the row's first and last granules hold of its neighbours becomes -inf, and `more` granules behind them
+    __device__ __forceinline__ void clean(int more) const {
         if (!ends()) return;
         const int lane = threadIdx.x & 31;
         T* const s = reinterpret_cast<T*>(at) - (long long)ua * N;
         const long long after = (long long)off + ru.V + lane;
         if (ua == 0 && lane < off) put(s + lane, -INFINITY);
-        if (un == ru.NU && after < (long long)(ru.NU + 1) * N) put(s + after, -INFINITY);
+        if (un == ru.NU && after < (long long)(ru.NU + more) * N) put(s + after, -INFINITY);
         __syncwarp();
     }
     __device__ __forceinline__ uint4 held(int u) const {
         const uint4* const g = reinterpret_cast<const uint4*>(at) + (u - ua);
-        return WHOLE || ru.sh == 0 ? *g : U::realign(g[0], g[1], ru.sh);
+        static_assert(L != ROWS_ANY, "units that lie across granules are score_kernel's");
+        return *g;
     }
     __device__ __forceinline__ bool owns(int x) const {
         const int u = ru.unit_of(x);
@@ -66,9 +84,10 @@ struct RowStage {
 };
 
 // Gradient of a warp's stretch, from its registers.  last: the row's last unit where it is not whole and in this stretch.
-template <typename T, bool WHOLE, bool ENT, int UPT>
-__device__ __forceinline__ void write_row(T* g, const uint4 (&w)[UPT], const uint4& last, bool has_last, const RowUnits<T, WHOLE>& ru, int ua,
+template <typename T, int L, bool ENT, int UPT>
+__device__ __forceinline__ void write_row(T* g, const uint4 (&w)[UPT], const uint4& last, bool has_last, const RowUnits<T, L>& ru, int ua,
                                           int un, int x, const RowGrad& r, const RowStats& st, float c1) {
+    constexpr bool WHOLE = L == ROWS_WHOLE;
     const int lane = threadIdx.x & 31;
     if (r.zero) {
         ru.store_zeros(g, ua, un, lane, 32);
@@ -103,17 +122,17 @@ __device__ __forceinline__ void write_row(T* g, const uint4 (&w)[UPT], const uin
     if (ox >= 0 && ox < un - ua && lane == (ox & 31)) grad_token<T, ENT>(g, x, st.zx, st.M, c1, r);
 }
 
-template <typename T, bool WHOLE, int NW, bool GRAD, bool ENT>
+template <typename T, int L, int NW, bool ENT>
 __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __grid_constant__ ScoreParams p) {
     using U = Unit<T>;
     constexpr int N = U::N, UPT = kSsUPT;
+    constexpr bool WHOLE = L == ROWS_WHOLE;
     const float floor_v = N == 8 ? ADASD_FLOOR_BF : kFloor;
     extern __shared__ __align__(128) unsigned char dyn_smem[];
-    __shared__ float4 part[2][GRAD ? kScMaxCluster * NW : 1];
+    __shared__ float4 part[2][kScMaxCluster * NW];
     __shared__ unsigned long long full_s[NW], got_s[2];
-    __shared__ RowHist hist[GRAD ? 32 : 1];
-    __shared__ float4 keep[NW][32];                          // GRAD: RowIn of the window's rows; else the partials of 32 rows
-    __shared__ int2 rows_s[GRAD ? 1 : 32];                   // ... and which rows, with their tokens
+    __shared__ RowHist hist[32];
+    __shared__ float4 keep[NW][32];                          // RowIn of the window's rows
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int CS = p.cs, ncl = (int)(gridDim.x / (unsigned)CS), cl = (int)(blockIdx.x / (unsigned)CS);
     const int rank = (int)(blockIdx.x - (unsigned)cl * (unsigned)CS);
@@ -137,7 +156,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
     const int ua = (rank * NW + warp) * p.per_cta, ub = ua + p.per_cta;          // (per_cta: units of a WARP here)
     auto units = [&](int row) {
         const T* const z = reinterpret_cast<const T*>(p.z) + (long long)row * p.row_stride;
-        return RowUnits<T, WHOLE>(z, GRAD ? reinterpret_cast<const T*>(p.grad) + (long long)row * p.g_stride : z, p.V);
+        return RowUnits<T, L>(z, reinterpret_cast<const T*>(p.grad) + (long long)row * p.g_stride, p.V);
     };
     RowWindow win;
     auto open = [&](int wi) {
@@ -150,20 +169,18 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
             kind = row_kind(p, (int)r, win.x);
             if (keeper && kind != 1) row_report_out(p, (int)r, kind);
         }
-        if (GRAD) {
-            RowIn in{0.f, 0.f, 0.f, 0.f};
-            if (kind == 1) in = row_in(p, (int)r);
-            __syncwarp();
-            keep[warp][lane] = make_float4(in.adv, in.old, in.ref, in.w);
-            __syncwarp();
-        }
+        RowIn in{0.f, 0.f, 0.f, 0.f};
+        if (kind == 1) in = row_in(p, (int)r);
+        __syncwarp();
+        keep[warp][lane] = make_float4(in.adv, in.old, in.ref, in.w);
+        __syncwarp();
         win.todo = __ballot_sync(0xFFFFFFFFu, kind == 1);
-        win.zero = GRAD ? __ballot_sync(0xFFFFFFFFu, kind == 0) : 0u;
+        win.zero = __ballot_sync(0xFFFFFFFFu, kind == 0);
     };
     auto zero_row = [&]() {                                  // one row set aside
         const int j = __ffs(win.zero) - 1, row = __shfl_sync(0xFFFFFFFFu, win.row, j);
         win.zero &= win.zero - 1;
-        const RowUnits<T, WHOLE> ru = units(row);
+        const RowUnits<T, L> ru = units(row);
         T* const g = reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride;
         ru.store_zeros(g, ua, min(ub, ru.NU), lane, 32);
     };
@@ -171,7 +188,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
     float4 inputs;                                           // of its loss
     auto next = [&]() {
         while (!win.todo) {
-            while (GRAD && win.zero) zero_row();
+            while (win.zero) zero_row();
             row = -1;
             if ((long long)cl + (long long)(win.wi + 32) * ncl >= p.n_rows) return;
             open(win.wi + 32);
@@ -180,12 +197,12 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         win.todo &= win.todo - 1;
         row = __shfl_sync(0xFFFFFFFFu, win.row, j);
         x = __shfl_sync(0xFFFFFFFFu, win.x, j);
-        if (GRAD) inputs = keep[warp][j];
+        inputs = keep[warp][j];
     };
     auto ask = [&]() {                                       // its stretch: granules from unit ua's first on that hold elements
         if (lane == 0) {
-            const RowUnits<T, WHOLE> ru = units(row);
-            const int g0 = max(ua, ru.glo), g1 = min(min(ub, ru.NU) + (!WHOLE && ru.sh ? 1 : 0), ru.ghi);
+            const RowUnits<T, L> ru = units(row);
+            const int g0 = max(ua, ru.glo), g1 = min(min(ub, ru.NU), ru.ghi);
             const uint32_t bytes = (uint32_t)max(g1 - g0, 0) * 16u;
             mbar_expect_tx(full, bytes);
             if (bytes) bulk_g2s(stage + (g0 - ua) * 16, ru.src + g0, bytes, full);
@@ -205,11 +222,11 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
     int done = 0;
     while (row >= 0) {
         const int my_row = row, my_x = x, par = done & 1;
-        const RowUnits<T, WHOLE> ru = units(my_row);
+        const RowUnits<T, L> ru = units(my_row);
         const int un = min(ub, ru.NU);
         const RowIn in{inputs.x, inputs.y, inputs.z, inputs.w};
         uint64_t* const got = reinterpret_cast<uint64_t*>(&got_s[par]);
-        if (GRAD && CS > 1 && warp == 0 && lane == 0) mbar_expect_tx(got, (uint32_t)(CS * NW) * 16u);
+        if (CS > 1 && warp == 0 && lane == 0) mbar_expect_tx(got, (uint32_t)(CS * NW) * 16u);
         if (asked) {
             const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(full, ph));
             if (!ok && lane == 0) atomicOr(p.status, ADASD_STATUS_TIMEOUT);
@@ -217,8 +234,8 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         }
         ph ^= 1u;
         uint32_t bad = alive ? 0u : 1u;
-        const RowStage<T, WHOLE> rs(stage, ru, ua, un);
-        rs.clean();
+        const RowStage<T, L> rs(stage, ru, ua, un);
+        rs.clean(0);
         uint4 w[UPT], last;
         typename U::Max mx = U::max0();
 #pragma unroll
@@ -226,7 +243,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
             const int u = ua + k * 32 + lane;
             w[k] = u < un ? rs.held(u) : U::none4();
         }
-        const bool has_last = GRAD && !WHOLE && ua < un && un > ru.whole_hi() && ru.NU - 1 >= ru.whole_lo();
+        const bool has_last = !WHOLE && ua < un && un > ru.whole_hi() && ru.NU - 1 >= ru.whole_lo();
         if (has_last) last = rs.held(ru.NU - 1);
 #pragma unroll
         for (int k = 0; k < UPT; ++k) U::max_add(mx, w[k]);
@@ -240,33 +257,6 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
         if (asked) ask();
         const float2 sums = sum_units<T, ENT, UPT>(w, m, c1, L2, [&](int k) { return ua + k * 32 < un; });
         const float4 mine = make_float4(m, __any_sync(0xFFFFFFFFu, bad) ? NAN : sums.x, sums.y, zx);
-        if (!GRAD) {
-            // forward pass: nothing waits for the totals; 32 rows are folded and reported at a time, by all warps of the cluster
-            if (lane == 0) {
-                keep[warp][done & 31] = mine;
-                if (warp == 0) rows_s[done & 31] = make_int2(my_row, my_x);
-            }
-            ++done;
-            if ((done & 31) == 0 || row < 0) {
-                const int n = ((done - 1) & 31) + 1;
-                if (CS > 1) cluster.sync();
-                else __syncthreads();
-                RowStats st;
-                int cnt = 0, which = 0;
-                for (int j = rank * NW + warp; j < n; j += CS * NW, ++cnt) {
-                    const RowStats f = fold_partials<kScMaxCluster * NW>(
-                        [&](int k) { return *cluster.map_shared_rank(&keep[k % NW][j], k / NW); }, CS * NW, c1, floor_v);
-                    if (lane == cnt) {
-                        st = f;
-                        which = j;
-                    }
-                }
-                if (lane < cnt) row_report(p, rows_s[which].x, row_in(p, rows_s[which].x), st);
-                if (CS > 1) cluster.sync();
-                else __syncthreads();
-            }
-            continue;
-        }
         if (CS > 1) {
             if (lane < CS) st_async_v4(mapa_u32(&part[par][rank * NW + warp], lane), mine, mapa_u32(got, lane));
             if (alive) {
@@ -287,11 +277,9 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
             st = fold_partials<kScMaxCluster * NW>([&](int k) { return part[par][k]; }, CS * NW, c1, floor_v);
         }
         if (!alive) st.S = NAN;
-        if (GRAD) {
-            const RowGrad r = row_grad(p, in, st, c1, L2, ENT);
-            T* const g = reinterpret_cast<T*>(p.grad) + (long long)my_row * p.g_stride;
-            write_row<T, WHOLE, ENT, UPT>(g, w, last, has_last, ru, ua, un, my_x, r, st, c1);
-        }
+        const RowGrad r = row_grad(p, in, st, c1, L2, ENT);
+        T* const g = reinterpret_cast<T*>(p.grad) + (long long)my_row * p.g_stride;
+        write_row<T, L, ENT, UPT>(g, w, last, has_last, ru, ua, un, my_x, r, st, c1);
         if (keeper && lane == 0) {
             RowHist& h = hist[done & 31];
             h.s = st;
@@ -304,7 +292,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) score_stream_kernel(const __
             __syncwarp();
         }
     }
-    if (GRAD && CS > 1) cluster.sync();                      // (nobody leaves while a warp's partials are on their way to it)
+    if (CS > 1) cluster.sync();                      // (nobody leaves while a warp's partials are on their way to it)
 }
 
 }  // namespace adasd
