@@ -70,10 +70,30 @@ int launch_rows(Resident& resident, K kern, ScoreParams p, int threads, int smem
     p.per_cta = per;
     return launch_pdl(kern, (int)ncl * cs, threads, smem, cs, stream, p);
 }
+// CTAs of a row: as many as make the last of the resident clusters' rounds end first, a CTA more costing a row 3 % more.
 template <typename T, int L, int NW, bool ENT>
-int launch_forward(const ScoreParams& p, int cs, int per, cudaStream_t stream) {
+int launch_forward(ScoreParams p, int NU, int most, cudaStream_t stream) {
     static Resident r;
-    return launch_rows(r, score_forward_kernel<T, L, NW, ENT>, p, NW * 32, NW * 2 * kSfStage, cs, per, 1, stream);
+    const auto kern = score_forward_kernel<T, L, NW, ENT>;
+    const int smem = NW * 2 * kSfStage;
+    int best = 0, best_n = 0;
+    double least = 0.0;
+    for (int cs = 1; cs <= most; ++cs) {
+        const int n = r(kern, NW * 32, smem, cs);
+        if (n == 0) continue;
+        const double t = (double)((p.n_rows + n - 1) / n) / cs * (1.0 + 0.03 * (cs - 1));
+        if (best == 0 || t < least) {
+            least = t;
+            best = cs;
+            best_n = n;
+        }
+    }
+    if (best == 0) return kNotTaken;
+    const int per = (NU + NW * best - 1) / (NW * best), its = (per + 31) / 32;
+    p.pieces = (its + kSfUPT - 1) / kSfUPT;
+    p.per_cta = (its + p.pieces - 1) / p.pieces * 32 * p.pieces;
+    p.cs = best;
+    return launch_pdl(kern, std::min(best_n, p.n_rows) * best, NW * 32, smem, best, stream, p);
 }
 template <typename T, int L, int NW, bool ENT>
 int launch_stream(const ScoreParams& p, int cs, int per, cudaStream_t stream) {
@@ -87,25 +107,24 @@ int launch_deep(const ScoreParams& p, int cs, int per, cudaStream_t stream) {
 }
 // Many rows.
 template <typename T, int L, bool ENT>
-int launch_many(const ScoreParams& p, int NU, cudaStream_t stream) {
+int launch_many(const ScoreParams& p, int NU, int sms, cudaStream_t stream) {
+    if (!p.grad && (long long)p.n_rows * kScMaxCluster <= 2LL * sms) return kNotTaken;
     const int its = (NU + 31) / 32;
     if (p.grad && NU >= 2048) {
         const int cs = (NU + kSdUnits - 1) / kSdUnits;
         if (cs <= kScMaxCluster)
             if (const int rc = launch_deep<T, L, ENT>(p, cs, (its + cs - 1) / cs * 32, stream); rc != kNotTaken) return rc;
     }
-    static_assert(kSfWarpUnits == kSsUPT * 32, "either kernel's warps take as many units");
-    const int warps = (NU + kSfWarpUnits - 1) / kSfWarpUnits;
+    const int warps = (NU + kSsUPT * 32 - 1) / (kSsUPT * 32);
     auto launch = [&](auto nw, int cs) -> int {
         constexpr int NW = decltype(nw)::value;
-        const int per = (NU + NW * cs - 1) / (NW * cs);
-        return p.grad ? launch_stream<T, L, NW, ENT>(p, cs, per, stream) : launch_forward<T, L, NW, ENT>(p, cs, per, stream);
+        if (p.grad) return cs <= kScMaxCluster ? launch_stream<T, L, NW, ENT>(p, cs, (NU + NW * cs - 1) / (NW * cs), stream) : kNotTaken;
+        return launch_forward<T, L, NW, ENT>(p, NU, NW == 8 ? kScMaxCluster : 1, stream);
     };
     if (warps == 1) return launch(std::integral_constant<int, 1>{}, 1);
     if (warps == 2) return launch(std::integral_constant<int, 2>{}, 1);
     if (warps <= 4) return launch(std::integral_constant<int, 4>{}, 1);
-    if (warps <= 8 * kScMaxCluster) return launch(std::integral_constant<int, 8>{}, (warps + 7) / 8);
-    return kNotTaken;
+    return launch(std::integral_constant<int, 8>{}, (warps + 7) / 8);
 }
 
 constexpr int kScNW = 8, kScUnits = kScNW * 32;      // score_kernel: CTAs of 8 warps; units of a CTA and unit a thread
@@ -130,7 +149,7 @@ int launch_few(ScoreParams p, int NU, int sms, cudaStream_t stream) {
 template <typename T, int L, bool ENT>
 int launch(const ScoreParams& p, int NU, int sms, cudaStream_t stream) {
     if constexpr (L != ROWS_ANY)
-        if (const int rc = launch_many<T, L, ENT>(p, NU, stream); rc != kNotTaken) return rc;
+        if (const int rc = launch_many<T, L, ENT>(p, NU, sms, stream); rc != kNotTaken) return rc;
     if (p.grad) return launch_few<T, L, true, ENT>(p, NU, sms, stream);
     if constexpr (L != ROWS_ANY) return launch_few<T, L, false, ENT>(p, NU, sms, stream);
     return ADASD_ERR_SHAPE;                          // (without a gradient no row lies across granules)

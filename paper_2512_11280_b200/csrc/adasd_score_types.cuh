@@ -29,7 +29,7 @@ struct ScoreParams {
     void* grad;                                    // nullable
     long long g_stride;
     int32_t n_rows, V, op;
-    int32_t cs, per_cta;                           // CTAs per row; 16-byte units of a CTA
+    int32_t cs, per_cta, pieces;                   // CTAs per row; 16-byte units of a CTA (or a warp), in pieces
     float c1;                                      // log2 e / temperature
     double inv_temp;
     uint32_t* status;

@@ -372,7 +372,8 @@ def test_they_run_together(torch):
     A = torch.randn(n, generator=g, device="cuda")
     grad, again = torch.empty_like(z), torch.empty_like(z)
     ctx.policy_loss(z, tok, A, rl, old_logp=lo, ref_logp=lr, kl_coef=0.2, logp_out=lp2, kl_out=kl, grad_out=grad)
-    assert torch.equal(lp, lp2)
+    # (either call is its tolerance off the truth at the most; they may sum in different orders)
+    assert bool(((lp.double() - lp2.double()).abs() <= 2 * (ref.E + ref.U32 * lp.double().abs())).all())
     l = lp.double().requires_grad_(True)
     ratio, r = torch.exp(l - lo.double()), lr.double() - l
     loss = -torch.minimum(ratio * A, ratio.clamp(0.8, 1.2) * A) + 0.2 * (torch.exp(r) - r - 1)
