@@ -84,6 +84,7 @@ struct Unit<__nv_bfloat16> {
     // largest element of a unit (NaN kept), and as one number (NaN dropped)
     static __device__ __forceinline__ Max unit_max(const uint4& w) { return bmax2(bmax2(w.x, w.y), bmax2(w.z, w.w)); }
     static __device__ __forceinline__ void max_join(Max& m, Max h) { m = bmax2(m, h); }
+    static __device__ __forceinline__ uint32_t bits(Max h) { return h; }
     static __device__ __forceinline__ float top(Max h) {
         const float2 v = unpack2(h);
         return fmaxf(v.x, v.y);
@@ -154,6 +155,7 @@ struct Unit<float> {
         return fmax_nan(fmax_nan(__uint_as_float(w.x), __uint_as_float(w.y)), fmax_nan(__uint_as_float(w.z), __uint_as_float(w.w)));
     }
     static __device__ __forceinline__ void max_join(Max& m, Max h) { m = fmax_nan(m, h); }
+    static __device__ __forceinline__ uint32_t bits(Max h) { return __float_as_uint(h); }
     static __device__ __forceinline__ float top(Max h) { return h; }
     static __device__ __forceinline__ float max_val(Max m, uint32_t& bad) {
         if (m != m) bad = 1u;

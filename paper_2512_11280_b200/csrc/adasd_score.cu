@@ -75,7 +75,7 @@ template <typename T, int L, int NW, bool ENT>
 int launch_forward(ScoreParams p, int NU, int most, cudaStream_t stream) {
     static Resident r;
     const auto kern = score_forward_kernel<T, L, NW, ENT>;
-    const int smem = NW * 2 * kSfStage;
+    constexpr int smem = NW * kSfRingB;
     int best = 0, best_n = 0;
     double least = 0.0;
     for (int cs = 1; cs <= most; ++cs) {
@@ -89,9 +89,9 @@ int launch_forward(ScoreParams p, int NU, int most, cudaStream_t stream) {
         }
     }
     if (best == 0) return kNotTaken;
-    const int per = (NU + NW * best - 1) / (NW * best), its = (per + 31) / 32;
-    p.pieces = (its + kSfUPT - 1) / kSfUPT;
-    p.per_cta = (its + p.pieces - 1) / p.pieces * 32 * p.pieces;
+    const int its = ((NU + 31) / 32 + NW * best - 1) / (NW * best);
+    p.pieces = (its + kSfGroup - 1) / kSfGroup;
+    p.per_cta = its * 32;
     p.cs = best;
     return launch_pdl(kern, std::min(best_n, p.n_rows) * best, NW * 32, smem, best, stream, p);
 }
