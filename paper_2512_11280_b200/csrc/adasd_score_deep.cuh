@@ -141,10 +141,6 @@ __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_
         for (int n = 0;; ++n) {
             const DeepItem it = items[n & 3];
             if (it.kind < 0) break;
-            wait(empty_s[n & 1], (uint32_t)(n >> 1) & 1u);
-            if (!alive) break;
-            post(n + 2);
-            posted = n + 2;
             wait(got_s[n & 3], (uint32_t)(n >> 2) & 1u);
             if (!alive) break;
             const RowStats st = fold_partials<kScMaxCluster * NW>([&](int k) { return part[n & 3][k]; }, CS * NW, c1, floor_v);
@@ -169,6 +165,11 @@ __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_
                 hist[n & 31].row = it.row;
             }
             __syncwarp();
+            // (its constants first: the workers are at the gradient of the row before, and will ask for them after the next sums)
+            wait(empty_s[n & 1], (uint32_t)(n >> 1) & 1u);
+            if (!alive) break;
+            post(n + 2);
+            posted = n + 2;
             if (rank == 0 && ((n & 31) == 31 || items[(n + 1) & 3].kind < 0)) {          // 32 rows' reports, a lane each
                 if (lane <= (n & 31)) row_report(p, hist[lane].row, row_in(p, hist[lane].row), hist[lane].s);
                 __syncwarp();

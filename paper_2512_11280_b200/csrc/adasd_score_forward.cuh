@@ -37,6 +37,20 @@ __device__ __noinline__ float2 big_sums(const RowUnits<T, L>& ru, int u0, int un
     return make_float2(warp_sum(S2.x + S2.y), ENT ? warp_sum(T2.x + T2.y) : 0.f);
 }
 
+// {S, T} of a warp under its largest logit M from its lanes' under their shifts s.
+template <bool ENT>
+__device__ __forceinline__ float2 join_lanes(float2 S2, float2 T2, float s, float M, float c1, float floor_v) {
+    if (!(M > floor_v)) return make_float2(0.f, 0.f);
+    const float sM = M * c1, d = fmaxf(s - sM, kLowT), f = ex2(d);
+    float2 r;
+    r.x = warp_sum(f * (S2.x + S2.y));
+    r.y = ENT ? warp_sum(f * fmaf(d, S2.x + S2.y, T2.x + T2.y)) : 0.f;
+    const float tm = fmaf(M, c1, -sM), em = ex2(tm);         // (as finish_sums)
+    if (ENT) r.y = (r.y - __fmul_rn(tm, r.x)) / em;
+    r.x /= em;
+    return r;
+}
+
 template <typename T, int L, int NW, bool ENT>
 __global__ void __launch_bounds__(NW * 32, kSfWarps / NW) score_forward_kernel(const __grid_constant__ ScoreParams p) {
     using U = Unit<T>;
@@ -189,18 +203,7 @@ __global__ void __launch_bounds__(NW * 32, kSfWarps / NW) score_forward_kernel(c
         uint32_t bad = 0u;
         const float v = U::max_val(mx, bad), M = warp_max_f32(v);
         if (M == INFINITY) bad = 1u;
-        float2 r;
-        if (M > floor_v && big_shift(M, c1)) {
-            r = big_sums<T, L, ENT>(ru, ua, un, M, c1);
-        } else {
-            const float sM = M > floor_v ? M * c1 : s, d = fmaxf(s - sM, kLowT), f = ex2(d);
-            r.x = warp_sum(f * (S2.x + S2.y));
-            r.y = ENT ? warp_sum(f * fmaf(d, S2.x + S2.y, T2.x + T2.y)) : 0.f;
-            const float tm = fmaf(M, c1, -sM), em = ex2(tm); // (as finish_sums)
-            if (ENT) r.y = (r.y - __fmul_rn(tm, r.x)) / em;
-            r.x /= em;
-            if (!(M > floor_v)) r = make_float2(0.f, 0.f);
-        }
+        const float2 r = M > floor_v && big_shift(M, c1) ? big_sums<T, L, ENT>(ru, ua, un, M, c1) : join_lanes<ENT>(S2, T2, s, M, c1, floor_v);
         const bool any_bad = __any_sync(0xFFFFFFFFu, bad);
         if (lane == 0) {
             keep[set][warp][at] = make_float4(M, any_bad ? NAN : r.x, r.y, zx);
