@@ -1155,11 +1155,13 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
         p.pref = s.pref;
         p.seq_logp = seq_logp_out_dev;
         p.pair_loss = pair_loss_out_dev;
+        p.loss = loss_out_dev;
         if (int rc = launch_pref_pairs(p, st)) return rc;
         if (grad_logits_dev && n_rows > 0)
             if (int rc = launch_pref_grad(p, ctx->cfg.dtype, st)) return rc;
+        return ADASD_OK;
     }
-    return loss_out_dev ? launch_total(pair_loss_out_dev, n_pairs, loss_out_dev, st) : ADASD_OK;
+    return loss_out_dev ? launch_total(nullptr, 0, loss_out_dev, st) : ADASD_OK;
 }
 
 int adasd_set_warpers(adasd_ctx* ctx, float temperature, int32_t top_k, float top_p) {

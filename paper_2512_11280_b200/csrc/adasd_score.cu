@@ -178,7 +178,12 @@ int launch_score(const ScoreParams& p, int dtype, bool entropy, int sm_count, cu
 }
 
 int launch_pref_pairs(const PrefParams& p, cudaStream_t stream) {
-    return launch_pdl(pref_pair_kernel, p.n_pairs, kPairThreads, 0, 0, stream, p);
+    if (p.loss && p.n_pairs <= kPairSum) {
+        const int cs = std::min(8, p.n_pairs);
+        return launch_pdl(pref_pair_kernel, cs, kPairThreads, 0, cs, stream, p, 1);
+    }
+    if (const int rc = launch_pdl(pref_pair_kernel, p.n_pairs, kPairThreads, 0, 1, stream, p, 0)) return rc;
+    return p.loss ? launch_total(p.pair_loss, p.n_pairs, p.loss, stream) : ADASD_OK;
 }
 
 int launch_pref_grad(PrefParams p, int dtype, cudaStream_t stream) {

@@ -134,19 +134,33 @@ __device__ __forceinline__ void exponents(const uint4& w, const Shift& c, float2
     }
 }
 
-// dL/dz of a unit: 2^q (b + a q).
+// 2^q on the FMA pipe, q <= 126: 2^n 2^f with n = q rounded, f in [-1/2, 1/2], 2^f by the degree-4 polynomial of least relative
+// error there, 2.6e-6 (fitted by reweighted least squares).  Below -126 it stays at 2^-126.
+__device__ __forceinline__ float2 exp2_fma(float2 q) {
+    const float2 big = make_float2(12582912.f, 12582912.f);              // 1.5 2^23: the sum's last bit is 1
+    q = make_float2(fmaxf(q.x, -126.f), fmaxf(q.y, -126.f));
+    const float2 r = __fadd2_rn(q, big);
+    const float2 f = __ffma2_rn(__fadd2_rn(r, make_float2(-12582912.f, -12582912.f)), make_float2(-1.f, -1.f), q);
+    float2 y = __ffma2_rn(f, make_float2(9.570102207362652e-3f, 9.570102207362652e-3f), make_float2(5.591785907745361e-2f, 5.591785907745361e-2f));
+    y = __ffma2_rn(y, f, make_float2(2.40247443318367e-1f, 2.40247443318367e-1f));
+    y = __ffma2_rn(y, f, make_float2(6.931217908859253e-1f, 6.931217908859253e-1f));
+    y = __ffma2_rn(y, f, make_float2(9.999992847442627e-1f, 9.999992847442627e-1f));
+    return make_float2(__int_as_float(__float_as_int(y.x) + (__float_as_int(r.x) << 23)), __int_as_float(__float_as_int(y.y) + (__float_as_int(r.y) << 23)));
+}
+
+// dL/dz of a unit: 2^q (b + a q).  FMA: pairs (of a bf16 unit's four) whose 2^q comes from the FMA pipe.
 struct GradConsts {
     Shift s;
     float2 a2, b2;
 };
-template <typename T, bool ENT, bool BIG>
+template <typename T, bool ENT, bool BIG, int FMA = 0>
 __device__ __forceinline__ uint4 grad_unit(const uint4& w, const GradConsts& c) {
     using U = Unit<T>;
     float2 q[U::N / 2];
     exponents<T, ENT, BIG>(w, c.s, q);
 #pragma unroll
     for (int j = 0; j < U::N / 2; ++j) {
-        const float2 e = make_float2(ex2(q[j].x), ex2(q[j].y));
+        const float2 e = sizeof(T) == 2 && !BIG && j < FMA ? exp2_fma(q[j]) : make_float2(ex2(q[j].x), ex2(q[j].y));
         q[j] = __fmul2_rn(e, ENT ? __ffma2_rn(q[j], c.a2, c.b2) : c.b2);
     }
     return pack16(q);
@@ -522,65 +536,86 @@ __global__ void __launch_bounds__(kTotThreads) total_kernel(const float* terms, 
     if (threadIdx.x == 0) *out = (float)v;
 }
 
-// A pair: log-probs of its two sequences, its loss, and dL/dl of its rows.
-constexpr int kPairThreads = 256;
-__global__ void __launch_bounds__(kPairThreads) pref_pair_kernel(const __grid_constant__ PrefParams p) {
-    __shared__ double s[kPairThreads / 32];
+// Pairs: log-probs of the two sequences, the loss, and dL/dl of their rows; either sequence has half of a CTA's threads.  total: the
+// launch is one cluster (of at most kPairSum pairs), which adds the losses up in the pairs' order; else a CTA a pair.
+constexpr int kPairThreads = 512, kPairHalf = kPairThreads / 2, kPairSum = 64;
+__global__ void __launch_bounds__(kPairThreads) pref_pair_kernel(const __grid_constant__ PrefParams p, int total) {
+    __shared__ double s[2][kPairThreads / 32];
+    __shared__ float losses[kPairSum];
+    const int P = p.n_pairs, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int k = threadIdx.x >= kPairHalf ? 1 : 0, t0 = (int)threadIdx.x - k * kPairHalf;      // 1: the rejected sequence
     pdl_wait();
     pdl_trigger();
-    const int P = p.n_pairs, i = blockIdx.x;
     const double iT = 1.0 / (double)p.temperature;
-    double l[2];
-    int first[2], end[2];
-    double count[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int i = blockIdx.x; i < P; i += (int)gridDim.x) {
         const int q = i + k * P;
-        first[k] = min(max(__ldcg(p.seq_start + q), 0), p.n_rows);
-        end[k] = min(max(__ldcg(p.seq_start + q + 1), first[k]), p.n_rows);
+        const int first = min(max(__ldcg(p.seq_start + q), 0), p.n_rows), end = min(max(__ldcg(p.seq_start + q + 1), first), p.n_rows);
         double t = 0.0, n = 0.0;
-        for (int r = first[k] + (int)threadIdx.x; r < end[k]; r += kPairThreads) {
+        for (int r = first + t0; r < end; r += kPairHalf) {
             const float4 e = __ldcg(reinterpret_cast<const float4*>(p.pref + r));
             if (__float_as_int(e.w) == 1) {
                 t += (double)e.z * iT - log((double)e.y);
                 n += 1.0;
             }
         }
-        l[k] = block_sum_f64<kPairThreads>(t, s);
-        count[k] = block_sum_f64<kPairThreads>(n, s);
-        if (p.average && count[k] > 0.0) l[k] /= count[k];
-    }
-    const double w = (double)p.scale * (p.pair_weight ? (double)__ldcg(p.pair_weight + i) : 1.0);
-    const double D = p.ref_logp ? (l[0] - (double)__ldcg(p.ref_logp + i)) - (l[1] - (double)__ldcg(p.ref_logp + P + i)) : l[0] - l[1];
-    const double beta = (double)p.beta, margin = (double)p.margin;
-    double loss, dD;
-    if (p.rule == ADASD_PREF_SIGMOID) {
-        // -(1 - e) ln sigma(u) - e ln sigma(-u) = max(-u, 0) + ln(1 + e^-|u|) + e u
-        const double u = beta * D - margin, ls = (double)p.label_smoothing, t = exp(-fabs(u));
-        loss = (u < 0.0 ? -u : u == u ? 0.0 : u) + log1p(t) + (ls != 0.0 ? ls * u : 0.0);
-        dD = beta * (ls - (u >= 0.0 ? t / (1.0 + t) : 1.0 / (1.0 + t)));
-    } else if (p.rule == ADASD_PREF_SQUARED) {
-        const double u = D - margin - 0.5 / beta;
-        loss = u * u;
-        dD = 2.0 * u;
-    } else {
-        const double u = 1.0 - (beta * D - margin);
-        loss = u > 0.0 ? u : u == u ? 0.0 : u;
-        dD = u > 0.0 ? -beta : u == u ? 0.0 : u;
-    }
-    const bool off = w == 0.0;
-    if (threadIdx.x == 0) {
-        p.seq_logp[i] = (float)l[0];
-        p.seq_logp[i + P] = (float)l[1];
-        p.pair_loss[i] = off ? 0.f : (float)(w * loss);
-    }
-    if (!p.grad) return;
+        t = warp_sum_f64(t);
+        n = warp_sum_f64(n);
+        __syncthreads();                                     // (the pair before has been read)
+        if (lane == 0) {
+            s[0][warp] = t;
+            s[1][warp] = n;
+        }
+        __syncthreads();
+        double l[2] = {0.0, 0.0}, count[2] = {0.0, 0.0};
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        double d = off ? 0.0 : (k ? -w : w) * dD;
-        if (p.average && count[k] > 0.0) d /= count[k];
-        const float df = (float)d;
-        for (int r = first[k] + (int)threadIdx.x; r < end[k]; r += kPairThreads) p.pref[r].dz = df;
+        for (int w = 0; w < kPairThreads / 32; ++w) {
+            l[w / (kPairHalf / 32)] += s[0][w];
+            count[w / (kPairHalf / 32)] += s[1][w];
+        }
+        if (p.average) {
+            if (count[0] > 0.0) l[0] /= count[0];
+            if (count[1] > 0.0) l[1] /= count[1];
+        }
+        const double w = (double)p.scale * (p.pair_weight ? (double)__ldcg(p.pair_weight + i) : 1.0);
+        const double D = p.ref_logp ? (l[0] - (double)__ldcg(p.ref_logp + i)) - (l[1] - (double)__ldcg(p.ref_logp + P + i)) : l[0] - l[1];
+        const double beta = (double)p.beta, margin = (double)p.margin;
+        double loss, dD;
+        if (p.rule == ADASD_PREF_SIGMOID) {
+            // -(1 - e) ln sigma(u) - e ln sigma(-u) = max(-u, 0) + ln(1 + e^-|u|) + e u
+            const double u = beta * D - margin, ls = (double)p.label_smoothing, e = exp(-fabs(u));
+            loss = (u < 0.0 ? -u : u == u ? 0.0 : u) + log1p(e) + (ls != 0.0 ? ls * u : 0.0);
+            dD = beta * (ls - (u >= 0.0 ? e / (1.0 + e) : 1.0 / (1.0 + e)));
+        } else if (p.rule == ADASD_PREF_SQUARED) {
+            const double u = D - margin - 0.5 / beta;
+            loss = u * u;
+            dD = 2.0 * u;
+        } else {
+            const double u = 1.0 - (beta * D - margin);
+            loss = u > 0.0 ? u : u == u ? 0.0 : u;
+            dD = u > 0.0 ? -beta : u == u ? 0.0 : u;
+        }
+        const bool off = w == 0.0;
+        const float term = off ? 0.f : (float)(w * loss);
+        if (threadIdx.x == 0) {
+            p.seq_logp[i] = (float)l[0];
+            p.seq_logp[i + P] = (float)l[1];
+            p.pair_loss[i] = term;
+            if (total) *cg::this_cluster().map_shared_rank(losses + i, 0) = term;
+        }
+        if (p.grad) {
+            double d = off ? 0.0 : (k ? -w : w) * dD;
+            if (p.average && count[k] > 0.0) d /= count[k];
+            const float df = (float)d;
+            for (int r = first + t0; r < end; r += kPairHalf) p.pref[r].dz = df;
+        }
+    }
+    if (total) {
+        cg::this_cluster().sync();
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            double v = 0.0;
+            for (int i = 0; i < P; ++i) v += (double)losses[i];
+            *p.loss = (float)v;
+        }
     }
 }
 

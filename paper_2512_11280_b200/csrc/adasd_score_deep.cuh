@@ -182,13 +182,17 @@ __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_
         auto unit_at = [&](int k) { return ua + (k * NW + warp) * 32 + lane; };
         // ... k = 0 .. count_of(un) - 1, un: end of the CTA's stretch
         auto count_of = [&](int un) { return max(0, (un - ua - warp * 32 + NW * 32 - 1) / (NW * 32)); };
+        // the worker that reads an end of the row
+        auto cleans = [&](const RowUnits<T, L>& ru, int un) {
+            return !WHOLE && ua < un && ((ua == 0 && warp == 0) || (un == ru.NU && ((un - 1 - ua) >> 5) % NW == warp));
+        };
         auto sum_row = [&](const DeepItem& it, int n) {
             const RowUnits<T, L> ru = units(it.row);
             const int un = min(ua + p.per_cta, ru.NU);
             const RowStage<T, L> st(dyn_smem + (n & 1) * kSdStage, ru, ua, un);
             uint32_t bad = 0u;
             // The ends of the row, by the worker that reads them.  (A row that starts elsewhere may have had a unit more.)
-            if (!WHOLE && ua < un && ((ua == 0 && warp == 0) || (un == ru.NU && ((un - 1 - ua) >> 5) % NW == warp))) st.clean(1);
+            if (cleans(ru, un)) st.clean(1);
             typename U::Max mx = U::max0();
             const int nk = count_of(un);
             for_units<UPT>(nk, [&](int k) { U::max_add(mx, st.held(unit_at(k))); });
@@ -230,7 +234,7 @@ __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_
                 });
                 if (has_last) last = st.held(ru.NU - 1);
                 __reduce_or_sync(0xFFFFFFFFu, v);            // (the loads have ended)
-                if (!WHOLE) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                if (cleans(ru, un)) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cta(bar(empty_s[n & 1]));
             }
@@ -258,7 +262,7 @@ __global__ void __launch_bounds__(kSdThreads, 2) score_deep_kernel(const __grid_
             auto write = [&](auto big) {
                 constexpr bool BIG = decltype(big)::value;
                 for_units<UPT>(nk, [&](int k) {
-                    const uint4 v = grad_unit<T, ENT, BIG>(w[k], r.c);
+                    const uint4 v = grad_unit<T, ENT, BIG, kFmaPairs<L, ENT>>(w[k], r.c);
                     const int u = unit_at(k);
                     if ((WHOLE || k > 0 || u >= lo) && u < hi) __stcs(ru.frame(g) + u, v);
                 });

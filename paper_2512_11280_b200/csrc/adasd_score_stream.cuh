@@ -83,6 +83,12 @@ struct RowStage {
     }
 };
 
+// One pair in four of a gradient's exponentials on the FMA pipe, where issue slots are left: rows without ends to look at, no
+// entropy.  2048 rows of 128256 bf16: 212 -> 192 us; two pairs 203; with an entropy 407 -> 429 (4096 rows of 151936), rows off
+// 16-byte boundaries 167 -> 178 (4000 rows of 50257).
+template <int L, bool ENT>
+constexpr int kFmaPairs = L == ROWS_WHOLE && !ENT ? 1 : 0;
+
 // Gradient of a warp's stretch, from its registers.  last: the row's last unit where it is not whole and in this stretch.
 template <typename T, int L, bool ENT, int UPT>
 __device__ __forceinline__ void write_row(T* g, const uint4 (&w)[UPT], const uint4& last, bool has_last, const RowUnits<T, L>& ru, int ua,
@@ -102,7 +108,7 @@ __device__ __forceinline__ void write_row(T* g, const uint4 (&w)[UPT], const uin
 #pragma unroll
                 for (int i = k; i < (k + 4 < UPT ? k + 4 : UPT); ++i) {
                     const int u = ua + i * 32 + lane;
-                    const uint4 v = grad_unit<T, ENT, BIG>(w[i], r.c);
+                    const uint4 v = grad_unit<T, ENT, BIG, kFmaPairs<L, ENT>>(w[i], r.c);
                     if ((WHOLE || i > 0 || u >= lo) && u < hi) __stcs(ru.frame(g) + u, v);
                 }
             }

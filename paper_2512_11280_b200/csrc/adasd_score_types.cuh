@@ -72,7 +72,7 @@ struct PrefParams {
 
 // All return ADASD_OK or a code of the header.  entropy: the call needs H or its gradient.
 int launch_score(const ScoreParams& p, int dtype, bool entropy, int sm_count, cudaStream_t stream);
-int launch_pref_pairs(const PrefParams& p, cudaStream_t stream);
+int launch_pref_pairs(const PrefParams& p, cudaStream_t stream);     // (the total too)
 int launch_pref_grad(PrefParams p, int dtype, cudaStream_t stream);
 int launch_total(const float* terms, int n, float* out, cudaStream_t stream);
 
