@@ -60,12 +60,13 @@ struct Resident {
         return std::max(n, 0);
     }
 };
-// A launch of a persistent kernel, a row a cluster at a time; kNotTaken unless there are more rows than `waves` for each cluster.
+// A launch of a persistent kernel, a row a cluster at a time; kNotTaken unless there are more rows than clusters.  (score_kernel /
+// score_deep_kernel from there on: 100 rows of 128256 bf16 18.9 / 16.5 us, 200 of 50256 18.2 / 15.1; 80 rows 15.8 / 15.3.)
 constexpr int kNotTaken = 1;
 template <typename K>
-int launch_rows(Resident& resident, K kern, ScoreParams p, int threads, int smem, int cs, int per, int waves, cudaStream_t stream) {
+int launch_rows(Resident& resident, K kern, ScoreParams p, int threads, int smem, int cs, int per, cudaStream_t stream) {
     const long long ncl = resident(kern, threads, smem, cs);
-    if (ncl == 0 || p.n_rows <= waves * ncl) return kNotTaken;
+    if (ncl == 0 || p.n_rows <= ncl) return kNotTaken;
     p.cs = cs;
     p.per_cta = per;
     return launch_pdl(kern, (int)ncl * cs, threads, smem, cs, stream, p);
@@ -98,21 +99,27 @@ int launch_forward(ScoreParams p, int NU, int most, cudaStream_t stream) {
 template <typename T, int L, int NW, bool ENT>
 int launch_stream(const ScoreParams& p, int cs, int per, cudaStream_t stream) {
     static Resident r;
-    return launch_rows(r, score_stream_kernel<T, L, NW, ENT>, p, NW * 32, NW * kSsStage, cs, per, 1, stream);
+    return launch_rows(r, score_stream_kernel<T, L, NW, ENT>, p, NW * 32, NW * kSsStage, cs, per, stream);
 }
 template <typename T, int L, bool ENT>
 int launch_deep(const ScoreParams& p, int cs, int per, cudaStream_t stream) {
     static Resident r;
-    return launch_rows(r, score_deep_kernel<T, L, ENT>, p, kSdThreads, kSdSmem, cs, per, 2, stream);
+    return launch_rows(r, score_deep_kernel<T, L, ENT>, p, kSdThreads, kSdSmem, cs, per, stream);
 }
 // Many rows.
+// Without a gradient: score_forward_kernel, as soon as clusters of eight would fill the SMs twice.
+// With one: score_deep_kernel, whose pipeline needs rows of 2048 units, where its stretches are about as full as
+// score_stream_kernel's.  Deep / stream, us for 2000 rows: bf16 V=12000 30.5 / 24.3, 16384 36.1 / 35.1, 20000 40.9 / 45.0, 64000
+// (80 and 98 % full) 103 / 100, 32000 (60 and 98 %) 61.6 / 55.0; 128256 (96 and 98 %, 2065 rows) 183 / 219; fp32 V=8200
+// 28.6 / 33.1, 16000 47.9 / 53.5, 64000 183 / 191.
 template <typename T, int L, bool ENT>
 int launch_many(const ScoreParams& p, int NU, int sms, cudaStream_t stream) {
     if (!p.grad && (long long)p.n_rows * kScMaxCluster <= 2LL * sms) return kNotTaken;
     const int its = (NU + 31) / 32;
     if (p.grad && NU >= 2048) {
-        const int cs = (NU + kSdUnits - 1) / kSdUnits;
-        if (cs <= kScMaxCluster)
+        constexpr int kStreamUnits = 8 * 32 * kSsUPT;        // of a CTA of score_stream_kernel
+        const int cs = (NU + kSdUnits - 1) / kSdUnits, cs2 = (NU + kStreamUnits - 1) / kStreamUnits;
+        if (cs <= kScMaxCluster && (cs2 > kScMaxCluster || 1.2 * cs2 * kStreamUnits >= 1.0 * cs * kSdUnits))
             if (const int rc = launch_deep<T, L, ENT>(p, cs, (its + cs - 1) / cs * 32, stream); rc != kNotTaken) return rc;
     }
     const int warps = (NU + kSsUPT * 32 - 1) / (kSsUPT * 32);

@@ -135,17 +135,20 @@ __device__ __forceinline__ void exponents(const uint4& w, const Shift& c, float2
 }
 
 // 2^q on the FMA pipe, q <= 126: 2^n 2^f with n = q rounded, f in [-1/2, 1/2], 2^f by the degree-4 polynomial of least relative
-// error there, 2.6e-6 (fitted by reweighted least squares).  Below -126 it stays at 2^-126.
+// error there, 2.6e-6 (fitted by reweighted least squares).  0 from -125 down, exactly: what the clamped argument gives is
+// taken off every value.
 __device__ __forceinline__ float2 exp2_fma(float2 q) {
     const float2 big = make_float2(12582912.f, 12582912.f);              // 1.5 2^23: the sum's last bit is 1
-    q = make_float2(fmaxf(q.x, -126.f), fmaxf(q.y, -126.f));
+    constexpr float least = 9.999992847442627e-1f * 0x1p-125f;           // (exact)
+    q = make_float2(fmaxf(q.x, -125.f), fmaxf(q.y, -125.f));
     const float2 r = __fadd2_rn(q, big);
     const float2 f = __ffma2_rn(__fadd2_rn(r, make_float2(-12582912.f, -12582912.f)), make_float2(-1.f, -1.f), q);
     float2 y = __ffma2_rn(f, make_float2(9.570102207362652e-3f, 9.570102207362652e-3f), make_float2(5.591785907745361e-2f, 5.591785907745361e-2f));
     y = __ffma2_rn(y, f, make_float2(2.40247443318367e-1f, 2.40247443318367e-1f));
     y = __ffma2_rn(y, f, make_float2(6.931217908859253e-1f, 6.931217908859253e-1f));
     y = __ffma2_rn(y, f, make_float2(9.999992847442627e-1f, 9.999992847442627e-1f));
-    return make_float2(__int_as_float(__float_as_int(y.x) + (__float_as_int(r.x) << 23)), __int_as_float(__float_as_int(y.y) + (__float_as_int(r.y) << 23)));
+    y = make_float2(__int_as_float(__float_as_int(y.x) + (__float_as_int(r.x) << 23)), __int_as_float(__float_as_int(y.y) + (__float_as_int(r.y) << 23)));
+    return __fadd2_rn(y, make_float2(-least, -least));
 }
 
 // dL/dz of a unit: 2^q (b + a q).  FMA: pairs (of a bf16 unit's four) whose 2^q comes from the FMA pipe.

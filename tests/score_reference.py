@@ -6,7 +6,8 @@ together under 100 2^-24 =: E.  l = z_x - m - ln S then is E off, plus half a st
 H = ln S - T / S: E for each of the two, relative to their sizes.  A gradient's p_v = 2^q: q up to 150 in size before p vanishes,
 rounded twice: 2 x 150 x 2^-24 ln 2 = 21 x 2^-24, and E from ln S and 2^-22: under 130 x 2^-24; the coefficients dL/dl hang on
 l (ratio e^(l - l_old), e^(l_ref - l)): E more.  R = 256 x 2^-24 of the sum of the terms' sizes covers all, then half a step of
-the gradient's type.
+the gradient's type.  Exponentials below 2^-125 are 0 on the device (2^t is flushed; S >= 1): 2^-125 of the row's coefficient
+|dL/dl| / T, which the size at the row's token holds, and of |dL/dH| / T times a logarithm of 125 ln 2 + H < 200 at the most.
 """
 import torch
 
@@ -17,9 +18,11 @@ def rows(z, tok, T=1.0):
     """ln p, p, l, H, lse, which rows count (float64; rows left out: zeros)."""
     V = z.shape[1]
     on = (tok >= 0) & (tok < V)
-    y = z.double() / T
-    lse = torch.logsumexp(y, -1)
-    lnp = y - lse[:, None]
+    m = z.double().amax(-1)
+    y = (z.double() - m[:, None]) / T            # (of z / T itself 64 bits lose the difference at temperatures of 1e-9)
+    lnS = torch.logsumexp(y, -1)
+    lse = m / T + lnS
+    lnp = y - lnS[:, None]
     p = torch.exp(lnp)
     l = lnp.gather(1, torch.where(on, tok, 0).long()[:, None])[:, 0]
     H = -torch.where(p > 0, p * lnp, 0.0).sum(-1)
@@ -53,7 +56,8 @@ def close_entropy(got, H, lse_minus_m):
 
 def close_grad(got, g, size, rel=R):
     half = torch.finfo(got.dtype).eps / 2
-    tol = rel * size + half * (g.abs() + rel * size) + 1e-37 * (1 + size)
+    flushed = 2.0 ** -125 * 200 * (1 + size.amax(-1, keepdim=True)) if size.numel() else 0.0
+    tol = rel * size + half * (g.abs() + rel * size) + flushed
     d = (got.double() - g).abs()
     worst = (d / tol).max() if d.numel() else 0
     assert bool((d <= tol).all()), (float(d.max()), float(worst))

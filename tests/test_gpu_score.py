@@ -441,6 +441,85 @@ def test_same_bits_every_time_on_streams_and_in_graphs(torch):
     assert ctx.status() == 0
 
 
+@pytest.mark.parametrize("n,V", [(5, 999), (400, 45003), (400, 9001), (400, 70000)])
+def test_first_call_inside_a_capture(torch, n, V):
+    """Nothing has to be called before a capture: what a launch looks up for itself the first time is allowed there."""
+    z, tok, g = logits(torch, n, V, torch.bfloat16, 51)
+    ctx = context(V, torch.bfloat16)
+    A = torch.randn(n, generator=g, device="cuda")
+    rl, lp = out(torch, n, 2)
+    grad = torch.empty_like(z)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.token_logprob(z, tok, lp)
+        ctx.policy_loss(z, tok, A, rl, grad_out=grad)
+    graph.replay()
+    torch.cuda.synchronize()
+    lnp, p, l, H, lse, on = ref.rows(z, tok)
+    ref.close_logp(lp, l)
+    want, size = ref.gradient(lnp, p, H, tok, on, -A.double(), torch.zeros_like(l), 1.0)
+    ref.close_grad(grad, want, size)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("V", [9, 4100, 9001, 33003, 50264])
+def test_many_rows_many_left_out(torch, V, dtype):
+    """Most rows left out, runs of them longer than what is looked at at once, the last ones too; nothing of them is read."""
+    dt = getattr(torch, dtype)
+    n = 3000 if V < 10000 else 1000
+    z, tok, g = logits(torch, n, V, dt, V)
+    keep = torch.rand(n, generator=g, device="cuda") < 0.2
+    keep[200:260] = False
+    keep[-3:] = False
+    z[~keep] = float("nan")
+    tok = torch.where(keep, tok, -100)
+    ctx = context(V, dt)
+    clean = torch.where(keep[:, None], z, torch.zeros_like(z))
+    lnp, p, l, H, lse, on = ref.rows(clean, tok)
+    lp, ent, rl = out(torch, n, 3)
+    ctx.token_logprob(z, tok, lp, ent)
+    ref.close_logp(lp, l)
+    assert bool((ent[~keep] == 0).all())
+    A = torch.randn(n, generator=g, device="cuda")
+    for coef in (0.0, 0.3):
+        grad = torch.full_like(z, 9.0)
+        ctx.policy_loss(z, tok, A, rl, entropy_coef=coef, grad_out=grad)
+        want, size = ref.gradient(lnp, p, H, tok, on, -A.double(), torch.full_like(l, -coef), 1.0)
+        ref.close_grad(grad, want, size)
+        assert bool((grad[~keep] == 0).all()) and bool((rl[~keep] == 0).all())
+        ctx.policy_loss(z.clone(), torch.full_like(tok, -1), A, rl, entropy_coef=coef, grad_out=grad)       # nothing to do at all
+        assert bool((grad == 0).all()) and bool((rl == 0).all())
+    assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("T", [1e-3, 1e-7, 1e-9, 1e4])
+@pytest.mark.parametrize("n,V", [(3, 5000), (400, 9001), (400, 20000)])
+def test_temperatures_at_the_ends(torch, n, V, T, dtype):
+    """Exponents (z - m) / T far beyond what 2^t resolves, and next to nothing; logits around 2000 and masks beside them."""
+    dt = getattr(torch, dtype)
+    z, tok, g = logits(torch, n, V, dt, V)
+    z[: n // 2] += 2000.0
+    z[:, 1::3] = float("-inf")
+    z[:, 2::7] = -1e30
+    tok = torch.where(torch.rand(n, generator=g, device="cuda") < 0.5, z.argmax(-1).int(), (tok // 21) * 21)     # (21 k: a logit)
+    ctx = context(V, dt, T)
+    T = float(torch.tensor(T, dtype=torch.float32))          # as the context holds it
+    lnp, p, l, H, lse, on = ref.rows(z, tok, T)
+    lp, = out(torch, n)
+    ctx.token_logprob(z, tok, lp)
+    # log2 e / T is held in 32 bits: exponents of size 1 and below, which alone count in S, are off by 2^-24 of it
+    assert bool(((lp.double() - l).abs() <= ref.E + 4 * ref.U32 * l.abs()).all())
+    a = torch.randn(n, generator=g, device="cuda")
+    grad = torch.empty_like(z)
+    ctx.token_logprob_grad(z, tok, a, grad)
+    want, size = ref.gradient(lnp, p, H, tok, on, a.double(), torch.zeros_like(l), T)
+    ref.close_grad(grad, want, size, rel=2 * ref.R)
+    assert bool((grad[:, 1::3][z[:, 1::3] == float("-inf")] == 0).all()) and bool((grad[z <= -1e30] == 0).all())
+    assert ctx.status() == 0
+
+
 def test_offsets_beyond_32_bits(torch):
     """Rows far enough apart that offsets in elements and bytes pass 2^31 and 2^32."""
     V, n, stride = 1000, 3, (1 << 31) + 8
