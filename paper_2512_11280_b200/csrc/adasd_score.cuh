@@ -8,9 +8,14 @@
 // its statistics and writes its gradient.  In a preference loss they hang on all rows of a pair: score_kernel leaves
 // the statistics, pref_pair_kernel forms the pairs' losses, pref_grad_kernel reads the rows again.
 //
-// score_kernel gives a row to a cluster of CTAs; a thread loads its 16-byte units into registers, and they stay
+// score_kernel takes few rows, rows whose gradient lies elsewhere relative to 16 bytes, and fp32 rows too long for the
+// others: a cluster of CTAs a row; a thread loads its 16-byte units into registers, and they stay
 // there between the sums and the gradient, so that a row crosses the memory once each way.  The warps' statistics go
-// to every CTA of the cluster (one barrier) and are folded by each warp in the same order.
+// to every CTA of the cluster (one barrier) and are folded by each warp in the same order.  What bounds it is the chain
+// launch -> load -> cluster barrier -> fold -> store: 7 fp32 rows of 32000 logits with a gradient 7 us.
+//
+// Many rows: score_forward_kernel (no gradient; adasd_score_forward.cuh), score_deep_kernel and score_stream_kernel (with one).
+// pref_grad_kernel is bound by memory: 3300 rows of 128256 bf16 logits 244 us, 6.9 TB/s; with the rows' statistics 138 us.
 #pragma once
 
 #include "adasd_async.cuh"
