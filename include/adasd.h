@@ -320,7 +320,9 @@ int adasd_vanilla_verify_static(int32_t B, int32_t V, int32_t Kmax, int32_t dtyp
  *   - Gradients are correctly rounded to within a unit or so of the element type; sums,
  *     statistics and losses are held in 32 bits or more.  Results do not vary from run to run.
  *   - These calls keep nothing in the context but the status word, so that calls of one context
- *     may overlap on several streams, as long as their arguments do not.
+ *     may overlap on several streams, as long as their arguments do not.  They may be captured
+ *     in a graph without a call ahead of it.
+ *   - After a wait that expired (ADASD_STATUS_TIMEOUT) the outputs of such a call are not to be used.
  */
 
 /* l, entropy and log-sum-exp (of z / T) of every row; each output [n_rows], entropy and lse nullable. */

@@ -494,6 +494,46 @@ def test_many_rows_many_left_out(torch, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("n,V", [(700, 900), (400, 8200), (400, 9001), (400, 20000), (300, 70001)])
+def test_unusable_rows_among_many_and_gradients_in_place(torch, n, V, dtype):
+    """NaN, +inf and rows without a finite logit spoil their own outputs alone; the logits may become the gradient."""
+    dt = getattr(torch, dtype)
+    z, tok, g = logits(torch, n, V, dt, n + V)
+    bad = torch.randperm(n, generator=g, device="cuda")[:12]
+    z[bad[:4], V // 3] = float("nan")
+    z[bad[4:8], V - 1] = float("inf")
+    z[bad[8:10]] = float("-inf")
+    z[bad[10:]] = torch.finfo(dt).min
+    fine = torch.ones(n, dtype=torch.bool, device="cuda")
+    fine[bad] = False
+    ctx = context(V, dt)
+    lnp, p, l, H, lse, on = ref.rows(z[fine], tok[fine])
+    lp, ent, rl = out(torch, n, 3)
+    ctx.token_logprob(z, tok, lp, ent)
+    assert ctx.status() == 4                                 # ADASD_STATUS_NAN
+    ref.close_logp(lp[fine], l)
+    assert bool(lp[~fine].isnan().all()) and bool(ent[~fine].isnan().all())
+    A = torch.randn(n, generator=g, device="cuda")
+    for coef in (0.0, 0.3):
+        grad, here = torch.full_like(z, 9.0), z.clone()
+        ctx.policy_loss(z, tok, A, rl, entropy_coef=coef, grad_out=grad)
+        assert ctx.status() == 4
+        want, size = ref.gradient(lnp, p, H, tok[fine], on, -A[fine].double(), torch.full_like(l, -coef), 1.0)
+        ref.close_grad(grad[fine], want, size)
+        assert bool(grad[~fine].isnan().all()) and bool(rl[~fine].isnan().all()) and not bool(rl[fine].isnan().any())
+        ctx.policy_loss(here, tok, A, rl, entropy_coef=coef, grad_out=here)
+        assert torch.equal(here.nan_to_num(5.0), grad.nan_to_num(5.0)) and ctx.status() == 4
+    clean = z[fine]
+    m = clean.shape[0]
+    start = torch.tensor([0, m // 3, m], dtype=torch.int32, device="cuda")
+    grad, here, scratch = torch.full_like(clean, 9.0), clean.clone(), torch.empty(16 * m, dtype=torch.uint8, device="cuda")
+    so, po = out(torch, 2)[0], out(torch, 1)[0]
+    ctx.preference_loss(clean, tok[fine], start, po, so, scratch, beta=1e-3, grad_out=grad)
+    ctx.preference_loss(here, tok[fine], start, po, so, scratch, beta=1e-3, grad_out=here)
+    assert torch.equal(here, grad) and ctx.status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
 @pytest.mark.parametrize("T", [1e-3, 1e-7, 1e-9, 1e4])
 @pytest.mark.parametrize("n,V", [(3, 5000), (400, 9001), (400, 20000)])
 def test_temperatures_at_the_ends(torch, n, V, T, dtype):
