@@ -10,8 +10,7 @@
 // What bounds it: memory for fp32, memory and the special-function pipe (75 % busy: one 2^t a logit) for bf16.  3300 rows of
 // 128256 bf16 logits 138 us (6.1 TB/s), 1776 fp32 rows of 50256 63 us (5.7 TB/s).  Bulk copies instead of the lanes' own, each
 // with as many bytes under way: a warp's stretch of 8 KB 168 us, pieces of 4 KB 168 and 86, a CTA's pieces of 32 KB asked for
-// by a control warp 152 and 92: a stage is free only when the last lane (or warp) has read it, and asking costs as much as
-// summing a kilobyte.
+// by a control warp 152 and 92: a stage is free only when its last reader has read it, and waiting for it is polling.
 #pragma once
 
 #include "adasd_score_stream.cuh"
