@@ -552,8 +552,11 @@ __global__ void __launch_bounds__(kPairThreads) pref_pair_kernel(const __grid_co
     __shared__ float losses[kPairSum];
     const int P = p.n_pairs, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int k = threadIdx.x >= kPairHalf ? 1 : 0, t0 = (int)threadIdx.x - k * kPairHalf;      // 1: the rejected sequence
+    cg::cluster_group cluster = cg::this_cluster();
+    if (total) cluster.barrier_arrive();            // (CTA 0 has started before anyone stores a loss into it)
     pdl_wait();
     pdl_trigger();
+    if (total) cluster.barrier_wait();
     const double iT = 1.0 / (double)p.temperature;
     for (int i = blockIdx.x; i < P; i += (int)gridDim.x) {
         const int q = i + k * P;
@@ -608,7 +611,7 @@ __global__ void __launch_bounds__(kPairThreads) pref_pair_kernel(const __grid_co
             p.seq_logp[i] = (float)l[0];
             p.seq_logp[i + P] = (float)l[1];
             p.pair_loss[i] = term;
-            if (total) *cg::this_cluster().map_shared_rank(losses + i, 0) = term;
+            if (total) *cluster.map_shared_rank(losses + i, 0) = term;
         }
         if (p.grad) {
             double d = off ? 0.0 : (k ? -w : w) * dD;
@@ -618,7 +621,7 @@ __global__ void __launch_bounds__(kPairThreads) pref_pair_kernel(const __grid_co
         }
     }
     if (total) {
-        cg::this_cluster().sync();
+        cluster.sync();
         if (blockIdx.x == 0 && threadIdx.x == 0) {
             double v = 0.0;
             for (int i = 0; i < P; ++i) v += (double)losses[i];

@@ -1,0 +1,35 @@
+"""Scoring and losses of given tokens where sizes, options and values leave the ordinary, against 64 bits."""
+import pytest
+
+from tests.test_gpu_score import context, logits, out, preference, torch  # noqa: F401  (torch: a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+# The losses of up to 64 pairs are added up by one cluster of up to eight CTAs, which take the pairs in turn; of more, by a launch
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("pairs", [2, 7, 8, 9, 17, 64, 65, 200])
+def test_preference_of_many_pairs(torch, pairs, dtype):  # noqa: F811
+    """Short ragged sequences, a third of them empty; the loss of every pair, its rows' gradient, the total, the same bits every time."""
+    dt, V = getattr(torch, dtype), 300
+    lengths = torch.randint(0, 6, (2 * pairs,), generator=torch.Generator().manual_seed(pairs))
+    lengths = torch.where(lengths < 2, 0, lengths)
+    start = torch.cat([torch.zeros(1, dtype=torch.long), lengths.cumsum(0)]).int().cuda()
+    n = max(1, int(start[-1]))
+    z, tok, g = logits(torch, n, V, dt, pairs)
+    tok[torch.rand(n, generator=g, device="cuda") < 0.2] = -1
+    ctx = context(V, dt)
+    pw = torch.rand(pairs, generator=g, device="cuda")
+    for rule in ("sigmoid", "squared", "hinge"):
+        preference(torch, ctx, z, z, tok, start, torch.full_like(z, 9.0), rule, pw=pw)
+        preference(torch, ctx, z, z, tok, start, torch.full_like(z, 9.0), rule, average=True)
+    want = None
+    for _ in range(20):
+        so, po, total = out(torch, 2 * pairs) + out(torch, pairs) + out(torch, 1)
+        grad = torch.full_like(z, 9.0)
+        scratch = torch.full((16 * n,), 255, dtype=torch.uint8, device="cuda")
+        ctx.preference_loss(z, tok, start, po, so, scratch, pair_weight=pw, loss_out=total, grad_out=grad)
+        assert float(total) == float(po.double().sum().float())          # (32-bit terms added in 64 bits: any order, one rounding)
+        want = want or (so, po, total, grad)
+        assert all(torch.equal(a, b) for a, b in zip((so, po, total, grad), want))
+    assert ctx.status() == 0
