@@ -85,6 +85,7 @@ __global__ void __launch_bounds__(kThreads) static_vanilla_kernel(VerifyParams p
     K_t = max(0, min(K_t, Kmax));
     if (i > K_t) return;                       // same decision in every CTA of the cluster
     const bool bonus = (i == K_t);
+    cluster.barrier_arrive();                  // (every CTA has started before anyone stores into it)
 
     __shared__ RowShared sh;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -109,6 +110,7 @@ __global__ void __launch_bounds__(kThreads) static_vanilla_kernel(VerifyParams p
             vA[1] = fmaxf(vA[1], xd[j]);
         }
     }
+    cluster.barrier_wait();
     cluster_allreduce<4, true>(vA, sh.warp, sh.xA, CS, rank, cluster);
     const bool bad = (vA[2] > 0.f) || !(vA[0] > kFloor) || !(vA[1] > kFloor) ||
                      (vA[0] == INFINITY) || (vA[1] == INFINITY);
