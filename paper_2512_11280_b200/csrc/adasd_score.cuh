@@ -647,6 +647,7 @@ __global__ void __launch_bounds__(kPgThreads) pref_grad_kernel(const __grid_cons
     T* const g = reinterpret_cast<T*>(p.grad) + (long long)row * p.g_stride;
     const RowUnits<T, L> ru(z, g, p.V);
     const int u0 = min(seg * p.per_cta, ru.NU), u1 = min(u0 + p.per_cta, ru.NU);
+    if (u0 >= u1) return;                           // (of rows of 2048 segments and more, the last may be empty)
     if (kind == 0 || e.z == 0.f) {
         ru.store_zeros(g, u0, u1, (int)threadIdx.x, kPgThreads);
         return;

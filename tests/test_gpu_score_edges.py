@@ -1,6 +1,7 @@
 """Scoring and losses of given tokens where sizes, options and values leave the ordinary, against 64 bits."""
 import pytest
 
+from tests import score_reference as ref
 from tests.test_gpu_score import context, logits, out, preference, torch  # noqa: F401  (torch: a fixture)
 
 pytestmark = pytest.mark.gpu
@@ -33,3 +34,29 @@ def test_preference_of_many_pairs(torch, pairs, dtype):  # noqa: F811
         want = want or (so, po, total, grad)
         assert all(torch.equal(a, b) for a, b in zip((so, po, total, grad), want))
     assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("dtype,V", [("bfloat16", 33538042), ("float32", 16769022)])
+def test_rows_whose_last_segment_is_empty(torch, V, dtype):  # noqa: F811
+    """A preference gradient cuts rows into segments of up to 2048 units by the units a row may have, one more than these rows
+    have: 2048 segments, the last with none.  The last element, a segment's before it, is the token's."""
+    dt = getattr(torch, dtype)
+    N = 16 // torch.finfo(dt).bits * 8
+    assert (V + 2 * N - 2) // N == 2047 * 2048 + 1 and (V + N - 1) // N == (V + 2 + N - 1) // N == 2047 * 2048
+    z, tok, _ = logits(torch, 2, V, dt, 5)
+    tok[:] = V - 1
+    ctx = context(V, dt)
+    start = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    so, po = out(torch, 2)[0], out(torch, 1)[0]
+    scratch = torch.empty(32, dtype=torch.uint8, device="cuda")
+    grad = torch.full_like(z, 9.0)
+    ctx.preference_loss(z, tok, start, po, so, scratch, rule="hinge", beta=0.01, grad_out=grad)
+    assert 0.0 < float(po) < 2.0 and ctx.status() == 0      # (inside the hinge: dL/dl is -beta and beta)
+    dl = torch.tensor([-0.01, 0.01], dtype=torch.float32, device="cuda").double()
+    lnp, p, l, H, lse, on = ref.rows(z, tok)
+    want, size = ref.gradient(lnp, p, H, tok, on, dl, 0 * dl, 1.0)
+    # (a CTA folds 128 blocks of units into its sums, at most 10 roundings of 2^-24 each)
+    ref.close_grad(grad, want, size, rel=ref.R + 1280 * 2.0 ** -24)
+    assert grad[:, -1].tolist() == pytest.approx([-0.01, 0.01], rel=2.0 ** -8)
+    ctx.preference_loss(z, tok, start, po, so, scratch, rule="hinge", beta=0.01, grad_out=z)
+    assert torch.equal(z, grad)
