@@ -41,7 +41,7 @@ def test_rows_whose_last_segment_is_empty(torch, V, dtype):  # noqa: F811
     """A preference gradient cuts rows into segments of up to 2048 units by the units a row may have, one more than these rows
     have: 2048 segments, the last with none.  The last element, a segment's before it, is the token's."""
     dt = getattr(torch, dtype)
-    N = 16 // torch.finfo(dt).bits * 8
+    N = 128 // torch.finfo(dt).bits
     assert (V + 2 * N - 2) // N == 2047 * 2048 + 1 and (V + N - 1) // N == (V + 2 + N - 1) // N == 2047 * 2048
     z, tok, _ = logits(torch, 2, V, dt, 5)
     tok[:] = V - 1
