@@ -311,8 +311,9 @@ __device__ __forceinline__ RowStats fold_partials(F get, int n, float c1, float 
     return r;
 }
 
-// Sums of a warp's units under their largest logit m: what sum_units returns is {S, T} of the whole warp.
-__device__ __forceinline__ bool sum_big(float m, float c1) { return m > -INFINITY && big_shift(m, c1); }
+// Sums of a warp's units under their largest logit m: what sum_units returns is {S, T} of the whole warp.  (m = -inf: a warp
+// without a logit, whose exponents at a small 1 / c1 have to be clamped like everybody's.)
+__device__ __forceinline__ bool sum_big(float m, float c1) { return big_shift(m > -INFINITY ? m : 0.f, c1); }
 __device__ __forceinline__ Shift sum_shift(float m, float c1, float2 L2) {
     Shift c;
     c.L2 = L2;

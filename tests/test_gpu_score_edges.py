@@ -60,3 +60,41 @@ def test_rows_whose_last_segment_is_empty(torch, V, dtype):  # noqa: F811
     assert grad[:, -1].tolist() == pytest.approx([-0.01, 0.01], rel=2.0 ** -8)
     ctx.preference_loss(z, tok, start, po, so, scratch, rule="hinge", beta=0.01, grad_out=z)
     assert torch.equal(z, grad)
+
+
+def masked(torch, n, V, dt, seed, bias=0.0):
+    """Logits with a third masked by -inf, some by the type's lowest value; tokens among what is left."""
+    z, tok, g = logits(torch, n, V, dt, seed)
+    z[::2] += bias
+    z[:, 1::3] = float("-inf")
+    z[:, 2::7] = torch.finfo(dt).min
+    tok = torch.where(torch.rand(n, generator=g, device="cuda") < 0.5, z.argmax(-1).int(), (tok // 21) * 21)     # (21 k: a logit)
+    return z, tok, g
+
+
+LAUNCHES = [(3, 40), (3, 5000), (2, 140000), (400, 9001), (400, 20000), (300, 70000), (90, 151936), (700, 1000)]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("T", [1e-8, 1e-9, 1e-20, 1e-30])
+@pytest.mark.parametrize("n,V", LAUNCHES)
+def test_entropies_at_the_lowest_temperatures(torch, n, V, T, dtype):  # noqa: F811
+    """Stretches of a row without a logit (masked, or behind a short row's end): nothing of them enters the entropy."""
+    dt = getattr(torch, dtype)
+    z, tok, g = masked(torch, n, V, dt, V)
+    z[:, V // 8: 7 * V // 8] = float("-inf")
+    tok = torch.where(z.gather(1, tok.long()[:, None])[:, 0] > -1e30, tok, 0)
+    ctx = context(V, dt, T)
+    T = float(torch.tensor(T, dtype=torch.float32))          # as the context holds it
+    lnp, p, l, H, lse, on = ref.rows(z, tok, T)
+    lp, ent, lo = out(torch, n, 3)
+    ctx.token_logprob(z, tok, lp, ent, lo)
+    ref.close_logp(lp, l)
+    ref.close_logp(lo, lse)
+    lnS = lse - z.double().amax(-1) / T
+    ref.close_entropy(ent, H, torch.where(lnS.abs() < 20, lnS, 0.0))     # (lse of 1e9 and more holds no ln S: of size ln 2)
+    grad = torch.full_like(z, 9.0)
+    ctx.token_logprob_grad(z, tok, torch.ones(n, device="cuda"), grad, grad_entropy=torch.zeros(n, device="cuda"))
+    want, size = ref.gradient(lnp, p, H, tok, on, torch.ones_like(l), torch.zeros_like(l), T)
+    ref.close_grad(grad, want, size, rel=2 * ref.R)
+    assert ctx.status() == 0
