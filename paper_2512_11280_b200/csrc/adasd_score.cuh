@@ -156,7 +156,8 @@ __device__ __forceinline__ float2 exp2_fma(float2 q) {
     return __fadd2_rn(y, make_float2(-least, -least));
 }
 
-// dL/dz of a unit: 2^q (b + a q).  FMA: pairs (of a bf16 unit's four) whose 2^q comes from the FMA pipe.
+// dL/dz of a unit: 2^q (b + a q); BIG: 2^q b + (2^q q) a, where 2^q q is 0 however large a is.  FMA: pairs (of a bf16 unit's
+// four) whose 2^q comes from the FMA pipe.
 struct GradConsts {
     Shift s;
     float2 a2, b2;
@@ -169,7 +170,7 @@ __device__ __forceinline__ uint4 grad_unit(const uint4& w, const GradConsts& c) 
 #pragma unroll
     for (int j = 0; j < U::N / 2; ++j) {
         const float2 e = sizeof(T) == 2 && !BIG && j < FMA ? exp2_fma(q[j]) : make_float2(ex2(q[j].x), ex2(q[j].y));
-        q[j] = __fmul2_rn(e, ENT ? __ffma2_rn(q[j], c.a2, c.b2) : c.b2);
+        q[j] = ENT && BIG ? __ffma2_rn(__fmul2_rn(e, q[j]), c.a2, __fmul2_rn(e, c.b2)) : __fmul2_rn(e, ENT ? __ffma2_rn(q[j], c.a2, c.b2) : c.b2);
     }
     return pack16(q);
 }
@@ -380,7 +381,8 @@ __device__ __forceinline__ void grad_consts(RowGrad& r, const RowStats& s, float
     const float rS = 1.f / s.S, h = s.M * c1;
     r.a = a * rS;
     r.b = fmaf(-a, log2f(s.S), b) * rS;
-    r.big = big_shift(s.M, c1);
+    // (a q has to be finite at a masked logit too, whose 2^q is 0: bf16 units clamp the logit, to -1e30, not the exponent)
+    r.big = big_shift(s.M, c1) || (a != 0.f && !(fabsf(r.a) * (1e30f * c1 + fabsf(h)) < 1e38f));
     r.c.s.L2 = L2;
     // t = fma(z, c1, -h) + x, x = h - M c1 exactly: 2^x goes to the constants
     const float x = r.big ? 0.f : -fmaf(s.M, c1, -h), f = ex2(x);
@@ -393,7 +395,8 @@ template <typename T, bool ENT>
 __device__ __forceinline__ void grad_token(T* g, int x, float zx, float m, float c1, const RowGrad& r) {
     float t = (zx - m) * c1;
     if (ENT) t = fmaxf(t, kLowT);
-    put(g + x, fmaf(ex2(t), ENT ? fmaf(t, r.a, r.b) : r.b, r.top));
+    const float e = ex2(t), v = fmaf(e, r.b, r.top);
+    put(g + x, ENT ? fmaf(e * t, r.a, v) : v);
 }
 __device__ __forceinline__ RowGrad row_grad(const ScoreParams& p, const RowIn& in, const RowStats& s, float c1, float2 L2, bool ent) {
     RowGrad r;

@@ -98,3 +98,27 @@ def test_entropies_at_the_lowest_temperatures(torch, n, V, T, dtype):  # noqa: F
     want, size = ref.gradient(lnp, p, H, tok, on, torch.ones_like(l), torch.zeros_like(l), T)
     ref.close_grad(grad, want, size, rel=2 * ref.R)
     assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("T,dH", [(1e-3, 1.0), (1e-5, 1.0), (1e-9, 1.0), (1e-2, 65536.0), (1e-4, 1e6), (0.7, 1e12)])
+@pytest.mark.parametrize("n,V", LAUNCHES)
+def test_entropy_gradients_of_masked_logits(torch, n, V, T, dH, dtype):  # noqa: F811
+    """Low temperatures and large coefficients: exponents of masked logits times a large factor stay finite, their gradient 0."""
+    dt = getattr(torch, dtype)
+    for bias in (0.0, 40.0):
+        z, tok, g = masked(torch, n, V, dt, V, bias)
+        ctx = context(V, dt, T)
+        t = float(torch.tensor(T, dtype=torch.float32))      # as the context holds it
+        a = torch.randn(n, generator=g, device="cuda")
+        b = dH * torch.randn(n, generator=g, device="cuda")
+        lnp, p, l, H, lse, on = ref.rows(z, tok, t)
+        grad = torch.full_like(z, 9.0)
+        ctx.token_logprob_grad(z, tok, a, grad, grad_entropy=b)
+        assert ctx.status() == 0 and bool(torch.isfinite(grad).all())
+        assert bool((grad[:, 1::3][z[:, 1::3] == float("-inf")] == 0).all()) and bool((grad[z <= -1e30] == 0).all())
+        want, size = ref.gradient(lnp, p, H, tok, on, a.double(), b.double(), t)
+        # H of the device enters as ln S - T / S, two numbers of the size of ln V that cancel: 2 E (1 + 2 ln V) of |dL/dH| p / T
+        lnS = lse - z.double().amax(-1) / t
+        extra = 2 * ref.E * (1 + lnS.abs() + (lnS - H).abs()) * b.double().abs() / t
+        ref.close_grad(grad, want, size + (extra[:, None] * p) / (2 * ref.R), rel=2 * ref.R)
