@@ -120,9 +120,12 @@ __device__ __forceinline__ void put(float* at, float v) { *at = v; }
 
 // Exponents.  t = (z - m) log2 e / T is formed as fma(z, c1, -s) with s = fl(m c1), one rounding, good however large the
 // logits' common offset; what s is off by is taken back from the sums (at t_m = fma(m, c1, -s), the exponent that the
-// largest logit gets instead of 0).  BIG: offsets or 1 / T so large that t_m is off by whole powers of two: (z - m) c1.
-constexpr float kBigShift = 1e7f;
-__device__ __forceinline__ bool big_shift(float m, float c1) { return !(fabsf(m * c1) < kBigShift) || !(c1 < kBigShift); }
+// largest logit gets instead of 0).  BIG: (z - m) c1, where offsets or 1 / T are so large that t_m is off by whole powers of
+// two, or T so large that the exponent of -1e30, which stands for a masked logit there, is not small.
+constexpr float kBigShift = 1e7f, kLowScale = 1e-20f;
+__device__ __forceinline__ bool big_shift(float m, float c1) {
+    return !(fabsf(m * c1) < kBigShift) || !(c1 < kBigShift) || c1 < kLowScale;
+}
 struct Shift {
     float2 L2, ns2, nm2;                   // c1; -s; -m
 };

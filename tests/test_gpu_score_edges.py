@@ -122,3 +122,32 @@ def test_entropy_gradients_of_masked_logits(torch, n, V, T, dH, dtype):  # noqa:
         lnS = lse - z.double().amax(-1) / t
         extra = 2 * ref.E * (1 + lnS.abs() + (lnS - H).abs()) * b.double().abs() / t
         ref.close_grad(grad, want, size + (extra[:, None] * p) / (2 * ref.R), rel=2 * ref.R)
+
+
+@pytest.mark.parametrize("T", [1e20, 1e28, 1e30, 1e33])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("n,V", LAUNCHES)
+def test_masked_logits_at_the_highest_temperatures(torch, n, V, T, dtype):  # noqa: F811
+    """Every logit left counts the same: H is the logarithm of their number, l its negative; a logit of -inf stays out."""
+    dt = getattr(torch, dtype)
+    z, tok, g = logits(torch, n, V, dt, V)
+    z[:, 1::3] = float("-inf")
+    tok = (tok // 3) * 3
+    ctx = context(V, dt, T)
+    T = float(torch.tensor(T, dtype=torch.float32))          # as the context holds it
+    lp, ent, lo, only = out(torch, n, 4)
+    ctx.token_logprob(z, tok, lp, ent, lo)
+    ctx.token_logprob(z, tok, only)
+    lnp, p, l, H, lse, on = ref.rows(z, tok, T)
+    assert int((p[0] > 0).sum()) == V - (V + 1) // 3
+    for got in (lp, only):
+        ref.close_logp(got, l)
+    ref.close_logp(lo, lse)
+    ref.close_entropy(ent, H, lse)
+    a, b = torch.randn(n, generator=g, device="cuda") * T, torch.randn(n, generator=g, device="cuda") * T
+    grad = torch.full_like(z, 9.0)
+    ctx.token_logprob_grad(z, tok, a, grad, grad_entropy=b)
+    assert bool((grad[:, 1::3] == 0).all()) and ctx.status() == 0
+    want, size = ref.gradient(lnp, p, H, tok, on, a.double(), b.double(), T)
+    extra = 2 * ref.E * (1 + 2 * H.abs()) * b.double().abs() / T
+    ref.close_grad(grad, want, size + (extra[:, None] * p) / ref.R)
