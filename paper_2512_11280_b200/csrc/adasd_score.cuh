@@ -599,9 +599,9 @@ __global__ void __launch_bounds__(kPairThreads) pref_pair_kernel(const __grid_co
         const double beta = (double)p.beta, margin = (double)p.margin;
         double loss, dD;
         if (p.rule == ADASD_PREF_SIGMOID) {
-            // -(1 - e) ln sigma(u) - e ln sigma(-u) = max(-u, 0) + ln(1 + e^-|u|) + e u
+            // -(1 - s) ln sigma(u) - s ln sigma(-u) = ln(1 + e^-|u|) + (1 - s) max(-u, 0) + s max(u, 0), for infinite u too
             const double u = beta * D - margin, ls = (double)p.label_smoothing, e = exp(-fabs(u));
-            loss = (u < 0.0 ? -u : u == u ? 0.0 : u) + log1p(e) + (ls != 0.0 ? ls * u : 0.0);
+            loss = log1p(e) + (u < 0.0 ? (ls - 1.0) * u : ls != 0.0 || u != u ? ls * u : 0.0);
             dD = beta * (ls - (u >= 0.0 ? e / (1.0 + e) : 1.0 / (1.0 + e)));
         } else if (p.rule == ADASD_PREF_SQUARED) {
             const double u = D - margin - 0.5 / beta;

@@ -151,3 +151,34 @@ def test_masked_logits_at_the_highest_temperatures(torch, n, V, T, dtype):  # no
     want, size = ref.gradient(lnp, p, H, tok, on, a.double(), b.double(), T)
     extra = 2 * ref.E * (1 + 2 * H.abs()) * b.double().abs() / T
     ref.close_grad(grad, want, size + (extra[:, None] * p) / ref.R)
+
+
+@pytest.mark.parametrize("smoothing", [0.0, 0.1, 0.5])
+@pytest.mark.parametrize("where", ["chosen", "rejected", "both"])
+def test_preference_of_tokens_of_probability_zero(torch, where, smoothing):  # noqa: F811
+    """A counted token whose logit is -inf: a sequence's log-prob of -inf, and the loss that the formula gives."""
+    V, n = 50, 6
+    z, tok, _ = logits(torch, n, V, torch.float32, 9)
+    if where != "rejected":
+        z[0, tok[0].long()] = float("-inf")                  # pair 0 (rows 0, 1 against 3, 4); pair 1 (row 2 against 5) is ordinary
+    if where != "chosen":
+        z[4, tok[4].long()] = float("-inf")
+    start = torch.tensor([0, 2, 3, 5, 6], dtype=torch.int32, device="cuda")
+    ctx = context(V, torch.float32)
+    for refs in (None, torch.zeros(4, device="cuda")):
+        so, po, total = out(torch, 4) + out(torch, 2) + out(torch, 1)
+        scratch = torch.empty(16 * n, dtype=torch.uint8, device="cuda")
+        grad = torch.full_like(z, 9.0)
+        ctx.preference_loss(z, tok, start, po, so, scratch, ref_logp=refs, label_smoothing=smoothing, loss_out=total, grad_out=grad)
+        assert ctx.status() == 0
+        assert [float(v) == float("-inf") for v in so] == [where != "rejected", False, where != "chosen", False]
+        u = {"chosen": -float("inf"), "rejected": float("inf"), "both": float("nan")}[where]
+        # -(1 - s) ln sigma(u) - s ln sigma(-u), a factor of 0 making its term 0
+        want = float("nan") if u != u else float("inf") if u < 0 or smoothing > 0 else 0.0
+        assert str(float(po[0])) == str(want) and str(float(total)) == str(want if want != 0 else float(po[1]))
+        assert 0.0 < float(po[1]) < 10.0
+        # the slope is finite: beta (s - 1) at -inf, beta s at +inf
+        if u == u:
+            d = 0.1 * (smoothing - 1 if u < 0 else smoothing)
+            assert float(grad[1, tok[1].long()]) == pytest.approx(d * (1 - float(torch.softmax(z[1], 0)[tok[1].long()])), rel=1e-4, abs=1e-9)
+            assert bool(torch.isfinite(grad).all())
