@@ -307,7 +307,8 @@ int adasd_vanilla_verify_static(int32_t B, int32_t V, int32_t Kmax, int32_t dtyp
  * and the token of each row:
  *   l_r = ln softmax(z_r / T)[token_r],  H_r = entropy of softmax(z_r / T), T the temperature of
  * adasd_set_warpers, as sampled tokens have it.  With top-k or top-p on, all four return
- * ADASD_ERR_DTYPE: a cut distribution has no gradient at the tokens it leaves out.
+ * ADASD_ERR_DTYPE: a cut distribution has no gradient at the tokens it leaves out.  At a temperature
+ * below 4.24e-39, where log2 e / T is beyond 32 bits, they return ADASD_ERR_SHAPE.
  *   - A row whose token is outside [0, V) is LEFT OUT (prompt, padding): its logits are not read,
  *     its outputs are 0 and its row of a gradient is zeros.
  *   - A row with a NaN, a +inf or no finite logit sets ADASD_STATUS_NAN; its outputs, every total it

@@ -1014,6 +1014,7 @@ static int check_rows(const adasd_ctx* ctx, const void* z, int64_t row_stride, c
     if (n_rows > 0 && (!z || !tokens)) return ADASD_ERR_NULL;
     if (int rc = check_device(ctx)) return rc;
     if (ctx->cuts_on()) return ADASD_ERR_DTYPE;
+    if (!std::isfinite(kLog2e / ctx->temperature)) return ADASD_ERR_SHAPE;
     const int64_t es = (int64_t)elt_size(ctx->cfg.dtype), V = ctx->cfg.V;
     if (!aligned_to(z, (size_t)es) || !aligned_to(grad, (size_t)es) || !aligned4({tokens})) return ADASD_ERR_ALIGN;
     // (2^27 rows: a launch has a CTA or more a row; strides: byte offsets stay within 64 bits)

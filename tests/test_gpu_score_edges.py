@@ -182,3 +182,30 @@ def test_preference_of_tokens_of_probability_zero(torch, where, smoothing):  # n
             d = 0.1 * (smoothing - 1 if u < 0 else smoothing)
             assert float(grad[1, tok[1].long()]) == pytest.approx(d * (1 - float(torch.softmax(z[1], 0)[tok[1].long()])), rel=1e-4, abs=1e-9)
             assert bool(torch.isfinite(grad).all())
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_temperatures_whose_reciprocal_32_bits_do_not_hold(torch, dtype):  # noqa: F811
+    """1 / T beyond the range of 32 bits: refused, nothing is launched; the lowest temperature above is served."""
+    import paper_2512_11280_b200 as adasd
+    dt, V = getattr(torch, dtype), 1000
+    z, tok, g = masked(torch, 5, V, dt, 1)
+    z[:, 0] = 100.0
+    tok[:3] = 0
+    lp, ent, rl = out(torch, 5, 3)
+    a = torch.full((5,), 0.1, device="cuda")
+    grad = torch.full_like(z, 9.0)
+    start = torch.tensor([0, 2, 5], dtype=torch.int32, device="cuda")
+    so, po, scratch = out(torch, 2)[0], out(torch, 1)[0], torch.empty(80, dtype=torch.uint8, device="cuda")
+    ctx = context(V, dt, 4.2e-39)
+    for call in (lambda: ctx.token_logprob(z, tok, lp), lambda: ctx.token_logprob_grad(z, tok, a, grad),
+                 lambda: ctx.policy_loss(z, tok, a, rl, grad_out=grad), lambda: ctx.preference_loss(z, tok, start, po, so, scratch, grad_out=grad)):
+        with pytest.raises(adasd.AdasdError) as e:
+            call()
+        assert e.value.code == adasd.ERR_SHAPE
+    assert bool((lp == -7).all()) and bool((grad == 9).all()) and ctx.status() == 0
+    ctx = context(V, dt, 4.3e-39)
+    ctx.token_logprob(z, tok, lp, ent)
+    assert bool((lp[:3] == 0).all()) and bool((ent == 0).all()) and bool((lp[3:] == float("-inf")).all())
+    ctx.token_logprob_grad(z, tok, a, grad, grad_entropy=a)
+    assert bool((grad[:3] == 0).all()) and bool(torch.isfinite(grad).all()) and ctx.status() == 0
