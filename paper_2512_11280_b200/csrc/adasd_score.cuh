@@ -124,7 +124,7 @@ __device__ __forceinline__ void put(float* at, float v) { *at = v; }
 // two, or T so large that the exponent of -1e30, which stands for a masked logit there, is not small.
 constexpr float kBigShift = 1e7f, kLowScale = 1e-20f;
 __device__ __forceinline__ bool big_shift(float m, float c1) {
-    return !(fabsf(m * c1) < kBigShift) || !(c1 < kBigShift) || c1 < kLowScale;
+    return !(fabsf(m * c1) < (c1 < kBigShift && c1 >= kLowScale ? kBigShift : 0.f));
 }
 struct Shift {
     float2 L2, ns2, nm2;                   // c1; -s; -m
