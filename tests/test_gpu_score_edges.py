@@ -209,3 +209,67 @@ def test_temperatures_whose_reciprocal_32_bits_do_not_hold(torch, dtype):  # noq
     assert bool((lp[:3] == 0).all()) and bool((ent == 0).all()) and bool((lp[3:] == float("-inf")).all())
     ctx.token_logprob_grad(z, tok, a, grad, grad_entropy=a)
     assert bool((grad[:3] == 0).all()) and bool(torch.isfinite(grad).all()) and ctx.status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("V", [1, 7, 16])
+def test_many_short_rows(torch, V, dtype):  # noqa: F811
+    """Rows of a unit or two, 300000 of them: log-probs, gradients, a preference loss of two long pairs."""
+    dt, n = getattr(torch, dtype), 300000
+    z, tok, g = logits(torch, n, V, dt, V)
+    tok[torch.rand(n, generator=g, device="cuda") < 0.3] = -1
+    ctx = context(V, dt)
+    lnp, p, l, H, lse, on = ref.rows(z, tok)
+    lp, ent = out(torch, n, 2)
+    ctx.token_logprob(z, tok, lp, ent)
+    ref.close_logp(lp, l)
+    ref.close_entropy(ent, H, torch.where(on, lse - z.double().amax(-1), 0.0))
+    a, b = torch.randn(n, generator=g, device="cuda"), torch.randn(n, generator=g, device="cuda")
+    want, size = ref.gradient(lnp, p, H, tok, on, a.double(), b.double(), 1.0)
+    for off in (0, 1):                                       # the gradient where the logits lie relative to 16 bytes, and elsewhere
+        buf = torch.full((n * V + 64,), 9.0, dtype=dt, device="cuda")
+        grad = buf[off:off + n * V].view(n, V)
+        ctx.token_logprob_grad(z, tok, a, grad, grad_entropy=b)
+        ref.close_grad(grad, want, size)
+        assert bool((buf[:off] == 9.0).all()) and bool((buf[off + n * V:] == 9.0).all())
+    start = torch.tensor([0, n // 5, n // 2, n // 2, n], dtype=torch.int32, device="cuda")
+    so, po, scratch = out(torch, 4)[0], out(torch, 2)[0], torch.empty(16 * n, dtype=torch.uint8, device="cuda")
+    grad = torch.full_like(z, 9.0)
+    ctx.preference_loss(z, tok, start, po, so, scratch, rule="hinge", beta=1e-7, average=True, grad_out=grad)
+    counts = [max(1, int(on[start[s]:start[s + 1]].sum())) for s in range(4)]
+    dl = torch.zeros(n, dtype=torch.float64, device="cuda")
+    beta = float(torch.tensor(1e-7))
+    for s in range(4):
+        dl[start[s]:start[s + 1]] = (-beta if s < 2 else beta) / counts[s]
+    want, size = ref.gradient(lnp, p, H, tok, on, torch.where(on, dl, 0.0), 0 * dl, 1.0)
+    ref.close_grad(grad, want, size)
+    assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("n,V", [(500, 5003), (60, 50257), (50, 131080)])
+def test_a_slice_of_padded_logits_and_a_dense_gradient(torch, n, V, dtype):  # noqa: F811
+    """logits[:, :V] of rows padded to a multiple of 64, the gradient [n, V]: they lie differently relative to 16 bytes."""
+    dt = getattr(torch, dtype)
+    pad = -(-(V + 1) // 64) * 64
+    z, tok, g = logits(torch, n, pad, dt, V)
+    z[:, V:] = float("nan")
+    tok = tok % V
+    tok[::5] = -1
+    z = z[:, :V]
+    ctx = context(V, dt, 0.8)
+    t = float(torch.tensor(0.8, dtype=torch.float32))
+    lnp, p, l, H, lse, on = ref.rows(z, tok, t)
+    A, rl, grad = torch.randn(n, generator=g, device="cuda"), out(torch, n)[0], torch.full((n, V), 9.0, dtype=dt, device="cuda")
+    for coef in (0.0, 0.3):
+        ctx.policy_loss(z, tok, A, rl, entropy_coef=coef, grad_out=grad)
+        want, size = ref.gradient(lnp, p, H, tok, on, torch.where(on, -A.double(), 0.0), torch.full_like(l, -coef), t)
+        ref.close_grad(grad, want, size)
+    start = torch.tensor([0, n // 2, n], dtype=torch.int32, device="cuda")
+    so, po, scratch = out(torch, 2)[0], out(torch, 1)[0], torch.empty(16 * n, dtype=torch.uint8, device="cuda")
+    ctx.preference_loss(z, tok, start, po, so, scratch, rule="hinge", beta=1e-4, grad_out=grad)
+    beta = float(torch.tensor(1e-4))
+    dl = torch.where(torch.arange(n, device="cuda") < n // 2, -beta, beta).double()
+    want, size = ref.gradient(lnp, p, H, tok, on, torch.where(on, dl, 0.0), 0 * dl, t)
+    ref.close_grad(grad, want, size)
+    assert ctx.status() == 0
