@@ -311,15 +311,26 @@ int adasd_vanilla_verify_static(int32_t B, int32_t V, int32_t Kmax, int32_t dtyp
  * below 4.24e-39, where log2 e / T is beyond 32 bits, they return ADASD_ERR_SHAPE.
  *   - A row whose token is outside [0, V) is LEFT OUT (prompt, padding): its logits are not read,
  *     its outputs are 0 and its row of a gradient is zeros.
- *   - A row with a NaN, a +inf or no finite logit sets ADASD_STATUS_NAN; its outputs, every total it
- *     enters and its row of a gradient are NaN.  A logit of -inf has probability 0 and gradient 0; as
- *     the token's own logit it gives l = -inf, and losses what their formulas give.
+ *   - A row with a NaN, a +inf or no logit above -1e30 (bf16: -9.95e29) sets ADASD_STATUS_NAN; its
+ *     outputs, every total it enters and its row of a gradient are NaN.  A logit of -inf has
+ *     probability 0 and gradient 0; as the token's own logit it gives l = -inf, losses what their
+ *     formulas give, and a gradient of dL/dl / T at the token.
  *   - grad_logits_dev (element type of the logits, row r at r * grad_row_stride) receives dL/dz; each
  *     element of the n_rows rows is written, what lies between rows is left as it was.  It may be
  *     the logits themselves (same address and stride): every row is read before it is
- *     overwritten.  Any other overlap of the two is refused (ADASD_ERR_SHAPE).
- *   - Gradients are correctly rounded to within a unit or so of the element type; sums,
- *     statistics and losses are held in 32 bits or more.  Results do not vary from run to run.
+ *     overwritten.  Otherwise the two must lie apart, each taken from its first row's first element
+ *     to its last row's last: rows that alternate with the logits' in one buffer are refused too
+ *     (ADASD_ERR_SHAPE).  Gradients that lie elsewhere than the logits relative to 16-byte
+ *     boundaries (another offset or, in a row, another stride modulo 16 bytes) cost 2.2 to 2.6 times
+ *     as much, gradients of rows of more than 131072 fp32 or 262144 bf16 logits twice as much.
+ *   - Sums, statistics and losses are held in 32 bits or more, what is reported is formed of them in
+ *     64 bits.  ln S (S: the sum of a row's exponentials over its largest) is off by at most
+ *     (V / 256 + 128) 2^-24.  A gradient's p_v comes with that and with (4 |ln p_v| + 8) 2^-24 of itself; bf16
+ *     gradients without an entropy's may have 2.7e-6 more.  What is made of p_v is formed in 32
+ *     bits and rounded once to the element type: correct to a unit or so of bf16, except where its
+ *     terms cancel (1 - p_v at a token of probability near 1; ln p_v + H near 0), where these errors are
+ *     relative to the terms.  dL/dl / T or dL/dH ln V / T beyond the range of 32 bits give infinities and
+ *     NaN.  Results do not vary from run to run.
  *   - These calls keep nothing in the context but the status word, so that calls of one context
  *     may overlap on several streams, as long as their arguments do not.  They may be captured
  *     in a graph without a call ahead of it.

@@ -71,7 +71,8 @@ int launch_rows(Resident& resident, K kern, ScoreParams p, int threads, int smem
     p.per_cta = per;
     return launch_pdl(kern, (int)ncl * cs, threads, smem, cs, stream, p);
 }
-// CTAs of a row: as many as make the last of the resident clusters' rounds end first, a CTA more costing a row 3 % more.
+// CTAs of a row: as many as make the last of the resident clusters' rounds end first, a CTA more costing a row 3 % more (an estimate:
+// the exchange and shorter stretches; not measured by itself).
 template <typename T, int L, int NW, bool ENT>
 int launch_forward(ScoreParams p, int NU, int most, cudaStream_t stream) {
     static Resident r;
@@ -111,7 +112,8 @@ int launch_deep(const ScoreParams& p, int cs, int per, cudaStream_t stream) {
 // With one: score_deep_kernel, whose pipeline needs rows of 2048 units, where its stretches are about as full as
 // score_stream_kernel's.  Deep / stream, us for 2000 rows: bf16 V=12000 30.5 / 24.3, 16384 36.1 / 35.1, 20000 40.9 / 45.0, 64000
 // (80 and 98 % full) 103 / 100, 32000 (60 and 98 %) 61.6 / 55.0; 128256 (96 and 98 %, 2065 rows) 183 / 219; fp32 V=8200
-// 28.6 / 33.1, 16000 47.9 / 53.5, 64000 183 / 191.
+// 28.6 / 33.1, 16000 47.9 / 53.5, 64000 183 / 191.  (One rule for both types, made for bf16: fp32 rows of 16000, which score_deep_kernel
+// would do in less, go to the other.)
 template <typename T, int L, bool ENT>
 int launch_many(const ScoreParams& p, int NU, int sms, cudaStream_t stream) {
     if (!p.grad && (long long)p.n_rows * kScMaxCluster <= 2LL * sms) return kNotTaken;

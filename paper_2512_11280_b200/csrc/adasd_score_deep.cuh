@@ -8,11 +8,12 @@
 // (its stage is free then), sums item n + 1 from the other stage, sends these partials, and only then takes the constants of
 // item n and writes.
 //
-// What bounds it: the special-function pipe (two 2^t a logit, a quarter of the second ones on the FMA pipe) and issue slots beside
-// memory.  2048 rows of 128256 bf16 logits 192 us (5.5 TB/s both ways; 212 with all 2^t on one pipe).  13 units a lane and two CTAs an
-// SM: 12 workers of 9 units measured 202 us; the lanes' own copies (as score_forward_kernel's) in place of the bulk copies
-// 198 us against 183 on 2065 rows and 219 against 149 on 4000 rows of 50257: their instructions come on top of a loop that is
-// short of issue slots.
+// What bounds it: no unit is saturated (counters at 1120 rows of 128256 bf16: special-function pipe 57 %, issue slots 49 %, DRAM 56 %);
+// what was taken off the special-function pipe and the issue slots made it faster.  2048 rows of 128256 bf16 logits 192 us (5.5 TB/s both
+// ways; 212 with all 2^t on one pipe).  A cluster's rows are every ncl-th, whether they are left out or not: with rows left out at random
+// the cluster with the most rows to do sets the time (2048 rows of 128256, a tenth left out: as long as with none).  13 units a lane
+// and two CTAs an SM: 12 workers of 9 units measured 202 us; the lanes' own copies (as score_forward_kernel's) in place of the bulk
+// copies 198 us against 183 on 2065 rows and 219 against 149 on 4000 rows of 50257: their instructions come on top.
 #pragma once
 
 #include "adasd_score_stream.cuh"

@@ -273,3 +273,33 @@ def test_a_slice_of_padded_logits_and_a_dense_gradient(torch, n, V, dtype):  # n
     want, size = ref.gradient(lnp, p, H, tok, on, torch.where(on, dl, 0.0), 0 * dl, t)
     ref.close_grad(grad, want, size)
     assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("n,V", [(100, 32000), (100, 151936), (60, 600000), (4, 600000)])
+def test_accuracy_as_stated(torch, n, V, dtype):  # noqa: F811
+    """ln S within (V / 256 + 128) 2^-24, p_v within that and (4 |ln p_v| + 8) 2^-24 of itself, on rows whose sums round the same way
+    again and again: rising logits (every group of units has a new largest one), equal ones, one far above the others."""
+    dt = getattr(torch, dtype)
+    g = torch.Generator(device="cuda").manual_seed(V)
+    z = torch.linspace(-4, 4, V, device="cuda")[None].repeat(n, 1)
+    z[1::3] = -3 * torch.rand(len(range(1, n, 3)), 1, generator=g, device="cuda")
+    z[2::3] = -10.0
+    z[:, 7] = 5.0
+    z = (z + torch.rand(n, 1, generator=g, device="cuda")).to(dt)
+    tok = torch.full((n,), V // 2, dtype=torch.int32, device="cuda")
+    ctx = context(V, dt)
+    lnp, p, l, H, lse, on = ref.rows(z, tok)
+    S = (V / 256 + 128) * ref.U32
+    lp, ent, lo = out(torch, n, 3)
+    ctx.token_logprob(z, tok, lp, ent, lo)
+    assert bool(((lp.double() - l).abs() <= S + ref.U32 * l.abs()).all())
+    assert bool(((lo.double() - lse).abs() <= S + ref.U32 * lse.abs()).all())
+    grad = torch.full_like(z, 9.0)
+    ctx.token_logprob_grad(z, tok, -torch.ones(n, device="cuda"), grad)      # p_v, the token's own less 1
+    got = grad.double()
+    got[:, V // 2] = p[:, V // 2]
+    tol = p * (S + (4 * lnp.abs() + 8) * ref.U32 + (2.7e-6 if dt is torch.bfloat16 else 0.0))
+    tol = tol + torch.finfo(dt).eps / 2 * (p + tol)
+    assert bool(((got - p).abs() <= tol).all()), float(((got - p).abs() / tol).max())
+    assert ctx.status() == 0
