@@ -17,8 +17,8 @@
  *     neither frees nor keeps it beyond the call.  Pointers without the suffix are
  *     host pointers.  `stream` is a cudaStream_t passed as void* (NULL = default).
  *   - Hot calls (draft_entropy, verify, update_thresholds, vanilla_verify, greedy_verify,
- *     gen_only_update, token_logprob, token_logprob_grad, policy_loss, preference_loss, get_thresholds,
- *     reset) only enqueue kernels on `stream`: they never allocate, free or synchronise.  create/destroy/state_export/state_import/status do.
+ *     gen_only_update, token_logprob, token_logprob_grad, policy_loss, preference_loss, adamw_step,
+ *     get_thresholds, reset) only enqueue kernels on `stream`: they never allocate, free or synchronise.  create/destroy/state_export/state_import/status do.
  *   - Logits are row-major with contiguous vocabulary; strides are in ELEMENTS.
  *     bf16 or fp32 as fixed at create time.  Rows may start at any multiple of their element
  *     size; they are copied by the aligned 16-byte granules that hold them, so that up to 14
@@ -424,6 +424,60 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
                           const adasd_preference_options* options, void* scratch_dev,
                           float* seq_logp_out_dev, float* pair_loss_out_dev, float* loss_out_dev,
                           void* grad_logits_dev, int64_t grad_row_stride, void* stream);
+
+/*
+ * ---- AdamW ------------------------------------------------------------------------------------
+ *
+ * What is done with gradients: one step of AdamW over many tensors at once.  (The paper has no counterpart.)  Per element, with
+ * g = grad_scale grad and the step's number t from 1 on:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t)  m / (sqrt(v / (1 - beta2^t)) + eps)
+ *
+ * States (m, v) are fp32 arrays, or 8-bit floats with a scale for every block of ADASD_ADAMW_BLOCK consecutive elements of a
+ * tensor (the last block may be shorter): m as e4m3 with scale (largest |m|) / 448, v as e5m2 with scale (largest v) / 57344; the value is code times
+ * scale.  A v above 0 is never held as 0; a block whose largest |m| (v) is below 2^-100 is held as zeros (as the smallest code).  The step
+ * itself uses m and v ahead of that rounding.  All zeros, codes and scales, are the states of a tensor that no step has seen.
+ */
+#define ADASD_ADAMW_BLOCK 256
+
+typedef struct {
+    void* param;             /* [n] ADASD_BF16 or ADASD_FP32, updated */
+    const void* grad;        /* [n] ADASD_BF16 or ADASD_FP32 */
+    void* exp_avg;           /* [n] m, updated */
+    void* exp_avg_sq;        /* [n] v, updated */
+    float* avg_scale;        /* [ceil(n / ADASD_ADAMW_BLOCK)] scales of m and of v, updated; not looked at with states in 32 bits */
+    float* sq_scale;
+    void* param_copy;        /* nullable [n] bf16: receives fp32 parameters rounded to the nearest */
+    int64_t n;               /* elements, 0 included */
+    float weight_decay;
+    int32_t param_dtype, grad_dtype;
+    int32_t state_bits;      /* 32 or 8 */
+} adasd_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2; /* betas in [0, 1) */
+    double eps;              /* >= 1e-30 */
+    double grad_scale;       /* factor of every gradient: 1 / accumulation steps, a clipping factor */
+    int32_t step;            /* t, >= 1 */
+    int32_t stochastic;      /* 0: 8-bit states and bf16 parameters are rounded to the nearest.  1: up or down, so that the mean is the
+                                value itself, by a hash of seed, t, the tensor's place in the call and the element's in the tensor.
+                                (A v that changes by a thousandth a step never leaves its code when rounded to the nearest.) */
+    uint32_t seed;
+    const float* lr_dev;          /* each nullable device scalar [1]; stands in for the value above when the step runs, so that */
+    const float* grad_scale_dev;  /* a captured step can be replayed (grad_scale_dev: is multiplied with grad_scale) */
+    const int32_t* step_dev;      /* (values below 1 count as 1) */
+} adasd_adamw_options;
+
+/*
+ * tensors: host array of n_tensors, read before the call returns.  Arrays are device arrays, aligned to their element type; no two may
+ * overlap.  (Arrays that start at multiples of 16 bytes, codes at 8, are faster.)  Only the context's device and status word are
+ * used: V and the context's dtype do not matter.  Where grad_scale_dev is given and the product is not finite (a norm that
+ * overflowed), nothing is changed and ADASD_STATUS_NAN is set.  A gradient that is not finite makes its parameter and
+ * states NaN or infinite as the formulas do, in 8 bits the states of its whole block.
+ * One launch for up to 384 tensors.  Results do not vary from run to run.
+ */
+int adasd_adamw_step(adasd_ctx* ctx, const adasd_adamw_tensor* tensors, int32_t n_tensors,
+                     const adasd_adamw_options* options, void* stream);
 
 /* Copies T_G and the list sizes |L_E^R|, |L_D^A|, |L_D^R| to caller arrays [B] (each nullable). */
 int adasd_get_thresholds(adasd_ctx* ctx, float* T_G_dev, int32_t* nE_dev, int32_t* nA_dev,

@@ -5,7 +5,8 @@ marshals arguments (device pointers of torch tensors, strides, streams).  There 
 no CPU fallback: importing works anywhere, but every call needs the built library
 and a CUDA device and raises otherwise.
 """
-from .binding import (ERR_ALIGN, ERR_CAPACITY, ERR_CUDA, ERR_DEVICE, ERR_DTYPE, ERR_NULL, ERR_SHAPE,
+from .binding import (ADAMW_BLOCK, AdamwOptions, AdamwTable, AdamwTensor, adasd_adamw_step,
+                      ERR_ALIGN, ERR_CAPACITY, ERR_CUDA, ERR_DEVICE, ERR_DTYPE, ERR_NULL, ERR_SHAPE,
                       ADASD_BF16, ADASD_FP32, ADASD_FUSE_UPDATE, ADASD_KMAX_LIMIT, PREF_HINGE,
                       PREF_SCRATCH_PER_ROW, PREF_SIGMOID, PREF_SQUARED, STATUS_CAPACITY,
                       STATUS_NAN, STATUS_TIMEOUT, AdasdConfig, AdasdError, Context, PolicyOptions, PreferenceOptions,

@@ -20,6 +20,7 @@ ADASD_KMAX_LIMIT = 32
 STATUS_CAPACITY, STATUS_TIMEOUT, STATUS_NAN = 1, 2, 4
 PREF_SIGMOID, PREF_SQUARED, PREF_HINGE = 0, 1, 2
 PREF_SCRATCH_PER_ROW = 16
+ADAMW_BLOCK = 256
 _PREF_RULES = {"sigmoid": PREF_SIGMOID, "squared": PREF_SQUARED, "hinge": PREF_HINGE}
 ERR_NULL, ERR_ALIGN, ERR_SHAPE, ERR_DTYPE, ERR_CAPACITY, ERR_CUDA, ERR_DEVICE = -1, -2, -3, -4, -5, -7, -9
 
@@ -50,6 +51,17 @@ class PolicyOptions(C.Structure):
 class PreferenceOptions(C.Structure):
     _fields_ = [("rule", C.c_int32), ("average", C.c_int32), ("beta", C.c_float), ("margin", C.c_float),
                 ("label_smoothing", C.c_float), ("scale", C.c_float)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("param", "grad", "exp_avg", "exp_avg_sq", "avg_scale", "sq_scale", "param_copy")] + [
+        ("n", C.c_int64), ("weight_decay", C.c_float), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("state_bits", C.c_int32)]
+
+
+class AdamwOptions(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps", "grad_scale")] + [
+        ("step", C.c_int32), ("stochastic", C.c_int32), ("seed", C.c_uint32), ("lr_dev", C.c_void_p), ("grad_scale_dev", C.c_void_p),
+        ("step_dev", C.c_void_p)]
 
 
 def library_path() -> str:
@@ -84,6 +96,7 @@ def lib() -> C.CDLL:
         "adasd_policy_loss": [P, P, I64, P, I32, P, P, P, P, C.POINTER(PolicyOptions), P, P, P, P, P, P, I64, P],
         "adasd_preference_loss": [P, P, I64, P, I32, P, I32, P, P, C.POINTER(PreferenceOptions), P, P, P, P, P,
                                   I64, P],
+        "adasd_adamw_step": [P, C.POINTER(AdamwTensor), I32, C.POINTER(AdamwOptions), P],
         "adasd_set_warpers": [P, C.c_float, I32, C.c_float],
         "adasd_get_thresholds": [P, P, P, P, P, P],
         "adasd_state_export": [P, I32, P, C.POINTER(C.c_size_t)],
@@ -217,6 +230,11 @@ def adasd_preference_loss(ctx, logits_dev, row_stride, tokens_dev, n_rows, seq_s
                                        grad_row_stride, stream)
 
 
+def adasd_adamw_step(ctx, tensors, n_tensors, options, stream) -> int:
+    """tensors: a ctypes array of AdamwTensor."""
+    return lib().adasd_adamw_step(ctx, tensors, n_tensors, C.byref(options) if options is not None else None, stream)
+
+
 def adasd_get_thresholds(ctx, T_G_dev, nE_dev, nA_dev, nR_dev, stream) -> int:
     return lib().adasd_get_thresholds(ctx, T_G_dev, nE_dev, nA_dev, nR_dev, stream)
 
@@ -240,6 +258,13 @@ def adasd_status(ctx):
 
 def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
+
+
+class AdamwTable:
+    """The tensors of an AdamW step, checked and laid out once (:meth:`Context.adamw_table`); keeps them alive."""
+
+    def __init__(self, entries, owned):
+        self.entries, self.n, self._owned = entries, len(entries), owned
 
 
 class Context:
@@ -267,6 +292,7 @@ class Context:
         self._vanilla_verify, self._greedy_verify = L.adasd_vanilla_verify, L.adasd_greedy_verify
         self._token_logprob, self._token_logprob_grad = L.adasd_token_logprob, L.adasd_token_logprob_grad
         self._policy_loss, self._preference_loss = L.adasd_policy_loss, L.adasd_preference_loss
+        self._adamw_step = L.adasd_adamw_step
         self._logit_dtype = torch.bfloat16 if dtype == ADASD_BF16 else torch.float32
         self._i32, self._f32, self._index = torch.int32, torch.float32, self.device.index
         self._raw_stream = torch._C._cuda_getCurrentRawStream
@@ -482,6 +508,63 @@ class Context:
                                    sc, seq, pl, total, g, g_stride, self._raw_stream(self._index))
         if rc:
             raise AdasdError(rc, where)
+
+    # ---- AdamW -----------------------------------------------------------------------------------------
+
+    def adamw_table(self, tensors) -> AdamwTable:
+        """tensors: dicts of device tensors ``param``, ``grad``, ``exp_avg``, ``exp_avg_sq``, with states in 8 bits ``avg_scale`` and
+        ``sq_scale``, and optionally ``param_copy`` (bf16) and the number ``weight_decay``.  States are float32, or float8_e4m3fn (exp_avg) and
+        float8_e5m2 (exp_avg_sq).  Every tensor is contiguous; no two may overlap.  The table holds addresses: make it again when a
+        tensor moves."""
+        t, where = self.torch, "adasd_adamw_step"
+        dtypes = {t.bfloat16: ADASD_BF16, t.float32: ADASD_FP32}
+        array, ranges = (AdamwTensor * max(1, len(tensors)))(), []
+        for e, d in zip(array, tensors):
+            n, bits = d["param"].numel(), 32 if d["exp_avg"].dtype is t.float32 else 8
+            want = [("param", dtypes, n), ("grad", dtypes, n), ("exp_avg", (t.float32 if bits == 32 else t.float8_e4m3fn,), n),
+                    ("exp_avg_sq", (t.float32 if bits == 32 else t.float8_e5m2,), n)]
+            if bits == 8:
+                want += [(k, (t.float32,), -(-n // ADAMW_BLOCK)) for k in ("avg_scale", "sq_scale")]
+            if d.get("param_copy") is not None:
+                want.append(("param_copy", (t.bfloat16,), n))
+            for name, types, size in want:
+                a = d[name]
+                if a.dtype not in types:
+                    raise AdasdError(ERR_DTYPE, where)
+                if a.get_device() != self._index:
+                    raise AdasdError(ERR_DEVICE, where)
+                if a.numel() != size or not a.is_contiguous():
+                    raise AdasdError(ERR_SHAPE, where)
+                setattr(e, name, a.data_ptr() if size else None)
+                if size:
+                    ranges.append((a.data_ptr(), a.data_ptr() + size * a.element_size()))
+            e.n, e.weight_decay, e.state_bits = n, float(d.get("weight_decay", 0.0)), bits
+            e.param_dtype, e.grad_dtype = dtypes[d["param"].dtype], dtypes[d["grad"].dtype]
+        ranges.sort()
+        if any(b[0] < a[1] for a, b in zip(ranges, ranges[1:])):
+            raise AdasdError(ERR_SHAPE, where)
+        table = AdamwTable(array, [dict(d) for d in tensors])
+        table.n = len(tensors)
+        return table
+
+    def adamw_step(self, table: AdamwTable, lr, step, betas=(0.9, 0.999), eps: float = 1e-8, grad_scale=1.0, rounding: str = "nearest",
+                   seed: int = 0, grad_scale_dev=None) -> None:
+        """lr (float32) and step (int32) may be device tensors of one element, which are read when the step runs, as grad_scale_dev
+        is; rounding: "nearest" or "stochastic"."""
+        if rounding not in ("nearest", "stochastic"):
+            raise AdasdError(ERR_DTYPE, "adasd_adamw_step")
+        lr_dev = step_dev = scale_dev = None
+        if hasattr(lr, "data_ptr"):
+            (lr_dev,), lr = self._arrays("adasd_adamw_step", self._f32, 1, (lr,)), 0.0
+        if hasattr(step, "data_ptr"):
+            (step_dev,), step = self._arrays("adasd_adamw_step", self._i32, 1, (step,)), 1
+        if grad_scale_dev is not None:
+            scale_dev, = self._arrays("adasd_adamw_step", self._f32, 1, (grad_scale_dev,))
+        rc = self._adamw_step(self.handle, table.entries, table.n,
+                              AdamwOptions(lr, betas[0], betas[1], eps, grad_scale, step, rounding == "stochastic", seed, lr_dev,
+                                           scale_dev, step_dev), self._raw_stream(self._index))
+        if rc:
+            raise AdasdError(rc, "adasd_adamw_step")
 
     def get_thresholds(self):
         """(T_G, nE, nA, nR) as new device tensors."""

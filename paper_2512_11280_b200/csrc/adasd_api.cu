@@ -22,6 +22,7 @@
 #include "adasd_topk.cuh"
 #include "adasd_modes.cuh"
 #include "adasd_score_types.cuh"
+#include "adasd_adamw_types.cuh"
 
 using namespace adasd;
 
@@ -1163,6 +1164,53 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
         return ADASD_OK;
     }
     return loss_out_dev ? launch_total(nullptr, 0, loss_out_dev, st) : ADASD_OK;
+}
+
+// ---- AdamW -----------------------------------------------------------------------------------
+
+int adasd_adamw_step(adasd_ctx* ctx, const adasd_adamw_tensor* tensors, int32_t n_tensors, const adasd_adamw_options* options, void* stream) {
+    if (!ctx || !options || (n_tensors > 0 && !tensors)) return ADASD_ERR_NULL;
+    const adasd_adamw_options& o = *options;
+    if (n_tensors < 0 || !std::isfinite(o.lr) || !(o.beta1 >= 0.0) || !(o.beta1 < 1.0) || !(o.beta2 >= 0.0) || !(o.beta2 < 1.0) || !(o.eps >= 1e-30) ||
+        !std::isfinite(o.eps) || !std::isfinite(o.grad_scale) || (o.step < 1 && !o.step_dev))
+        return ADASD_ERR_SHAPE;
+    if (o.stochastic != 0 && o.stochastic != 1) return ADASD_ERR_DTYPE;
+    if (!aligned4({o.lr_dev, o.grad_scale_dev, o.step_dev})) return ADASD_ERR_ALIGN;
+    auto dtype_ok = [](int d) { return d == ADASD_BF16 || d == ADASD_FP32; };
+    for (int k = 0; k < n_tensors; ++k) {
+        const adasd_adamw_tensor& t = tensors[k];
+        if (!dtype_ok(t.param_dtype) || !dtype_ok(t.grad_dtype) || (t.state_bits != 8 && t.state_bits != 32)) return ADASD_ERR_DTYPE;
+        if (t.param_copy && t.param_dtype != ADASD_FP32) return ADASD_ERR_DTYPE;
+        if (t.n < 0 || t.n > (int64_t)1 << 40 || !std::isfinite(t.weight_decay)) return ADASD_ERR_SHAPE;
+        if (t.n == 0) continue;
+        if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq || (t.state_bits == 8 && (!t.avg_scale || !t.sq_scale))) return ADASD_ERR_NULL;
+        if (!aligned_to(t.param, elt_size(t.param_dtype)) || !aligned_to(t.grad, elt_size(t.grad_dtype)) || !aligned_to(t.param_copy, 2)) return ADASD_ERR_ALIGN;
+        if (t.state_bits == 32 ? !aligned4({t.exp_avg, t.exp_avg_sq}) : !aligned4({t.avg_scale, t.sq_scale})) return ADASD_ERR_ALIGN;
+    }
+    if (int rc = check_device(ctx)) return rc;
+    AdParams p;
+    memset(&p, 0, sizeof(p));
+    p.b1 = (float)o.beta1;
+    p.b1c = (float)(1.0 - o.beta1);
+    p.b2 = (float)o.beta2;
+    p.b2c = (float)(1.0 - o.beta2);
+    p.eps = (float)o.eps;
+    p.lr = o.lr;
+    p.log_b1 = std::log(o.beta1);
+    p.log_b2 = std::log(o.beta2);
+    p.step = o.step;
+    p.seed = o.seed;
+    p.stochastic = o.stochastic;
+    p.lr_dev = o.lr_dev;
+    p.grad_scale_dev = o.grad_scale_dev;
+    p.step_dev = o.step_dev;
+    p.status = ctx->st.status;
+    p.coef.step = (uint32_t)o.step;
+    p.coef.lr = (float)o.lr;
+    p.coef.rate = (float)(o.lr / -std::expm1(o.step * p.log_b1));
+    p.coef.root = (float)(1.0 / std::sqrt(-std::expm1(o.step * p.log_b2)));
+    p.coef.grad_scale = (float)o.grad_scale;
+    return launch_adamw(p, tensors, n_tensors, ctx->sm_count, (cudaStream_t)stream);
 }
 
 int adasd_set_warpers(adasd_ctx* ctx, float temperature, int32_t top_k, float top_p) {
