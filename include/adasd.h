@@ -17,8 +17,8 @@
  *     neither frees nor keeps it beyond the call.  Pointers without the suffix are
  *     host pointers.  `stream` is a cudaStream_t passed as void* (NULL = default).
  *   - Hot calls (draft_entropy, verify, update_thresholds, vanilla_verify, greedy_verify,
- *     gen_only_update, token_logprob, token_logprob_grad, policy_loss, preference_loss, adamw_step,
- *     get_thresholds, reset) only enqueue kernels on `stream`: they never allocate, free or synchronise.  create/destroy/state_export/state_import/status do.
+ *     gen_only_update, token_logprob, token_logprob_grad, policy_loss, preference_loss, head_logprob,
+ *     head_logprob_grad, head_cross_entropy, adamw_step, get_thresholds, reset) only enqueue kernels on `stream`: they never allocate, free or synchronise.  create/destroy/state_export/state_import/status do.
  *   - Logits are row-major with contiguous vocabulary; strides are in ELEMENTS.
  *     bf16 or fp32 as fixed at create time.  Rows may start at any multiple of their element
  *     size; they are copied by the aligned 16-byte granules that hold them, so that up to 14
@@ -424,6 +424,71 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
                           const adasd_preference_options* options, void* scratch_dev,
                           float* seq_logp_out_dev, float* pair_loss_out_dev, float* loss_out_dev,
                           void* grad_logits_dev, int64_t grad_row_stride, void* stream);
+
+/*
+ * ---- Scoring and training from hidden states --------------------------------------------------
+ *
+ * The calls above take logits that the caller has made.  These take what the logits are made of: hidden states h [n_rows, dim] ahead of
+ * the output projection ("head") and its weight w [V, dim], both bf16, z = h w^T in fp32; log-probs, loss and gradients come
+ * out, and no array of n_rows x V is ever held.  Tokens, rows left out, T, l and H are as above; top-k and top-p are refused
+ * (ADASD_ERR_DTYPE), and so is a context of fp32 rows.
+ *   - hidden_dev: row r at r * hidden_stride (elements), any alignment.  weight_dev: row v at v * weight_stride; it starts at a
+ *     multiple of 16 bytes and weight_stride is a multiple of 8 (ADASD_ERR_ALIGN, ADASD_ERR_SHAPE).  dim: a multiple of 8 up to
+ *     65536.  n_rows up to 2^22, 0 included.
+ *   - Gradients are bf16: grad_hidden_dev as the hidden states, grad_weight_dev as the weight (each nullable, with its stride).  Every element of the
+ *     n_rows and of the V rows is written, what lies between rows is left as it was.  A row left out has a gradient of zeros and adds nothing
+ *     to the weight's, whatever its hidden states hold (NaN too).  Gradients, inputs and scratch must not overlap (ADASD_ERR_SHAPE).
+ *   - A row whose logits are not all finite sets ADASD_STATUS_NAN: its outputs, the totals it enters and both its gradient and the
+ *     whole of the weight's are NaN.
+ *   - scratch_dev: at least the bytes that adasd_head_scratch gives for the call's n_rows and dim, 16-byte aligned, contents of no
+ *     meaning between calls.  Two calls that may overlap (streams, captured graphs) need one each.  It grows with n_rows: in the main
+ *     16 bytes a row for every 256 of V, with gradients at most the larger of 256 MB and 4096 bytes a row, and 6 dim bytes a row.
+ *   - Sums and statistics are held in 32 bits or more.  z is off by the rounding of an fp32 sum of dim exact products; ln S as above.  A
+ *     gradient's p_v comes with (4 |ln p_v| + 2 |lse| + 16) 2^-24 of itself and that; dL/dz is rounded to bf16 (2^-8 of itself at
+ *     most) ahead of the products with w and h, which are summed in fp32 and rounded to bf16 once.  Results do not vary from run to run.
+ *   - Keeps nothing in the context but the status word; may be captured in a graph without a call ahead of it.
+ *   - After a wait that expired (ADASD_STATUS_TIMEOUT) the outputs of such a call are not to be used.
+ */
+
+/* Bytes of scratch of the calls below for n_rows rows (or fewer) of dim elements; with_grad: 1 for a call with a gradient. */
+int adasd_head_scratch(adasd_ctx* ctx, int32_t n_rows, int32_t dim, int32_t with_grad, size_t* bytes_out);
+
+/* l, entropy and log-sum-exp (of z / T) of every row; each output [n_rows], entropy and lse nullable. */
+int adasd_head_logprob(adasd_ctx* ctx, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev,
+                       int64_t weight_stride, int32_t dim, const int32_t* tokens_dev, int32_t n_rows, void* scratch_dev,
+                       size_t scratch_bytes, float* logp_out_dev, float* entropy_out_dev, float* lse_out_dev, void* stream);
+
+/*
+ * Backward pass of adasd_head_logprob: gradients of a loss with dL/dl = grad_logp_dev [n_rows] and dL/dH = grad_entropy_dev
+ * [n_rows] (nullable: 0), from what the forward pass reported: lse_dev [n_rows], and entropy_dev [n_rows] where grad_entropy_dev
+ * is given.  A row for which both are 0 counts as left out.  At least one of the two gradients is given.
+ */
+int adasd_head_logprob_grad(adasd_ctx* ctx, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev,
+                            int64_t weight_stride, int32_t dim, const int32_t* tokens_dev, int32_t n_rows,
+                            const float* lse_dev, const float* entropy_dev, const float* grad_logp_dev,
+                            const float* grad_entropy_dev, void* scratch_dev, size_t scratch_bytes, void* grad_hidden_dev,
+                            int64_t grad_hidden_stride, void* grad_weight_dev, int64_t grad_weight_stride, void* stream);
+
+typedef struct {
+    float label_smoothing; /* e in [0, 1) */
+    float z_loss;          /* c >= 0 */
+    float scale;           /* factor of every row's loss, as 1 / rows counted */
+} adasd_cross_entropy_options;
+
+/*
+ * Cross entropy and its gradients.  Per row, with weight w_r:
+ *   row_loss = scale w_r ( -(1 - e) l - e / V sum_v ln p_v + c lse^2 );   the total is the sum of the row losses
+ *   row_weight_dev   [n_rows] (nullable: 1); a row of weight 0 counts as left out
+ *   options          host struct
+ *   row_loss_out_dev [n_rows]; loss_out_dev [1], logp_out_dev, lse_out_dev [n_rows], nullable
+ *   both gradients nullable: the loss alone
+ */
+int adasd_head_cross_entropy(adasd_ctx* ctx, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev,
+                             int64_t weight_stride, int32_t dim, const int32_t* tokens_dev, int32_t n_rows,
+                             const float* row_weight_dev, const adasd_cross_entropy_options* options, void* scratch_dev,
+                             size_t scratch_bytes, float* row_loss_out_dev, float* loss_out_dev, float* logp_out_dev,
+                             float* lse_out_dev, void* grad_hidden_dev, int64_t grad_hidden_stride, void* grad_weight_dev,
+                             int64_t grad_weight_stride, void* stream);
 
 /*
  * ---- AdamW ------------------------------------------------------------------------------------

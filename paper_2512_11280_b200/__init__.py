@@ -5,7 +5,8 @@ marshals arguments (device pointers of torch tensors, strides, streams).  There 
 no CPU fallback: importing works anywhere, but every call needs the built library
 and a CUDA device and raises otherwise.
 """
-from .binding import (ADAMW_BLOCK, AdamwOptions, AdamwTable, AdamwTensor, adasd_adamw_step,
+from .binding import (ADAMW_BLOCK, AdamwOptions, AdamwTable, AdamwTensor, CrossEntropyOptions, adasd_adamw_step,
+                      adasd_head_cross_entropy, adasd_head_logprob, adasd_head_logprob_grad, adasd_head_scratch,
                       ERR_ALIGN, ERR_CAPACITY, ERR_CUDA, ERR_DEVICE, ERR_DTYPE, ERR_NULL, ERR_SHAPE,
                       ADASD_BF16, ADASD_FP32, ADASD_FUSE_UPDATE, ADASD_KMAX_LIMIT, PREF_HINGE,
                       PREF_SCRATCH_PER_ROW, PREF_SIGMOID, PREF_SQUARED, STATUS_CAPACITY,

@@ -53,6 +53,10 @@ class PreferenceOptions(C.Structure):
                 ("label_smoothing", C.c_float), ("scale", C.c_float)]
 
 
+class CrossEntropyOptions(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("label_smoothing", "z_loss", "scale")]
+
+
 class AdamwTensor(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("param", "grad", "exp_avg", "exp_avg_sq", "avg_scale", "sq_scale", "param_copy")] + [
         ("n", C.c_int64), ("weight_decay", C.c_float), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("state_bits", C.c_int32)]
@@ -96,6 +100,11 @@ def lib() -> C.CDLL:
         "adasd_policy_loss": [P, P, I64, P, I32, P, P, P, P, C.POINTER(PolicyOptions), P, P, P, P, P, P, I64, P],
         "adasd_preference_loss": [P, P, I64, P, I32, P, I32, P, P, C.POINTER(PreferenceOptions), P, P, P, P, P,
                                   I64, P],
+        "adasd_head_scratch": [P, I32, I32, I32, C.POINTER(C.c_size_t)],
+        "adasd_head_logprob": [P, P, I64, P, I64, I32, P, I32, P, C.c_size_t, P, P, P, P],
+        "adasd_head_logprob_grad": [P, P, I64, P, I64, I32, P, I32, P, P, P, P, P, C.c_size_t, P, I64, P, I64, P],
+        "adasd_head_cross_entropy": [P, P, I64, P, I64, I32, P, I32, P, C.POINTER(CrossEntropyOptions), P, C.c_size_t, P, P, P, P, P,
+                                     I64, P, I64, P],
         "adasd_adamw_step": [P, C.POINTER(AdamwTensor), I32, C.POINTER(AdamwOptions), P],
         "adasd_set_warpers": [P, C.c_float, I32, C.c_float],
         "adasd_get_thresholds": [P, P, P, P, P, P],
@@ -230,6 +239,36 @@ def adasd_preference_loss(ctx, logits_dev, row_stride, tokens_dev, n_rows, seq_s
                                        grad_row_stride, stream)
 
 
+def adasd_head_scratch(ctx, n_rows, dim, with_grad):
+    """Returns (code, bytes)."""
+    n = C.c_size_t(0)
+    rc = lib().adasd_head_scratch(ctx, n_rows, dim, with_grad, C.byref(n))
+    return rc, n.value
+
+
+def adasd_head_logprob(ctx, hidden_dev, hidden_stride, weight_dev, weight_stride, dim, tokens_dev, n_rows, scratch_dev, scratch_bytes,
+                       logp_out_dev, entropy_out_dev, lse_out_dev, stream) -> int:
+    return lib().adasd_head_logprob(ctx, hidden_dev, hidden_stride, weight_dev, weight_stride, dim, tokens_dev, n_rows, scratch_dev,
+                                    scratch_bytes, logp_out_dev, entropy_out_dev, lse_out_dev, stream)
+
+
+def adasd_head_logprob_grad(ctx, hidden_dev, hidden_stride, weight_dev, weight_stride, dim, tokens_dev, n_rows, lse_dev, entropy_dev,
+                            grad_logp_dev, grad_entropy_dev, scratch_dev, scratch_bytes, grad_hidden_dev, grad_hidden_stride,
+                            grad_weight_dev, grad_weight_stride, stream) -> int:
+    return lib().adasd_head_logprob_grad(ctx, hidden_dev, hidden_stride, weight_dev, weight_stride, dim, tokens_dev, n_rows, lse_dev,
+                                         entropy_dev, grad_logp_dev, grad_entropy_dev, scratch_dev, scratch_bytes, grad_hidden_dev,
+                                         grad_hidden_stride, grad_weight_dev, grad_weight_stride, stream)
+
+
+def adasd_head_cross_entropy(ctx, hidden_dev, hidden_stride, weight_dev, weight_stride, dim, tokens_dev, n_rows, row_weight_dev, options,
+                             scratch_dev, scratch_bytes, row_loss_out_dev, loss_out_dev, logp_out_dev, lse_out_dev, grad_hidden_dev,
+                             grad_hidden_stride, grad_weight_dev, grad_weight_stride, stream) -> int:
+    return lib().adasd_head_cross_entropy(ctx, hidden_dev, hidden_stride, weight_dev, weight_stride, dim, tokens_dev, n_rows,
+                                          row_weight_dev, C.byref(options) if options is not None else None, scratch_dev,
+                                          scratch_bytes, row_loss_out_dev, loss_out_dev, logp_out_dev, lse_out_dev, grad_hidden_dev,
+                                          grad_hidden_stride, grad_weight_dev, grad_weight_stride, stream)
+
+
 def adasd_adamw_step(ctx, tensors, n_tensors, options, stream) -> int:
     """tensors: a ctypes array of AdamwTensor."""
     return lib().adasd_adamw_step(ctx, tensors, n_tensors, C.byref(options) if options is not None else None, stream)
@@ -293,6 +332,8 @@ class Context:
         self._token_logprob, self._token_logprob_grad = L.adasd_token_logprob, L.adasd_token_logprob_grad
         self._policy_loss, self._preference_loss = L.adasd_policy_loss, L.adasd_preference_loss
         self._adamw_step = L.adasd_adamw_step
+        self._head_logprob, self._head_logprob_grad = L.adasd_head_logprob, L.adasd_head_logprob_grad
+        self._head_cross_entropy, self._bf16 = L.adasd_head_cross_entropy, torch.bfloat16
         self._logit_dtype = torch.bfloat16 if dtype == ADASD_BF16 else torch.float32
         self._i32, self._f32, self._index = torch.int32, torch.float32, self.device.index
         self._raw_stream = torch._C._cuda_getCurrentRawStream
@@ -506,6 +547,68 @@ class Context:
                                    PreferenceOptions(_PREF_RULES[rule], 1 if average else 0, beta, margin, label_smoothing,
                                                      scale),
                                    sc, seq, pl, total, g, g_stride, self._raw_stream(self._index))
+        if rc:
+            raise AdasdError(rc, where)
+
+    # ---- scoring and training from hidden states [n, dim] and the head's weight [V, dim] -----------------
+
+    def head_scratch(self, n_rows: int, dim: int, grad: bool = False) -> int:
+        """Bytes of the scratch tensor (any dtype) that the calls below need for up to n_rows rows."""
+        rc, n = adasd_head_scratch(self.handle, n_rows, dim, 1 if grad else 0)
+        self._check(rc, "adasd_head_scratch")
+        return n
+
+    def _matrix(self, where: str, t, rows: int, dim: int):
+        """(address, row stride) of a bf16 matrix; (None, 0) for None."""
+        if t is None:
+            return None, 0
+        if t.dtype is not self._bf16:
+            raise AdasdError(ERR_DTYPE, where)
+        if t.get_device() != self._index:
+            raise AdasdError(ERR_DEVICE, where)
+        shape, strides = t.shape, t.stride()
+        if len(shape) != 2 or shape[0] != rows or shape[1] != dim or (strides[1] != 1 and dim > 1):
+            raise AdasdError(ERR_SHAPE, where)
+        return t.data_ptr(), strides[0] if rows > 1 or strides[0] > dim else dim      # (the stride of a single row says nothing)
+
+    def _head(self, where: str, hidden, weight, tokens, scratch):
+        """The arguments that the head calls share, and rows and width."""
+        if len(hidden.shape) != 2:
+            raise AdasdError(ERR_SHAPE, where)
+        n, dim = hidden.shape
+        (h, hs), (w, ws) = self._matrix(where, hidden, n, dim), self._matrix(where, weight, self.V, dim)
+        tok, = self._arrays(where, self._i32, n, (tokens,))
+        sc, = self._arrays(where, scratch.dtype, 0, (scratch,))
+        return (self.handle, h, hs, w, ws, dim, tok, n), (sc, scratch.numel() * scratch.element_size()), n, dim
+
+    def head_logprob(self, hidden, weight, tokens, logp_out, scratch, entropy_out=None, lse_out=None) -> None:
+        where = "adasd_head_logprob"
+        first, sc, n, _ = self._head(where, hidden, weight, tokens, scratch)
+        rc = self._head_logprob(*first, *sc, *self._arrays(where, self._f32, n, (logp_out, entropy_out, lse_out)), self._raw_stream(self._index))
+        if rc:
+            raise AdasdError(rc, where)
+
+    def head_logprob_grad(self, hidden, weight, tokens, lse, grad_logp, scratch, entropy=None, grad_entropy=None, grad_hidden_out=None,
+                          grad_weight_out=None) -> None:
+        """lse and entropy: what :meth:`head_logprob` reported for the same rows."""
+        where = "adasd_head_logprob_grad"
+        first, sc, n, dim = self._head(where, hidden, weight, tokens, scratch)
+        rc = self._head_logprob_grad(*first, *self._arrays(where, self._f32, n, (lse, entropy, grad_logp, grad_entropy)), *sc,
+                                     *self._matrix(where, grad_hidden_out, n, dim), *self._matrix(where, grad_weight_out, self.V, dim),
+                                     self._raw_stream(self._index))
+        if rc:
+            raise AdasdError(rc, where)
+
+    def head_cross_entropy(self, hidden, weight, tokens, row_loss_out, scratch, row_weight=None, label_smoothing: float = 0.0,
+                           z_loss: float = 0.0, scale: float = 1.0, loss_out=None, logp_out=None, lse_out=None, grad_hidden_out=None,
+                           grad_weight_out=None) -> None:
+        where = "adasd_head_cross_entropy"
+        first, sc, n, dim = self._head(where, hidden, weight, tokens, scratch)
+        rw, rl, lp, lse = self._arrays(where, self._f32, n, (row_weight, row_loss_out, logp_out, lse_out))
+        total, = self._arrays(where, self._f32, 1, (loss_out,))
+        rc = self._head_cross_entropy(*first, rw, CrossEntropyOptions(label_smoothing, z_loss, scale), *sc, rl, total, lp, lse,
+                                      *self._matrix(where, grad_hidden_out, n, dim), *self._matrix(where, grad_weight_out, self.V, dim),
+                                      self._raw_stream(self._index))
         if rc:
             raise AdasdError(rc, where)
 

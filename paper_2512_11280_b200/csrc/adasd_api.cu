@@ -23,6 +23,7 @@
 #include "adasd_modes.cuh"
 #include "adasd_score_types.cuh"
 #include "adasd_adamw_types.cuh"
+#include "adasd_head_types.cuh"
 
 using namespace adasd;
 
@@ -1164,6 +1165,132 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
         return ADASD_OK;
     }
     return loss_out_dev ? launch_total(nullptr, 0, loss_out_dev, st) : ADASD_OK;
+}
+
+// ---- scoring and training from hidden states --------------------------------------------------
+
+namespace {
+struct Extent {
+    uintptr_t at, end;
+};
+Extent rows_extent(const void* p, int64_t stride, int64_t n, int64_t width) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    return {a, p && n > 0 ? a + (uintptr_t)(((n - 1) * stride + width) * 2) : a};
+}
+bool meet(const Extent& a, const Extent& b) { return a.at < b.end && b.at < a.end && a.at != a.end && b.at != b.end; }
+}  // namespace
+
+// Checks what the head calls have in common; fills in what they share.
+static int check_head(const adasd_ctx* ctx, HeadCall& c, int32_t op, const void* hidden, int64_t h_stride, const void* weight, int64_t w_stride,
+                      int32_t dim, const int32_t* tokens, int32_t n_rows, void* scratch, size_t scratch_bytes, void* grad_h, int64_t gh_stride,
+                      void* grad_w, int64_t gw_stride) {
+    constexpr int64_t most = (int64_t)1 << 33;
+    if (n_rows < 0 || n_rows > (1 << 22) || dim < 8 || dim > 65536 || dim % 8 != 0) return ADASD_ERR_SHAPE;
+    if (n_rows > 0 && (!hidden || !weight || !tokens || !scratch)) return ADASD_ERR_NULL;
+    if (!aligned_to(hidden, 2) || !aligned16(weight) || !aligned16(scratch) || !aligned4({tokens}) || !aligned_to(grad_h, 2) || !aligned16(grad_w))
+        return ADASD_ERR_ALIGN;
+    if (h_stride < dim || h_stride > most || w_stride < dim || w_stride > most || w_stride % 8 != 0) return ADASD_ERR_SHAPE;
+    if (grad_h && (gh_stride < dim || gh_stride > most)) return ADASD_ERR_SHAPE;
+    if (grad_w && (gw_stride < dim || gw_stride > most || gw_stride % 8 != 0)) return ADASD_ERR_SHAPE;
+    if (int rc = check_device(ctx)) return rc;
+    if (ctx->cfg.dtype != ADASD_BF16 || ctx->cuts_on()) return ADASD_ERR_DTYPE;
+    if (!std::isfinite(kLog2e / ctx->temperature)) return ADASD_ERR_SHAPE;
+    const int V = ctx->cfg.V;
+    const Extent h = rows_extent(hidden, h_stride, n_rows, dim), w = rows_extent(weight, w_stride, V, dim),
+                 gh = rows_extent(grad_h, gh_stride, n_rows, dim), gw = rows_extent(grad_w, gw_stride, V, dim),
+                 s = {reinterpret_cast<uintptr_t>(scratch), reinterpret_cast<uintptr_t>(scratch) + (scratch ? scratch_bytes : 0)};
+    if (meet(h, gh) || meet(h, gw) || meet(w, gh) || meet(w, gw) || meet(gh, gw) || meet(s, h) || meet(s, w) || meet(s, gh) || meet(s, gw))
+        return ADASD_ERR_SHAPE;
+    if (n_rows > 0 && scratch_bytes < head_scratch_bytes(n_rows, V, dim, grad_h || grad_w, ctx->sm_count)) return ADASD_ERR_CAPACITY;
+    memset(&c, 0, sizeof(c));
+    c.op = op;
+    c.n_rows = n_rows;
+    c.V = V;
+    c.D = dim;
+    c.hidden = hidden;
+    c.h_stride = h_stride;
+    c.weight = weight;
+    c.w_stride = w_stride;
+    c.tok = tokens;
+    c.temperature = ctx->temperature;
+    c.status = ctx->st.status;
+    c.scratch = scratch;
+    c.grad_h = grad_h;
+    c.gh_stride = gh_stride;
+    c.grad_w = grad_w;
+    c.gw_stride = gw_stride;
+    c.sm_count = ctx->sm_count;
+    return ADASD_OK;
+}
+static int run_head(const HeadCall& c, cudaStream_t stream) {
+    if (c.n_rows > 0) return launch_head(c, stream);
+    if (c.grad_w) CUDA_TRY(cudaMemset2DAsync(c.grad_w, (size_t)c.gw_stride * 2, 0, (size_t)c.D * 2, (size_t)c.V, stream));
+    return ADASD_OK;
+}
+
+int adasd_head_scratch(adasd_ctx* ctx, int32_t n_rows, int32_t dim, int32_t with_grad, size_t* bytes_out) {
+    if (!ctx || !bytes_out) return ADASD_ERR_NULL;
+    if (n_rows < 0 || n_rows > (1 << 22) || dim < 8 || dim > 65536 || dim % 8 != 0 || with_grad < 0 || with_grad > 1) return ADASD_ERR_SHAPE;
+    *bytes_out = head_scratch_bytes(n_rows, ctx->cfg.V, dim, with_grad != 0, ctx->sm_count);
+    return ADASD_OK;
+}
+
+int adasd_head_logprob(adasd_ctx* ctx, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride, int32_t dim,
+                       const int32_t* tokens_dev, int32_t n_rows, void* scratch_dev, size_t scratch_bytes, float* logp_out_dev,
+                       float* entropy_out_dev, float* lse_out_dev, void* stream) {
+    if (!ctx || (n_rows > 0 && !logp_out_dev)) return ADASD_ERR_NULL;
+    if (!aligned4({logp_out_dev, entropy_out_dev, lse_out_dev})) return ADASD_ERR_ALIGN;
+    HeadCall c;
+    if (int rc = check_head(ctx, c, HEAD_LOGPROB, hidden_dev, hidden_stride, weight_dev, weight_stride, dim, tokens_dev, n_rows, scratch_dev,
+                            scratch_bytes, nullptr, 0, nullptr, 0))
+        return rc;
+    c.logp = logp_out_dev;
+    c.H = entropy_out_dev;
+    c.lse = lse_out_dev;
+    return run_head(c, (cudaStream_t)stream);
+}
+
+int adasd_head_logprob_grad(adasd_ctx* ctx, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride, int32_t dim,
+                            const int32_t* tokens_dev, int32_t n_rows, const float* lse_dev, const float* entropy_dev, const float* grad_logp_dev,
+                            const float* grad_entropy_dev, void* scratch_dev, size_t scratch_bytes, void* grad_hidden_dev,
+                            int64_t grad_hidden_stride, void* grad_weight_dev, int64_t grad_weight_stride, void* stream) {
+    if (!ctx || (n_rows > 0 && (!lse_dev || !grad_logp_dev || (grad_entropy_dev && !entropy_dev)))) return ADASD_ERR_NULL;
+    if (!grad_hidden_dev && !grad_weight_dev) return ADASD_ERR_NULL;
+    if (!aligned4({lse_dev, entropy_dev, grad_logp_dev, grad_entropy_dev})) return ADASD_ERR_ALIGN;
+    HeadCall c;
+    if (int rc = check_head(ctx, c, HEAD_GIVEN, hidden_dev, hidden_stride, weight_dev, weight_stride, dim, tokens_dev, n_rows, scratch_dev,
+                            scratch_bytes, grad_hidden_dev, grad_hidden_stride, grad_weight_dev, grad_weight_stride))
+        return rc;
+    c.lse_in = lse_dev;
+    c.H_in = entropy_dev;
+    c.g_logp = grad_logp_dev;
+    c.g_H = grad_entropy_dev;
+    return run_head(c, (cudaStream_t)stream);
+}
+
+int adasd_head_cross_entropy(adasd_ctx* ctx, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride, int32_t dim,
+                             const int32_t* tokens_dev, int32_t n_rows, const float* row_weight_dev, const adasd_cross_entropy_options* options,
+                             void* scratch_dev, size_t scratch_bytes, float* row_loss_out_dev, float* loss_out_dev, float* logp_out_dev,
+                             float* lse_out_dev, void* grad_hidden_dev, int64_t grad_hidden_stride, void* grad_weight_dev,
+                             int64_t grad_weight_stride, void* stream) {
+    if (!ctx || !options || (n_rows > 0 && !row_loss_out_dev)) return ADASD_ERR_NULL;
+    const adasd_cross_entropy_options& o = *options;
+    if (!(o.label_smoothing >= 0.f) || !(o.label_smoothing < 1.f) || !(o.z_loss >= 0.f) || !std::isfinite(o.z_loss) || !std::isfinite(o.scale))
+        return ADASD_ERR_SHAPE;
+    if (!aligned4({row_weight_dev, row_loss_out_dev, loss_out_dev, logp_out_dev, lse_out_dev})) return ADASD_ERR_ALIGN;
+    HeadCall c;
+    if (int rc = check_head(ctx, c, HEAD_CE, hidden_dev, hidden_stride, weight_dev, weight_stride, dim, tokens_dev, n_rows, scratch_dev, scratch_bytes,
+                            grad_hidden_dev, grad_hidden_stride, grad_weight_dev, grad_weight_stride))
+        return rc;
+    c.row_weight = row_weight_dev;
+    c.smoothing = o.label_smoothing;
+    c.z_loss = o.z_loss;
+    c.scale = o.scale;
+    c.row_loss = row_loss_out_dev;
+    c.logp = logp_out_dev;
+    c.lse = lse_out_dev;
+    if (int rc = run_head(c, (cudaStream_t)stream)) return rc;
+    return loss_out_dev ? launch_total(row_loss_out_dev, n_rows, loss_out_dev, (cudaStream_t)stream) : ADASD_OK;
 }
 
 // ---- AdamW -----------------------------------------------------------------------------------

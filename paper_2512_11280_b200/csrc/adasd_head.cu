@@ -1,0 +1,182 @@
+// Launches of the head kernels (adasd_head.cuh).
+#include "adasd_head.cuh"
+#include "adasd_launch.cuh"
+#include "adasd_score_types.cuh"
+
+#include <algorithm>
+#include <atomic>
+
+namespace adasd {
+namespace {
+
+// What a call keeps in its scratch.  (Statistics of the tiles and a piece of the gradient are never needed at once: they share their place.)
+struct Layout {
+    int n_pad, D8, Dp, tiles;
+    int piece, splits;                               // columns of a piece; parts that the products along them are cut into
+    size_t h, index, tok, n_active, zx, coef, big, acc, total;
+};
+
+constexpr size_t kPieceBytes = (size_t)256 << 20;
+
+Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
+    Layout L;
+    L.n_pad = (std::max(n_rows, 1) + kHgM - 1) / kHgM * kHgM;
+    L.D8 = (D + 7) / 8 * 8;
+    L.Dp = (D + 63) / 64 * 64;
+    L.tiles = (V + kHgN - 1) / kHgN;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += (bytes + 1023) & ~(size_t)1023;
+        return here;
+    };
+    L.n_active = take(16);
+    L.index = take((size_t)L.n_pad * 4);
+    L.tok = take((size_t)L.n_pad * 4);
+    L.zx = take((size_t)L.n_pad * 4);
+    L.coef = take(gradient ? (size_t)L.n_pad * sizeof(HeadCoef) : 0);
+    L.h = take((size_t)L.n_pad * L.D8 * 2);
+    const size_t part = (size_t)L.n_pad * L.tiles * sizeof(float4);
+    L.piece = L.splits = 0;
+    size_t g = 0, acc = 0;
+    if (gradient) {
+        const long long fit = (long long)(kPieceBytes / (2 * (size_t)L.n_pad)) / kHgN * kHgN;
+        L.piece = (int)std::min<long long>((long long)L.tiles * kHgN, std::max<long long>(fit, 2048));
+        const long long tiles = (long long)(L.n_pad / kHgM) * ((D + kHgN - 1) / kHgN);
+        L.splits = (int)std::max<long long>(1, std::min<long long>(sm_count / tiles, std::min(32, L.piece / 1024)));
+        g = (size_t)L.n_pad * L.piece * 2;
+        acc = (size_t)L.splits * L.n_pad * L.Dp * 4;
+    }
+    L.big = take(std::max(part, g));
+    L.acc = take(acc);
+    L.total = at;
+    return L;
+}
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+    static const EncodeTiled f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return f;
+}
+// Map of a row-major bf16 matrix in boxes of 64 columns.
+int make_map(CUtensorMap* map, const void* base, long long rows, long long columns, long long stride, int box_rows) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return ADASD_ERR_CUDA;
+    const cuuint64_t dims[2] = {(cuuint64_t)columns, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, step[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? ADASD_OK
+               : ADASD_ERR_CUDA;
+}
+
+template <int TILE>
+int launch_tiles(const HeadTiles& p, int sm_count, cudaStream_t stream) {
+    static std::atomic<bool> allowed[64];
+    int dev = 0;
+    CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return ADASD_ERR_CUDA;
+    if (!allowed[dev].load(std::memory_order_acquire)) {
+        CUDA_TRY(cudaFuncSetAttribute(head_tile_kernel<TILE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHgSmem));
+        allowed[dev].store(true, std::memory_order_release);
+    }
+    return launch_pdl(head_tile_kernel<TILE>, sm_count, kHgThreads, kHgSmem, 0, stream, p);
+}
+
+}  // namespace
+
+size_t head_scratch_bytes(int n_rows, int V, int D, bool gradient, int sm_count) { return layout_of(n_rows, V, D, gradient, sm_count).total; }
+
+int launch_head(const HeadCall& c, cudaStream_t stream) {
+    const bool gradient = c.gradient();
+    const Layout L = layout_of(c.n_rows, c.V, c.D, gradient, c.sm_count);
+    char* s = static_cast<char*>(c.scratch);
+
+    HeadRows r;
+    memset(&r, 0, sizeof(r));
+    r.c = c;
+    r.h = reinterpret_cast<uint16_t*>(s + L.h);
+    r.D8 = L.D8;
+    r.tiles = L.tiles;
+    r.index = reinterpret_cast<int32_t*>(s + L.index);
+    r.tok = reinterpret_cast<int32_t*>(s + L.tok);
+    r.n_active = reinterpret_cast<int32_t*>(s + L.n_active);
+    r.zx = reinterpret_cast<float*>(s + L.zx);
+    r.coef = gradient ? reinterpret_cast<HeadCoef*>(s + L.coef) : nullptr;
+    r.part = reinterpret_cast<const float4*>(s + L.big);
+    r.acc = reinterpret_cast<const float*>(s + L.acc);
+    r.acc_slot = (long long)L.n_pad * L.Dp;
+    r.Dp = L.Dp;
+    r.splits = L.splits;
+    r.c1 = (float)(1.4426950408889634 / (double)c.temperature);
+    r.inv_T = 1.0 / (double)c.temperature;
+    if (int rc = launch_pdl(head_rows_kernel, (c.n_rows + kHrRows - 1) / kHrRows, kHrThreads, 0, 0, stream, r)) return rc;
+
+    CUtensorMap map_h, map_w;
+    if (int rc = make_map(&map_h, r.h, L.n_pad, c.D, L.D8, 64)) return rc;
+    if (int rc = make_map(&map_w, c.weight, c.V, c.D, c.w_stride, 64)) return rc;
+    HeadTiles t;
+    memset(&t, 0, sizeof(t));
+    t.a = map_h;
+    t.b = map_w;
+    t.D = c.D;
+    t.V = c.V;
+    t.vn = c.V;
+    t.n_active = r.n_active;
+    t.c1 = r.c1;
+    t.part = reinterpret_cast<float4*>(s + L.big);
+    t.tiles = L.tiles;
+    t.zx = r.zx;
+    t.tok = r.tok;
+    t.coef = r.coef;
+    t.acc = reinterpret_cast<float*>(s + L.acc);
+    t.acc_slot = r.acc_slot;
+    t.Dp = L.Dp;
+    t.splits = L.splits;
+    t.status = c.status;
+    if (c.op != HEAD_GIVEN) {
+        if (int rc = launch_tiles<TILE_STATS>(t, c.sm_count, stream)) return rc;
+        if (int rc = launch_pdl(head_stats_kernel, (c.n_rows + kHrThreads / 32 - 1) / (kHrThreads / 32), kHrThreads, 0, 0, stream, r)) return rc;
+    }
+    if (!gradient) return ADASD_OK;
+
+    CUtensorMap map_g, map_g_out, map_gw_out;
+    char* g = s + L.big;
+    if (int rc = make_map(&map_g, g, L.n_pad, L.piece, L.piece, 64)) return rc;
+    if (int rc = make_map(&map_g_out, g, L.n_pad, L.piece, L.piece, 32)) return rc;
+    if (c.grad_w)
+        if (int rc = make_map(&map_gw_out, c.grad_w, c.V, c.D, c.gw_stride, 32)) return rc;
+    for (int v0 = 0; v0 < c.V; v0 += L.piece) {
+        t.v0 = v0;
+        t.vn = std::min(L.piece, c.V - v0);
+        t.first = v0 == 0;
+        t.a = map_h;
+        t.b = map_w;
+        t.out = map_g_out;
+        if (int rc = launch_tiles<TILE_G>(t, c.sm_count, stream)) return rc;
+        t.a = map_g;
+        if (c.grad_w) {
+            t.b = map_h;
+            t.out = map_gw_out;
+            if (int rc = launch_tiles<TILE_GW>(t, c.sm_count, stream)) return rc;
+        }
+        if (c.grad_h) {
+            t.b = map_w;
+            if (int rc = launch_tiles<TILE_GH>(t, c.sm_count, stream)) return rc;
+        }
+    }
+    if (!c.grad_h) return ADASD_OK;
+    const long long warps = (long long)c.n_rows * ((c.D + 255) / 256);
+    return launch_pdl(head_grad_rows_kernel, (int)((warps + kHrThreads / 32 - 1) / (kHrThreads / 32)), kHrThreads, 0, 0, stream, r);
+}
+
+}  // namespace adasd

@@ -1,0 +1,588 @@
+// Log-probs, cross entropy and gradients straight from hidden states h [n, D] and the head's weight w [V, D]: the logits
+// z = h w^T exist only tile by tile.
+//
+//   forward   z tile -> per row and tile: largest t = z log2 e / T, S = sum 2^(t - max), sum 2^(t - max) (t - max), sum z, the token's z
+//   rows      the tiles' statistics -> l, H, lse, loss, and the constants of the row's gradient
+//   backward  for a piece of the vocabulary at a time: the same z tile again -> G = dL/dz (bf16) in the caller's scratch;
+//             grad_w of the piece = G^T h;  grad_h += G w, in fp32
+//
+// All four are products on the tensor cores: 2 n V D operations each.  Logits are worked out twice so that what is kept is a piece of G (at
+// most 256 MB, or 2048 columns) instead of n V values.  G is rounded to bf16, as the products' operands are; gradients are rounded to
+// bf16 once more when they are written.
+//
+// Rows left out are not worked on: the rows that count are copied together first (head_rows_kernel), how many there are is known on the
+// device alone.
+#pragma once
+
+#include "adasd_head_types.cuh"
+#include "adasd_tensor.cuh"
+
+namespace adasd {
+
+constexpr int kHgM = 128, kHgN = 256, kHgK = 64;             // tile of a CTA; a step along K
+constexpr int kHgStages = 4;
+constexpr int kHgABytes = kHgM * kHgK * 2, kHgBBytes = kHgN * kHgK * 2, kHgStageBytes = kHgABytes + kHgBBytes;
+constexpr int kHgBox = 64 * 64 * 2;
+constexpr int kHgOut = 32 * 64 * 2;                          // 32 rows of 64 bf16: what a warp stores at a time
+constexpr int kHgThreads = 192;                              // copies, products, four warps of epilogue
+constexpr int kHgSmem = 1024 + kHgStages * kHgStageBytes + 4 * 2 * kHgOut + 256;
+
+enum HeadTile : int { TILE_STATS, TILE_G, TILE_GW, TILE_GH };
+
+// Of a row that counts: g_v = p (A + E u) + C, and at the token B more, where u = log2 p.
+struct __align__(16) HeadCoef {
+    float lse2, A, B, C;
+    float E;
+    int32_t tok;
+    float pad[2];
+};
+
+struct HeadTiles {
+    CUtensorMap a, b, out;
+    int32_t D, V, v0, vn;                // piece of the vocabulary: columns v0 .. v0 + vn - 1
+    const int32_t* n_active;
+    float c1;                            // log2 e / T
+    float4* part;                        // TILE_STATS: [row][tiles]
+    int32_t tiles;
+    float* zx;
+    const int32_t* tok;
+    const HeadCoef* coef;                // TILE_G
+    float* acc;                          // TILE_GH: [splits][rows][Dp]
+    long long acc_slot;
+    int32_t Dp, splits, first;
+    uint32_t* status;
+};
+
+template <int TILE>
+struct HeadWork {
+    int mt, nt, total, ksteps;           // tiles along M and N; steps along K, of one split
+    __device__ __forceinline__ HeadWork(const HeadTiles& p, int n_active) {
+        if (TILE == TILE_STATS || TILE == TILE_G) {
+            mt = (n_active + kHgM - 1) / kHgM;
+            nt = (p.vn + kHgN - 1) / kHgN;
+            ksteps = (p.D + kHgK - 1) / kHgK;
+            total = mt * nt;
+        } else if (TILE == TILE_GW) {
+            mt = (p.vn + kHgM - 1) / kHgM;
+            nt = (p.D + kHgN - 1) / kHgN;
+            ksteps = (n_active + kHgK - 1) / kHgK;
+            total = mt * nt;
+        } else {
+            mt = (n_active + kHgM - 1) / kHgM;
+            nt = (p.D + kHgN - 1) / kHgN;
+            ksteps = ((p.vn + kHgK - 1) / kHgK + p.splits - 1) / p.splits;
+            total = mt * nt * p.splits;
+        }
+    }
+    // tile i: first row along M, first column along N, first and one past the last step along K
+    __device__ __forceinline__ void tile(const HeadTiles& p, int i, int& m0, int& n0, int& k0, int& k1, int& split) const {
+        split = 0;
+        k0 = 0;
+        k1 = ksteps;
+        if (TILE == TILE_STATS || TILE == TILE_G) {          // (the rows of one part of w one after the other)
+            m0 = i % mt * kHgM;
+            n0 = i / mt * kHgN;
+        } else if (TILE == TILE_GW) {
+            n0 = i % nt * kHgN;
+            m0 = i / nt * kHgM;
+        } else {
+            n0 = i % nt * kHgN;
+            m0 = i / nt % mt * kHgM;
+            split = i / (nt * mt);
+            k0 = split * ksteps;
+            k1 = min(k0 + ksteps, (p.vn + kHgK - 1) / kHgK);
+        }
+    }
+};
+
+// ---- epilogues: a thread has a row (lane) and 32 columns at a time ------------------------------------
+struct RowStats {
+    float m, S, T, Z;
+    __device__ __forceinline__ void clear() {
+        m = kFloor;
+        S = T = Z = 0.f;
+    }
+    __device__ __forceinline__ void add(float (&z)[32], int nv, float c1) {
+        float top = kFloor, sum = 0.f;
+        if (nv < 32) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                if (j < nv) sum += z[j];
+                else z[j] = kFloor;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sum += z[j];
+        }
+        Z += sum;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) top = fmaxf(top, z[j]);
+        const float m1 = fmaxf(m, top * c1), f = ex2(m - m1);
+        T = f * (T + S * (m - m1));
+        S = f * S;
+        m = m1;
+        float s = 0.f, t = 0.f;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const float u = nv < 32 && j >= nv ? kFloor : fmaf(z[j], c1, -m1), e = ex2(u);
+            s += e;
+            t = fmaf(e, u, t);
+        }
+        S += s;
+        T += t;
+    }
+};
+
+// v[k], and v[k] = x, of registers (as conditional moves: an index that varies would send the array to local memory)
+__device__ __forceinline__ float pick(const float (&v)[32], int k) {
+    float r = 0.f;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %3;\n\t@p mov.f32 %0, %2;\n\t}" : "+f"(r) : "r"(k), "f"(v[j]), "r"(j));
+    return r;
+}
+__device__ __forceinline__ void put_at(float (&v)[32], int k, float x) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %3;\n\t@p mov.f32 %0, %2;\n\t}" : "+f"(v[j]) : "r"(k), "f"(x), "r"(j));
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// 32 columns of a lane's row into its warp's stage: units half * 4 .. half * 4 + 3 of eight, swizzled as the tensor map reads them
+__device__ __forceinline__ void stage_bf16(uint32_t stage, int lane, int half, const float (&v)[32]) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        st_shared_v4(stage + lane * 128 + (((half * 4 + u) ^ (lane & 7)) << 4), pack_bf16(v[8 * u], v[8 * u + 1]), pack_bf16(v[8 * u + 2], v[8 * u + 3]),
+                     pack_bf16(v[8 * u + 4], v[8 * u + 5]), pack_bf16(v[8 * u + 6], v[8 * u + 7]));
+}
+
+template <int TILE>
+__global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_constant__ HeadTiles p) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t out_stage = base + kHgStages * kHgStageBytes, bars = out_stage + 4 * 2 * kHgOut;
+    // barriers: full[stage], empty[stage], accumulator full[2], empty[2], drained
+    const uint32_t bar_full = bars, bar_empty = bars + 8 * kHgStages, acc_full = bars + 16 * kHgStages, acc_empty = acc_full + 16, bar_drained = acc_empty + 16;
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile uint32_t s_gave_up;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr bool kAMn = TILE == TILE_GW, kBMn = TILE == TILE_GW || TILE == TILE_GH;
+
+    if (threadIdx.x == 0) {
+        s_gave_up = 0u;
+        for (int i = 0; i < kHgStages; ++i) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_full + 8 * i) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_empty + 8 * i) : "memory");
+        }
+        for (int i = 0; i < 2; ++i) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(acc_full + 8 * i) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 4;" ::"r"(acc_empty + 8 * i) : "memory");
+        }
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_drained) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tensor_alloc(smem_u32(&s_tmem), 512);
+    tensor_fence_before();
+    __syncthreads();
+    tensor_fence_after();
+    const uint32_t tmem = s_tmem;
+    pdl_wait();
+    pdl_trigger();
+    const int n_active = __ldcg(p.n_active);
+    const HeadWork<TILE> w(p, n_active);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t step = 0;
+            bool ok = true;
+            for (int i = blockIdx.x; ok && i < w.total; i += gridDim.x) {
+                int m0, n0, k0, k1, split;
+                w.tile(p, i, m0, n0, k0, k1, split);
+                for (int k = k0; k < k1; ++k, ++step) {
+                    const uint32_t s = step % kHgStages, ph = (step / kHgStages) & 1u;
+                    ok = wait_or_give_up(bar_empty + 8 * s, ph ^ 1u, &s_gave_up);
+                    if (!ok) break;
+                    const uint32_t a = base + s * kHgStageBytes, b = a + kHgABytes, bar = bar_full + 8 * s;
+                    mbar_expect(bar, kHgStageBytes);
+#pragma unroll
+                    for (int j = 0; j < kHgM / 64; ++j)
+                        kAMn ? tma_load(a + j * kHgBox, &p.a, m0 + 64 * j, k * kHgK, bar) : tma_load(a + j * kHgBox, &p.a, k * kHgK, m0 + 64 * j, bar);
+#pragma unroll
+                    for (int j = 0; j < kHgN / 64; ++j) {
+                        if (TILE == TILE_GW) tma_load(b + j * kHgBox, &p.b, n0 + 64 * j, k * kHgK, bar);
+                        else if (TILE == TILE_GH) tma_load(b + j * kHgBox, &p.b, n0 + 64 * j, p.v0 + k * kHgK, bar);
+                        else tma_load(b + j * kHgBox, &p.b, k * kHgK, p.v0 + n0 + 64 * j, bar);
+                    }
+                }
+            }
+            // no copy outlives the CTA: what was asked for and may not have been waited for is waited for here
+            for (uint32_t q = step > kHgStages ? step - kHgStages : 0; q < step; ++q)
+                mbar_wait_bounded(reinterpret_cast<uint64_t*>(__cvta_shared_to_generic(bar_full + 8 * (q % kHgStages))), (q / kHgStages) & 1u);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t kind = product_kind(kHgM, kHgN, kAMn, kBMn);
+            uint32_t step = 0, n = 0;
+            bool ok = true;
+            for (int i = blockIdx.x; ok && i < w.total; i += gridDim.x, ++n) {
+                int m0, n0, k0, k1, split;
+                w.tile(p, i, m0, n0, k0, k1, split);
+                const uint32_t buf = n & 1u;
+                ok = wait_or_give_up(acc_empty + 8 * buf, ((n >> 1) & 1u) ^ 1u, &s_gave_up);
+                tensor_fence_after();
+                for (int k = k0; ok && k < k1; ++k, ++step) {
+                    const uint32_t s = step % kHgStages;
+                    ok = wait_or_give_up(bar_full + 8 * s, (step / kHgStages) & 1u, &s_gave_up);
+                    if (!ok) break;
+                    tensor_fence_after();
+                    const uint32_t a = base + s * kHgStageBytes, b = a + kHgABytes;
+#pragma unroll
+                    for (int j = 0; j < kHgK / 16; ++j) {
+                        const uint64_t da = kAMn ? operand_mn(a + j * 2048, kHgBox) : operand_k(a + j * 32);
+                        const uint64_t db = kBMn ? operand_mn(b + j * 2048, kHgBox) : operand_k(b + j * 32);
+                        product(tmem + buf * kHgN, da, db, kind, k > k0 || j > 0);
+                    }
+                    product_commit(bar_empty + 8 * s);
+                }
+                if (ok) product_commit(acc_full + 8 * buf);
+            }
+            // products under way end before tensor memory is freed
+            product_commit(bar_drained);
+            mbar_wait_bounded(reinterpret_cast<uint64_t*>(__cvta_shared_to_generic(bar_drained)), 0);
+        }
+    } else {
+        const int quarter = warp & 3;
+        const uint32_t stage0 = out_stage + (warp - 2) * 2 * kHgOut;
+        uint32_t n = 0, stores = 0;
+        bool ok = true;
+        for (int i = blockIdx.x; i < w.total; i += gridDim.x, ++n) {
+            int m0, n0, k0, k1, split;
+            w.tile(p, i, m0, n0, k0, k1, split);
+            const uint32_t buf = n & 1u;
+            ok = __all_sync(0xFFFFFFFFu, wait_or_give_up(acc_full + 8 * buf, (n >> 1) & 1u, &s_gave_up));
+            if (!ok) break;
+            tensor_fence_after();
+            const uint32_t acc = tmem + buf * kHgN + ((uint32_t)quarter << 21);
+            const int row = m0 + quarter * 32 + lane;
+            const bool none = k1 <= k0;                      // no product was formed: the sum is 0
+            float za[32], zb[32];
+            tensor_load(acc, za);
+            // 32 columns at a time, the next 32 under way; behind the last load the accumulator is free for another tile
+            auto columns = [&](auto use) {
+                auto one = [&](int c, float(&v)[32], float(&next)[32]) {
+                    tensor_wait(v);
+                    if (c + 1 < kHgN / 32) {
+                        tensor_load(acc + (c + 1) * 32, next);
+                    } else {
+                        tensor_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
+                    }
+                    use(c, v);
+                };
+#pragma unroll 1
+                for (int c = 0; c < kHgN / 32; c += 2) {
+                    one(c, za, zb);
+                    one(c + 1, zb, za);
+                }
+            };
+            // bf16 out: two such parts fill a stage; a stage is written again once the store before the last one has read it
+            // (a group for every stage, a store in it or not: the waits count groups)
+            auto put = [&](int c, const float(&v)[32], int y, bool in) {
+                const uint32_t stage = stage0 + ((stores & 1u) ? kHgOut : 0);
+                if ((c & 1) == 0) {
+                    if (lane == 0) bulk_wait_read<1>();
+                    __syncwarp();
+                }
+                stage_bf16(stage, lane, c & 1, v);
+                if (c & 1) {
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (in) tma_store(&p.out, n0 + 32 * (c - 1), y, stage);
+                        bulk_commit();
+                    }
+                    ++stores;
+                }
+            };
+            if constexpr (TILE == TILE_STATS) {
+                const bool in = row < n_active;
+                const int x = in ? __ldcg(p.tok + row) - p.v0 - n0 : -1;
+                RowStats r;
+                r.clear();
+                columns([&](int c, float(&v)[32]) {
+                    const int nv = p.V - p.v0 - n0 - 32 * c;
+                    if (nv <= 0) return;
+                    const bool here = x >= 32 * c && x < 32 * c + 32;
+                    if (__any_sync(0xFFFFFFFFu, here)) {
+                        const float zx = pick(v, x - 32 * c);
+                        if (here) p.zx[row] = zx;
+                    }
+                    r.add(v, nv, p.c1);
+                });
+                if (in) p.part[(long long)row * p.tiles + n0 / kHgN] = make_float4(r.m, r.S, r.T, r.Z);
+            } else if constexpr (TILE == TILE_G) {
+                const bool in = row < n_active;
+                float4 f = make_float4(0.f, 0.f, 0.f, 0.f), f2 = f;          // HeadCoef
+                if (in) {
+                    f = __ldcg(reinterpret_cast<const float4*>(p.coef + row));
+                    f2 = __ldcg(reinterpret_cast<const float4*>(p.coef + row) + 1);
+                }
+                const float lse2 = f.x, A = f.y, B = f.z, C = f.w, E = f2.x;
+                const int x = in ? __float_as_int(f2.y) - p.v0 - n0 : -1;
+                columns([&](int c, float(&v)[32]) {
+                    const int nv = in ? p.V - p.v0 - n0 - 32 * c : 0;
+                    const bool here = x >= 32 * c && x < 32 * c + 32;
+                    float at = 0.f;
+                    const bool any = __any_sync(0xFFFFFFFFu, here);
+                    if (any) {
+                        const float zx = pick(v, x - 32 * c);
+                        // A p + B as A (p - 1) + (A + B): p - 1 without the difference of two numbers near 1
+                        const float u = fmaf(zx, p.c1, -lse2);
+                        at = fmaf(A, expm1f(u * kLn2), A + B) + fmaf(ex2(u) * E, u, C);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const float u = fmaf(v[j], p.c1, -lse2);
+                        v[j] = j < nv ? fmaf(ex2(u), fmaf(E, u, A), C) : 0.f;
+                    }
+                    if (any) put_at(v, here ? x - 32 * c : -1, at);
+                    put(c, v, m0 + quarter * 32, true);
+                });
+            } else if constexpr (TILE == TILE_GW) {
+                const int y = p.v0 + m0 + quarter * 32;
+                columns([&](int c, float(&v)[32]) {
+                    if (none) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = 0.f;
+                    }
+                    put(c, v, y, y < p.V && m0 + quarter * 32 < p.vn && n0 + 32 * (c - 1) < p.D);
+                });
+            } else {
+                float* dst = p.acc + split * p.acc_slot + (long long)row * p.Dp + n0;
+                columns([&](int c, float(&v)[32]) {
+                    if (n0 + 32 * c >= p.Dp) return;
+                    float4* d4 = reinterpret_cast<float4*>(dst + 32 * c);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        float4 s = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                        if (!p.first) {
+                            const float4 o = __ldcg(d4 + j);
+                            s = make_float4(s.x + o.x, s.y + o.y, s.z + o.z, s.w + o.w);
+                        }
+                        d4[j] = s;
+                    }
+                });
+            }
+        }
+        if (TILE == TILE_G || TILE == TILE_GW)
+            if (lane == 0) bulk_wait_all();                  // (written before the launch counts as done)
+    }
+    __syncwarp();
+    tensor_fence_before();
+    __syncthreads();
+    tensor_fence_after();
+    if (warp == 1) tensor_free(tmem, 512);
+    if (threadIdx.x == 0 && s_gave_up) atomicOr(p.status, ADASD_STATUS_TIMEOUT);
+}
+
+// ---- rows -------------------------------------------------------------------------------------------
+
+struct HeadRows {
+    HeadCall c;
+    uint16_t* h;                         // [n_pad][D8]: the rows that count, together
+    int32_t D8, tiles;
+    int32_t* index;                      // of a row that counts: its place among the call's rows
+    int32_t* tok;
+    int32_t* n_active;
+    float* zx;
+    HeadCoef* coef;
+    const float4* part;
+    const float* acc;
+    long long acc_slot;
+    int32_t Dp, splits;
+    float c1;
+    double inv_T;
+};
+
+constexpr int kHrThreads = 256, kHrRows = 32;
+
+__device__ __forceinline__ bool head_counts(const HeadCall& c, int r) {
+    const int x = c.tok[r];
+    if (x < 0 || x >= c.V) return false;
+    if (c.op == HEAD_CE) return !c.row_weight || c.row_weight[r] != 0.f;
+    if (c.op == HEAD_GIVEN) return c.g_logp[r] != 0.f || (c.g_H && c.g_H[r] != 0.f);
+    return true;
+}
+
+// A CTA looks at 32 rows of the call: counts the rows ahead of them that count, copies those of its own that do to their place, and writes the
+// outputs of those that do not.  HEAD_GIVEN: the gradient's constants too.  The last CTA writes the count and zeros up to the next multiple of
+// 64 rows (the products along the rows take 64 at a time).
+__global__ void __launch_bounds__(kHrThreads) head_rows_kernel(const __grid_constant__ HeadRows p) {
+    __shared__ int s_count[kHrThreads / 32], s_place[kHrRows], s_total;
+    const HeadCall& c = p.c;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r0 = blockIdx.x * kHrRows;
+    pdl_wait();
+    pdl_trigger();
+    int before = 0;
+    for (int r = tid; r < r0; r += kHrThreads) before += head_counts(c, r) ? 1 : 0;
+    before = __reduce_add_sync(0xFFFFFFFFu, before);
+    if (lane == 0) s_count[warp] = before;
+    __syncthreads();
+    if (warp == 0) {
+        before = lane < kHrThreads / 32 ? s_count[lane] : 0;
+        before = __reduce_add_sync(0xFFFFFFFFu, before);
+        const int r = r0 + lane;
+        const bool in = r < c.n_rows, on = in && head_counts(c, r);
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, on);
+        const int place = before + __popc(mask & ((1u << lane) - 1u));
+        s_place[lane] = on ? place : in ? -1 : -2;
+        if (lane == 0) {
+            s_total = before + __popc(mask);
+            if (blockIdx.x == gridDim.x - 1) *p.n_active = s_total;
+        }
+        if (on) {
+            p.index[place] = r;
+            p.tok[place] = c.tok[r];
+            if (c.op == HEAD_GIVEN) {
+                const float dl = c.g_logp[r], dH = c.g_H ? c.g_H[r] : 0.f, H = dH != 0.f ? c.H_in[r] : 0.f, lse = c.lse_in[r];
+                HeadCoef f;
+                f.lse2 = isfinite(lse) ? lse * kLog2e : __int_as_float(0x7FC00000);
+                f.A = (float)((-(double)dl - (double)dH * H) * p.inv_T);
+                f.B = (float)((double)dl * p.inv_T);
+                f.C = 0.f;
+                f.E = (float)(-(double)dH * 0.6931471805599453 * p.inv_T);
+                f.tok = c.tok[r];
+                f.pad[0] = f.pad[1] = 0.f;
+                p.coef[place] = f;
+                if (!isfinite(lse)) atomicOr(c.status, ADASD_STATUS_NAN);
+            }
+        } else if (in) {
+            if (c.logp) c.logp[r] = 0.f;
+            if (c.H) c.H[r] = 0.f;
+            if (c.lse) c.lse[r] = 0.f;
+            if (c.row_loss) c.row_loss[r] = 0.f;
+        }
+    }
+    __syncthreads();
+    const uint16_t* hidden = static_cast<const uint16_t*>(c.hidden);
+    uint16_t* gh = static_cast<uint16_t*>(c.grad_h);
+    const bool wide = (reinterpret_cast<uintptr_t>(hidden) & 15u) == 0 && c.h_stride % 8 == 0 && c.D % 8 == 0;
+    const bool gwide = (reinterpret_cast<uintptr_t>(gh) & 15u) == 0 && c.gh_stride % 8 == 0 && c.D % 8 == 0;
+    for (int k = warp; k < kHrRows; k += kHrThreads / 32) {
+        const int place = s_place[k];
+        const long long r = r0 + k;
+        if (place >= 0) {
+            const uint16_t* src = hidden + r * c.h_stride;
+            uint16_t* dst = p.h + (long long)place * p.D8;
+            if (wide)
+                for (int j = lane; j < c.D / 8; j += 32) reinterpret_cast<uint4*>(dst)[j] = __ldcg(reinterpret_cast<const uint4*>(src) + j);
+            else
+                for (int j = lane; j < c.D; j += 32) dst[j] = src[j];
+        } else if (place == -1 && gh) {
+            uint16_t* dst = gh + r * c.gh_stride;
+            if (gwide)
+                for (int j = lane; j < c.D / 8; j += 32) reinterpret_cast<uint4*>(dst)[j] = make_uint4(0u, 0u, 0u, 0u);
+            else
+                for (int j = lane; j < c.D; j += 32) dst[j] = 0;
+        }
+    }
+    if (blockIdx.x == gridDim.x - 1) {
+        const int n = s_total, end = (n + 63) & ~63;
+        uint4* dst = reinterpret_cast<uint4*>(p.h + (long long)n * p.D8);
+        for (long long j = tid; j < (long long)(end - n) * (p.D8 / 8); j += kHrThreads) dst[j] = make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+// A warp a row: the tiles' statistics joined, the row's outputs, its gradient's constants.
+__global__ void __launch_bounds__(kHrThreads) head_stats_kernel(const __grid_constant__ HeadRows p) {
+    const HeadCall& c = p.c;
+    const int lane = threadIdx.x & 31, row = (int)((blockIdx.x * kHrThreads + threadIdx.x) >> 5);
+    pdl_wait();
+    pdl_trigger();
+    if (row >= __ldcg(p.n_active)) return;
+    const float4* part = p.part + (long long)row * p.tiles;
+    float m = kFloor, S = 0.f, T = 0.f;
+    double Z = 0.0;
+    bool bad = false;
+    for (int k = lane; k < p.tiles; k += 32) {
+        const float4 q = __ldcg(part + k);
+        bad |= !(q.y > 0.f && q.y < INFINITY) || !(fabsf(q.x) < -kFloor);
+        const float m1 = fmaxf(m, q.x), f0 = ex2(m - m1), f1 = ex2(q.x - m1);
+        T = f0 * (T + S * (m - m1)) + f1 * (q.z + q.y * (q.x - m1));
+        S = f0 * S + f1 * q.y;
+        Z += (double)q.w;
+        m = m1;
+    }
+    const float top = warp_max(m), f0 = ex2(m - top);
+    T = f0 * (T + S * (m - top));
+    S = f0 * S;
+    S = warp_sum(S);
+    T = warp_sum(T);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) Z += __shfl_xor_sync(0xFFFFFFFFu, Z, o);
+    bad = __any_sync(0xFFFFFFFFu, bad);
+    if (lane != 0) return;
+    const int r = __ldcg(p.index + row);
+    const double ln2 = 0.6931471805599453, lnS = log((double)S);
+    const float nan = __int_as_float(0x7FC00000);
+    double l = ln2 * (double)fmaf(__ldcg(p.zx + row), p.c1, -top) - lnS, lse = ln2 * (double)top + lnS, H = lnS - ln2 * ((double)T / (double)S);
+    if (bad) {
+        l = lse = H = (double)nan;
+        atomicOr(c.status, ADASD_STATUS_NAN);
+    }
+    if (c.logp) c.logp[r] = (float)l;
+    if (c.H) c.H[r] = (float)(H < 0.0 ? 0.0 : H);
+    if (c.lse) c.lse[r] = (float)lse;
+    if (c.op == HEAD_CE) {
+        const double w = (c.row_weight ? (double)c.row_weight[r] : 1.0) * (double)c.scale, e = (double)c.smoothing, zc = (double)c.z_loss;
+        double L = -(1.0 - e) * l + zc * lse * lse;
+        if (e != 0.0) L -= e * (Z * p.inv_T / c.V - lse);
+        c.row_loss[r] = (float)(w * L);
+        if (p.coef) {
+            HeadCoef f;
+            f.lse2 = (float)((double)top + log2((double)S));
+            f.A = (float)(w * (1.0 + 2.0 * zc * lse) * p.inv_T);
+            f.B = (float)(-w * (1.0 - e) * p.inv_T);
+            f.C = (float)(-w * e / c.V * p.inv_T);
+            f.E = 0.f;
+            f.tok = __ldcg(p.tok + row);
+            f.pad[0] = f.pad[1] = 0.f;
+            p.coef[row] = f;
+        }
+    }
+}
+
+// A warp a row and 256 columns: the splits' sums, rounded to bf16, to the row's place.
+__global__ void __launch_bounds__(kHrThreads) head_grad_rows_kernel(const __grid_constant__ HeadRows p) {
+    const HeadCall& c = p.c;
+    const int lane = threadIdx.x & 31;
+    const long long item = ((long long)blockIdx.x * kHrThreads + threadIdx.x) >> 5;
+    const int per = (c.D + 255) / 256, row = (int)(item / per), d0 = (int)(item % per) * 256 + lane * 8;
+    pdl_wait();
+    pdl_trigger();
+    if (row >= __ldcg(p.n_active) || d0 >= c.D) return;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < p.splits; ++k) {
+        const float4* a = reinterpret_cast<const float4*>(p.acc + k * p.acc_slot + (long long)row * p.Dp + d0);
+        const float4 u = __ldcg(a), v = __ldcg(a + 1);
+        s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
+        s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
+    }
+    uint16_t* dst = static_cast<uint16_t*>(c.grad_h) + (long long)__ldcg(p.index + row) * c.gh_stride + d0;
+    const uint4 w = make_uint4(pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3]), pack_bf16(s[4], s[5]), pack_bf16(s[6], s[7]));
+    if ((reinterpret_cast<uintptr_t>(dst) & 15u) == 0) {     // (D is a multiple of 8)
+        *reinterpret_cast<uint4*>(dst) = w;
+    } else {
+        const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dst[j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
+    }
+}
+
+}  // namespace adasd
