@@ -11,9 +11,9 @@ namespace {
 
 // What a call keeps in its scratch.  (Statistics of the tiles and a piece of the gradient are never needed at once: they share their place.)
 struct Layout {
-    int n_pad, D8, Dp, tiles;
-    int piece, splits;                               // columns of a piece; parts that the products along them are cut into
-    size_t h, index, tok, n_active, zx, coef, big, acc, total;
+    int n_pad, D8, Dp, tiles, halves;                // 256 and 128 columns of the vocabulary
+    int piece, splits, planes;                       // columns of a piece; parts that the products along them are cut into; planes of G
+    size_t h, index, tok, n_active, zx, coef, res, big, acc, total;
 };
 
 constexpr size_t kPieceBytes = (size_t)256 << 20;
@@ -24,6 +24,7 @@ Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
     L.D8 = (D + 7) / 8 * 8;
     L.Dp = (D + 63) / 64 * 64;
     L.tiles = (V + kHgN - 1) / kHgN;
+    L.halves = (V + kHgHalf - 1) / kHgHalf;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -36,7 +37,9 @@ Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
     L.zx = take((size_t)L.n_pad * 4);
     L.coef = take(gradient ? (size_t)L.n_pad * sizeof(HeadCoef) : 0);
     L.h = take((size_t)L.n_pad * L.D8 * 2);
-    const size_t part = (size_t)L.n_pad * L.tiles * sizeof(float4);
+    const size_t part = (size_t)L.n_pad * L.halves * sizeof(float4);
+    L.planes = n_rows <= kHgPlaneRows ? 2 : 1;
+    L.res = take(gradient && L.planes == 1 ? (size_t)L.n_pad * L.halves * sizeof(float) : 0);
     L.piece = L.splits = 0;
     size_t g = 0, acc = 0;
     if (gradient) {
@@ -106,7 +109,9 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     r.c = c;
     r.h = reinterpret_cast<uint16_t*>(s + L.h);
     r.D8 = L.D8;
-    r.tiles = L.tiles;
+    r.halves = L.halves;
+    r.planes = L.planes;
+    r.res = c.grad_h && L.planes == 1 ? reinterpret_cast<float*>(s + L.res) : nullptr;
     r.index = reinterpret_cast<int32_t*>(s + L.index);
     r.tok = reinterpret_cast<int32_t*>(s + L.tok);
     r.n_active = reinterpret_cast<int32_t*>(s + L.n_active);
@@ -134,7 +139,9 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     t.n_active = r.n_active;
     t.c1 = r.c1;
     t.part = reinterpret_cast<float4*>(s + L.big);
-    t.tiles = L.tiles;
+    t.halves = r.halves;
+    t.planes = L.planes;
+    t.res = const_cast<float*>(r.res);
     t.zx = r.zx;
     t.tok = r.tok;
     t.coef = r.coef;
@@ -175,8 +182,7 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
         }
     }
     if (!c.grad_h) return ADASD_OK;
-    const long long warps = (long long)c.n_rows * ((c.D + 255) / 256);
-    return launch_pdl(head_grad_rows_kernel, (int)((warps + kHrThreads / 32 - 1) / (kHrThreads / 32)), kHrThreads, 0, 0, stream, r);
+    return launch_pdl(head_grad_rows_kernel, c.n_rows, kHrThreads, 0, 0, stream, r);
 }
 
 }  // namespace adasd

@@ -7,8 +7,15 @@
 //             grad_w of the piece = G^T h;  grad_h += G w, in fp32
 //
 // All four are products on the tensor cores: 2 n V D operations each.  Logits are worked out twice so that what is kept is a piece of G (at
-// most 256 MB, or 2048 columns) instead of n V values.  G is rounded to bf16, as the products' operands are; gradients are rounded to
-// bf16 once more when they are written.
+// most 256 MB, or 2048 columns) instead of n V values.
+//
+// Precision.  The accumulator in tensor memory is cut, not rounded, to 24 bits with every 16 products: after 4096 of them logits were 9e-6 of their size
+// too small.  Logits are therefore summed from parts of 256 products, the parts added in fp32 by the threads of the epilogue (below 1e-6).
+// G is rounded to bf16, as the products' operands are (2^-8 at most; both gradients are rounded to bf16 once more when they are written).  In grad_h = sum_v g_v w_v
+// the rounding errors e_v do not cancel as the g_v do, which add up to 0 in a row, and what the w_v have in common (a mean, the tokens' frequencies) is
+// multiplied with their sum; so the row's sum of e_v times w_x is taken off again (what is left are errors times differences of w_v): 0.009 -> 0.002 of
+// the gradient for weights with a strong common direction.  With up to 64 rows, where the products are bound by memory, G is held in two bf16
+// planes instead, as twice the rows.
 //
 // Rows left out are not worked on: the rows that count are copied together first (head_rows_kernel), how many there are is known on the
 // device alone.
@@ -23,9 +30,12 @@ constexpr int kHgM = 128, kHgN = 256, kHgK = 64;             // tile of a CTA; a
 constexpr int kHgStages = 4;
 constexpr int kHgABytes = kHgM * kHgK * 2, kHgBBytes = kHgN * kHgK * 2, kHgStageBytes = kHgABytes + kHgBBytes;
 constexpr int kHgBox = 64 * 64 * 2;
+constexpr int kHgHalf = kHgN / 2;
 constexpr int kHgOut = 32 * 64 * 2;                          // 32 rows of 64 bf16: what a warp stores at a time
-constexpr int kHgThreads = 192;                              // copies, products, four warps of epilogue
-constexpr int kHgSmem = 1024 + kHgStages * kHgStageBytes + 4 * 2 * kHgOut + 256;
+constexpr int kHgEpi = 8, kHgThreads = 64 + 32 * kHgEpi;     // warps: copies, products, epilogue (32 rows and 128 columns each)
+constexpr int kHgPart = 4;                                   // steps along K of a part of the logits' sums
+constexpr int kHgSmem = 1024 + kHgStages * kHgStageBytes + kHgEpi * kHgOut + 256;
+constexpr int kHgPlaneRows = 64;                             // rows of a plane of G, where there are two
 
 enum HeadTile : int { TILE_STATS, TILE_G, TILE_GW, TILE_GH };
 
@@ -42,8 +52,9 @@ struct HeadTiles {
     int32_t D, V, v0, vn;                // piece of the vocabulary: columns v0 .. v0 + vn - 1
     const int32_t* n_active;
     float c1;                            // log2 e / T
-    float4* part;                        // TILE_STATS: [row][tiles]
-    int32_t tiles;
+    float4* part;                        // TILE_STATS: [row][halves], parts of 128 columns of the vocabulary
+    float* res;                          // TILE_G: [row][halves] sums of what rounding took from G; nullable
+    int32_t halves, planes;              // planes of G (1 or 2)
     float* zx;
     const int32_t* tok;
     const HeadCoef* coef;                // TILE_G
@@ -65,10 +76,10 @@ struct HeadWork {
         } else if (TILE == TILE_GW) {
             mt = (p.vn + kHgM - 1) / kHgM;
             nt = (p.D + kHgN - 1) / kHgN;
-            ksteps = (n_active + kHgK - 1) / kHgK;
+            ksteps = (n_active + kHgK - 1) / kHgK * p.planes;       // (two planes: of one step each)
             total = mt * nt;
         } else {
-            mt = (n_active + kHgM - 1) / kHgM;
+            mt = (n_active + kHgM - 1) / kHgM;                      // (two planes: one tile)
             nt = (p.D + kHgN - 1) / kHgN;
             ksteps = ((p.vn + kHgK - 1) / kHgK + p.splits - 1) / p.splits;
             total = mt * nt * p.splits;
@@ -165,12 +176,13 @@ template <int TILE>
 __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_constant__ HeadTiles p) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t out_stage = base + kHgStages * kHgStageBytes, bars = out_stage + 4 * 2 * kHgOut;
+    const uint32_t out_stage = base + kHgStages * kHgStageBytes, bars = out_stage + kHgEpi * kHgOut;
     // barriers: full[stage], empty[stage], accumulator full[2], empty[2], drained
     const uint32_t bar_full = bars, bar_empty = bars + 8 * kHgStages, acc_full = bars + 16 * kHgStages, acc_empty = acc_full + 16, bar_drained = acc_empty + 16;
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_gave_up;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr bool kParts = TILE == TILE_STATS || TILE == TILE_G;
     constexpr bool kAMn = TILE == TILE_GW, kBMn = TILE == TILE_GW || TILE == TILE_GH;
 
     if (threadIdx.x == 0) {
@@ -181,7 +193,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
         }
         for (int i = 0; i < 2; ++i) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(acc_full + 8 * i) : "memory");
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], 4;" ::"r"(acc_empty + 8 * i) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(acc_empty + 8 * i), "r"(kHgEpi) : "memory");
         }
         asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_drained) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -214,7 +226,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                         kAMn ? tma_load(a + j * kHgBox, &p.a, m0 + 64 * j, k * kHgK, bar) : tma_load(a + j * kHgBox, &p.a, k * kHgK, m0 + 64 * j, bar);
 #pragma unroll
                     for (int j = 0; j < kHgN / 64; ++j) {
-                        if (TILE == TILE_GW) tma_load(b + j * kHgBox, &p.b, n0 + 64 * j, k * kHgK, bar);
+                        if (TILE == TILE_GW) tma_load(b + j * kHgBox, &p.b, n0 + 64 * j, p.planes == 2 ? 0 : k * kHgK, bar);
                         else if (TILE == TILE_GH) tma_load(b + j * kHgBox, &p.b, n0 + 64 * j, p.v0 + k * kHgK, bar);
                         else tma_load(b + j * kHgBox, &p.b, k * kHgK, p.v0 + n0 + 64 * j, bar);
                     }
@@ -229,155 +241,187 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
             constexpr uint32_t kind = product_kind(kHgM, kHgN, kAMn, kBMn);
             uint32_t step = 0, n = 0;
             bool ok = true;
-            for (int i = blockIdx.x; ok && i < w.total; i += gridDim.x, ++n) {
+            for (int i = blockIdx.x; ok && i < w.total; i += gridDim.x) {
                 int m0, n0, k0, k1, split;
                 w.tile(p, i, m0, n0, k0, k1, split);
-                const uint32_t buf = n & 1u;
-                ok = wait_or_give_up(acc_empty + 8 * buf, ((n >> 1) & 1u) ^ 1u, &s_gave_up);
-                tensor_fence_after();
-                for (int k = k0; ok && k < k1; ++k, ++step) {
-                    const uint32_t s = step % kHgStages;
-                    ok = wait_or_give_up(bar_full + 8 * s, (step / kHgStages) & 1u, &s_gave_up);
-                    if (!ok) break;
+                int k = k0;
+                do {                                         // (a part, or the whole of the tile's sum)
+                    const int end = kParts ? min(k + kHgPart, k1) : k1;
+                    const uint32_t buf = n & 1u;
+                    ok = wait_or_give_up(acc_empty + 8 * buf, ((n >> 1) & 1u) ^ 1u, &s_gave_up);
                     tensor_fence_after();
-                    const uint32_t a = base + s * kHgStageBytes, b = a + kHgABytes;
+                    for (bool add = false; ok && k < end; ++k, ++step) {
+                        const uint32_t s = step % kHgStages;
+                        ok = wait_or_give_up(bar_full + 8 * s, (step / kHgStages) & 1u, &s_gave_up);
+                        if (!ok) break;
+                        tensor_fence_after();
+                        const uint32_t a = base + s * kHgStageBytes, b = a + kHgABytes;
 #pragma unroll
-                    for (int j = 0; j < kHgK / 16; ++j) {
-                        const uint64_t da = kAMn ? operand_mn(a + j * 2048, kHgBox) : operand_k(a + j * 32);
-                        const uint64_t db = kBMn ? operand_mn(b + j * 2048, kHgBox) : operand_k(b + j * 32);
-                        product(tmem + buf * kHgN, da, db, kind, k > k0 || j > 0);
+                        for (int j = 0; j < kHgK / 16; ++j) {
+                            const uint64_t da = kAMn ? operand_mn(a + j * 2048, kHgBox) : operand_k(a + j * 32);
+                            const uint64_t db = kBMn ? operand_mn(b + j * 2048, kHgBox) : operand_k(b + j * 32);
+                            product(tmem + buf * kHgN, da, db, kind, add);
+                            add = true;
+                        }
+                        product_commit(bar_empty + 8 * s);
                     }
-                    product_commit(bar_empty + 8 * s);
-                }
-                if (ok) product_commit(acc_full + 8 * buf);
+                    if (ok) product_commit(acc_full + 8 * buf);
+                    ++n;
+                } while (ok && k < k1);
             }
             // products under way end before tensor memory is freed
             product_commit(bar_drained);
             mbar_wait_bounded(reinterpret_cast<uint64_t*>(__cvta_shared_to_generic(bar_drained)), 0);
         }
     } else {
-        const int quarter = warp & 3;
-        const uint32_t stage0 = out_stage + (warp - 2) * 2 * kHgOut;
-        uint32_t n = 0, stores = 0;
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t stage = out_stage + (warp - 2) * kHgOut;
+        uint32_t n = 0;
         bool ok = true;
-        for (int i = blockIdx.x; i < w.total; i += gridDim.x, ++n) {
+        for (int i = blockIdx.x; ok && i < w.total; i += gridDim.x) {
             int m0, n0, k0, k1, split;
             w.tile(p, i, m0, n0, k0, k1, split);
-            const uint32_t buf = n & 1u;
-            ok = __all_sync(0xFFFFFFFFu, wait_or_give_up(acc_full + 8 * buf, (n >> 1) & 1u, &s_gave_up));
-            if (!ok) break;
-            tensor_fence_after();
-            const uint32_t acc = tmem + buf * kHgN + ((uint32_t)quarter << 21);
-            const int row = m0 + quarter * 32 + lane;
-            const bool none = k1 <= k0;                      // no product was formed: the sum is 0
-            float za[32], zb[32];
-            tensor_load(acc, za);
-            // 32 columns at a time, the next 32 under way; behind the last load the accumulator is free for another tile
-            auto columns = [&](auto use) {
-                auto one = [&](int c, float(&v)[32], float(&next)[32]) {
-                    tensor_wait(v);
-                    if (c + 1 < kHgN / 32) {
-                        tensor_load(acc + (c + 1) * 32, next);
-                    } else {
-                        tensor_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
-                    }
-                    use(c, v);
-                };
-#pragma unroll 1
-                for (int c = 0; c < kHgN / 32; c += 2) {
-                    one(c, za, zb);
-                    one(c + 1, zb, za);
+            const int row = m0 + quarter * 32 + lane, c0 = n0 + half * kHgHalf;     // the thread's row and first column
+            auto next = [&]() -> uint32_t {                  // the accumulator's next sum, in this warp's rows and columns
+                const uint32_t buf = n & 1u;
+                ok = __all_sync(0xFFFFFFFFu, wait_or_give_up(acc_full + 8 * buf, (n >> 1) & 1u, &s_gave_up));
+                tensor_fence_after();
+                return tmem + buf * kHgN + half * kHgHalf + ((uint32_t)quarter << 21);
+            };
+            auto release = [&]() {
+                tensor_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(acc_empty + 8 * (n & 1u));
+                ++n;
+            };
+            // 64 columns as bf16: into the warp's stage once the store before has read it, and from there to row y on
+            auto store64 = [&](const float(&a)[32], const float(&b)[32], int x, int y, bool in) {
+                if (lane == 0) bulk_wait_read<0>();
+                __syncwarp();
+                stage_bf16(stage, lane, 0, a);
+                stage_bf16(stage, lane, 1, b);
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0 && in) {
+                    tma_store(&p.out, x, y, stage);
+                    bulk_commit();
                 }
             };
-            // bf16 out: two such parts fill a stage; a stage is written again once the store before the last one has read it
-            // (a group for every stage, a store in it or not: the waits count groups)
-            auto put = [&](int c, const float(&v)[32], int y, bool in) {
-                const uint32_t stage = stage0 + ((stores & 1u) ? kHgOut : 0);
-                if ((c & 1) == 0) {
-                    if (lane == 0) bulk_wait_read<1>();
-                    __syncwarp();
-                }
-                stage_bf16(stage, lane, c & 1, v);
-                if (c & 1) {
-                    fence_async_shared();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (in) tma_store(&p.out, n0 + 32 * (c - 1), y, stage);
-                        bulk_commit();
-                    }
-                    ++stores;
-                }
-            };
-            if constexpr (TILE == TILE_STATS) {
-                const bool in = row < n_active;
-                const int x = in ? __ldcg(p.tok + row) - p.v0 - n0 : -1;
-                RowStats r;
-                r.clear();
-                columns([&](int c, float(&v)[32]) {
-                    const int nv = p.V - p.v0 - n0 - 32 * c;
-                    if (nv <= 0) return;
-                    const bool here = x >= 32 * c && x < 32 * c + 32;
-                    if (__any_sync(0xFFFFFFFFu, here)) {
-                        const float zx = pick(v, x - 32 * c);
-                        if (here) p.zx[row] = zx;
-                    }
-                    r.add(v, nv, p.c1);
-                });
-                if (in) p.part[(long long)row * p.tiles + n0 / kHgN] = make_float4(r.m, r.S, r.T, r.Z);
-            } else if constexpr (TILE == TILE_G) {
-                const bool in = row < n_active;
-                float4 f = make_float4(0.f, 0.f, 0.f, 0.f), f2 = f;          // HeadCoef
-                if (in) {
-                    f = __ldcg(reinterpret_cast<const float4*>(p.coef + row));
-                    f2 = __ldcg(reinterpret_cast<const float4*>(p.coef + row) + 1);
-                }
-                const float lse2 = f.x, A = f.y, B = f.z, C = f.w, E = f2.x;
-                const int x = in ? __float_as_int(f2.y) - p.v0 - n0 : -1;
-                columns([&](int c, float(&v)[32]) {
-                    const int nv = in ? p.V - p.v0 - n0 - 32 * c : 0;
-                    const bool here = x >= 32 * c && x < 32 * c + 32;
-                    float at = 0.f;
-                    const bool any = __any_sync(0xFFFFFFFFu, here);
-                    if (any) {
-                        const float zx = pick(v, x - 32 * c);
-                        // A p + B as A (p - 1) + (A + B): p - 1 without the difference of two numbers near 1
-                        const float u = fmaf(zx, p.c1, -lse2);
-                        at = fmaf(A, expm1f(u * kLn2), A + B) + fmaf(ex2(u) * E, u, C);
-                    }
+            if constexpr (kParts) {
+                float z[4][32];                              // the logits of 128 columns
+                {
+                    const uint32_t acc = next();
+                    if (!ok) break;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const float u = fmaf(v[j], p.c1, -lse2);
-                        v[j] = j < nv ? fmaf(ex2(u), fmaf(E, u, A), C) : 0.f;
+                    for (int g = 0; g < 4; ++g) tensor_load(acc + 32 * g, z[g]);
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) tensor_wait(z[g]);
+                    release();
+                }
+                for (int k = k0 + kHgPart; k < k1; k += kHgPart) {
+                    const uint32_t acc = next();
+                    if (!ok) break;
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) tensor_load_add16(acc + 16 * g, &z[g >> 1][16 * (g & 1)]);
+                    release();
+                }
+                if (!ok) break;
+                const bool in = row < n_active;
+                if constexpr (TILE == TILE_STATS) {
+                    const int x = in ? __ldcg(p.tok + row) - p.v0 - c0 : -1;
+                    RowStats r;
+                    r.clear();
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int nv = p.V - p.v0 - c0 - 32 * g;
+                        if (nv > 0) {
+                            const bool here = x >= 32 * g && x < 32 * g + 32;
+                            if (__any_sync(0xFFFFFFFFu, here)) {
+                                const float zx = pick(z[g], x - 32 * g);
+                                if (here) p.zx[row] = zx;
+                            }
+                            r.add(z[g], nv, p.c1);
+                        }
                     }
-                    if (any) put_at(v, here ? x - 32 * c : -1, at);
-                    put(c, v, m0 + quarter * 32, true);
-                });
-            } else if constexpr (TILE == TILE_GW) {
-                const int y = p.v0 + m0 + quarter * 32;
-                columns([&](int c, float(&v)[32]) {
+                    if (in && c0 < p.vn) p.part[(long long)row * p.halves + c0 / kHgHalf] = make_float4(r.m, r.S, r.T, r.Z);
+                } else {
+                    float4 f = make_float4(0.f, 0.f, 0.f, 0.f), f2 = f;      // HeadCoef
+                    if (in) {
+                        f = __ldcg(reinterpret_cast<const float4*>(p.coef + row));
+                        f2 = __ldcg(reinterpret_cast<const float4*>(p.coef + row) + 1);
+                    }
+                    const float lse2 = f.x, A = f.y, B = f.z, C = f.w, E = f2.x;
+                    const int x = in ? __float_as_int(f2.y) - p.v0 - c0 : -1;
+                    const bool rows_kept = p.planes == 1 || m0 + quarter * 32 < kHgPlaneRows;
+                    float lost = 0.f;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        float(&v)[32] = z[g];
+                        const int nv = in ? p.V - p.v0 - c0 - 32 * g : 0;
+                        const bool here = x >= 32 * g && x < 32 * g + 32;
+                        float at = 0.f;
+                        const bool any = __any_sync(0xFFFFFFFFu, here);
+                        if (any) {
+                            // A p + B as A (p - 1) + (A + B): p - 1 without the difference of two numbers near 1
+                            const float u = fmaf(pick(v, x - 32 * g), p.c1, -lse2);
+                            at = fmaf(A, expm1f(u * kLn2), A + B) + fmaf(ex2(u) * E, u, C);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float u = fmaf(v[j], p.c1, -lse2);
+                            v[j] = j < nv ? fmaf(ex2(u), fmaf(E, u, A), C) : 0.f;
+                        }
+                        if (any) put_at(v, here ? x - 32 * g : -1, at);
+                        if (g & 1) {
+                            const int y = m0 + quarter * 32;
+                            store64(z[g - 1], v, c0 + 32 * (g - 1), y, rows_kept);
+                            if (p.planes == 2 || p.res) {
+#pragma unroll
+                                for (int q = g - 1; q <= g; ++q)
+#pragma unroll
+                                    for (int j = 0; j < 32; ++j) {
+                                        z[q][j] -= __uint_as_float(pack_bf16(0.f, z[q][j]) & 0xFFFF0000u);
+                                        lost += z[q][j];
+                                    }
+                            }
+                            if (p.planes == 2) store64(z[g - 1], v, c0 + 32 * (g - 1), y + kHgPlaneRows, rows_kept);
+                        }
+                    }
+                    if (in && p.res && c0 < p.vn) p.res[(long long)row * p.halves + (p.v0 + c0) / kHgHalf] = lost;
+                }
+            } else {
+                const uint32_t acc = next();
+                if (!ok) break;
+                const bool none = k1 <= k0;                  // no product was formed: the sum is 0
+                float va[32], vb[32];
+#pragma unroll 1
+                for (int g = 0; g < 4; g += 2) {
+                    tensor_load(acc + 32 * g, va);
+                    tensor_load(acc + 32 * g + 32, vb);
+                    tensor_wait(va);
+                    tensor_wait(vb);
+                    if (g == 2) release();
                     if (none) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = 0.f;
+                        for (int j = 0; j < 32; ++j) va[j] = vb[j] = 0.f;
                     }
-                    put(c, v, y, y < p.V && m0 + quarter * 32 < p.vn && n0 + 32 * (c - 1) < p.D);
-                });
-            } else {
-                float* dst = p.acc + split * p.acc_slot + (long long)row * p.Dp + n0;
-                columns([&](int c, float(&v)[32]) {
-                    if (n0 + 32 * c >= p.Dp) return;
-                    float4* d4 = reinterpret_cast<float4*>(dst + 32 * c);
+                    if constexpr (TILE == TILE_GW) {
+                        const int y = p.v0 + m0 + quarter * 32;
+                        store64(va, vb, c0 + 32 * g, y, y < p.V && m0 + quarter * 32 < p.vn && c0 + 32 * g < p.D);
+                    } else if (c0 + 32 * g < p.Dp) {         // (Dp: a multiple of 64)
+                        float4* d4 = reinterpret_cast<float4*>(p.acc + split * p.acc_slot + (long long)row * p.Dp + c0 + 32 * g);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float4 s = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-                        if (!p.first) {
-                            const float4 o = __ldcg(d4 + j);
-                            s = make_float4(s.x + o.x, s.y + o.y, s.z + o.z, s.w + o.w);
+                        for (int j = 0; j < 16; ++j) {
+                            float4 s = j < 8 ? make_float4(va[4 * (j & 7)], va[4 * (j & 7) + 1], va[4 * (j & 7) + 2], va[4 * (j & 7) + 3])
+                                             : make_float4(vb[4 * (j & 7)], vb[4 * (j & 7) + 1], vb[4 * (j & 7) + 2], vb[4 * (j & 7) + 3]);
+                            if (!p.first) {
+                                const float4 o = __ldcg(d4 + j);
+                                s = make_float4(s.x + o.x, s.y + o.y, s.z + o.z, s.w + o.w);
+                            }
+                            d4[j] = s;
                         }
-                        d4[j] = s;
                     }
-                });
+                }
             }
         }
         if (TILE == TILE_G || TILE == TILE_GW)
@@ -396,7 +440,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
 struct HeadRows {
     HeadCall c;
     uint16_t* h;                         // [n_pad][D8]: the rows that count, together
-    int32_t D8, tiles;
+    int32_t D8, halves;
     int32_t* index;                      // of a row that counts: its place among the call's rows
     int32_t* tok;
     int32_t* n_active;
@@ -404,8 +448,9 @@ struct HeadRows {
     HeadCoef* coef;
     const float4* part;
     const float* acc;
+    const float* res;                    // nullable
     long long acc_slot;
-    int32_t Dp, splits;
+    int32_t Dp, splits, planes;
     float c1;
     double inv_T;
 };
@@ -506,11 +551,11 @@ __global__ void __launch_bounds__(kHrThreads) head_stats_kernel(const __grid_con
     pdl_wait();
     pdl_trigger();
     if (row >= __ldcg(p.n_active)) return;
-    const float4* part = p.part + (long long)row * p.tiles;
+    const float4* part = p.part + (long long)row * p.halves;
     float m = kFloor, S = 0.f, T = 0.f;
     double Z = 0.0;
     bool bad = false;
-    for (int k = lane; k < p.tiles; k += 32) {
+    for (int k = lane; k < p.halves; k += 32) {
         const float4 q = __ldcg(part + k);
         bad |= !(q.y > 0.f && q.y < INFINITY) || !(fabsf(q.x) < -kFloor);
         const float m1 = fmaxf(m, q.x), f0 = ex2(m - m1), f1 = ex2(q.x - m1);
@@ -558,30 +603,49 @@ __global__ void __launch_bounds__(kHrThreads) head_stats_kernel(const __grid_con
     }
 }
 
-// A warp a row and 256 columns: the splits' sums, rounded to bf16, to the row's place.
+// A CTA a row: the splits' sums (and those of both planes), what rounding took from the row's G times w_x, rounded to bf16, to the row's place.
 __global__ void __launch_bounds__(kHrThreads) head_grad_rows_kernel(const __grid_constant__ HeadRows p) {
+    __shared__ float s_lost[kHrThreads / 32];
     const HeadCall& c = p.c;
-    const int lane = threadIdx.x & 31;
-    const long long item = ((long long)blockIdx.x * kHrThreads + threadIdx.x) >> 5;
-    const int per = (c.D + 255) / 256, row = (int)(item / per), d0 = (int)(item % per) * 256 + lane * 8;
+    const int row = blockIdx.x;
     pdl_wait();
     pdl_trigger();
-    if (row >= __ldcg(p.n_active) || d0 >= c.D) return;
-    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < p.splits; ++k) {
-        const float4* a = reinterpret_cast<const float4*>(p.acc + k * p.acc_slot + (long long)row * p.Dp + d0);
-        const float4 u = __ldcg(a), v = __ldcg(a + 1);
-        s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
-        s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
-    }
-    uint16_t* dst = static_cast<uint16_t*>(c.grad_h) + (long long)__ldcg(p.index + row) * c.gh_stride + d0;
-    const uint4 w = make_uint4(pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3]), pack_bf16(s[4], s[5]), pack_bf16(s[6], s[7]));
-    if ((reinterpret_cast<uintptr_t>(dst) & 15u) == 0) {     // (D is a multiple of 8)
-        *reinterpret_cast<uint4*>(dst) = w;
-    } else {
-        const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+    if (row >= __ldcg(p.n_active)) return;
+    float lost = 0.f;
+    if (p.res) {
+        for (int k = threadIdx.x; k < p.halves; k += kHrThreads) lost += __ldcg(p.res + (long long)row * p.halves + k);
+        lost = warp_sum(lost);
+        if ((threadIdx.x & 31) == 0) s_lost[threadIdx.x >> 5] = lost;
+        __syncthreads();
+        lost = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dst[j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
+        for (int k = 0; k < kHrThreads / 32; ++k) lost += s_lost[k];
+    }
+    const uint16_t* wx = static_cast<const uint16_t*>(c.weight) + (long long)__ldcg(p.tok + row) * c.w_stride;
+    uint16_t* dst = static_cast<uint16_t*>(c.grad_h) + (long long)__ldcg(p.index + row) * c.gh_stride;
+    for (int d = threadIdx.x * 8; d < c.D; d += kHrThreads * 8) {            // (D is a multiple of 8)
+        float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < p.splits; ++k)
+            for (int q = 0; q < p.planes; ++q) {
+                const float4* a = reinterpret_cast<const float4*>(p.acc + k * p.acc_slot + (long long)(row + q * kHgPlaneRows) * p.Dp + d);
+                const float4 u = __ldcg(a), v = __ldcg(a + 1);
+                s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
+                s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
+            }
+        if (p.res) {
+            float x[8];
+            unpack16(__ldcg(reinterpret_cast<const uint4*>(wx + d)), x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] = fmaf(lost, x[j], s[j]);
+        }
+        const uint4 w = make_uint4(pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3]), pack_bf16(s[4], s[5]), pack_bf16(s[6], s[7]));
+        if ((reinterpret_cast<uintptr_t>(dst + d) & 15u) == 0) {
+            *reinterpret_cast<uint4*>(dst + d) = w;
+        } else {
+            const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) dst[d + j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
+        }
     }
 }
 

@@ -6,6 +6,7 @@ t = z log2 e / T: constant and product, 2 U |t|.  A row's S: 32 additions in a t
 Es = (32 + 8 + V / 8192 + 5 + 4 + 8) U, the 8 for the exponent's rounding t 2^t <= 0.54 and the rescaling.  l = z_x / T - lse: twice Ez / T, Es, 2 U (|z_x / T| + |lse|),
 U |l|.  H = lse - sum p t: Es for either sum of their sizes.
 G: p comes with the error of its exponent (2 Ez / T + 2 U (|t| + |lse|) + Es): of that size relative to p's terms; then half a step of bf16, 2^-8.
+grad_h: the errors e_v of G's roundings enter as sum e_v (w_v - w_x), of size |e_v| (|w_v| + |w_x|) at most (with up to 64 rows, held in two planes, they do not enter).
 A product with G adds its V (or n) terms in fp32: (K / 16 + 2) 2 U of the sum of sizes, a rounding U for each of at most 32 parts and of the pieces, half a step of bf16 at the end.
 """
 import torch
@@ -74,6 +75,8 @@ class Head:
                                          (grad_w, G.t() @ self.h, dG.t() @ self.h.abs(), G.abs().t() @ self.h.abs(), self.n)):
             if got is None:
                 continue
+            if got is grad_h:
+                tol = tol + H16 * G.abs().sum(-1, keepdim=True) * self.w[self.x].abs()
             tol = tol + ((K / 16 + 2) * 2 + parts) * U * (terms + tol)
             tol = tol + H16 * (want.abs() + tol)
             d = (got.double() - want).abs()
