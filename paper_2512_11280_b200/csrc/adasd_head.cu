@@ -16,11 +16,15 @@ struct Layout {
     size_t h, index, tok, n_active, zx, coef, res, big, acc, total;
 };
 
+// Tiles of pairs where the rows fill more than one CTA's.
+inline bool in_pairs(int n_rows) { return n_rows > kHgM; }
+
 constexpr size_t kPieceBytes = (size_t)256 << 20;
 
 Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
     Layout L;
-    L.n_pad = (std::max(n_rows, 1) + kHgM - 1) / kHgM * kHgM;
+    const int m = in_pairs(n_rows) ? 2 * kHgM : kHgM;
+    L.n_pad = (std::max(n_rows, 1) + m - 1) / m * m;
     L.D8 = (D + 7) / 8 * 8;
     L.Dp = (D + 63) / 64 * 64;
     L.tiles = (V + kHgN - 1) / kHgN;
@@ -45,8 +49,8 @@ Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
     if (gradient) {
         const long long fit = (long long)(kPieceBytes / (2 * (size_t)L.n_pad)) / kHgN * kHgN;
         L.piece = (int)std::min<long long>((long long)L.tiles * kHgN, std::max<long long>(fit, 2048));
-        const long long tiles = (long long)(L.n_pad / kHgM) * ((D + kHgN - 1) / kHgN);
-        L.splits = (int)std::max<long long>(1, std::min<long long>(sm_count / tiles, std::min(32, L.piece / 1024)));
+        const long long tiles = (long long)(L.n_pad / m) * ((D + kHgN - 1) / kHgN);
+        L.splits = (int)std::max<long long>(1, std::min<long long>(sm_count * kHgM / m / tiles, std::min(32, L.piece / 1024)));
         g = (size_t)L.n_pad * L.piece * 2;
         acc = (size_t)L.splits * L.n_pad * L.Dp * 4;
     }
@@ -82,19 +86,22 @@ int make_map(CUtensorMap* map, const void* base, long long rows, long long colum
                : ADASD_ERR_CUDA;
 }
 
-template <int TILE>
+template <int TILE, int CG>
 int launch_tiles(const HeadTiles& p, int sm_count, cudaStream_t stream) {
     static std::atomic<bool> allowed[64];
     int dev = 0;
     CUDA_TRY(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) return ADASD_ERR_CUDA;
     if (!allowed[dev].load(std::memory_order_acquire)) {
-        CUDA_TRY(cudaFuncSetAttribute(head_tile_kernel<TILE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHgSmem));
+        CUDA_TRY(cudaFuncSetAttribute(head_tile_kernel<TILE, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHgSmem));
         allowed[dev].store(true, std::memory_order_release);
     }
-    return launch_pdl(head_tile_kernel<TILE>, sm_count, kHgThreads, kHgSmem, 0, stream, p);
+    return launch_pdl(head_tile_kernel<TILE, CG>, sm_count / CG * CG, kHgThreads, kHgSmem, CG, stream, p);
 }
-
+template <int TILE>
+int launch_tiles(const HeadTiles& p, bool pairs, int sm_count, cudaStream_t stream) {
+    return pairs ? launch_tiles<TILE, 2>(p, sm_count, stream) : launch_tiles<TILE, 1>(p, sm_count, stream);
+}
 }  // namespace
 
 size_t head_scratch_bytes(int n_rows, int V, int D, bool gradient, int sm_count) { return layout_of(n_rows, V, D, gradient, sm_count).total; }
@@ -151,7 +158,7 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     t.splits = L.splits;
     t.status = c.status;
     if (c.op != HEAD_GIVEN) {
-        if (int rc = launch_tiles<TILE_STATS>(t, c.sm_count, stream)) return rc;
+        if (int rc = launch_tiles<TILE_STATS>(t, in_pairs(c.n_rows), c.sm_count, stream)) return rc;
         if (int rc = launch_pdl(head_stats_kernel, (c.n_rows + kHrThreads / 32 - 1) / (kHrThreads / 32), kHrThreads, 0, 0, stream, r)) return rc;
     }
     if (!gradient) return ADASD_OK;
@@ -169,16 +176,16 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
         t.a = map_h;
         t.b = map_w;
         t.out = map_g_out;
-        if (int rc = launch_tiles<TILE_G>(t, c.sm_count, stream)) return rc;
+        if (int rc = launch_tiles<TILE_G>(t, in_pairs(c.n_rows), c.sm_count, stream)) return rc;
         t.a = map_g;
         if (c.grad_w) {
             t.b = map_h;
             t.out = map_gw_out;
-            if (int rc = launch_tiles<TILE_GW>(t, c.sm_count, stream)) return rc;
+            if (int rc = launch_tiles<TILE_GW>(t, in_pairs(c.n_rows), c.sm_count, stream)) return rc;
         }
         if (c.grad_h) {
             t.b = map_w;
-            if (int rc = launch_tiles<TILE_GH>(t, c.sm_count, stream)) return rc;
+            if (int rc = launch_tiles<TILE_GH>(t, in_pairs(c.n_rows), c.sm_count, stream)) return rc;
         }
     }
     if (!c.grad_h) return ADASD_OK;

@@ -26,15 +26,23 @@
 
 namespace adasd {
 
-constexpr int kHgM = 128, kHgN = 256, kHgK = 64;             // tile of a CTA; a step along K
-constexpr int kHgStages = 4;
-constexpr int kHgABytes = kHgM * kHgK * 2, kHgBBytes = kHgN * kHgK * 2, kHgStageBytes = kHgABytes + kHgBBytes;
+// Tiles.  One CTA: 128 x 256.  A pair: 256 x 256, either CTA with 128 rows of A, half of B's columns and 128 rows of the sum; a step along K then
+// brings 32 KB to an SM instead of 48 (what the L2 gives, 12 to 15 TB/s, is the bound of the first: 1200 TFLOP/s need 14).
+constexpr int kHgM = 128, kHgN = 256, kHgK = 64;             // rows of a CTA, columns; a step along K
+constexpr int kHgABytes = kHgM * kHgK * 2;
+template <int CG>
+struct HeadStage {
+    static constexpr int kColumns = kHgN / CG;               // of B in a CTA
+    static constexpr int kBytes = kHgABytes + kColumns * kHgK * 2, kCount = CG == 1 ? 4 : 6;
+};
 constexpr int kHgBox = 64 * 64 * 2;
 constexpr int kHgHalf = kHgN / 2;
 constexpr int kHgOut = 32 * 64 * 2;                          // 32 rows of 64 bf16: what a warp stores at a time
 constexpr int kHgEpi = 8, kHgThreads = 64 + 32 * kHgEpi;     // warps: copies, products, epilogue (32 rows and 128 columns each)
 constexpr int kHgPart = 4;                                   // steps along K of a part of the logits' sums
-constexpr int kHgSmem = 1024 + kHgStages * kHgStageBytes + kHgEpi * kHgOut + 256;
+constexpr int kHgRing = 192 * 1024;                         // 4 stages of 48 KB or 6 of 32
+constexpr int kHgSmem = 1024 + kHgRing + kHgEpi * kHgOut + 256;
+constexpr uint32_t kHgPause = 1u << 16;                       // polls that a copy under way surely ends within
 constexpr int kHgPlaneRows = 64;                             // rows of a plane of G, where there are two
 
 enum HeadTile : int { TILE_STATS, TILE_G, TILE_GW, TILE_GH };
@@ -64,22 +72,23 @@ struct HeadTiles {
     uint32_t* status;
 };
 
-template <int TILE>
+template <int TILE, int CG>
 struct HeadWork {
+    static constexpr int kM = kHgM * CG;
     int mt, nt, total, ksteps;           // tiles along M and N; steps along K, of one split
     __device__ __forceinline__ HeadWork(const HeadTiles& p, int n_active) {
         if (TILE == TILE_STATS || TILE == TILE_G) {
-            mt = (n_active + kHgM - 1) / kHgM;
+            mt = (n_active + kM - 1) / kM;
             nt = (p.vn + kHgN - 1) / kHgN;
             ksteps = (p.D + kHgK - 1) / kHgK;
             total = mt * nt;
         } else if (TILE == TILE_GW) {
-            mt = (p.vn + kHgM - 1) / kHgM;
+            mt = (p.vn + kM - 1) / kM;
             nt = (p.D + kHgN - 1) / kHgN;
             ksteps = (n_active + kHgK - 1) / kHgK * p.planes;       // (two planes: of one step each)
             total = mt * nt;
         } else {
-            mt = (n_active + kHgM - 1) / kHgM;                      // (two planes: one tile)
+            mt = (n_active + kM - 1) / kM;                      // (two planes: one tile)
             nt = (p.D + kHgN - 1) / kHgN;
             ksteps = ((p.vn + kHgK - 1) / kHgK + p.splits - 1) / p.splits;
             total = mt * nt * p.splits;
@@ -91,14 +100,14 @@ struct HeadWork {
         k0 = 0;
         k1 = ksteps;
         if (TILE == TILE_STATS || TILE == TILE_G) {          // (the rows of one part of w one after the other)
-            m0 = i % mt * kHgM;
+            m0 = i % mt * kM;
             n0 = i / mt * kHgN;
         } else if (TILE == TILE_GW) {
             n0 = i % nt * kHgN;
-            m0 = i / nt * kHgM;
+            m0 = i / nt * kM;
         } else {
             n0 = i % nt * kHgN;
-            m0 = i / nt % mt * kHgM;
+            m0 = i / nt % mt * kM;
             split = i / (nt * mt);
             k0 = split * ksteps;
             k1 = min(k0 + ksteps, (p.vn + kHgK - 1) / kHgK);
@@ -172,13 +181,16 @@ __device__ __forceinline__ void stage_bf16(uint32_t stage, int lane, int half, c
                      pack_bf16(v[8 * u + 4], v[8 * u + 5]), pack_bf16(v[8 * u + 6], v[8 * u + 7]));
 }
 
-template <int TILE>
+template <int TILE, int CG>
 __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_constant__ HeadTiles p) {
+    using Stage = HeadStage<CG>;
+    constexpr int kHgStages = Stage::kCount, kHgStageBytes = Stage::kBytes;
+    static_assert(kHgStages * kHgStageBytes == kHgRing, "the ring's size is one for both");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t out_stage = base + kHgStages * kHgStageBytes, bars = out_stage + kHgEpi * kHgOut;
     // barriers: full[stage], empty[stage], accumulator full[2], empty[2], drained
-    const uint32_t bar_full = bars, bar_empty = bars + 8 * kHgStages, acc_full = bars + 16 * kHgStages, acc_empty = acc_full + 16, bar_drained = acc_empty + 16;
+    const uint32_t bar_full = bars, bar_empty = bars + 8 * kHgStages, acc_full = bars + 16 * kHgStages, acc_empty = acc_full + 16, bar_drained = acc_empty + 16, bar_never = bar_drained + 8;
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_gave_up;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -193,55 +205,67 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
         }
         for (int i = 0; i < 2; ++i) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(acc_full + 8 * i) : "memory");
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(acc_empty + 8 * i), "r"(kHgEpi) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(acc_empty + 8 * i), "r"(kHgEpi * CG) : "memory");
         }
         asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_drained) : "memory");
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_never) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tensor_alloc(smem_u32(&s_tmem), 512);
+    if (warp == 1) tensor_alloc<CG>(smem_u32(&s_tmem), 512);
     tensor_fence_before();
-    __syncthreads();
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();                                          // (a pair's barriers stand before either uses the other's)
     tensor_fence_after();
+    const uint32_t rank = CG == 2 ? cluster.block_rank() : 0u;
+    const int unit = blockIdx.x / CG, units = gridDim.x / CG;
+    // of the pair's first CTA: what both CTAs' copies and epilogues arrive on
+    const uint32_t lead_full = CG == 2 ? mapa_u32(smem_raw + (bar_full - smem_u32(smem_raw)), 0) : bar_full;
+    const uint32_t lead_acc_empty = CG == 2 ? mapa_u32(smem_raw + (acc_empty - smem_u32(smem_raw)), 0) : acc_empty;
     const uint32_t tmem = s_tmem;
     pdl_wait();
     pdl_trigger();
     const int n_active = __ldcg(p.n_active);
-    const HeadWork<TILE> w(p, n_active);
+    const HeadWork<TILE, CG> w(p, n_active);
 
     if (warp == 0) {
         if (lane == 0) {
             uint32_t step = 0;
             bool ok = true;
-            for (int i = blockIdx.x; ok && i < w.total; i += gridDim.x) {
+            for (int i = unit; ok && i < w.total; i += units) {
                 int m0, n0, k0, k1, split;
                 w.tile(p, i, m0, n0, k0, k1, split);
                 for (int k = k0; k < k1; ++k, ++step) {
                     const uint32_t s = step % kHgStages, ph = (step / kHgStages) & 1u;
                     ok = wait_or_give_up(bar_empty + 8 * s, ph ^ 1u, &s_gave_up);
                     if (!ok) break;
-                    const uint32_t a = base + s * kHgStageBytes, b = a + kHgABytes, bar = bar_full + 8 * s;
-                    mbar_expect(bar, kHgStageBytes);
+                    const uint32_t a = base + s * kHgStageBytes, b = a + kHgABytes, bar = lead_full + 8 * s;
+                    const int mc = m0 + kHgM * rank, nc = n0 + Stage::kColumns * rank;
+                    if (rank == 0) mbar_expect(bar_full + 8 * s, CG * kHgStageBytes);
 #pragma unroll
                     for (int j = 0; j < kHgM / 64; ++j)
-                        kAMn ? tma_load(a + j * kHgBox, &p.a, m0 + 64 * j, k * kHgK, bar) : tma_load(a + j * kHgBox, &p.a, k * kHgK, m0 + 64 * j, bar);
+                        kAMn ? tma_load<CG>(a + j * kHgBox, &p.a, mc + 64 * j, k * kHgK, bar) : tma_load<CG>(a + j * kHgBox, &p.a, k * kHgK, mc + 64 * j, bar);
 #pragma unroll
-                    for (int j = 0; j < kHgN / 64; ++j) {
-                        if (TILE == TILE_GW) tma_load(b + j * kHgBox, &p.b, n0 + 64 * j, p.planes == 2 ? 0 : k * kHgK, bar);
-                        else if (TILE == TILE_GH) tma_load(b + j * kHgBox, &p.b, n0 + 64 * j, p.v0 + k * kHgK, bar);
-                        else tma_load(b + j * kHgBox, &p.b, k * kHgK, p.v0 + n0 + 64 * j, bar);
+                    for (int j = 0; j < Stage::kColumns / 64; ++j) {
+                        if (TILE == TILE_GW) tma_load<CG>(b + j * kHgBox, &p.b, nc + 64 * j, p.planes == 2 ? 0 : k * kHgK, bar);
+                        else if (TILE == TILE_GH) tma_load<CG>(b + j * kHgBox, &p.b, nc + 64 * j, p.v0 + k * kHgK, bar);
+                        else tma_load<CG>(b + j * kHgBox, &p.b, k * kHgK, p.v0 + nc + 64 * j, bar);
                     }
                 }
             }
-            // no copy outlives the CTA: what was asked for and may not have been waited for is waited for here
-            for (uint32_t q = step > kHgStages ? step - kHgStages : 0; q < step; ++q)
-                mbar_wait_bounded(reinterpret_cast<uint64_t*>(__cvta_shared_to_generic(bar_full + 8 * (q % kHgStages))), (q / kHgStages) & 1u);
+            // no copy outlives the CTA: what was asked for and may not have been waited for is waited for here (a pair's second CTA cannot see its
+            // own arrive: after a wait that gave up it stays for a while, and both stay until the other is done)
+            if (rank == 0)
+                for (uint32_t q = step > kHgStages ? step - kHgStages : 0; q < step; ++q)
+                    mbar_wait_bounded(reinterpret_cast<uint64_t*>(__cvta_shared_to_generic(bar_full + 8 * (q % kHgStages))), (q / kHgStages) & 1u, ok ? kCWaitSpins : kHgPause);
+            else if (!ok)
+                mbar_wait_bounded(reinterpret_cast<uint64_t*>(__cvta_shared_to_generic(bar_never)), 0, kHgPause);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t kind = product_kind(kHgM, kHgN, kAMn, kBMn);
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t kind = product_kind(kHgM * CG, kHgN, kAMn, kBMn);
             uint32_t step = 0, n = 0;
             bool ok = true;
-            for (int i = blockIdx.x; ok && i < w.total; i += gridDim.x) {
+            for (int i = unit; ok && i < w.total; i += units) {
                 int m0, n0, k0, k1, split;
                 w.tile(p, i, m0, n0, k0, k1, split);
                 int k = k0;
@@ -260,17 +284,17 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                         for (int j = 0; j < kHgK / 16; ++j) {
                             const uint64_t da = kAMn ? operand_mn(a + j * 2048, kHgBox) : operand_k(a + j * 32);
                             const uint64_t db = kBMn ? operand_mn(b + j * 2048, kHgBox) : operand_k(b + j * 32);
-                            product(tmem + buf * kHgN, da, db, kind, add);
+                            product<CG>(tmem + buf * kHgN, da, db, kind, add);
                             add = true;
                         }
-                        product_commit(bar_empty + 8 * s);
+                        product_commit<CG>(bar_empty + 8 * s);
                     }
-                    if (ok) product_commit(acc_full + 8 * buf);
+                    if (ok) product_commit<CG>(acc_full + 8 * buf);
                     ++n;
                 } while (ok && k < k1);
             }
             // products under way end before tensor memory is freed
-            product_commit(bar_drained);
+            product_commit_here<CG>(bar_drained);
             mbar_wait_bounded(reinterpret_cast<uint64_t*>(__cvta_shared_to_generic(bar_drained)), 0);
         }
     } else {
@@ -278,9 +302,10 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
         const uint32_t stage = out_stage + (warp - 2) * kHgOut;
         uint32_t n = 0;
         bool ok = true;
-        for (int i = blockIdx.x; ok && i < w.total; i += gridDim.x) {
+        for (int i = unit; ok && i < w.total; i += units) {
             int m0, n0, k0, k1, split;
             w.tile(p, i, m0, n0, k0, k1, split);
+            m0 += kHgM * rank;
             const int row = m0 + quarter * 32 + lane, c0 = n0 + half * kHgHalf;     // the thread's row and first column
             auto next = [&]() -> uint32_t {                  // the accumulator's next sum, in this warp's rows and columns
                 const uint32_t buf = n & 1u;
@@ -291,7 +316,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
             auto release = [&]() {
                 tensor_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(acc_empty + 8 * (n & 1u));
+                if (lane == 0) mbar_arrive(lead_acc_empty + 8 * (n & 1u));
                 ++n;
             };
             // 64 columns as bf16: into the warp's stage once the store before has read it, and from there to row y on
@@ -429,9 +454,9 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
     }
     __syncwarp();
     tensor_fence_before();
-    __syncthreads();
+    cluster.sync();                                          // (neither CTA of a pair leaves, or frees its part, while the other is at work)
     tensor_fence_after();
-    if (warp == 1) tensor_free(tmem, 512);
+    if (warp == 1) tensor_free<CG>(tmem, 512);
     if (threadIdx.x == 0 && s_gave_up) atomicOr(p.status, ADASD_STATUS_TIMEOUT);
 }
 
