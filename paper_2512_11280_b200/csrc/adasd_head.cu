@@ -93,6 +93,11 @@ int launch_tiles(const HeadTiles& p, int sm_count, cudaStream_t stream) {
     CUDA_TRY(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) return ADASD_ERR_CUDA;
     if (!allowed[dev].load(std::memory_order_acquire)) {
+        if (TILE == TILE_STATS || TILE == TILE_G) {          // (the split of the registers counts on them)
+            cudaFuncAttributes fa;
+            CUDA_TRY(cudaFuncGetAttributes(&fa, head_tile_kernel<TILE, CG>));
+            if (fa.numRegs < kHgLaunchRegs) return ADASD_ERR_CUDA;
+        }
         CUDA_TRY(cudaFuncSetAttribute(head_tile_kernel<TILE, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHgSmem));
         allowed[dev].store(true, std::memory_order_release);
     }

@@ -38,8 +38,15 @@ struct HeadStage {
 constexpr int kHgBox = 64 * 64 * 2;
 constexpr int kHgHalf = kHgN / 2;
 constexpr int kHgOut = 32 * 64 * 2;                          // 32 rows of 64 bf16: what a warp stores at a time
-constexpr int kHgEpi = 8, kHgThreads = 64 + 32 * kHgEpi;     // warps: copies, products, epilogue (32 rows and 128 columns each)
-constexpr int kHgPart = 4;                                   // steps along K of a part of the logits' sums
+// Warps: 0 copies, 1 products (2 and 3 fill up their group), 4 .. 11 epilogue, 32 rows and 128 columns each.  The epilogue of a logits' tile holds 128 sums
+// a thread: its two groups take the registers that the first gives up (56 + 2 x 224 = 3 x 168, what the launch has).
+constexpr int kHgEpi = 8, kHgFirst = 4, kHgThreads = 32 * (kHgFirst + kHgEpi);
+constexpr int kHgLaunchRegs = 168, kHgFewRegs = 56, kHgManyRegs = 224;
+static_assert(kHgFewRegs * kHgFirst + kHgManyRegs * kHgEpi <= kHgLaunchRegs * (kHgFirst + kHgEpi), "a group that takes more than others gave would wait for good");
+#ifndef PART
+#define PART 8
+#endif
+constexpr int kHgPart = PART;                                   // steps along K of a part of the logits' sums
 constexpr int kHgRing = 192 * 1024;                         // 4 stages of 48 KB or 6 of 32
 constexpr int kHgSmem = 1024 + kHgRing + kHgEpi * kHgOut + 256;
 constexpr uint32_t kHgPause = 1u << 16;                       // polls that a copy under way surely ends within
@@ -227,6 +234,8 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
     const int n_active = __ldcg(p.n_active);
     const HeadWork<TILE, CG> w(p, n_active);
 
+    if (warp < kHgFirst) {
+        if constexpr (kParts) registers_give<kHgFewRegs>();
     if (warp == 0) {
         if (lane == 0) {
             uint32_t step = 0;
@@ -297,9 +306,11 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
             product_commit_here<CG>(bar_drained);
             mbar_wait_bounded(reinterpret_cast<uint64_t*>(__cvta_shared_to_generic(bar_drained)), 0);
         }
+    }
     } else {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
-        const uint32_t stage = out_stage + (warp - 2) * kHgOut;
+        if constexpr (kParts) registers_take<kHgManyRegs>();
+        const int quarter = warp & 3, half = (warp - kHgFirst) >> 2;
+        const uint32_t stage = out_stage + (warp - kHgFirst) * kHgOut;
         uint32_t n = 0;
         bool ok = true;
         for (int i = unit; ok && i < w.total; i += units) {
@@ -347,8 +358,19 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                     const uint32_t acc = next();
                     if (!ok) break;
 #pragma unroll
-                    for (int g = 0; g < 8; ++g) tensor_load_add16(acc + 16 * g, &z[g >> 1][16 * (g & 1)]);
-                    release();
+                    for (int g = 0; g < 4; g += 2) {
+                        float va[32], vb[32];
+                        tensor_load(acc + 32 * g, va);
+                        tensor_load(acc + 32 * g + 32, vb);
+                        tensor_wait(va);
+                        tensor_wait(vb);
+                        if (g == 2) release();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            z[g][j] += va[j];
+                            z[g + 1][j] += vb[j];
+                        }
+                    }
                 }
                 if (!ok) break;
                 const bool in = row < n_active;

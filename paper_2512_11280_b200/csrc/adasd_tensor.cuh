@@ -116,19 +116,11 @@ __device__ __forceinline__ void tensor_wait(float (&r)[32]) {
                  : "memory");
 }
 
-// 16 columns, added to r[0 .. 15]
-__device__ __forceinline__ void tensor_load_add16(uint32_t addr, float* r) {
-    float v[16];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]),
-          "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
-        : "r"(addr)
-        : "memory");
-#pragma unroll
-    for (int j = 0; j < 16; ++j) r[j] += v[j];
-}
+// Registers of a warp group's threads, by all its warps (a multiple of 8).
+template <int N>
+__device__ __forceinline__ void registers_give() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void registers_take() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 
 // ---- waits that give up ----------------------------------------------------------------------------
 // A wait ends when the phase is over, after kCWaitSpins polls, or soon after another warp of the CTA has given up (*gave_up).
