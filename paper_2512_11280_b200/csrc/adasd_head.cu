@@ -5,19 +5,55 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 namespace adasd {
 namespace {
 
 // What a call keeps in its scratch.  (Statistics of the tiles and a piece of the gradient are never needed at once: they share their place.)
 struct Layout {
-    int n_pad, D8, Dp, tiles, halves;                // 256 and 128 columns of the vocabulary
-    int piece, splits, planes;                       // columns of a piece; parts that the products along them are cut into; planes of G
+    int n_pad, D8, Dp, tiles;                        // tiles: 256 columns of the vocabulary
+    int columns, halves, res_halves;                 // columns of a tile of the statistics; as in HeadTiles
+    int piece, splits, planes;                       // columns of a piece; parts that grad_h's sums along them are cut into; planes of G
     size_t h, index, tok, n_active, zx, coef, res, big, acc, total;
 };
 
 // Tiles of pairs where the rows fill more than one CTA's.
 inline bool in_pairs(int n_rows) { return n_rows > kHgM; }
+
+// Columns of a tile of the statistics where a CTA works on its own, its time is that of reading w and there are few tiles: those with which the fullest CTA has
+// least to read.  (V = 32000 on 148 SMs: 125 tiles of 256 or 143 of 224.)
+int tile_columns(int V, int sm_count) {
+    int best = kHgN;
+    long long least = -1;
+    for (int c = kHgN; c >= 160; c -= 32) {
+        const long long tiles = (V + c - 1) / c, t = (tiles + sm_count - 1) / sm_count * (c + 16);
+        if (least < 0 || t < least) {
+            least = t;
+            best = c;
+        }
+    }
+    return best;
+}
+// Parts that grad_h's sums over a piece are cut into: as many as make the launch end first by this estimate, in steps along K: a step of the products of a
+// CTA (0.3 us) against what a part's fp32 sums cost to write and read.  The mean of calls with and without grad_w: one number for both, so that grad_h is
+// the same in both to the bit.
+int splits_of(int n_pad, int piece, int D, int planes, int m, int sm_count) {
+    const double units = sm_count * (double)kHgM / m, steps = piece / (double)kHgK, nt = (D + kHgN - 1) / kHgN, tiles = (double)(n_pad / m) * nt;
+    const double w = (piece / (double)m) * nt * ((planes == 2 ? 2 : n_pad / kHgK) + 3);
+    const double part = (double)n_pad * D * 8.0 / 6.5e6 / 0.3;
+    int best = 1;
+    double least = 0.0;
+    for (int s = 1; s <= 32 && steps / s >= 8; ++s) {
+        const double len = std::ceil(steps / s), alone = std::ceil(tiles * s / units) * len;
+        const double t = 0.5 * (alone + std::max((tiles * s * len + w) / units, len)) + s * part;
+        if (s == 1 || t < least) {
+            least = t;
+            best = s;
+        }
+    }
+    return best;
+}
 
 constexpr size_t kPieceBytes = (size_t)256 << 20;
 
@@ -28,7 +64,9 @@ Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
     L.D8 = (D + 7) / 8 * 8;
     L.Dp = (D + 63) / 64 * 64;
     L.tiles = (V + kHgN - 1) / kHgN;
-    L.halves = (V + kHgHalf - 1) / kHgHalf;
+    L.columns = in_pairs(n_rows) ? kHgN : tile_columns(V, sm_count);
+    L.halves = (V + L.columns - 1) / L.columns * 2;
+    L.res_halves = (V + kHgHalf - 1) / kHgHalf;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -43,14 +81,13 @@ Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
     L.h = take((size_t)L.n_pad * L.D8 * 2);
     const size_t part = (size_t)L.n_pad * L.halves * sizeof(float4);
     L.planes = n_rows <= kHgPlaneRows ? 2 : 1;
-    L.res = take(gradient && L.planes == 1 ? (size_t)L.n_pad * L.halves * sizeof(float) : 0);
+    L.res = take(gradient && L.planes == 1 ? (size_t)L.n_pad * L.res_halves * sizeof(float) : 0);
     L.piece = L.splits = 0;
     size_t g = 0, acc = 0;
     if (gradient) {
         const long long fit = (long long)(kPieceBytes / (2 * (size_t)L.n_pad)) / kHgN * kHgN;
         L.piece = (int)std::min<long long>((long long)L.tiles * kHgN, std::max<long long>(fit, 2048));
-        const long long tiles = (long long)(L.n_pad / m) * ((D + kHgN - 1) / kHgN);
-        L.splits = (int)std::max<long long>(1, std::min<long long>(sm_count * kHgM / m / tiles, std::min(32, L.piece / 1024)));
+        L.splits = splits_of(L.n_pad, L.piece, D, L.planes, m, sm_count);
         g = (size_t)L.n_pad * L.piece * 2;
         acc = (size_t)L.splits * L.n_pad * L.Dp * 4;
     }
@@ -93,7 +130,7 @@ int launch_tiles(const HeadTiles& p, int sm_count, cudaStream_t stream) {
     CUDA_TRY(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) return ADASD_ERR_CUDA;
     if (!allowed[dev].load(std::memory_order_acquire)) {
-        if (TILE == TILE_STATS || TILE == TILE_G) {          // (the split of the registers counts on them)
+        if (TILE != TILE_GRADS) {          // (the split of the registers counts on them)
             cudaFuncAttributes fa;
             CUDA_TRY(cudaFuncGetAttributes(&fa, head_tile_kernel<TILE, CG>));
             if (fa.numRegs < kHgLaunchRegs) return ADASD_ERR_CUDA;
@@ -122,6 +159,7 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     r.h = reinterpret_cast<uint16_t*>(s + L.h);
     r.D8 = L.D8;
     r.halves = L.halves;
+    r.res_halves = L.res_halves;
     r.planes = L.planes;
     r.res = c.grad_h && L.planes == 1 ? reinterpret_cast<float*>(s + L.res) : nullptr;
     r.index = reinterpret_cast<int32_t*>(s + L.index);
@@ -136,22 +174,38 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     r.splits = L.splits;
     r.c1 = (float)(1.4426950408889634 / (double)c.temperature);
     r.inv_T = 1.0 / (double)c.temperature;
-    if (int rc = launch_pdl(head_rows_kernel, (c.n_rows + kHrRows - 1) / kHrRows, kHrThreads, 0, 0, stream, r)) return rc;
+    r.rows = c.n_rows <= 2048 ? kHrThreads / 32 : kHrRows;
 
-    CUtensorMap map_h, map_w;
-    if (int rc = make_map(&map_h, r.h, L.n_pad, c.D, L.D8, 64)) return rc;
-    if (int rc = make_map(&map_w, c.weight, c.V, c.D, c.w_stride, 64)) return rc;
     HeadTiles t;
     memset(&t, 0, sizeof(t));
-    t.a = map_h;
-    t.b = map_w;
+    // One tile's rows and no gradient: nothing is gained by putting the rows that count together.
+    const bool as_they_lie = !gradient && c.n_rows <= kHgM && (reinterpret_cast<uintptr_t>(c.hidden) & 15u) == 0 && c.h_stride % 8 == 0;
+    // A CTA on its own brings in no more than the rows there are, in eights.  (Rows beyond a matrix cost a load more than those within: 128 of them for one row
+    // made 36 us of 30.)
+    const bool pairs = in_pairs(c.n_rows);
+    t.h_boxes = c.n_rows > 64 ? 2 : 1;
+    t.h_box_rows = ((c.n_rows + t.h_boxes - 1) / t.h_boxes + 7) / 8 * 8;
+    const int box_rows = pairs ? 64 : t.h_box_rows;
+    if (as_they_lie) {
+        r.n_active = nullptr;
+        r.index = nullptr;
+        r.tok = const_cast<int32_t*>(c.tok);
+        if (int rc = make_map(&t.h, c.hidden, c.n_rows, c.D, c.h_stride, box_rows)) return rc;
+    } else {
+        if (int rc = make_map(&t.h, r.h, L.n_pad, c.D, L.D8, box_rows)) return rc;
+        if (int rc = launch_pdl(head_rows_kernel, (c.n_rows + r.rows - 1) / r.rows, kHrThreads, 0, 0, stream, r)) return rc;
+    }
+    if (int rc = make_map(&t.w, c.weight, c.V, c.D, c.w_stride, pairs ? 64 : L.columns / 4)) return rc;
     t.D = c.D;
     t.V = c.V;
     t.vn = c.V;
     t.n_active = r.n_active;
+    t.n_rows = c.n_rows;
     t.c1 = r.c1;
+    t.columns = L.columns;
     t.part = reinterpret_cast<float4*>(s + L.big);
-    t.halves = r.halves;
+    t.halves = L.halves;
+    t.res_halves = L.res_halves;
     t.planes = L.planes;
     t.res = const_cast<float*>(r.res);
     t.zx = r.zx;
@@ -160,41 +214,47 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     t.acc = reinterpret_cast<float*>(s + L.acc);
     t.acc_slot = r.acc_slot;
     t.Dp = L.Dp;
-    t.splits = L.splits;
+    t.splits = r.splits;
+    t.want_w = c.grad_w != nullptr;
+    t.want_h = c.grad_h != nullptr;
     t.status = c.status;
     if (c.op != HEAD_GIVEN) {
-        if (int rc = launch_tiles<TILE_STATS>(t, in_pairs(c.n_rows), c.sm_count, stream)) return rc;
+        if (int rc = launch_tiles<TILE_STATS>(t, pairs, c.sm_count, stream)) return rc;
         if (int rc = launch_pdl(head_stats_kernel, (c.n_rows + kHrThreads / 32 - 1) / (kHrThreads / 32), kHrThreads, 0, 0, stream, r)) return rc;
     }
     if (!gradient) return ADASD_OK;
 
-    CUtensorMap map_g, map_g_out, map_gw_out;
+    CUtensorMap g_out, gw_out;
     char* g = s + L.big;
-    if (int rc = make_map(&map_g, g, L.n_pad, L.piece, L.piece, 64)) return rc;
-    if (int rc = make_map(&map_g_out, g, L.n_pad, L.piece, L.piece, 32)) return rc;
+    // (G's tiles have 256 columns; the gradients' products take boxes of 64 rows of both)
+    CUtensorMap w_tile = t.w, h_tile = t.h, w_grad = t.w, h_grad = t.h;
+    if (!pairs) {
+        if (L.columns != kHgN)
+            if (int rc = make_map(&w_tile, c.weight, c.V, c.D, c.w_stride, 64)) return rc;
+        w_grad = w_tile;
+        if (box_rows != 64)
+            if (int rc = make_map(&h_grad, r.h, L.n_pad, c.D, L.D8, 64)) return rc;
+    }
+    if (int rc = make_map(&t.g, g, L.n_pad, L.piece, L.piece, 64)) return rc;
+    if (int rc = make_map(&g_out, g, L.n_pad, L.piece, L.piece, 32)) return rc;
     if (c.grad_w)
-        if (int rc = make_map(&map_gw_out, c.grad_w, c.V, c.D, c.gw_stride, 32)) return rc;
+        if (int rc = make_map(&gw_out, c.grad_w, c.V, c.D, c.gw_stride, 32)) return rc;
     for (int v0 = 0; v0 < c.V; v0 += L.piece) {
         t.v0 = v0;
         t.vn = std::min(L.piece, c.V - v0);
         t.first = v0 == 0;
-        t.a = map_h;
-        t.b = map_w;
-        t.out = map_g_out;
-        if (int rc = launch_tiles<TILE_G>(t, in_pairs(c.n_rows), c.sm_count, stream)) return rc;
-        t.a = map_g;
-        if (c.grad_w) {
-            t.b = map_h;
-            t.out = map_gw_out;
-            if (int rc = launch_tiles<TILE_GW>(t, in_pairs(c.n_rows), c.sm_count, stream)) return rc;
-        }
-        if (c.grad_h) {
-            t.b = map_w;
-            if (int rc = launch_tiles<TILE_GH>(t, in_pairs(c.n_rows), c.sm_count, stream)) return rc;
-        }
+        t.out = g_out;
+        t.w = w_tile;
+        t.h = h_tile;
+        if (int rc = launch_tiles<TILE_G>(t, pairs, c.sm_count, stream)) return rc;
+        t.w = w_grad;
+        t.h = h_grad;
+        if (c.grad_w) t.out = gw_out;
+        if (int rc = launch_tiles<TILE_GRADS>(t, pairs, c.sm_count, stream)) return rc;
     }
     if (!c.grad_h) return ADASD_OK;
-    return launch_pdl(head_grad_rows_kernel, c.n_rows, kHrThreads, 0, 0, stream, r);
+    const int columns = kHrThreads / head_groups(r.splits * r.planes) * 8;
+    return launch_pdl(head_grad_rows_kernel, c.n_rows * ((c.D + columns - 1) / columns), kHrThreads, 0, 0, stream, r);
 }
 
 }  // namespace adasd

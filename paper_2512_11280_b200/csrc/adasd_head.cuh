@@ -52,7 +52,7 @@ constexpr int kHgSmem = 1024 + kHgRing + kHgEpi * kHgOut + 256;
 constexpr uint32_t kHgPause = 1u << 16;                       // polls that a copy under way surely ends within
 constexpr int kHgPlaneRows = 64;                             // rows of a plane of G, where there are two
 
-enum HeadTile : int { TILE_STATS, TILE_G, TILE_GW, TILE_GH };
+enum HeadTile : int { TILE_STATS, TILE_G, TILE_GRADS };
 
 // Of a row that counts: g_v = p (A + E u) + C, and at the token B more, where u = log2 p.
 struct __align__(16) HeadCoef {
@@ -63,62 +63,100 @@ struct __align__(16) HeadCoef {
 };
 
 struct HeadTiles {
-    CUtensorMap a, b, out;
+    CUtensorMap h, w, g;                 // hidden states, weight, the piece of G
+    CUtensorMap out;                     // TILE_G: of G; TILE_GRADS: of grad_w
     int32_t D, V, v0, vn;                // piece of the vocabulary: columns v0 .. v0 + vn - 1
-    const int32_t* n_active;
-    float c1;                            // log2 e / T
-    float4* part;                        // TILE_STATS: [row][halves], parts of 128 columns of the vocabulary
-    float* res;                          // TILE_G: [row][halves] sums of what rounding took from G; nullable
-    int32_t halves, planes;              // planes of G (1 or 2)
-    float* zx;
+    const int32_t* n_active;             // nullable: n_rows
+    int32_t n_rows;
     const int32_t* tok;
+    float c1;                            // log2 e / T
+    int32_t columns;                     // TILE_STATS: of a tile
+    int32_t h_boxes, h_box_rows;         // one CTA's tiles of logits: its rows come in so many boxes of so many rows (below the last: whatever is there)
+    float4* part;                        // TILE_STATS: [row][halves], a tile's first 128 columns and the others
+    float* res;                          // TILE_G: [row][res_halves], 128 columns each: sums of what rounding took from G; nullable
+    int32_t halves, res_halves, planes;              // planes of G (1 or 2)
+    float* zx;
     const HeadCoef* coef;                // TILE_G
-    float* acc;                          // TILE_GH: [splits][rows][Dp]
+    float* acc;                          // TILE_GRADS: [splits][rows][Dp]
     long long acc_slot;
-    int32_t Dp, splits, first;
+    int32_t Dp, splits, first;           // splits: parts along K that the sums of grad_h are cut into
+    int32_t want_w, want_h;              // TILE_GRADS: which gradients
     uint32_t* status;
 };
 
+struct HeadPlace {
+    int m0, n0, k0, k1, split;           // first row along M, first column along N, steps along K
+    bool gh;                             // TILE_GRADS: a tile of grad_h, else of grad_w
+};
+
+// A CTA's or pair's tiles, in their order.
+// Both gradients' products are one launch: grad_h has few tiles with long sums (along the vocabulary), grad_w many with short ones (along the
+// rows).  Every unit takes its share of the long ones first, units that have one less start on short ones, and the rest of these goes round.
+// (2048 rows, a piece of 65536, dim 2048: 64 long tiles leave 10 of 74 pairs idle on their own.)
 template <int TILE, int CG>
 struct HeadWork {
     static constexpr int kM = kHgM * CG;
-    int mt, nt, total, ksteps;           // tiles along M and N; steps along K, of one split
+    int unit, units, count;
+    int mt, nt, ksteps;                  // tiles along M and N, steps along K; TILE_GRADS: of grad_w
+    int h_mt, h_ksteps, h_all, h_own, h_total;
+    int early, few, few_at, early_own;   // short tiles of a unit with one long tile less, units of this kind, its place among them, its own such tiles
+    int columns;
     __device__ __forceinline__ HeadWork(const HeadTiles& p, int n_active) {
-        if (TILE == TILE_STATS || TILE == TILE_G) {
+        unit = blockIdx.x / CG;
+        units = gridDim.x / CG;
+        columns = TILE == TILE_STATS ? p.columns : kHgN;
+        if (TILE != TILE_GRADS) {
             mt = (n_active + kM - 1) / kM;
-            nt = (p.vn + kHgN - 1) / kHgN;
+            nt = (p.vn + columns - 1) / columns;
             ksteps = (p.D + kHgK - 1) / kHgK;
-            total = mt * nt;
-        } else if (TILE == TILE_GW) {
-            mt = (p.vn + kM - 1) / kM;
-            nt = (p.D + kHgN - 1) / kHgN;
-            ksteps = (n_active + kHgK - 1) / kHgK * p.planes;       // (two planes: of one step each)
-            total = mt * nt;
-        } else {
-            mt = (n_active + kM - 1) / kM;                      // (two planes: one tile)
-            nt = (p.D + kHgN - 1) / kHgN;
-            ksteps = ((p.vn + kHgK - 1) / kHgK + p.splits - 1) / p.splits;
-            total = mt * nt * p.splits;
+            count = (mt * nt - unit + units - 1) / units;
+            return;
         }
+        nt = (p.D + kHgN - 1) / kHgN;
+        h_mt = (n_active + kM - 1) / kM;                            // (two planes: one tile)
+        h_all = (p.vn + kHgK - 1) / kHgK;
+        h_ksteps = (h_all + p.splits - 1) / p.splits;
+        h_total = p.want_h ? h_mt * nt * p.splits : 0;
+        h_own = (h_total - unit + units - 1) / units;
+        mt = (p.vn + kM - 1) / kM;
+        ksteps = (n_active + kHgK - 1) / kHgK * p.planes;           // (two planes: one step each)
+        const int w_total = p.want_w ? mt * nt : 0, extra = h_total % units;
+        few = extra ? units - extra : 0;
+        few_at = unit - extra;
+        // (a tile's way out costs about as much as three steps)
+        early = few ? min((h_ksteps + ksteps / 2 + 4) / (ksteps + 3), (w_total + few - 1) / few) : 0;
+        const int rest = max(w_total - early * few, 0);
+        count = h_own + (few && few_at >= 0 ? max(min(early, (w_total - few_at + few - 1) / few), 0) : 0);
+        early_own = count - h_own;
+        count += rest > unit ? (rest - unit + units - 1) / units : 0;
     }
-    // tile i: first row along M, first column along N, first and one past the last step along K
-    __device__ __forceinline__ void tile(const HeadTiles& p, int i, int& m0, int& n0, int& k0, int& k1, int& split) const {
-        split = 0;
-        k0 = 0;
-        k1 = ksteps;
-        if (TILE == TILE_STATS || TILE == TILE_G) {          // (the rows of one part of w one after the other)
-            m0 = i % mt * kM;
-            n0 = i / mt * kHgN;
-        } else if (TILE == TILE_GW) {
-            n0 = i % nt * kHgN;
-            m0 = i / nt * kM;
-        } else {
-            n0 = i % nt * kHgN;
-            m0 = i / nt % mt * kM;
-            split = i / (nt * mt);
-            k0 = split * ksteps;
-            k1 = min(k0 + ksteps, (p.vn + kHgK - 1) / kHgK);
+    __device__ __forceinline__ HeadPlace place(int i) const {
+        HeadPlace t;
+        t.split = 0;
+        t.k0 = 0;
+        t.k1 = ksteps;
+        t.gh = false;
+        if (TILE != TILE_GRADS) {                                   // (the rows of one part of w one after the other)
+            i = unit + i * units;
+            t.m0 = i % mt * kM;
+            t.n0 = i / mt * columns;
+            return t;
         }
+        if (i < h_own) {
+            i = unit + i * units;
+            t.gh = true;
+            t.n0 = i % nt * kHgN;
+            t.m0 = i / nt % h_mt * kM;
+            t.split = i / (nt * h_mt);
+            t.k0 = t.split * h_ksteps;
+            t.k1 = min(t.k0 + h_ksteps, h_all);
+            return t;
+        }
+        i -= h_own;
+        i = i < early_own ? few_at + i * few : early * few + unit + (i - early_own) * units;
+        t.n0 = i % nt * kHgN;
+        t.m0 = i / nt * kM;
+        return t;
     }
 };
 
@@ -201,8 +239,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_gave_up;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr bool kParts = TILE == TILE_STATS || TILE == TILE_G;
-    constexpr bool kAMn = TILE == TILE_GW, kBMn = TILE == TILE_GW || TILE == TILE_GH;
+    constexpr bool kParts = TILE != TILE_GRADS;              // sums in parts
 
     if (threadIdx.x == 0) {
         s_gave_up = 0u;
@@ -224,14 +261,13 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
     cluster.sync();                                          // (a pair's barriers stand before either uses the other's)
     tensor_fence_after();
     const uint32_t rank = CG == 2 ? cluster.block_rank() : 0u;
-    const int unit = blockIdx.x / CG, units = gridDim.x / CG;
     // of the pair's first CTA: what both CTAs' copies and epilogues arrive on
     const uint32_t lead_full = CG == 2 ? mapa_u32(smem_raw + (bar_full - smem_u32(smem_raw)), 0) : bar_full;
     const uint32_t lead_acc_empty = CG == 2 ? mapa_u32(smem_raw + (acc_empty - smem_u32(smem_raw)), 0) : acc_empty;
     const uint32_t tmem = s_tmem;
     pdl_wait();
     pdl_trigger();
-    const int n_active = __ldcg(p.n_active);
+    const int n_active = p.n_active ? __ldcg(p.n_active) : p.n_rows;
     const HeadWork<TILE, CG> w(p, n_active);
 
     if (warp < kHgFirst) {
@@ -240,25 +276,52 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
         if (lane == 0) {
             uint32_t step = 0;
             bool ok = true;
-            for (int i = unit; ok && i < w.total; i += units) {
-                int m0, n0, k0, k1, split;
-                w.tile(p, i, m0, n0, k0, k1, split);
-                for (int k = k0; k < k1; ++k, ++step) {
-                    const uint32_t s = step % kHgStages, ph = (step / kHgStages) & 1u;
-                    ok = wait_or_give_up(bar_empty + 8 * s, ph ^ 1u, &s_gave_up);
-                    if (!ok) break;
-                    const uint32_t a = base + s * kHgStageBytes, b = a + kHgABytes, bar = lead_full + 8 * s;
-                    const int mc = m0 + kHgM * rank, nc = n0 + Stage::kColumns * rank;
-                    if (rank == 0) mbar_expect(bar_full + 8 * s, CG * kHgStageBytes);
-#pragma unroll
-                    for (int j = 0; j < kHgM / 64; ++j)
-                        kAMn ? tma_load<CG>(a + j * kHgBox, &p.a, mc + 64 * j, k * kHgK, bar) : tma_load<CG>(a + j * kHgBox, &p.a, k * kHgK, mc + 64 * j, bar);
-#pragma unroll
-                    for (int j = 0; j < Stage::kColumns / 64; ++j) {
-                        if (TILE == TILE_GW) tma_load<CG>(b + j * kHgBox, &p.b, nc + 64 * j, p.planes == 2 ? 0 : k * kHgK, bar);
-                        else if (TILE == TILE_GH) tma_load<CG>(b + j * kHgBox, &p.b, nc + 64 * j, p.v0 + k * kHgK, bar);
-                        else tma_load<CG>(b + j * kHgBox, &p.b, k * kHgK, p.v0 + nc + 64 * j, bar);
+            for (int i = 0; ok && i < w.count; ++i) {
+                const HeadPlace t = w.place(i);
+                const int mc = t.m0 + kHgM * rank, nc = t.n0 + Stage::kColumns * rank;
+                // (every load names its map: a map chosen by a variable costs the issuing thread more than a step's products take)
+                const uint32_t bytes = kParts && CG == 1 ? (p.h_boxes * p.h_box_rows + w.columns) * kHgK * 2 : CG * kHgStageBytes;
+                auto steps = [&](auto load) {
+                    for (int k = t.k0; k < t.k1; ++k, ++step) {
+                        const uint32_t s = step % kHgStages, ph = (step / kHgStages) & 1u;
+                        ok = wait_or_give_up(bar_empty + 8 * s, ph ^ 1u, &s_gave_up);
+                        if (!ok) break;
+                        if (rank == 0) mbar_expect(bar_full + 8 * s, bytes);
+                        const uint32_t a = base + s * kHgStageBytes;
+                        load(a, a + kHgABytes, lead_full + 8 * s, k * kHgK);
                     }
+                };
+                constexpr int kA = kHgM / 64, kB = Stage::kColumns / 64;
+                if constexpr (kParts && CG == 1) {           // (the weight's map has boxes of a quarter of the tile's columns)
+                    const int rows = w.columns / 4, h_rows = p.h_box_rows;
+                    const bool two = p.h_boxes == 2;
+                    steps([&](uint32_t a, uint32_t b, uint32_t bar, int k) {
+                        tma_load<CG>(a, &p.h, k, mc, bar);
+                        if (two) tma_load<CG>(a + h_rows * 128, &p.h, k, mc + h_rows, bar);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) tma_load<CG>(b + j * rows * 128, &p.w, k, p.v0 + nc + rows * j, bar);
+                    });
+                } else if constexpr (kParts) {
+                    steps([&](uint32_t a, uint32_t b, uint32_t bar, int k) {
+#pragma unroll
+                        for (int j = 0; j < kA; ++j) tma_load<CG>(a + j * kHgBox, &p.h, k, mc + 64 * j, bar);
+#pragma unroll
+                        for (int j = 0; j < kB; ++j) tma_load<CG>(b + j * kHgBox, &p.w, k, p.v0 + nc + 64 * j, bar);
+                    });
+                } else if (t.gh) {
+                    steps([&](uint32_t a, uint32_t b, uint32_t bar, int k) {
+#pragma unroll
+                        for (int j = 0; j < kA; ++j) tma_load<CG>(a + j * kHgBox, &p.g, k, mc + 64 * j, bar);
+#pragma unroll
+                        for (int j = 0; j < kB; ++j) tma_load<CG>(b + j * kHgBox, &p.w, nc + 64 * j, p.v0 + k, bar);
+                    });
+                } else {
+                    steps([&](uint32_t a, uint32_t b, uint32_t bar, int k) {
+#pragma unroll
+                        for (int j = 0; j < kA; ++j) tma_load<CG>(a + j * kHgBox, &p.g, mc + 64 * j, k, bar);
+#pragma unroll
+                        for (int j = 0; j < kB; ++j) tma_load<CG>(b + j * kHgBox, &p.h, nc + 64 * j, p.planes == 2 ? 0 : k, bar);
+                    });
                 }
             }
             // no copy outlives the CTA: what was asked for and may not have been waited for is waited for here (a pair's second CTA cannot see its
@@ -271,15 +334,15 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            constexpr uint32_t kind = product_kind(kHgM * CG, kHgN, kAMn, kBMn);
             uint32_t step = 0, n = 0;
             bool ok = true;
-            for (int i = unit; ok && i < w.total; i += units) {
-                int m0, n0, k0, k1, split;
-                w.tile(p, i, m0, n0, k0, k1, split);
-                int k = k0;
+            for (int i = 0; ok && i < w.count; ++i) {
+                const HeadPlace t = w.place(i);
+                const bool a_mn = !kParts && !t.gh;          // G lies along the vocabulary, h and w along dim
+                const uint32_t kind = product_kind(kHgM * CG, TILE == TILE_STATS && CG == 1 ? w.columns : kHgN, a_mn, !kParts);
+                int k = t.k0;
                 do {                                         // (a part, or the whole of the tile's sum)
-                    const int end = kParts ? min(k + kHgPart, k1) : k1;
+                    const int end = kParts ? min(k + kHgPart, t.k1) : t.k1;
                     const uint32_t buf = n & 1u;
                     ok = wait_or_give_up(acc_empty + 8 * buf, ((n >> 1) & 1u) ^ 1u, &s_gave_up);
                     tensor_fence_after();
@@ -289,18 +352,18 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                         if (!ok) break;
                         tensor_fence_after();
                         const uint32_t a = base + s * kHgStageBytes, b = a + kHgABytes;
+                        uint64_t da = a_mn ? operand_mn(a, kHgBox) : operand_k(a), db = kParts ? operand_k(b) : operand_mn(b, kHgBox);
+                        const uint64_t na = a_mn ? 2048 >> 4 : 32 >> 4, nb = kParts ? 32 >> 4 : 2048 >> 4;      // 16 of K on
 #pragma unroll
                         for (int j = 0; j < kHgK / 16; ++j) {
-                            const uint64_t da = kAMn ? operand_mn(a + j * 2048, kHgBox) : operand_k(a + j * 32);
-                            const uint64_t db = kBMn ? operand_mn(b + j * 2048, kHgBox) : operand_k(b + j * 32);
-                            product<CG>(tmem + buf * kHgN, da, db, kind, add);
+                            product<CG>(tmem + buf * kHgN, da + j * na, db + j * nb, kind, add);
                             add = true;
                         }
                         product_commit<CG>(bar_empty + 8 * s);
                     }
                     if (ok) product_commit<CG>(acc_full + 8 * buf);
                     ++n;
-                } while (ok && k < k1);
+                } while (ok && k < t.k1);
             }
             // products under way end before tensor memory is freed
             product_commit_here<CG>(bar_drained);
@@ -313,10 +376,9 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
         const uint32_t stage = out_stage + (warp - kHgFirst) * kHgOut;
         uint32_t n = 0;
         bool ok = true;
-        for (int i = unit; ok && i < w.total; i += units) {
-            int m0, n0, k0, k1, split;
-            w.tile(p, i, m0, n0, k0, k1, split);
-            m0 += kHgM * rank;
+        for (int i = 0; ok && i < w.count; ++i) {
+            const HeadPlace t = w.place(i);
+            const int m0 = t.m0 + kHgM * rank, n0 = t.n0, k0 = t.k0, k1 = t.k1;
             const int row = m0 + quarter * 32 + lane, c0 = n0 + half * kHgHalf;     // the thread's row and first column
             auto next = [&]() -> uint32_t {                  // the accumulator's next sum, in this warp's rows and columns
                 const uint32_t buf = n & 1u;
@@ -375,12 +437,14 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                 if (!ok) break;
                 const bool in = row < n_active;
                 if constexpr (TILE == TILE_STATS) {
-                    const int x = in ? __ldcg(p.tok + row) - p.v0 - c0 : -1;
+                    if (m0 + quarter * 32 >= n_active) continue;
+                    // (a token outside the vocabulary, however far: in no column)
+                    const int x = in ? (int)min((uint32_t)__ldcg(p.tok + row), 0x7FFFFFFFu) - p.v0 - c0 : -1;
                     RowStats r;
                     r.clear();
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        const int nv = p.V - p.v0 - c0 - 32 * g;
+                        const int nv = min(p.V - p.v0, n0 + w.columns) - c0 - 32 * g;
                         if (nv > 0) {
                             const bool here = x >= 32 * g && x < 32 * g + 32;
                             if (__any_sync(0xFFFFFFFFu, here)) {
@@ -390,7 +454,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                             r.add(z[g], nv, p.c1);
                         }
                     }
-                    if (in && c0 < p.vn) p.part[(long long)row * p.halves + c0 / kHgHalf] = make_float4(r.m, r.S, r.T, r.Z);
+                    if (in) p.part[(long long)row * p.halves + n0 / w.columns * 2 + half] = make_float4(r.m, r.S, r.T, r.Z);
                 } else {
                     float4 f = make_float4(0.f, 0.f, 0.f, 0.f), f2 = f;      // HeadCoef
                     if (in) {
@@ -434,7 +498,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                             if (p.planes == 2) store64(z[g - 1], v, c0 + 32 * (g - 1), y + kHgPlaneRows, rows_kept);
                         }
                     }
-                    if (in && p.res && c0 < p.vn) p.res[(long long)row * p.halves + (p.v0 + c0) / kHgHalf] = lost;
+                    if (in && p.res && c0 < p.vn) p.res[(long long)row * p.res_halves + (p.v0 + c0) / kHgHalf] = lost;
                 }
             } else {
                 const uint32_t acc = next();
@@ -452,11 +516,11 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
 #pragma unroll
                         for (int j = 0; j < 32; ++j) va[j] = vb[j] = 0.f;
                     }
-                    if constexpr (TILE == TILE_GW) {
+                    if (!t.gh) {
                         const int y = p.v0 + m0 + quarter * 32;
                         store64(va, vb, c0 + 32 * g, y, y < p.V && m0 + quarter * 32 < p.vn && c0 + 32 * g < p.D);
                     } else if (c0 + 32 * g < p.Dp) {         // (Dp: a multiple of 64)
-                        float4* d4 = reinterpret_cast<float4*>(p.acc + split * p.acc_slot + (long long)row * p.Dp + c0 + 32 * g);
+                        float4* d4 = reinterpret_cast<float4*>(p.acc + t.split * p.acc_slot + (long long)row * p.Dp + c0 + 32 * g);
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
                             float4 s = j < 8 ? make_float4(va[4 * (j & 7)], va[4 * (j & 7) + 1], va[4 * (j & 7) + 2], va[4 * (j & 7) + 3])
@@ -471,7 +535,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                 }
             }
         }
-        if (TILE == TILE_G || TILE == TILE_GW)
+        if (TILE != TILE_STATS)
             if (lane == 0) bulk_wait_all();                  // (written before the launch counts as done)
     }
     __syncwarp();
@@ -488,6 +552,7 @@ struct HeadRows {
     HeadCall c;
     uint16_t* h;                         // [n_pad][D8]: the rows that count, together
     int32_t D8, halves;
+    int32_t rows;                        // of a CTA of head_rows_kernel
     int32_t* index;                      // of a row that counts: its place among the call's rows
     int32_t* tok;
     int32_t* n_active;
@@ -495,14 +560,15 @@ struct HeadRows {
     HeadCoef* coef;
     const float4* part;
     const float* acc;
-    const float* res;                    // nullable
+    const float* res;                    // nullable [row][res_halves]
+    int32_t res_halves;
     long long acc_slot;
     int32_t Dp, splits, planes;
     float c1;
     double inv_T;
 };
 
-constexpr int kHrThreads = 256, kHrRows = 32;
+constexpr int kHrThreads = 256, kHrRows = 32;                // rows of a CTA of head_rows_kernel, at most
 
 __device__ __forceinline__ bool head_counts(const HeadCall& c, int r) {
     const int x = c.tok[r];
@@ -512,13 +578,20 @@ __device__ __forceinline__ bool head_counts(const HeadCall& c, int r) {
     return true;
 }
 
-// A CTA looks at 32 rows of the call: counts the rows ahead of them that count, copies those of its own that do to their place, and writes the
+__device__ __forceinline__ void head_left_out(const HeadCall& c, int r) {
+    if (c.logp) c.logp[r] = 0.f;
+    if (c.H) c.H[r] = 0.f;
+    if (c.lse) c.lse[r] = 0.f;
+    if (c.row_loss) c.row_loss[r] = 0.f;
+}
+
+// A CTA looks at some rows of the call (8, of many 32): counts the rows ahead of them that count, copies those of its own that do to their place, and writes the
 // outputs of those that do not.  HEAD_GIVEN: the gradient's constants too.  The last CTA writes the count and zeros up to the next multiple of
 // 64 rows (the products along the rows take 64 at a time).
 __global__ void __launch_bounds__(kHrThreads) head_rows_kernel(const __grid_constant__ HeadRows p) {
     __shared__ int s_count[kHrThreads / 32], s_place[kHrRows], s_total;
     const HeadCall& c = p.c;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r0 = blockIdx.x * kHrRows;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r0 = blockIdx.x * p.rows;
     pdl_wait();
     pdl_trigger();
     int before = 0;
@@ -530,7 +603,7 @@ __global__ void __launch_bounds__(kHrThreads) head_rows_kernel(const __grid_cons
         before = lane < kHrThreads / 32 ? s_count[lane] : 0;
         before = __reduce_add_sync(0xFFFFFFFFu, before);
         const int r = r0 + lane;
-        const bool in = r < c.n_rows, on = in && head_counts(c, r);
+        const bool in = lane < p.rows && r < c.n_rows, on = in && head_counts(c, r);
         const uint32_t mask = __ballot_sync(0xFFFFFFFFu, on);
         const int place = before + __popc(mask & ((1u << lane) - 1u));
         s_place[lane] = on ? place : in ? -1 : -2;
@@ -555,10 +628,7 @@ __global__ void __launch_bounds__(kHrThreads) head_rows_kernel(const __grid_cons
                 if (!isfinite(lse)) atomicOr(c.status, ADASD_STATUS_NAN);
             }
         } else if (in) {
-            if (c.logp) c.logp[r] = 0.f;
-            if (c.H) c.H[r] = 0.f;
-            if (c.lse) c.lse[r] = 0.f;
-            if (c.row_loss) c.row_loss[r] = 0.f;
+            head_left_out(c, r);
         }
     }
     __syncthreads();
@@ -566,13 +636,14 @@ __global__ void __launch_bounds__(kHrThreads) head_rows_kernel(const __grid_cons
     uint16_t* gh = static_cast<uint16_t*>(c.grad_h);
     const bool wide = (reinterpret_cast<uintptr_t>(hidden) & 15u) == 0 && c.h_stride % 8 == 0 && c.D % 8 == 0;
     const bool gwide = (reinterpret_cast<uintptr_t>(gh) & 15u) == 0 && c.gh_stride % 8 == 0 && c.D % 8 == 0;
-    for (int k = warp; k < kHrRows; k += kHrThreads / 32) {
+    for (int k = warp; k < p.rows; k += kHrThreads / 32) {
         const int place = s_place[k];
         const long long r = r0 + k;
         if (place >= 0) {
             const uint16_t* src = hidden + r * c.h_stride;
             uint16_t* dst = p.h + (long long)place * p.D8;
             if (wide)
+#pragma unroll 8
                 for (int j = lane; j < c.D / 8; j += 32) reinterpret_cast<uint4*>(dst)[j] = __ldcg(reinterpret_cast<const uint4*>(src) + j);
             else
                 for (int j = lane; j < c.D; j += 32) dst[j] = src[j];
@@ -591,26 +662,41 @@ __global__ void __launch_bounds__(kHrThreads) head_rows_kernel(const __grid_cons
     }
 }
 
-// A warp a row: the tiles' statistics joined, the row's outputs, its gradient's constants.
+// A warp a row: the tiles' statistics joined, the row's outputs, its gradient's constants.  Without an index the rows were taken as they lie, those left
+// out among them.
 __global__ void __launch_bounds__(kHrThreads) head_stats_kernel(const __grid_constant__ HeadRows p) {
     const HeadCall& c = p.c;
     const int lane = threadIdx.x & 31, row = (int)((blockIdx.x * kHrThreads + threadIdx.x) >> 5);
     pdl_wait();
     pdl_trigger();
-    if (row >= __ldcg(p.n_active)) return;
+    if (row >= (p.n_active ? __ldcg(p.n_active) : c.n_rows)) return;
+    if (!p.index && !head_counts(c, row)) {
+        if (lane == 0) head_left_out(c, row);
+        return;
+    }
     const float4* part = p.part + (long long)row * p.halves;
     float m = kFloor, S = 0.f, T = 0.f;
     double Z = 0.0;
     bool bad = false;
-    for (int k = lane; k < p.halves; k += 32) {
-        const float4 q = __ldcg(part + k);
+    auto join = [&](const float4& q) {
+        bad |= !(fabsf(q.w) < INFINITY);                     // (a logit that is not finite shows in their sum)
+        if (q.y == 0.f && q.x == kFloor) return;             // (a half without columns)
         bad |= !(q.y > 0.f && q.y < INFINITY) || !(fabsf(q.x) < -kFloor);
         const float m1 = fmaxf(m, q.x), f0 = ex2(m - m1), f1 = ex2(q.x - m1);
         T = f0 * (T + S * (m - m1)) + f1 * (q.z + q.y * (q.x - m1));
         S = f0 * S + f1 * q.y;
         Z += (double)q.w;
         m = m1;
+    };
+    int k = lane;
+    for (; k + 7 * 32 < p.halves; k += 8 * 32) {             // (eight loads under way)
+        float4 q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] = __ldcg(part + k + 32 * j);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) join(q[j]);
     }
+    for (; k < p.halves; k += 32) join(__ldcg(part + k));
     const float top = warp_max(m), f0 = ex2(m - top);
     T = f0 * (T + S * (m - top));
     S = f0 * S;
@@ -620,7 +706,7 @@ __global__ void __launch_bounds__(kHrThreads) head_stats_kernel(const __grid_con
     for (int o = 16; o > 0; o >>= 1) Z += __shfl_xor_sync(0xFFFFFFFFu, Z, o);
     bad = __any_sync(0xFFFFFFFFu, bad);
     if (lane != 0) return;
-    const int r = __ldcg(p.index + row);
+    const int r = p.index ? __ldcg(p.index + row) : row;
     const double ln2 = 0.6931471805599453, lnS = log((double)S);
     const float nan = __int_as_float(0x7FC00000);
     double l = ln2 * (double)fmaf(__ldcg(p.zx + row), p.c1, -top) - lnS, lse = ln2 * (double)top + lnS, H = lnS - ln2 * ((double)T / (double)S);
@@ -650,49 +736,64 @@ __global__ void __launch_bounds__(kHrThreads) head_stats_kernel(const __grid_con
     }
 }
 
-// A CTA a row: the splits' sums (and those of both planes), what rounding took from the row's G times w_x, rounded to bf16, to the row's place.
+// A CTA a part of a row, eight columns a thread; where there are several sums (splits, and both planes of each), groups of threads deal them out among
+// them.  The sums' total, what rounding took from the row's G times w_x, rounded to bf16, to the row's place.
+__host__ __device__ inline int head_groups(int sums) { return sums >= 4 ? 4 : sums >= 2 ? 2 : 1; }
 __global__ void __launch_bounds__(kHrThreads) head_grad_rows_kernel(const __grid_constant__ HeadRows p) {
     __shared__ float s_lost[kHrThreads / 32];
+    __shared__ float4 s_sum[kHrThreads][2];
     const HeadCall& c = p.c;
-    const int row = blockIdx.x;
+    const int sums = p.splits * p.planes, groups = head_groups(sums), width = kHrThreads / groups;
+    const int parts = (c.D + width * 8 - 1) / (width * 8), row = blockIdx.x / parts;
+    const int group = threadIdx.x / width, t = threadIdx.x - group * width, d = ((int)(blockIdx.x - row * parts) * width + t) * 8;
     pdl_wait();
     pdl_trigger();
     if (row >= __ldcg(p.n_active)) return;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (d < c.D) {                                           // (D is a multiple of 8)
+#pragma unroll 4
+        for (int k = group; k < sums; k += groups) {
+            const int split = k / p.planes, plane = k - split * p.planes;
+            const float4* a = reinterpret_cast<const float4*>(p.acc + split * p.acc_slot + (long long)(row + plane * kHgPlaneRows) * p.Dp + d);
+            const float4 u = __ldcg(a), v = __ldcg(a + 1);
+            s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
+            s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
+        }
+    }
     float lost = 0.f;
     if (p.res) {
-        for (int k = threadIdx.x; k < p.halves; k += kHrThreads) lost += __ldcg(p.res + (long long)row * p.halves + k);
+        for (int k = threadIdx.x; k < p.res_halves; k += kHrThreads) lost += __ldcg(p.res + (long long)row * p.res_halves + k);
         lost = warp_sum(lost);
         if ((threadIdx.x & 31) == 0) s_lost[threadIdx.x >> 5] = lost;
-        __syncthreads();
+    }
+    if (groups > 1) {
+        s_sum[threadIdx.x][0] = make_float4(s[0], s[1], s[2], s[3]);
+        s_sum[threadIdx.x][1] = make_float4(s[4], s[5], s[6], s[7]);
+    }
+    __syncthreads();
+    if (group != 0 || d >= c.D) return;
+    for (int k = 1; k < groups; ++k) {
+        const float4 u = s_sum[t + k * width][0], v = s_sum[t + k * width][1];
+        s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
+        s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
+    }
+    if (p.res) {
         lost = 0.f;
 #pragma unroll
         for (int k = 0; k < kHrThreads / 32; ++k) lost += s_lost[k];
+        float x[8];
+        unpack16(__ldcg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(c.weight) + (long long)__ldcg(p.tok + row) * c.w_stride + d)), x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = fmaf(lost, x[j], s[j]);
     }
-    const uint16_t* wx = static_cast<const uint16_t*>(c.weight) + (long long)__ldcg(p.tok + row) * c.w_stride;
-    uint16_t* dst = static_cast<uint16_t*>(c.grad_h) + (long long)__ldcg(p.index + row) * c.gh_stride;
-    for (int d = threadIdx.x * 8; d < c.D; d += kHrThreads * 8) {            // (D is a multiple of 8)
-        float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < p.splits; ++k)
-            for (int q = 0; q < p.planes; ++q) {
-                const float4* a = reinterpret_cast<const float4*>(p.acc + k * p.acc_slot + (long long)(row + q * kHgPlaneRows) * p.Dp + d);
-                const float4 u = __ldcg(a), v = __ldcg(a + 1);
-                s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
-                s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
-            }
-        if (p.res) {
-            float x[8];
-            unpack16(__ldcg(reinterpret_cast<const uint4*>(wx + d)), x);
+    uint16_t* dst = static_cast<uint16_t*>(c.grad_h) + (long long)__ldcg(p.index + row) * c.gh_stride + d;
+    const uint4 w = make_uint4(pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3]), pack_bf16(s[4], s[5]), pack_bf16(s[6], s[7]));
+    if ((reinterpret_cast<uintptr_t>(dst) & 15u) == 0) {
+        *reinterpret_cast<uint4*>(dst) = w;
+    } else {
+        const uint32_t q[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] = fmaf(lost, x[j], s[j]);
-        }
-        const uint4 w = make_uint4(pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3]), pack_bf16(s[4], s[5]), pack_bf16(s[6], s[7]));
-        if ((reinterpret_cast<uintptr_t>(dst + d) & 15u) == 0) {
-            *reinterpret_cast<uint4*>(dst + d) = w;
-        } else {
-            const uint32_t q[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) dst[d + j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
-        }
+        for (int j = 0; j < 8; ++j) dst[j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
     }
 }
 

@@ -246,6 +246,24 @@ def test_rows_that_are_not_finite(torch):
     ref.close_logp(torch.where(bad, 0.0, lp))
 
 
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("n", [6, 200])
+def test_weights_that_are_not_finite(torch, n, value):
+    """One such weight makes a logit of every row -inf, inf or NaN."""
+    import paper_2512_11280_b200 as adasd
+    h, w, tok, _ = inputs(torch, n, 900, 64, 8, out=0.0)
+    tok[:] = tok.clamp(0, 899)
+    h[:, 5] = 1.0
+    w[333, 5] = value
+    ctx = context(900)
+    sc, _ = scratch_for(torch, ctx, n, 64, False)
+    lp, H, lse = out(torch, n, 3)
+    ctx.head_logprob(h, w, tok, lp, sc, H, lse)
+    assert ctx.status() == adasd.STATUS_NAN
+    for t in (lp, H, lse):
+        assert bool(torch.isnan(t).all())
+
+
 def test_confident_rows(torch):
     """p of the token near 1: p - 1 is not lost; a token of tiny probability."""
     n, V, D = 130, 600, 64
