@@ -521,7 +521,7 @@ typedef struct {
 
 typedef struct {
     double lr, beta1, beta2; /* betas in [0, 1) */
-    double eps;              /* >= 1e-30 */
+    double eps;              /* >= 1e-16 */
     double grad_scale;       /* factor of every gradient: 1 / accumulation steps, a clipping factor */
     int32_t step;            /* t, >= 1 */
     int32_t stochastic;      /* 0: 8-bit states and bf16 parameters are rounded to the nearest.  1: up or down, so that the mean is the
@@ -539,7 +539,7 @@ typedef struct {
  * used: V and the context's dtype do not matter.  Where grad_scale_dev is given and the product is not finite (a norm that
  * overflowed), nothing is changed and ADASD_STATUS_NAN is set.  A gradient that is not finite makes its parameter and
  * states NaN or infinite as the formulas do, in 8 bits the states of its whole block.
- * One launch for up to 384 tensors.  Results do not vary from run to run.
+ * One launch for up to 384 tensors with states of one width.  Results do not vary from run to run.
  */
 int adasd_adamw_step(adasd_ctx* ctx, const adasd_adamw_tensor* tensors, int32_t n_tensors,
                      const adasd_adamw_options* options, void* stream);

@@ -10,27 +10,29 @@ namespace {
 
 constexpr int kAdFew = 24, kAdMany = 384;        // tensors of a launch: 2 and 32 KB of arguments
 
-template <int N>
-int launch_table(const AdParams& p, const AdTable<N>& table, int sm_count, cudaStream_t stream) {
-    return launch_pdl(adamw_kernel<N>, table.items, kAdThreads, 0, 0, stream, p, table);
-}
-
 inline bool at(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-template <int N>
+// The tensors with states in 8 bits (EIGHT) or in 32.
+template <int N, bool EIGHT>
 int launch_all(const AdParams& p, const adasd_adamw_tensor* in, int n, int sm_count, cudaStream_t stream) {
     AdTable<N> table;
     table.n = table.items = 0;
+    // Rounds of an item: up to 8, as long as there are 16 items for every SM.
+    long long all = 0;
+    for (int k = 0; k < n; ++k)
+        if ((in[k].state_bits == 8) == EIGHT) all += (in[k].n + kAdRound - 1) / kAdRound;
+    if (all == 0) return ADASD_OK;
+    table.rounds = (int)std::max<long long>(1, std::min<long long>(8, all / (16LL * sm_count)));
+    const long long item = (long long)table.rounds * kAdRound;
+    auto launch = [&] { return launch_pdl(adamw_kernel<N, EIGHT>, table.items, kAdThreads, 0, 0, stream, p, table); };
     for (int k = 0; k < n; ++k) {
         const adasd_adamw_tensor& s = in[k];
-        // tensors larger than a launch's items can count are cut: 2^30 items are 2^41 elements, more than the device holds
-        const long long items = (s.n + kAdItem - 1) / kAdItem;
-        if (items > (1 << 30)) return ADASD_ERR_SHAPE;
-        if (table.n == N || (long long)table.items + items > 0x7FFFFFFFLL) {
-            if (const int rc = launch_table(p, table, sm_count, stream)) return rc;
+        const long long items = (s.n + item - 1) / item;
+        if ((s.state_bits == 8) != EIGHT || items == 0) continue;
+        if (table.n == N || table.items + items > 0x7FFFFFFFLL) {        // (a tensor by itself has up to 2^40 elements, 2^29 items)
+            if (const int rc = launch()) return rc;
             table.n = table.items = 0;
         }
-        if (items == 0) continue;
         AdTensor& t = table.t[table.n++];
         t.param = s.param;
         t.grad = s.grad;
@@ -43,12 +45,17 @@ int launch_all(const AdParams& p, const adasd_adamw_tensor* in, int n, int sm_co
         t.weight_decay = s.weight_decay;
         t.first_item = table.items;
         t.index = k;
-        t.kind = (uint8_t)((s.param_dtype == ADASD_FP32 ? 1 : 0) | (s.grad_dtype == ADASD_FP32 ? 2 : 0) | (s.state_bits == 8 ? 4 : 0));
-        const uintptr_t states = s.state_bits == 8 ? 8 : 16;
+        t.kind = (uint8_t)((s.param_dtype == ADASD_FP32 ? 1 : 0) | (s.grad_dtype == ADASD_FP32 ? 2 : 0));
+        const uintptr_t states = EIGHT ? 8 : 16;
         t.aligned = at(s.param, 16) && at(s.grad, 16) && at(s.param_copy, 16) && at(s.exp_avg, states) && at(s.exp_avg_sq, states);
         table.items += (int32_t)items;
     }
-    return table.items > 0 ? launch_table(p, table, sm_count, stream) : ADASD_OK;
+    return launch();
+}
+template <int N>
+int launch_all(const AdParams& p, const adasd_adamw_tensor* tensors, int n, int sm_count, cudaStream_t stream) {
+    if (const int rc = launch_all<N, true>(p, tensors, n, sm_count, stream)) return rc;
+    return launch_all<N, false>(p, tensors, n, sm_count, stream);
 }
 
 }  // namespace

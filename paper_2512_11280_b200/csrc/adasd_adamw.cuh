@@ -14,6 +14,8 @@
 
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 namespace adasd {
 
 constexpr float kAdAvgMax = 448.f, kAdSqMax = 57344.f;       // largest e4m3, e5m2
@@ -29,9 +31,10 @@ __device__ __forceinline__ float ad_max(float a, float b) {  // NaN kept
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
-__device__ __forceinline__ float ad_sqrt(float x) {          // 2^-23 of itself: the step's size is lr, far below p
+// Square root and reciprocal are 2^-23 of themselves off: they make the step, whose size is lr, far below p.  (Both flush: eps is 1e-16 at the least.)
+__device__ __forceinline__ float ad_sqrt(float x) {
     float y;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ float ad_rcp(float x) {
@@ -39,151 +42,178 @@ __device__ __forceinline__ float ad_rcp(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float2 ad_two(float x) { return make_float2(x, x); }
+// Products that are rounded by themselves, whatever they are added to: as single numbers (products and sums of pairs get joined to multiply-adds).
+__device__ __forceinline__ float2 ad_mul(float2 a, float b) { return make_float2(__fmul_rn(a.x, b), __fmul_rn(a.y, b)); }
 
-// |y| moved down to a value of a small float, once `bits` / 2^DROP of a step have been added: of DROP bits fewer than fp32 where it is normal, in
-// steps of `least` below.  In the mean over the bits this is y itself.
-template <int DROP>
-__device__ __forceinline__ float ad_to_grid(float y, uint32_t bits, float least) {
-    const float a = fabsf(y), per = 1.f / least;             // (least is a power of two)
-    const float big = __uint_as_float((__float_as_uint(a) + bits) & ~((1u << DROP) - 1u));
-    const float small = floorf(__fadd_rn(__fmul_rn(a, per), __fmul_rn((float)bits, 1.f / (float)(1u << DROP)))) * least;
-    return copysignf(a < least * (float)(1 << (23 - DROP)) ? small : big, y);
+// |y| moved down to a value of a small float, once DROP bits of `bits` / 2^DROP of a step have been added: of DROP bits fewer than fp32 where it is normal,
+// in steps of 1 / PER below.  In the mean over the bits this is |y| itself.  (The bits become a fraction as the mantissa of a number in [1, 2); the floor is
+// an addition of 2^23, rounded down: conversions and roundings would wait for the special-function unit, which roots and reciprocals need.)
+template <int DROP, int PER>
+__device__ __forceinline__ float2 ad_to_grid(float2 a, uint32_t bits0, uint32_t bits1) {
+    constexpr uint32_t kMask = (1u << DROP) - 1u;
+    const float2 r = __fadd2_rn(make_float2(__uint_as_float(0x3F800000u | (bits0 & kMask) << (23 - DROP)), __uint_as_float(0x3F800000u | (bits1 & kMask) << (23 - DROP))),
+                                ad_two(-1.f));
+    const float2 t = __ffma2_rn(a, ad_two((float)PER), r);
+    const float2 f = __fmul2_rn(__fadd2_rn(make_float2(__fadd_rd(t.x, 8388608.f), __fadd_rd(t.y, 8388608.f)), ad_two(-8388608.f)), ad_two(1.f / (float)PER));
+    constexpr float kNormal = (float)(1 << (23 - DROP)) / (float)PER;
+    return make_float2(a.x < kNormal ? f.x : __uint_as_float((__float_as_uint(a.x) + (bits0 & kMask)) & ~kMask),
+                       a.y < kNormal ? f.y : __uint_as_float((__float_as_uint(a.y) + (bits1 & kMask)) & ~kMask));
 }
 
 // ---- eight elements of a lane ------------------------------------------------------------------
 // WHOLE: the block has 256 elements and its arrays start at 16 bytes (8-bit codes: 8): lane l holds elements 8 l .. 8 l + 7.  Else elements
-// l + 32 j, one by one, those at or beyond n as zeros.
+// l + 32 j, one by one, those at or beyond n as zeros.  What is loaded is kept as it lies until it is needed, so that the next block's can be on
+// its way.
 template <bool WHOLE, typename T>
-__device__ __forceinline__ void ad_load(const T* a, int lane, int n, float (&x)[8]) {
-    if constexpr (WHOLE && sizeof(T) == 4) {
-        const float4 u = __ldcg(reinterpret_cast<const float4*>(a) + 2 * lane), w = __ldcg(reinterpret_cast<const float4*>(a) + 2 * lane + 1);
-        x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
-        x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
-    } else if constexpr (WHOLE) {
-        unpack16(__ldcg(reinterpret_cast<const uint4*>(a) + lane), x);
-    } else {
+struct AdNumbers {                       // of T float or bf16
+    uint4 w[sizeof(T) == 4 || !WHOLE ? 2 : 1];
+    __device__ __forceinline__ void load(const void* p, long long first, int lane, int n) {
+        const T* a = static_cast<const T*>(p) + first;
+        if constexpr (WHOLE) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = lane + 32 * j < n ? to_f32(a[lane + 32 * j]) : 0.f;
+            for (int k = 0; k < (int)sizeof(T) / 2; ++k) w[k] = __ldcg(reinterpret_cast<const uint4*>(a) + (int)sizeof(T) / 2 * lane + k);
+        } else {
+            uint32_t* u = &w[0].x;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) u[j] = lane + 32 * j < n ? __float_as_uint(to_f32(a[lane + 32 * j])) : 0u;
+        }
     }
-}
-__device__ __forceinline__ uint32_t ad_pack2(float lo, float hi) {
+    __device__ __forceinline__ void get(float2 (&x)[4]) const {
+        const uint32_t* u = &w[0].x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (WHOLE && sizeof(T) == 2) x[j] = make_float2(__uint_as_float(u[j] << 16), __uint_as_float(u[j] & 0xFFFF0000u));
+            else x[j] = make_float2(__uint_as_float(u[2 * j]), __uint_as_float(u[2 * j + 1]));
+        }
+    }
+};
+__device__ __forceinline__ uint32_t ad_pack2(float2 v) {
     uint32_t d;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(v.y), "f"(v.x));
     return d;
 }
 template <bool WHOLE, typename T>
-__device__ __forceinline__ void ad_store(T* a, int lane, int n, const float (&x)[8]) {
+__device__ __forceinline__ void ad_store(void* p, long long first, int lane, int n, const float2 (&x)[4]) {
+    T* a = static_cast<T*>(p) + first;
     if constexpr (WHOLE && sizeof(T) == 4) {
-        reinterpret_cast<float4*>(a)[2 * lane] = make_float4(x[0], x[1], x[2], x[3]);
-        reinterpret_cast<float4*>(a)[2 * lane + 1] = make_float4(x[4], x[5], x[6], x[7]);
+        reinterpret_cast<float4*>(a)[2 * lane] = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
+        reinterpret_cast<float4*>(a)[2 * lane + 1] = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
     } else if constexpr (WHOLE) {
-        reinterpret_cast<uint4*>(a)[lane] = make_uint4(ad_pack2(x[0], x[1]), ad_pack2(x[2], x[3]), ad_pack2(x[4], x[5]), ad_pack2(x[6], x[7]));
+        reinterpret_cast<uint4*>(a)[lane] = make_uint4(ad_pack2(x[0]), ad_pack2(x[1]), ad_pack2(x[2]), ad_pack2(x[3]));
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (lane + 32 * j < n) {
-                if constexpr (sizeof(T) == 4) a[lane + 32 * j] = x[j];
-                else a[lane + 32 * j] = __float2bfloat16_rn(x[j]);
+                const float v = j & 1 ? x[j / 2].y : x[j / 2].x;
+                if constexpr (sizeof(T) == 4) a[lane + 32 * j] = v;
+                else a[lane + 32 * j] = __float2bfloat16_rn(v);
             }
     }
 }
-// Codes: E5M2 false: e4m3, true: e5m2.
-template <bool E5M2>
-__device__ __forceinline__ float2 ad_decode2(uint32_t two) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, E5M2 ? __NV_E5M2 : __NV_E4M3);
-    return __half22float2(*reinterpret_cast<const __half2*>(&h));
-}
-template <bool E5M2>
-__device__ __forceinline__ uint32_t ad_encode2(float a, float b) {
-    return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, E5M2 ? __NV_E5M2 : __NV_E4M3);
-}
+// Codes.  E5M2 false: e4m3, true: e5m2.
 template <bool WHOLE, bool E5M2>
-__device__ __forceinline__ void ad_load_codes(const uint8_t* a, int lane, int n, float (&x)[8]) {
-    uint32_t c[4];
-    if constexpr (WHOLE) {
-        const uint2 w = __ldcg(reinterpret_cast<const uint2*>(a) + lane);
-        c[0] = w.x & 0xFFFFu; c[1] = w.x >> 16; c[2] = w.y & 0xFFFFu; c[3] = w.y >> 16;
-    } else {
+struct AdCodes {
+    uint2 w;
+    __device__ __forceinline__ void load(const void* p, long long first, int lane, int n) {
+        const uint8_t* a = static_cast<const uint8_t*>(p) + first;
+        if constexpr (WHOLE) {
+            w = __ldcg(reinterpret_cast<const uint2*>(a) + lane);
+        } else {
+            uint32_t u[2] = {0u, 0u};
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            c[j] = (lane + 64 * j < n ? (uint32_t)a[lane + 64 * j] : 0u) | (lane + 64 * j + 32 < n ? (uint32_t)a[lane + 64 * j + 32] << 8 : 0u);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float2 f = ad_decode2<E5M2>(c[j]);
-        x[2 * j] = f.x;
-        x[2 * j + 1] = f.y;
-    }
-}
-template <bool WHOLE>
-__device__ __forceinline__ void ad_store_codes(uint8_t* a, int lane, int n, const uint32_t (&c)[4]) {
-    if constexpr (WHOLE) {
-        reinterpret_cast<uint2*>(a)[lane] = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (lane + 64 * j < n) a[lane + 64 * j] = (uint8_t)c[j];
-            if (lane + 64 * j + 32 < n) a[lane + 64 * j + 32] = (uint8_t)(c[j] >> 8);
+            for (int j = 0; j < 8; ++j)
+                if (lane + 32 * j < n) u[j / 4] |= (uint32_t)a[lane + 32 * j] << (8 * (j & 3));
+            w = make_uint2(u[0], u[1]);
         }
     }
-}
+    __device__ __forceinline__ void get(float2 (&x)[4]) const {
+        const uint32_t u[2] = {w.x, w.y};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const __nv_fp8x2_storage_t two = (__nv_fp8x2_storage_t)(u[j / 2] >> (16 * (j & 1)));
+            const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(two, E5M2 ? __NV_E5M2 : __NV_E4M3);
+            x[j] = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        }
+    }
+    static __device__ __forceinline__ void put(void* p, long long first, int lane, int n, const float2 (&x)[4]) {
+        uint8_t* a = static_cast<uint8_t*>(p) + first;
+        uint32_t c[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[j] = __nv_cvt_float2_to_fp8x2(x[j], __NV_SATFINITE, E5M2 ? __NV_E5M2 : __NV_E4M3);
+        if constexpr (WHOLE) {
+            reinterpret_cast<uint2*>(a)[lane] = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (lane + 32 * j < n) a[lane + 32 * j] = (uint8_t)(c[j / 2] >> (8 * (j & 1)));
+        }
+    }
+};
 
 // ---- a block ---------------------------------------------------------------------------------
 // Products and sums of the states are rounded one by one (no multiply-add), so that what is held in 8 bits does not hang on how the compiler joins
 // them: a state that another program works out by the formula gets the same codes.
 template <typename P, typename G, bool EIGHT, bool WHOLE>
 struct AdBlock {
-    float p[8], g[8], m[8], v[8], sm, sv;
+    AdNumbers<WHOLE, P> p;
+    AdNumbers<WHOLE, G> g;
+    std::conditional_t<EIGHT, AdCodes<WHOLE, false>, AdNumbers<WHOLE, float>> m;
+    std::conditional_t<EIGHT, AdCodes<WHOLE, true>, AdNumbers<WHOLE, float>> v;
+    float sm, sv;
 
     __device__ __forceinline__ void load(const AdTensor& t, long long first, int lane, int n) {
-        ad_load<WHOLE>(static_cast<const P*>(t.param) + first, lane, n, p);
-        ad_load<WHOLE>(static_cast<const G*>(t.grad) + first, lane, n, g);
+        p.load(t.param, first, lane, n);
+        g.load(t.grad, first, lane, n);
+        m.load(t.exp_avg, first, lane, n);
+        v.load(t.exp_avg_sq, first, lane, n);
         if constexpr (EIGHT) {
-            ad_load_codes<WHOLE, false>(static_cast<const uint8_t*>(t.exp_avg) + first, lane, n, m);
-            ad_load_codes<WHOLE, true>(static_cast<const uint8_t*>(t.exp_avg_sq) + first, lane, n, v);
             sm = __ldcg(t.avg_scale + first / kAdBlock);
             sv = __ldcg(t.sq_scale + first / kAdBlock);
-        } else {
-            ad_load<WHOLE>(static_cast<const float*>(t.exp_avg) + first, lane, n, m);
-            ad_load<WHOLE>(static_cast<const float*>(t.exp_avg_sq) + first, lane, n, v);
         }
     }
-    __device__ __forceinline__ void step(const AdParams& a, const AdCoef& c, float keep, const AdTensor& t, uint32_t key, long long first, int lane, int n) {
+    __device__ __forceinline__ void step(const AdParams& a, const AdCoef& c, float keep, const AdTensor& t, uint32_t key, long long first, int lane, int n) const {
+        float2 x[4], y[4], q[4], d[4];
+        m.get(y);
+        v.get(q);
+        g.get(d);
+        p.get(x);
         float m_top = 0.f, v_top = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float gj = __fmul_rn(g[j], c.grad_scale);
+        for (int j = 0; j < 4; ++j) {
+            const float2 gj = __fmul2_rn(d[j], ad_two(c.grad_scale));
             if constexpr (EIGHT) {
-                m[j] = __fmul_rn(m[j], sm);
-                v[j] = __fmul_rn(v[j], sv);
+                y[j] = __fmul2_rn(y[j], ad_two(sm));
+                q[j] = __fmul2_rn(q[j], ad_two(sv));
             }
-            m[j] = __fadd_rn(__fmul_rn(m[j], a.b1), __fmul_rn(gj, a.b1c));
-            v[j] = __fadd_rn(__fmul_rn(v[j], a.b2), __fmul_rn(__fmul_rn(gj, gj), a.b2c));
-            const float denom = fmaf(ad_sqrt(v[j]), c.root, a.eps);
-            p[j] = fmaf(-c.rate, m[j] * ad_rcp(denom), p[j] * keep);
+            y[j] = __fadd2_rn(ad_mul(y[j], a.b1), ad_mul(gj, a.b1c));
+            q[j] = __fadd2_rn(ad_mul(q[j], a.b2), ad_mul(__fmul2_rn(gj, gj), a.b2c));
+            const float2 denom = __ffma2_rn(make_float2(ad_sqrt(q[j].x), ad_sqrt(q[j].y)), ad_two(c.root), ad_two(a.eps));
+            x[j] = __ffma2_rn(__fmul2_rn(y[j], make_float2(ad_rcp(denom.x), ad_rcp(denom.y))), ad_two(-c.rate), __fmul2_rn(x[j], ad_two(keep)));
             if constexpr (EIGHT) {
-                m_top = ad_max(m_top, fabsf(m[j]));
-                v_top = ad_max(v_top, v[j]);
+                m_top = ad_max(ad_max(m_top, fabsf(y[j].x)), fabsf(y[j].y));
+                v_top = ad_max(ad_max(v_top, q[j].x), q[j].y);
             }
         }
         uint32_t h[8];
         if (a.stochastic && (EIGHT || sizeof(P) == 2)) {
+            const uint32_t at = (uint32_t)first + key + (WHOLE ? 8 * lane : lane);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) h[j] = ad_mix((uint32_t)first + (WHOLE ? 8 * lane + j : lane + 32 * j) + key);
-            if constexpr (sizeof(P) == 2) {
+            for (int j = 0; j < 8; ++j) h[j] = ad_mix(at + (WHOLE ? j : 32 * j));
+            if constexpr (sizeof(P) == 2) {                  // (infinities stay what they are by themselves, NaN would not)
+                auto up = [](float v, uint32_t hash) {
+                    return v == v ? __uint_as_float((__float_as_uint(v) + ((hash * 0x9E3779B1u) >> 16)) & 0xFFFF0000u) : v;
+                };
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {                // (infinities and NaN as they are)
-                    const uint32_t b = __float_as_uint(p[j]);
-                    if ((b & 0x7F800000u) != 0x7F800000u) p[j] = __uint_as_float((b + ((h[j] * 0x9E3779B1u) >> 16)) & 0xFFFF0000u);
-                }
+                for (int j = 0; j < 4; ++j) x[j] = make_float2(up(x[j].x, h[2 * j]), up(x[j].y, h[2 * j + 1]));
             }
         }
-        ad_store<WHOLE>(static_cast<P*>(t.param) + first, lane, n, p);
+        ad_store<WHOLE, P>(t.param, first, lane, n, x);
         if constexpr (sizeof(P) == 4)
-            if (t.param_copy) ad_store<WHOLE>(static_cast<__nv_bfloat16*>(t.param_copy) + first, lane, n, p);
+            if (t.param_copy) ad_store<WHOLE, __nv_bfloat16>(t.param_copy, first, lane, n, x);
         if constexpr (!EIGHT) {
-            ad_store<WHOLE>(static_cast<float*>(t.exp_avg) + first, lane, n, m);
-            ad_store<WHOLE>(static_cast<float*>(t.exp_avg_sq) + first, lane, n, v);
+            ad_store<WHOLE, float>(t.exp_avg, first, lane, n, y);
+            ad_store<WHOLE, float>(t.exp_avg_sq, first, lane, n, q);
         } else {
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) {
@@ -195,41 +225,45 @@ struct AdBlock {
                 t.sq_scale[first / kAdBlock] = __fmul_rn(v_top, 1.f / kAdSqMax);
             }
             const float im = m_top >= kAdLeast ? __fdiv_rn(kAdAvgMax, m_top) : 0.f, iv = v_top >= kAdLeast ? __fdiv_rn(kAdSqMax, v_top) : 0.f;
-            uint32_t cm[4], cv[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                float y[2], q[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    y[k] = __fmul_rn(m[2 * j + k], im);
-                    q[k] = __fmul_rn(v[2 * j + k], iv);
-                    if (a.stochastic) {
-                        y[k] = ad_to_grid<20>(y[k], h[2 * j + k] & 0xFFFFFu, 0x1p-9f);
-                        q[k] = ad_to_grid<21>(q[k], h[2 * j + k] >> 11, 0x1p-16f);
-                    }
-                }
-                cm[j] = ad_encode2<false>(y[0], y[1]);
-                cv[j] = ad_encode2<true>(q[0], q[1]);
                 // a v above 0 is never held as 0: m might be kept where it is not, and m / eps is no step
-                if (v[2 * j] > 0.f && (cv[j] & 0xFFu) == 0u) cv[j] |= 1u;
-                if (v[2 * j + 1] > 0.f && (cv[j] >> 8) == 0u) cv[j] |= 0x100u;
+                const float2 least = make_float2(q[j].x > 0.f ? 0x1p-16f : 0.f, q[j].y > 0.f ? 0x1p-16f : 0.f);
+                y[j] = __fmul2_rn(y[j], ad_two(im));
+                q[j] = __fmul2_rn(q[j], ad_two(iv));
+                if (a.stochastic) {
+                    const float2 r = ad_to_grid<20, 512>(make_float2(fabsf(y[j].x), fabsf(y[j].y)), h[2 * j], h[2 * j + 1]);
+                    y[j] = make_float2(copysignf(r.x, y[j].x), copysignf(r.y, y[j].y));
+                    q[j] = ad_to_grid<21, 65536>(q[j], h[2 * j] >> 11, h[2 * j + 1] >> 11);
+                }
+                q[j] = make_float2(ad_max(q[j].x, least.x), ad_max(q[j].y, least.y));
             }
-            ad_store_codes<WHOLE>(static_cast<uint8_t*>(t.exp_avg) + first, lane, n, cm);
-            ad_store_codes<WHOLE>(static_cast<uint8_t*>(t.exp_avg_sq) + first, lane, n, cv);
+            AdCodes<WHOLE, false>::put(t.exp_avg, first, lane, n, y);
+            AdCodes<WHOLE, true>::put(t.exp_avg_sq, first, lane, n, q);
         }
     }
 };
 
-// A warp's block of an item.
+// A warp's blocks of an item, one for each round of its CTA: the next one's loads are under way while one is worked on.
 template <typename P, typename G, bool EIGHT>
-__device__ __forceinline__ void ad_blocks(const AdParams& a, const AdCoef& c, float keep, const AdTensor& t, uint32_t key, long long first, int lane) {
-    const long long left = t.n - first;
-    if (left <= 0) return;
+__device__ __forceinline__ void ad_blocks(const AdParams& a, const AdCoef& c, float keep, const AdTensor& t, uint32_t key, long long first, int rounds, int lane) {
+    long long left = t.n - first;
     if (t.aligned && left >= kAdBlock) {
         AdBlock<P, G, EIGHT, true> b;
         b.load(t, first, lane, kAdBlock);
-        b.step(a, c, keep, t, key, first, lane, kAdBlock);
-    } else {
+        for (;;) {
+            --rounds;
+            left -= kAdRound;
+            const bool more = rounds > 0 && left >= kAdBlock;
+            AdBlock<P, G, EIGHT, true> next;
+            if (more) next.load(t, first + kAdRound, lane, kAdBlock);
+            b.step(a, c, keep, t, key, first, lane, kAdBlock);
+            first += kAdRound;
+            if (!more) break;
+            b = next;
+        }
+    }
+    for (; rounds > 0 && left > 0; --rounds, first += kAdRound, left -= kAdRound) {
         const int n = (int)min(left, (long long)kAdBlock);
         AdBlock<P, G, EIGHT, false> b;
         b.load(t, first, lane, n);
@@ -237,7 +271,7 @@ __device__ __forceinline__ void ad_blocks(const AdParams& a, const AdCoef& c, fl
     }
 }
 
-template <int TABLE>
+template <int TABLE, bool EIGHT>
 __global__ void __launch_bounds__(kAdThreads) adamw_kernel(const __grid_constant__ AdParams a, const __grid_constant__ AdTable<TABLE> table) {
     __shared__ AdCoef s_coef;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -261,27 +295,22 @@ __global__ void __launch_bounds__(kAdThreads) adamw_kernel(const __grid_constant
             return;
         }
     }
-    for (int item = blockIdx.x; item < table.items; item += gridDim.x) {
-        int lo = 0, hi = table.n - 1;                        // the last tensor that starts at or before the item
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (table.t[mid].first_item <= item) lo = mid;
-            else hi = mid - 1;
-        }
-        const AdTensor& t = table.t[lo];
-        const long long first = (long long)(item - t.first_item) * kAdItem + warp * kAdBlock;
-        const float keep = fmaf(-c.lr, t.weight_decay, 1.f);
-        const uint32_t key = ad_mix(a.seed ^ ad_mix(c.step + 0x9E3779B9u * (uint32_t)(t.index + 1)));
-        switch (t.kind) {
-            case 0: ad_blocks<__nv_bfloat16, __nv_bfloat16, false>(a, c, keep, t, key, first, lane); break;
-            case 1: ad_blocks<float, __nv_bfloat16, false>(a, c, keep, t, key, first, lane); break;
-            case 2: ad_blocks<__nv_bfloat16, float, false>(a, c, keep, t, key, first, lane); break;
-            case 3: ad_blocks<float, float, false>(a, c, keep, t, key, first, lane); break;
-            case 4: ad_blocks<__nv_bfloat16, __nv_bfloat16, true>(a, c, keep, t, key, first, lane); break;
-            case 5: ad_blocks<float, __nv_bfloat16, true>(a, c, keep, t, key, first, lane); break;
-            case 6: ad_blocks<__nv_bfloat16, float, true>(a, c, keep, t, key, first, lane); break;
-            default: ad_blocks<float, float, true>(a, c, keep, t, key, first, lane); break;
-        }
+    const int item = blockIdx.x;
+    int lo = 0, hi = table.n - 1;                            // the last tensor that starts at or before the item
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (table.t[mid].first_item <= item) lo = mid;
+        else hi = mid - 1;
+    }
+    const AdTensor& t = table.t[lo];
+    const long long first = (long long)(item - t.first_item) * table.rounds * kAdRound + warp * kAdBlock;
+    const float keep = fmaf(-c.lr, t.weight_decay, 1.f);
+    const uint32_t key = ad_mix(a.seed ^ ad_mix(c.step + 0x9E3779B9u * (uint32_t)(t.index + 1)));
+    switch (t.kind) {
+        case 0: ad_blocks<__nv_bfloat16, __nv_bfloat16, EIGHT>(a, c, keep, t, key, first, table.rounds, lane); break;
+        case 1: ad_blocks<float, __nv_bfloat16, EIGHT>(a, c, keep, t, key, first, table.rounds, lane); break;
+        case 2: ad_blocks<__nv_bfloat16, float, EIGHT>(a, c, keep, t, key, first, table.rounds, lane); break;
+        default: ad_blocks<float, float, EIGHT>(a, c, keep, t, key, first, table.rounds, lane); break;
     }
 }
 

@@ -10,7 +10,7 @@ namespace adasd {
 
 constexpr int kAdBlock = ADASD_ADAMW_BLOCK;      // elements of a warp, and of a scale
 constexpr int kAdThreads = 256;
-constexpr int kAdItem = kAdThreads / 32 * kAdBlock;
+constexpr int kAdRound = kAdThreads / 32 * kAdBlock;     // a CTA's warps, a block each
 
 struct AdTensor {
     void* param;
@@ -24,12 +24,12 @@ struct AdTensor {
     float weight_decay;
     int32_t first_item;                          // of the launch
     int32_t index;                               // in the call
-    uint8_t kind, aligned;                       // 1: fp32 parameters, 2: fp32 gradients, 4: states in 8 bits
+    uint8_t kind, aligned;                       // 1: fp32 parameters, 2: fp32 gradients
 };
 // The tensors of a launch travel as its argument: nothing of them is kept on the device, and a graph holds its own copy.
 template <int N>
 struct AdTable {
-    int32_t n, items;
+    int32_t n, items, rounds;                    // an item: so many rounds of a CTA
     AdTensor t[N];
 };
 struct AdCoef {
