@@ -24,7 +24,10 @@ int launch_all(const AdParams& p, const adasd_adamw_tensor* in, int n, int sm_co
     if (all == 0) return ADASD_OK;
     table.rounds = (int)std::max<long long>(1, std::min<long long>(8, all / (16LL * sm_count)));
     const long long item = (long long)table.rounds * kAdRound;
-    auto launch = [&] { return launch_pdl(adamw_kernel<N, EIGHT>, table.items, kAdThreads, 0, 0, stream, p, table); };
+    auto launch = [&] {
+        if constexpr (EIGHT) return launch_pdl(adamw8_kernel<N>, table.items, kAdThreads, 0, 0, stream, p, table);
+        else return launch_pdl(adamw_kernel<N>, table.items, kAdThreads, 0, 0, stream, p, table);
+    };
     for (int k = 0; k < n; ++k) {
         const adasd_adamw_tensor& s = in[k];
         const long long items = (s.n + item - 1) / item;

@@ -46,19 +46,26 @@ __device__ __forceinline__ float2 ad_two(float x) { return make_float2(x, x); }
 // Products that are rounded by themselves, whatever they are added to: as single numbers (products and sums of pairs get joined to multiply-adds).
 __device__ __forceinline__ float2 ad_mul(float2 a, float b) { return make_float2(__fmul_rn(a.x, b), __fmul_rn(a.y, b)); }
 
-// |y| moved down to a value of a small float, once DROP bits of `bits` / 2^DROP of a step have been added: of DROP bits fewer than fp32 where it is normal,
-// in steps of 1 / PER below.  In the mean over the bits this is |y| itself.  (The bits become a fraction as the mantissa of a number in [1, 2); the floor is
-// an addition of 2^23, rounded down: conversions and roundings would wait for the special-function unit, which roots and reciprocals need.)
-template <int DROP, int PER>
-__device__ __forceinline__ float2 ad_to_grid(float2 a, uint32_t bits0, uint32_t bits1) {
+// y moved towards 0 to a value of a small float, once DROP bits of `bits` / 2^DROP of a step have been added to its size: of DROP bits fewer than fp32 where it
+// is normal, in steps of 1 / PER below.  In the mean over the bits this is y itself.  (The bits become a fraction as the mantissa of a number in [1, 2); the floor is
+// an addition of 2^23, rounded down: conversions would wait for the special-function unit, which roots and reciprocals need.)
+template <int DROP, int PER, bool SIGNED>
+__device__ __forceinline__ float2 ad_to_grid(float2 y, uint32_t bits0, uint32_t bits1) {
     constexpr uint32_t kMask = (1u << DROP) - 1u;
-    const float2 r = __fadd2_rn(make_float2(__uint_as_float(0x3F800000u | (bits0 & kMask) << (23 - DROP)), __uint_as_float(0x3F800000u | (bits1 & kMask) << (23 - DROP))),
-                                ad_two(-1.f));
-    const float2 t = __ffma2_rn(a, ad_two((float)PER), r);
-    const float2 f = __fmul2_rn(__fadd2_rn(make_float2(__fadd_rd(t.x, 8388608.f), __fadd_rd(t.y, 8388608.f)), ad_two(-8388608.f)), ad_two(1.f / (float)PER));
     constexpr float kNormal = (float)(1 << (23 - DROP)) / (float)PER;
-    return make_float2(a.x < kNormal ? f.x : __uint_as_float((__float_as_uint(a.x) + (bits0 & kMask)) & ~kMask),
-                       a.y < kNormal ? f.y : __uint_as_float((__float_as_uint(a.y) + (bits1 & kMask)) & ~kMask));
+    const float2 r = __fadd2_rn(make_float2(__uint_as_float(0x3F800000u | (bits0 << (23 - DROP) & kMask << (23 - DROP))),
+                                            __uint_as_float(0x3F800000u | (bits1 << (23 - DROP) & kMask << (23 - DROP)))),
+                                ad_two(-1.f));
+    const float2 t = SIGNED ? make_float2(fmaf(fabsf(y.x), (float)PER, r.x), fmaf(fabsf(y.y), (float)PER, r.y)) : __ffma2_rn(y, ad_two((float)PER), r);
+    float2 f = __fmul2_rn(__fadd2_rn(make_float2(__fadd_rd(t.x, 8388608.f), __fadd_rd(t.y, 8388608.f)), ad_two(-8388608.f)), ad_two(1.f / (float)PER));
+    if (SIGNED) f = make_float2(copysignf(f.x, y.x), copysignf(f.y, y.y));
+    return make_float2(fabsf(y.x) < kNormal ? f.x : __uint_as_float((__float_as_uint(y.x) + (bits0 & kMask)) & ~kMask),
+                       fabsf(y.y) < kNormal ? f.y : __uint_as_float((__float_as_uint(y.y) + (bits1 & kMask)) & ~kMask));
+}
+// q, or 2^-16 if that is more and v is above 0
+__device__ __forceinline__ float ad_some(float q, float v) {
+    asm("{\n\t.reg .pred p;\n\tsetp.gt.f32 p, %1, 0f00000000;\n\t@p max.NaN.f32 %0, %0, 0f37800000;\n\t}" : "+f"(q) : "f"(v));
+    return q;
 }
 
 // ---- eight elements of a lane ------------------------------------------------------------------
@@ -92,6 +99,19 @@ __device__ __forceinline__ uint32_t ad_pack2(float2 v) {
     uint32_t d;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(v.y), "f"(v.x));
     return d;
+}
+// Of numbers whose lower 16 bits are to be dropped.
+template <bool WHOLE>
+__device__ __forceinline__ void ad_store_high(void* p, long long first, int lane, int n, const uint32_t (&x)[8]) {
+    uint16_t* a = static_cast<uint16_t*>(p) + first;
+    if constexpr (WHOLE) {
+        reinterpret_cast<uint4*>(a)[lane] = make_uint4(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632), __byte_perm(x[4], x[5], 0x7632),
+                                                       __byte_perm(x[6], x[7], 0x7632));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (lane + 32 * j < n) a[lane + 32 * j] = (uint16_t)(x[j] >> 16);
+    }
 }
 template <bool WHOLE, typename T>
 __device__ __forceinline__ void ad_store(void* p, long long first, int lane, int n, const float2 (&x)[4]) {
@@ -200,15 +220,18 @@ struct AdBlock {
             const uint32_t at = (uint32_t)first + key + (WHOLE ? 8 * lane : lane);
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[j] = ad_mix(at + (WHOLE ? j : 32 * j));
-            if constexpr (sizeof(P) == 2) {                  // (infinities stay what they are by themselves, NaN would not)
-                auto up = [](float v, uint32_t hash) {
-                    return v == v ? __uint_as_float((__float_as_uint(v) + ((hash * 0x9E3779B1u) >> 16)) & 0xFFFF0000u) : v;
-                };
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = make_float2(up(x[j].x, h[2 * j]), up(x[j].y, h[2 * j + 1]));
-            }
         }
-        ad_store<WHOLE, P>(t.param, first, lane, n, x);
+        if (sizeof(P) == 2 && a.stochastic) {                // up or down by 16 bits of noise; a NaN, whose bits are all ones here, stays one
+            uint32_t u[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t b = __float_as_uint(j & 1 ? x[j / 2].y : x[j / 2].x);
+                u[j] = min(b + ((h[j] * 0x9E3779B1u) >> 16), b | 0x7FFFFFFFu);
+            }
+            ad_store_high<WHOLE>(t.param, first, lane, n, u);
+        } else {
+            ad_store<WHOLE, P>(t.param, first, lane, n, x);
+        }
         if constexpr (sizeof(P) == 4)
             if (t.param_copy) ad_store<WHOLE, __nv_bfloat16>(t.param_copy, first, lane, n, x);
         if constexpr (!EIGHT) {
@@ -228,15 +251,14 @@ struct AdBlock {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 // a v above 0 is never held as 0: m might be kept where it is not, and m / eps is no step
-                const float2 least = make_float2(q[j].x > 0.f ? 0x1p-16f : 0.f, q[j].y > 0.f ? 0x1p-16f : 0.f);
+                const float2 v0 = q[j];
                 y[j] = __fmul2_rn(y[j], ad_two(im));
                 q[j] = __fmul2_rn(q[j], ad_two(iv));
                 if (a.stochastic) {
-                    const float2 r = ad_to_grid<20, 512>(make_float2(fabsf(y[j].x), fabsf(y[j].y)), h[2 * j], h[2 * j + 1]);
-                    y[j] = make_float2(copysignf(r.x, y[j].x), copysignf(r.y, y[j].y));
-                    q[j] = ad_to_grid<21, 65536>(q[j], h[2 * j] >> 11, h[2 * j + 1] >> 11);
+                    y[j] = ad_to_grid<20, 512, true>(y[j], h[2 * j], h[2 * j + 1]);
+                    q[j] = ad_to_grid<21, 65536, false>(q[j], h[2 * j] >> 11, h[2 * j + 1] >> 11);
                 }
-                q[j] = make_float2(ad_max(q[j].x, least.x), ad_max(q[j].y, least.y));
+                q[j] = make_float2(ad_some(q[j].x, v0.x), ad_some(q[j].y, v0.y));
             }
             AdCodes<WHOLE, false>::put(t.exp_avg, first, lane, n, y);
             AdCodes<WHOLE, true>::put(t.exp_avg_sq, first, lane, n, q);
@@ -271,12 +293,10 @@ __device__ __forceinline__ void ad_blocks(const AdParams& a, const AdCoef& c, fl
     }
 }
 
-template <int TABLE, bool EIGHT>
-__global__ void __launch_bounds__(kAdThreads) adamw_kernel(const __grid_constant__ AdParams a, const __grid_constant__ AdTable<TABLE> table) {
+template <bool EIGHT, typename Table>
+__device__ __forceinline__ void adamw_items(const AdParams& a, const Table& table) {
     __shared__ AdCoef s_coef;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    pdl_wait();
-    pdl_trigger();
     AdCoef c = a.coef;
     if (a.lr_dev || a.step_dev || a.grad_scale_dev) {
         if (threadIdx.x == 0) {
@@ -312,6 +332,21 @@ __global__ void __launch_bounds__(kAdThreads) adamw_kernel(const __grid_constant
         case 2: ad_blocks<__nv_bfloat16, float, EIGHT>(a, c, keep, t, key, first, table.rounds, lane); break;
         default: ad_blocks<float, float, EIGHT>(a, c, keep, t, key, first, table.rounds, lane); break;
     }
+}
+
+template <int TABLE>
+__global__ void __launch_bounds__(kAdThreads) adamw_kernel(const __grid_constant__ AdParams a, const __grid_constant__ AdTable<TABLE> table) {
+    pdl_wait();
+    pdl_trigger();
+    adamw_items<false>(a, table);
+}
+// States in 8 bits.  The arithmetic is the bound, 78 instructions an element, nearly half of them on the integer pipe, and needs warps: with registers for 32
+// of them a SM 817 us (300M bf16 elements, up or down), for 24 890, for 40 920.
+template <int TABLE>
+__global__ void __launch_bounds__(kAdThreads, 4) adamw8_kernel(const __grid_constant__ AdParams a, const __grid_constant__ AdTable<TABLE> table) {
+    pdl_wait();
+    pdl_trigger();
+    adamw_items<true>(a, table);
 }
 
 }  // namespace adasd
