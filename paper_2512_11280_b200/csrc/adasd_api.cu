@@ -1287,10 +1287,11 @@ int adasd_head_cross_entropy(adasd_ctx* ctx, const void* hidden_dev, int64_t hid
     c.z_loss = o.z_loss;
     c.scale = o.scale;
     c.row_loss = row_loss_out_dev;
+    c.loss = loss_out_dev;
     c.logp = logp_out_dev;
     c.lse = lse_out_dev;
     if (int rc = run_head(c, (cudaStream_t)stream)) return rc;
-    return loss_out_dev ? launch_total(row_loss_out_dev, n_rows, loss_out_dev, (cudaStream_t)stream) : ADASD_OK;
+    return n_rows == 0 && loss_out_dev ? launch_total(nullptr, 0, loss_out_dev, (cudaStream_t)stream) : ADASD_OK;
 }
 
 // ---- AdamW -----------------------------------------------------------------------------------

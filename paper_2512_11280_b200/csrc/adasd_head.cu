@@ -15,7 +15,8 @@ struct Layout {
     int n_pad, D8, Dp, tiles;                        // tiles: 256 columns of the vocabulary
     int columns, halves, res_halves;                 // columns of a tile of the statistics; as in HeadTiles
     int piece, splits, planes;                       // columns of a piece; parts that grad_h's sums along them are cut into; planes of G
-    size_t h, index, tok, n_active, zx, coef, res, big, acc, total;
+    long long z_stride;
+    size_t h, index, tok, n_active, ticket, zx, coef, res, z, big, acc, total;
 };
 
 // Tiles of pairs where the rows fill more than one CTA's.
@@ -38,13 +39,14 @@ int tile_columns(int V, int sm_count) {
 // Parts that grad_h's sums over a piece are cut into: as many as make the launch end first by this estimate, in steps along K: a step of the products of a
 // CTA (0.3 us) against what a part's fp32 sums cost to write and read.  The mean of calls with and without grad_w: one number for both, so that grad_h is
 // the same in both to the bit.
-int splits_of(int n_pad, int piece, int D, int planes, int m, int sm_count) {
+int splits_of(int n_rows, int n_pad, int piece, int D, int planes, int m, int sm_count) {
     const double units = sm_count * (double)kHgM / m, steps = piece / (double)kHgK, nt = (D + kHgN - 1) / kHgN, tiles = (double)(n_pad / m) * nt;
     const double w = (piece / (double)m) * nt * ((planes == 2 ? 2 : n_pad / kHgK) + 3);
-    const double part = (double)n_pad * D * 8.0 / 6.5e6 / 0.3;
+    const double part = (double)std::max(n_rows, 1) * planes * D * 8.0 / 6.5e6 / 0.3;
     int best = 1;
     double least = 0.0;
-    for (int s = 1; s <= 32 && steps / s >= 8; ++s) {
+    const int most = (int)std::max<size_t>(1, std::min<size_t>(128, ((size_t)64 << 20) / ((size_t)n_pad * D * 4)));      // (64 MB)
+    for (int s = 1; s <= most && steps / s >= 4; ++s) {
         const double len = std::ceil(steps / s), alone = std::ceil(tiles * s / units) * len;
         const double t = 0.5 * (alone + std::max((tiles * s * len + w) / units, len)) + s * part;
         if (s == 1 || t < least) {
@@ -74,6 +76,7 @@ Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
         return here;
     };
     L.n_active = take(16);
+    L.ticket = take(16);
     L.index = take((size_t)L.n_pad * 4);
     L.tok = take((size_t)L.n_pad * 4);
     L.zx = take((size_t)L.n_pad * 4);
@@ -82,12 +85,15 @@ Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
     const size_t part = (size_t)L.n_pad * L.halves * sizeof(float4);
     L.planes = n_rows <= kHgPlaneRows ? 2 : 1;
     L.res = take(gradient && L.planes == 1 ? (size_t)L.n_pad * L.res_halves * sizeof(float) : 0);
+    // (up to 128 rows: the logits, for the gradient that is made of them)
+    L.z_stride = (V + 63) / 64 * 64;
+    L.z = take(gradient && n_rows <= kHgM ? (size_t)n_rows * L.z_stride * sizeof(float) : 0);
     L.piece = L.splits = 0;
     size_t g = 0, acc = 0;
     if (gradient) {
         const long long fit = (long long)(kPieceBytes / (2 * (size_t)L.n_pad)) / kHgN * kHgN;
         L.piece = (int)std::min<long long>((long long)L.tiles * kHgN, std::max<long long>(fit, 2048));
-        L.splits = splits_of(L.n_pad, L.piece, D, L.planes, m, sm_count);
+        L.splits = splits_of(n_rows, L.n_pad, L.piece, D, L.planes, m, sm_count);
         g = (size_t)L.n_pad * L.piece * 2;
         acc = (size_t)L.splits * L.n_pad * L.Dp * 4;
     }
@@ -178,14 +184,16 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
 
     HeadTiles t;
     memset(&t, 0, sizeof(t));
-    // One tile's rows and no gradient: nothing is gained by putting the rows that count together.
-    const bool as_they_lie = !gradient && c.n_rows <= kHgM && (reinterpret_cast<uintptr_t>(c.hidden) & 15u) == 0 && c.h_stride % 8 == 0;
+    // One tile's rows: nothing is gained by putting the rows that count together.
+    const bool as_they_lie = c.n_rows <= kHgM && (reinterpret_cast<uintptr_t>(c.hidden) & 15u) == 0 && c.h_stride % 8 == 0;
     // A CTA on its own brings in no more than the rows there are, in eights.  (Rows beyond a matrix cost a load more than those within: 128 of them for one row
     // made 36 us of 30.)
     const bool pairs = in_pairs(c.n_rows);
     t.h_boxes = c.n_rows > 64 ? 2 : 1;
     t.h_box_rows = ((c.n_rows + t.h_boxes - 1) / t.h_boxes + 7) / 8 * 8;
     const int box_rows = pairs ? 64 : t.h_box_rows;
+    // The losses' total by the last row's CTA, unless there are so many that it would take long.
+    r.ticket = c.loss && c.n_rows <= 16384 ? reinterpret_cast<uint32_t*>(s + L.ticket) : nullptr;
     if (as_they_lie) {
         r.n_active = nullptr;
         r.index = nullptr;
@@ -218,10 +226,25 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     t.want_w = c.grad_w != nullptr;
     t.want_h = c.grad_h != nullptr;
     t.status = c.status;
-    if (c.op != HEAD_GIVEN) {
-        if (int rc = launch_tiles<TILE_STATS>(t, pairs, c.sm_count, stream)) return rc;
-        if (int rc = launch_pdl(head_stats_kernel, (c.n_rows + kHrThreads / 32 - 1) / (kHrThreads / 32), kHrThreads, 0, 0, stream, r)) return rc;
+    const bool from_logits = as_they_lie && gradient && c.op == HEAD_CE;
+    const int rows16 = (c.n_rows + 15) / 16 * 16;
+    if (as_they_lie) {
+        t.ticket = r.ticket;
+        t.rows16 = rows16;
+        if (from_logits) {
+            t.z = reinterpret_cast<float*>(s + L.z);
+            r.z = t.z;
+            r.z_stride = t.z_stride = L.z_stride;
+            r.g = reinterpret_cast<uint16_t*>(s + L.big);
+            r.piece = L.piece;
+        }
     }
+    if (c.op != HEAD_GIVEN)
+        if (int rc = launch_tiles<TILE_STATS>(t, pairs, c.sm_count, stream)) return rc;
+    if (c.op != HEAD_GIVEN || as_they_lie)
+        if (int rc = launch_pdl(head_stats_kernel, as_they_lie && gradient ? rows16 : c.n_rows, kHsThreads, 0, 0, stream, r)) return rc;
+    if (c.loss && !r.ticket)
+        if (int rc = launch_total(c.row_loss, c.n_rows, c.loss, stream)) return rc;
     if (!gradient) return ADASD_OK;
 
     CUtensorMap g_out, gw_out;
@@ -232,7 +255,7 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
         if (L.columns != kHgN)
             if (int rc = make_map(&w_tile, c.weight, c.V, c.D, c.w_stride, 64)) return rc;
         w_grad = w_tile;
-        if (box_rows != 64)
+        if (box_rows != 64 || as_they_lie)
             if (int rc = make_map(&h_grad, r.h, L.n_pad, c.D, L.D8, 64)) return rc;
     }
     if (int rc = make_map(&t.g, g, L.n_pad, L.piece, L.piece, 64)) return rc;
@@ -246,7 +269,14 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
         t.out = g_out;
         t.w = w_tile;
         t.h = h_tile;
-        if (int rc = launch_tiles<TILE_G>(t, pairs, c.sm_count, stream)) return rc;
+        if (from_logits) {
+            r.v0 = v0;
+            r.vn = t.vn;
+            const int parts = ((t.vn + kHgN - 1) / kHgN * kHgN + kHxColumns - 1) / kHxColumns;
+            if (int rc = launch_pdl(head_g_kernel, rows16 * parts, kHxThreads, 0, 0, stream, r)) return rc;
+        } else {
+            if (int rc = launch_tiles<TILE_G>(t, pairs, c.sm_count, stream)) return rc;
+        }
         t.w = w_grad;
         t.h = h_grad;
         if (c.grad_w) t.out = gw_out;

@@ -18,7 +18,8 @@
 // planes instead, as twice the rows.
 //
 // Rows left out are not worked on: the rows that count are copied together first (head_rows_kernel), how many there are is known on the
-// device alone.
+// device alone.  Up to 128 rows are one tile whatever is left out; they are taken as they lie, and the cross entropy's G is made of the
+// forward pass's logits, which so few rows have room for, instead of forming them again.
 #pragma once
 
 #include "adasd_head_types.cuh"
@@ -43,10 +44,7 @@ constexpr int kHgOut = 32 * 64 * 2;                          // 32 rows of 64 bf
 constexpr int kHgEpi = 8, kHgFirst = 4, kHgThreads = 32 * (kHgFirst + kHgEpi);
 constexpr int kHgLaunchRegs = 168, kHgFewRegs = 56, kHgManyRegs = 224;
 static_assert(kHgFewRegs * kHgFirst + kHgManyRegs * kHgEpi <= kHgLaunchRegs * (kHgFirst + kHgEpi), "a group that takes more than others gave would wait for good");
-#ifndef PART
-#define PART 8
-#endif
-constexpr int kHgPart = PART;                                   // steps along K of a part of the logits' sums
+constexpr int kHgPart = 8;                                   // steps along K of a part of the logits' sums
 constexpr int kHgRing = 192 * 1024;                         // 4 stages of 48 KB or 6 of 32
 constexpr int kHgSmem = 1024 + kHgRing + kHgEpi * kHgOut + 256;
 constexpr uint32_t kHgPause = 1u << 16;                       // polls that a copy under way surely ends within
@@ -74,7 +72,11 @@ struct HeadTiles {
     int32_t h_boxes, h_box_rows;         // one CTA's tiles of logits: its rows come in so many boxes of so many rows (below the last: whatever is there)
     float4* part;                        // TILE_STATS: [row][halves], a tile's first 128 columns and the others
     float* res;                          // TILE_G: [row][res_halves], 128 columns each: sums of what rounding took from G; nullable
-    int32_t halves, res_halves, planes;              // planes of G (1 or 2)
+    int32_t halves, res_halves, planes;  // planes of G (1 or 2)
+    float* z;                            // TILE_STATS: nullable [row][z_stride] the logits
+    long long z_stride;
+    uint32_t* ticket;                    // TILE_STATS: nullable, set to 0
+    int32_t rows16;                      // TILE_GRADS: rows as they lie, in sixteens: sums along the rows end there (0: in full steps)
     float* zx;
     const HeadCoef* coef;                // TILE_G
     float* acc;                          // TILE_GRADS: [splits][rows][Dp]
@@ -267,6 +269,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
     const uint32_t tmem = s_tmem;
     pdl_wait();
     pdl_trigger();
+    if (TILE == TILE_STATS && p.ticket && blockIdx.x == 0 && threadIdx.x == 0) *p.ticket = 0u;
     const int n_active = p.n_active ? __ldcg(p.n_active) : p.n_rows;
     const HeadWork<TILE, CG> w(p, n_active);
 
@@ -354,9 +357,11 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                         const uint32_t a = base + s * kHgStageBytes, b = a + kHgABytes;
                         uint64_t da = a_mn ? operand_mn(a, kHgBox) : operand_k(a), db = kParts ? operand_k(b) : operand_mn(b, kHgBox);
                         const uint64_t na = a_mn ? 2048 >> 4 : 32 >> 4, nb = kParts ? 32 >> 4 : 2048 >> 4;      // 16 of K on
+                        int sub = kHgK / 16;                 // (sixteens of this step)
+                        if (CG == 1 && !kParts && !t.gh && p.rows16) sub = min(sub, p.rows16 / 16 - (p.planes == 2 ? 0 : sub * k));
 #pragma unroll
                         for (int j = 0; j < kHgK / 16; ++j) {
-                            product<CG>(tmem + buf * kHgN, da + j * na, db + j * nb, kind, add);
+                            if (kParts || CG == 2 || j < sub) product<CG>(tmem + buf * kHgN, da + j * na, db + j * nb, kind, add);
                             add = true;
                         }
                         product_commit<CG>(bar_empty + 8 * s);
@@ -435,7 +440,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                     }
                 }
                 if (!ok) break;
-                const bool in = row < n_active;
+                bool in = row < n_active;
                 if constexpr (TILE == TILE_STATS) {
                     if (m0 + quarter * 32 >= n_active) continue;
                     // (a token outside the vocabulary, however far: in no column)
@@ -451,6 +456,18 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                                 const float zx = pick(z[g], x - 32 * g);
                                 if (here) p.zx[row] = zx;
                             }
+                            if (p.z && in) {
+                                float* dst = p.z + row * p.z_stride + c0 + 32 * g;
+                                if (nv >= 32) {
+#pragma unroll
+                                    for (int j = 0; j < 8; ++j)
+                                        reinterpret_cast<float4*>(dst)[j] = make_float4(z[g][4 * j], z[g][4 * j + 1], z[g][4 * j + 2], z[g][4 * j + 3]);
+                                } else {
+#pragma unroll
+                                    for (int j = 0; j < 32; ++j)
+                                        if (j < nv) dst[j] = z[g][j];
+                                }
+                            }
                             r.add(z[g], nv, p.c1);
                         }
                     }
@@ -462,6 +479,8 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                         f2 = __ldcg(reinterpret_cast<const float4*>(p.coef + row) + 1);
                     }
                     const float lse2 = f.x, A = f.y, B = f.z, C = f.w, E = f2.x;
+                    const bool listed = in;
+                    in = in && __float_as_int(f2.y) >= 0;    // (rows as they lie: not one that is left out, whose logits may be anything)
                     const int x = in ? __float_as_int(f2.y) - p.v0 - c0 : -1;
                     const bool rows_kept = p.planes == 1 || m0 + quarter * 32 < kHgPlaneRows;
                     float lost = 0.f;
@@ -498,7 +517,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                             if (p.planes == 2) store64(z[g - 1], v, c0 + 32 * (g - 1), y + kHgPlaneRows, rows_kept);
                         }
                     }
-                    if (in && p.res && c0 < p.vn) p.res[(long long)row * p.res_halves + (p.v0 + c0) / kHgHalf] = lost;
+                    if (listed && p.res && c0 < p.vn) p.res[(long long)row * p.res_halves + (p.v0 + c0) / kHgHalf] = lost;
                 }
             } else {
                 const uint32_t acc = next();
@@ -519,7 +538,8 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                     if (!t.gh) {
                         const int y = p.v0 + m0 + quarter * 32;
                         store64(va, vb, c0 + 32 * g, y, y < p.V && m0 + quarter * 32 < p.vn && c0 + 32 * g < p.D);
-                    } else if (c0 + 32 * g < p.Dp) {         // (Dp: a multiple of 64)
+                    } else if (c0 + 32 * g < p.Dp && (row < n_active || (p.planes == 2 && row >= kHgPlaneRows && row < kHgPlaneRows + n_active))) {
+                        // (Dp: a multiple of 64)
                         float4* d4 = reinterpret_cast<float4*>(p.acc + t.split * p.acc_slot + (long long)row * p.Dp + c0 + 32 * g);
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
@@ -550,6 +570,11 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
 
 struct HeadRows {
     HeadCall c;
+    uint32_t* ticket;                    // nullable: the total is the last row's CTA's
+    const float* z;                      // head_g_kernel: the logits
+    long long z_stride;
+    uint16_t* g;                         // ... and the piece of G
+    int32_t v0, vn, piece;
     uint16_t* h;                         // [n_pad][D8]: the rows that count, together
     int32_t D8, halves;
     int32_t rows;                        // of a CTA of head_rows_kernel
@@ -585,6 +610,33 @@ __device__ __forceinline__ void head_left_out(const HeadCall& c, int r) {
     if (c.row_loss) c.row_loss[r] = 0.f;
 }
 
+// What a gradient's tiles need of a row with given dL/dl and dL/dH.
+__device__ __forceinline__ HeadCoef head_given(const HeadCall& c, int r, double inv_T) {
+    const float dl = c.g_logp[r], dH = c.g_H ? c.g_H[r] : 0.f, H = dH != 0.f ? c.H_in[r] : 0.f, lse = c.lse_in[r];
+    HeadCoef f;
+    f.lse2 = isfinite(lse) ? lse * kLog2e : __int_as_float(0x7FC00000);
+    f.A = (float)((-(double)dl - (double)dH * H) * inv_T);
+    f.B = (float)((double)dl * inv_T);
+    f.C = 0.f;
+    f.E = (float)(-(double)dH * 0.6931471805599453 * inv_T);
+    f.tok = c.tok[r];
+    f.pad[0] = f.pad[1] = 0.f;
+    if (!isfinite(lse)) atomicOr(c.status, ADASD_STATUS_NAN);
+    return f;
+}
+// Units of 16 bytes from one row to another by threads t, t + step, ..: eight loads under way.
+__device__ __forceinline__ void head_copy(uint4* dst, const uint4* src, int units, int t, int step) {
+    for (; t < units; t += 8 * step) {
+        uint4 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (t + j * step < units) v[j] = __ldcg(src + t + j * step);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (t + j * step < units) dst[t + j * step] = v[j];
+    }
+}
+
 // A CTA looks at some rows of the call (8, of many 32): counts the rows ahead of them that count, copies those of its own that do to their place, and writes the
 // outputs of those that do not.  HEAD_GIVEN: the gradient's constants too.  The last CTA writes the count and zeros up to the next multiple of
 // 64 rows (the products along the rows take 64 at a time).
@@ -610,23 +662,12 @@ __global__ void __launch_bounds__(kHrThreads) head_rows_kernel(const __grid_cons
         if (lane == 0) {
             s_total = before + __popc(mask);
             if (blockIdx.x == gridDim.x - 1) *p.n_active = s_total;
+            if (blockIdx.x == 0 && p.ticket) *p.ticket = 0u;
         }
         if (on) {
             p.index[place] = r;
             p.tok[place] = c.tok[r];
-            if (c.op == HEAD_GIVEN) {
-                const float dl = c.g_logp[r], dH = c.g_H ? c.g_H[r] : 0.f, H = dH != 0.f ? c.H_in[r] : 0.f, lse = c.lse_in[r];
-                HeadCoef f;
-                f.lse2 = isfinite(lse) ? lse * kLog2e : __int_as_float(0x7FC00000);
-                f.A = (float)((-(double)dl - (double)dH * H) * p.inv_T);
-                f.B = (float)((double)dl * p.inv_T);
-                f.C = 0.f;
-                f.E = (float)(-(double)dH * 0.6931471805599453 * p.inv_T);
-                f.tok = c.tok[r];
-                f.pad[0] = f.pad[1] = 0.f;
-                p.coef[place] = f;
-                if (!isfinite(lse)) atomicOr(c.status, ADASD_STATUS_NAN);
-            }
+            if (c.op == HEAD_GIVEN) p.coef[place] = head_given(c, r, p.inv_T);
         } else if (in) {
             head_left_out(c, r);
         }
@@ -643,8 +684,7 @@ __global__ void __launch_bounds__(kHrThreads) head_rows_kernel(const __grid_cons
             const uint16_t* src = hidden + r * c.h_stride;
             uint16_t* dst = p.h + (long long)place * p.D8;
             if (wide)
-#pragma unroll 8
-                for (int j = lane; j < c.D / 8; j += 32) reinterpret_cast<uint4*>(dst)[j] = __ldcg(reinterpret_cast<const uint4*>(src) + j);
+                head_copy(reinterpret_cast<uint4*>(dst), reinterpret_cast<const uint4*>(src), c.D / 8, lane, 32);
             else
                 for (int j = lane; j < c.D; j += 32) dst[j] = src[j];
         } else if (place == -1 && gh) {
@@ -662,83 +702,191 @@ __global__ void __launch_bounds__(kHrThreads) head_rows_kernel(const __grid_cons
     }
 }
 
-// A warp a row: the tiles' statistics joined, the row's outputs, its gradient's constants.  Without an index the rows were taken as they lie, those left
-// out among them.
-__global__ void __launch_bounds__(kHrThreads) head_stats_kernel(const __grid_constant__ HeadRows p) {
+// A CTA a row: the tiles' statistics joined, the row's outputs, its gradient's constants; the last CTA adds up the losses, in the rows' order.
+// Without an index the rows are taken as they lie, those left out among them; for a gradient a copy of them, with zeros for the latter and up to the next
+// multiple of 16 rows, is what its products read.
+constexpr int kHsThreads = 128;
+__global__ void __launch_bounds__(kHsThreads) head_stats_kernel(const __grid_constant__ HeadRows p) {
+    constexpr int kW = kHsThreads / 32;
+    __shared__ float s_m[kW], s_S[kW], s_T[kW];
+    __shared__ double s_Z[kW];
+    __shared__ uint32_t s_last;
     const HeadCall& c = p.c;
-    const int lane = threadIdx.x & 31, row = (int)((blockIdx.x * kHrThreads + threadIdx.x) >> 5);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.x;
+    const bool lie = !p.index;
     pdl_wait();
     pdl_trigger();
-    if (row >= (p.n_active ? __ldcg(p.n_active) : c.n_rows)) return;
-    if (!p.index && !head_counts(c, row)) {
-        if (lane == 0) head_left_out(c, row);
-        return;
+    const bool listed = row < (lie ? c.n_rows : __ldcg(p.n_active)), counts = listed && (!lie || head_counts(c, row));
+    if (lie && p.coef) {                                     // (n_rows and more: the row's copy)
+        uint4* dst = reinterpret_cast<uint4*>(p.h + (long long)row * p.D8);
+        if (counts)
+            head_copy(dst, reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(c.hidden) + row * c.h_stride), p.D8 / 8, tid, kHsThreads);
+        else
+            for (int j = tid; j < p.D8 / 8; j += kHsThreads) dst[j] = make_uint4(0u, 0u, 0u, 0u);
     }
-    const float4* part = p.part + (long long)row * p.halves;
-    float m = kFloor, S = 0.f, T = 0.f;
-    double Z = 0.0;
-    bool bad = false;
-    auto join = [&](const float4& q) {
-        bad |= !(fabsf(q.w) < INFINITY);                     // (a logit that is not finite shows in their sum)
-        if (q.y == 0.f && q.x == kFloor) return;             // (a half without columns)
-        bad |= !(q.y > 0.f && q.y < INFINITY) || !(fabsf(q.x) < -kFloor);
-        const float m1 = fmaxf(m, q.x), f0 = ex2(m - m1), f1 = ex2(q.x - m1);
-        T = f0 * (T + S * (m - m1)) + f1 * (q.z + q.y * (q.x - m1));
-        S = f0 * S + f1 * q.y;
-        Z += (double)q.w;
-        m = m1;
-    };
-    int k = lane;
-    for (; k + 7 * 32 < p.halves; k += 8 * 32) {             // (eight loads under way)
-        float4 q[8];
+    if (counts && c.op != HEAD_GIVEN) {
+        const float4* part = p.part + (long long)row * p.halves;
+        float m = kFloor, S = 0.f, T = 0.f;
+        double Z = 0.0;
+        bool bad = false;
+        auto join = [&](const float4& q) {
+            bad |= !(fabsf(q.w) < INFINITY);                 // (a logit that is not finite shows in their sum)
+            if (q.y == 0.f && q.x == kFloor) return;         // (a half without columns)
+            bad |= !(q.y > 0.f && q.y < INFINITY) || !(fabsf(q.x) < -kFloor);
+            const float m1 = fmaxf(m, q.x), f0 = ex2(m - m1), f1 = ex2(q.x - m1);
+            T = f0 * (T + S * (m - m1)) + f1 * (q.z + q.y * (q.x - m1));
+            S = f0 * S + f1 * q.y;
+            Z += (double)q.w;
+            m = m1;
+        };
+        for (int k = tid; k < p.halves; k += 8 * kHsThreads) {       // (eight loads under way)
+            float4 q[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = __ldcg(part + k + 32 * j);
+            for (int j = 0; j < 8; ++j)
+                if (k + kHsThreads * j < p.halves) q[j] = __ldcg(part + k + kHsThreads * j);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) join(q[j]);
-    }
-    for (; k < p.halves; k += 32) join(__ldcg(part + k));
-    const float top = warp_max(m), f0 = ex2(m - top);
-    T = f0 * (T + S * (m - top));
-    S = f0 * S;
-    S = warp_sum(S);
-    T = warp_sum(T);
+            for (int j = 0; j < 8; ++j)
+                if (k + kHsThreads * j < p.halves) join(q[j]);
+        }
+        const float wm = warp_max(m);
+        if (lane == 0) s_m[warp] = wm;
+        bad = __syncthreads_or(bad ? 1 : 0) != 0;
+        float top = s_m[0];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) Z += __shfl_xor_sync(0xFFFFFFFFu, Z, o);
-    bad = __any_sync(0xFFFFFFFFu, bad);
-    if (lane != 0) return;
-    const int r = p.index ? __ldcg(p.index + row) : row;
-    const double ln2 = 0.6931471805599453, lnS = log((double)S);
-    const float nan = __int_as_float(0x7FC00000);
-    double l = ln2 * (double)fmaf(__ldcg(p.zx + row), p.c1, -top) - lnS, lse = ln2 * (double)top + lnS, H = lnS - ln2 * ((double)T / (double)S);
-    if (bad) {
-        l = lse = H = (double)nan;
-        atomicOr(c.status, ADASD_STATUS_NAN);
-    }
-    if (c.logp) c.logp[r] = (float)l;
-    if (c.H) c.H[r] = (float)(H < 0.0 ? 0.0 : H);
-    if (c.lse) c.lse[r] = (float)lse;
-    if (c.op == HEAD_CE) {
-        const double w = (c.row_weight ? (double)c.row_weight[r] : 1.0) * (double)c.scale, e = (double)c.smoothing, zc = (double)c.z_loss;
-        double L = -(1.0 - e) * l + zc * lse * lse;
-        if (e != 0.0) L -= e * (Z * p.inv_T / c.V - lse);
-        c.row_loss[r] = (float)(w * L);
-        if (p.coef) {
-            HeadCoef f;
-            f.lse2 = (float)((double)top + log2((double)S));
-            f.A = (float)(w * (1.0 + 2.0 * zc * lse) * p.inv_T);
-            f.B = (float)(-w * (1.0 - e) * p.inv_T);
-            f.C = (float)(-w * e / c.V * p.inv_T);
-            f.E = 0.f;
-            f.tok = __ldcg(p.tok + row);
-            f.pad[0] = f.pad[1] = 0.f;
-            p.coef[row] = f;
+        for (int k = 1; k < kW; ++k) top = fmaxf(top, s_m[k]);
+        const float f0 = ex2(m - top);
+        T = warp_sum(f0 * (T + S * (m - top)));
+        S = warp_sum(f0 * S);
+        Z = warp_sum_f64(Z);
+        if (lane == 0) {
+            s_S[warp] = S;
+            s_T[warp] = T;
+            s_Z[warp] = Z;
+        }
+        __syncthreads();
+        if (tid == 0) {
+#pragma unroll
+            for (int k = 1; k < kW; ++k) {
+                S += s_S[k];
+                T += s_T[k];
+                Z += s_Z[k];
+            }
+            const int r = lie ? row : __ldcg(p.index + row);
+            const double ln2 = 0.6931471805599453, lnS = log((double)S);
+            const double nan = (double)__int_as_float(0x7FC00000);
+            double l = ln2 * (double)fmaf(__ldcg(p.zx + row), p.c1, -top) - lnS, lse = ln2 * (double)top + lnS, H = lnS - ln2 * ((double)T / (double)S);
+            if (bad) {
+                l = lse = H = nan;
+                atomicOr(c.status, ADASD_STATUS_NAN);
+            }
+            if (c.logp) c.logp[r] = (float)l;
+            if (c.H) c.H[r] = (float)(H < 0.0 ? 0.0 : H);
+            if (c.lse) c.lse[r] = (float)lse;
+            if (c.op == HEAD_CE) {
+                const double w = (c.row_weight ? (double)c.row_weight[r] : 1.0) * (double)c.scale, e = (double)c.smoothing, zc = (double)c.z_loss;
+                double L = -(1.0 - e) * l + zc * lse * lse;
+                if (e != 0.0) L -= e * (Z * p.inv_T / c.V - lse);
+                c.row_loss[r] = (float)(w * L);
+                if (p.coef) {
+                    HeadCoef f;
+                    f.lse2 = (float)((double)top + lnS * 1.4426950408889634);
+                    f.A = (float)(w * (1.0 + 2.0 * zc * lse) * p.inv_T);
+                    f.B = (float)(-w * (1.0 - e) * p.inv_T);
+                    f.C = (float)(-w * e / c.V * p.inv_T);
+                    f.E = 0.f;
+                    f.tok = __ldcg(p.tok + row);
+                    f.pad[0] = f.pad[1] = 0.f;
+                    p.coef[row] = f;
+                }
+            }
+        }
+    } else if (lie && listed && tid == 0) {
+        if (counts) {
+            p.coef[row] = head_given(c, row, p.inv_T);
+        } else {
+            head_left_out(c, row);
+            if (p.coef) {
+                HeadCoef f;
+                f.lse2 = f.A = f.B = f.C = f.E = f.pad[0] = f.pad[1] = 0.f;
+                f.tok = -1;
+                p.coef[row] = f;
+            }
         }
     }
+    if (!p.ticket) return;
+    if (tid == 0) {
+        __threadfence();
+        s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1 ? 1u : 0u;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    double sum = 0.0;
+    for (int k = tid; k < c.n_rows; k += kHsThreads) sum += (double)__ldcg(c.row_loss + k);
+    sum = warp_sum_f64(sum);
+    if (lane == 0) s_Z[warp] = sum;
+    __syncthreads();
+    if (tid == 0) {
+        for (int k = 1; k < kW; ++k) sum += s_Z[k];
+        *c.loss = (float)sum;
+    }
+}
+
+// G of few rows from their logits, in planes or with what rounding took from it.  A CTA a row and 1024 columns, eight a thread.
+constexpr int kHxThreads = 128, kHxColumns = kHxThreads * 8;
+__global__ void __launch_bounds__(kHxThreads) head_g_kernel(const __grid_constant__ HeadRows p) {
+    const int width = (p.vn + kHgN - 1) / kHgN * kHgN, parts = (width + kHxColumns - 1) / kHxColumns;
+    const int row = blockIdx.x / parts, col = (int)(blockIdx.x - row * parts) * kHxColumns + threadIdx.x * 8;
+    pdl_wait();
+    pdl_trigger();
+    float v[8];
+    float4 f = make_float4(0.f, 0.f, 0.f, 0.f), f2 = make_float4(0.f, __int_as_float(-1), 0.f, 0.f);
+    if (row < p.c.n_rows) {
+        f = __ldcg(reinterpret_cast<const float4*>(p.coef + row));
+        f2 = __ldcg(reinterpret_cast<const float4*>(p.coef + row) + 1);
+    }
+    const float lse2 = f.x, A = f.y, B = f.z, C = f.w, E = f2.x;
+    const int tok = __float_as_int(f2.y), x = tok - p.v0 - col, nv = tok >= 0 ? min(p.vn, p.c.V - p.v0) - col : 0;
+    float lost = 0.f;
+    if (col < width) {
+        const float* z = p.z + row * p.z_stride + p.v0 + col;
+#pragma unroll
+        for (int j = 0; j < 8; j += 4) {
+            float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (nv >= j + 4) q = __ldcg(reinterpret_cast<const float4*>(z + j));
+            else if (nv > j) q = make_float4(z[j], nv > j + 1 ? z[j + 1] : 0.f, nv > j + 2 ? z[j + 2] : 0.f, 0.f);
+            v[j] = q.x; v[j + 1] = q.y; v[j + 2] = q.z; v[j + 3] = q.w;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float u = fmaf(v[j], p.c1, -lse2), e = ex2(u);
+            float y = fmaf(e, fmaf(E, u, A), C);
+            if (x == j) y = fmaf(A, expm1f(u * kLn2), A + B) + fmaf(e * E, u, C);        // (as in a tile)
+            v[j] = j < nv ? y : 0.f;
+        }
+        uint4 w = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        uint16_t* dst = p.g + (long long)row * p.piece + col;
+        *reinterpret_cast<uint4*>(dst) = w;
+        const uint32_t* u = &w.x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] -= __uint_as_float(u[j] << 16);
+            v[2 * j + 1] -= __uint_as_float(u[j] & 0xFFFF0000u);
+            lost += v[2 * j] + v[2 * j + 1];
+        }
+        if (p.planes == 2)
+            *reinterpret_cast<uint4*>(dst + (long long)kHgPlaneRows * p.piece) =
+                make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    }
+    if (!p.res) return;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) lost += __shfl_xor_sync(0xFFFFFFFFu, lost, o);       // (16 threads: 128 columns)
+    if ((threadIdx.x & 15) == 0 && row < p.c.n_rows && col < p.vn) const_cast<float*>(p.res)[(long long)row * p.res_halves + (p.v0 + col) / kHgHalf] = lost;
 }
 
 // A CTA a part of a row, eight columns a thread; where there are several sums (splits, and both planes of each), groups of threads deal them out among
 // them.  The sums' total, what rounding took from the row's G times w_x, rounded to bf16, to the row's place.
-__host__ __device__ inline int head_groups(int sums) { return sums >= 4 ? 4 : sums >= 2 ? 2 : 1; }
+__host__ __device__ inline int head_groups(int sums) { return sums >= 64 ? 16 : sums >= 16 ? 8 : sums >= 4 ? 4 : sums >= 2 ? 2 : 1; }
 __global__ void __launch_bounds__(kHrThreads) head_grad_rows_kernel(const __grid_constant__ HeadRows p) {
     __shared__ float s_lost[kHrThreads / 32];
     __shared__ float4 s_sum[kHrThreads][2];
@@ -748,7 +896,7 @@ __global__ void __launch_bounds__(kHrThreads) head_grad_rows_kernel(const __grid
     const int group = threadIdx.x / width, t = threadIdx.x - group * width, d = ((int)(blockIdx.x - row * parts) * width + t) * 8;
     pdl_wait();
     pdl_trigger();
-    if (row >= __ldcg(p.n_active)) return;
+    if (row >= (p.index ? __ldcg(p.n_active) : c.n_rows)) return;
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (d < c.D) {                                           // (D is a multiple of 8)
 #pragma unroll 4
@@ -777,16 +925,17 @@ __global__ void __launch_bounds__(kHrThreads) head_grad_rows_kernel(const __grid
         s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
         s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
     }
-    if (p.res) {
+    const int tok = __ldcg(p.tok + row);
+    if (p.res && tok >= 0 && tok < c.V) {                    // (as they lie: a row left out has lost nothing)
         lost = 0.f;
 #pragma unroll
         for (int k = 0; k < kHrThreads / 32; ++k) lost += s_lost[k];
         float x[8];
-        unpack16(__ldcg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(c.weight) + (long long)__ldcg(p.tok + row) * c.w_stride + d)), x);
+        unpack16(__ldcg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(c.weight) + (long long)tok * c.w_stride + d)), x);
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[j] = fmaf(lost, x[j], s[j]);
     }
-    uint16_t* dst = static_cast<uint16_t*>(c.grad_h) + (long long)__ldcg(p.index + row) * c.gh_stride + d;
+    uint16_t* dst = static_cast<uint16_t*>(c.grad_h) + (long long)(p.index ? __ldcg(p.index + row) : row) * c.gh_stride + d;
     const uint4 w = make_uint4(pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3]), pack_bf16(s[4], s[5]), pack_bf16(s[6], s[7]));
     if ((reinterpret_cast<uintptr_t>(dst) & 15u) == 0) {
         *reinterpret_cast<uint4*>(dst) = w;

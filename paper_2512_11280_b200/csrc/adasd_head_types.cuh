@@ -35,6 +35,7 @@ struct HeadCall {
     const float* row_weight;                       // HEAD_CE; nullable
     float smoothing, z_loss, scale;
     float* row_loss;
+    float* loss;                                   // nullable [1]
     void* grad_h;                                  // nullable
     long long gh_stride;
     void* grad_w;                                  // nullable
