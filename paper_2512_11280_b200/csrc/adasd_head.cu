@@ -211,6 +211,7 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     t.n_rows = c.n_rows;
     t.c1 = r.c1;
     t.columns = L.columns;
+    t.entropy = c.H != nullptr;
     t.part = reinterpret_cast<float4*>(s + L.big);
     t.halves = L.halves;
     t.res_halves = L.res_halves;

@@ -69,6 +69,7 @@ struct HeadTiles {
     const int32_t* tok;
     float c1;                            // log2 e / T
     int32_t columns;                     // TILE_STATS: of a tile
+    int32_t entropy;                     // TILE_STATS: the entropy's sums too
     int32_t h_boxes, h_box_rows;         // one CTA's tiles of logits: its rows come in so many boxes of so many rows (below the last: whatever is there)
     float4* part;                        // TILE_STATS: [row][halves], a tile's first 128 columns and the others
     float* res;                          // TILE_G: [row][res_halves], 128 columns each: sums of what rounding took from G; nullable
@@ -163,40 +164,66 @@ struct HeadWork {
 };
 
 // ---- epilogues: a thread has a row (lane) and 32 columns at a time ------------------------------------
+__device__ __forceinline__ float2 two(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 pair_of(const float (&z)[32], int j) { return make_float2(z[2 * j], z[2 * j + 1]); }
+
 struct RowStats {
     float m, S, T, Z;
     __device__ __forceinline__ void clear() {
         m = kFloor;
         S = T = Z = 0.f;
     }
-    __device__ __forceinline__ void add(float (&z)[32], int nv, float c1) {
-        float top = kFloor, sum = 0.f;
-        if (nv < 32) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                if (j < nv) sum += z[j];
-                else z[j] = kFloor;
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) sum += z[j];
-        }
-        Z += sum;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) top = fmaxf(top, z[j]);
-        const float m1 = fmaxf(m, top * c1), f = ex2(m - m1);
+    // the largest so far is now m1
+    __device__ __forceinline__ void move(float m1) {
+        const float f = ex2(m - m1);
         T = f * (T + S * (m - m1));
         S = f * S;
         m = m1;
-        float s = 0.f, t = 0.f;
+    }
+    // 32 logits; ENT: with sum 2^u u
+    template <bool ENT>
+    __device__ __forceinline__ void add(const float (&z)[32], float c1) {
+        float top[4] = {kFloor, kFloor, kFloor, kFloor};
+        float2 sum[2] = {two(0.f), two(0.f)};
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const float u = nv < 32 && j >= nv ? kFloor : fmaf(z[j], c1, -m1), e = ex2(u);
-            s += e;
-            t = fmaf(e, u, t);
+        for (int j = 0; j < 16; ++j) {
+            sum[j & 1] = __fadd2_rn(sum[j & 1], pair_of(z, j));
+            top[j & 3] = fmaxf(top[j & 3], fmaxf(z[2 * j], z[2 * j + 1]));
         }
-        S += s;
-        T += t;
+        sum[0] = __fadd2_rn(sum[0], sum[1]);
+        Z += sum[0].x + sum[0].y;
+        move(fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c1));
+        float2 s[2] = {two(0.f), two(0.f)}, t[2] = {two(0.f), two(0.f)};
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float2 u = __ffma2_rn(pair_of(z, j), two(c1), two(-m)), e = make_float2(ex2(u.x), ex2(u.y));
+            s[j & 1] = __fadd2_rn(s[j & 1], e);
+            if (ENT) t[j & 1] = __ffma2_rn(e, u, t[j & 1]);
+        }
+        s[0] = __fadd2_rn(s[0], s[1]);
+        S += s[0].x + s[0].y;
+        if (ENT) {
+            t[0] = __fadd2_rn(t[0], t[1]);
+            T += t[0].x + t[0].y;
+        }
+    }
+    // the first nv of 32
+    __device__ __forceinline__ void add_some(const float (&z)[32], int nv, float c1) {
+        float top = kFloor;
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < nv) {
+                Z += z[j];
+                top = fmaxf(top, z[j]);
+            }
+        move(fmaxf(m, top * c1));
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < nv) {
+                const float u = fmaf(z[j], c1, -m), e = ex2(u);
+                S += e;
+                T = fmaf(e, u, T);
+            }
     }
 };
 
@@ -411,6 +438,15 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                 }
             };
             if constexpr (kParts) {
+                bool in = row < n_active;
+                int tok = -1;                                // (asked for ahead of the sums)
+                float4 f = make_float4(0.f, 0.f, 0.f, 0.f), f2 = f;          // HeadCoef
+                if (TILE == TILE_STATS) {
+                    if (in) tok = __ldcg(p.tok + row);
+                } else if (in) {
+                    f = __ldcg(reinterpret_cast<const float4*>(p.coef + row));
+                    f2 = __ldcg(reinterpret_cast<const float4*>(p.coef + row) + 1);
+                }
                 float z[4][32];                              // the logits of 128 columns
                 {
                     const uint32_t acc = next();
@@ -433,18 +469,20 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                         tensor_wait(vb);
                         if (g == 2) release();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            z[g][j] += va[j];
-                            z[g + 1][j] += vb[j];
+                        for (int j = 0; j < 16; ++j) {
+                            const float2 x = __fadd2_rn(pair_of(z[g], j), pair_of(va, j)), y = __fadd2_rn(pair_of(z[g + 1], j), pair_of(vb, j));
+                            z[g][2 * j] = x.x;
+                            z[g][2 * j + 1] = x.y;
+                            z[g + 1][2 * j] = y.x;
+                            z[g + 1][2 * j + 1] = y.y;
                         }
                     }
                 }
                 if (!ok) break;
-                bool in = row < n_active;
                 if constexpr (TILE == TILE_STATS) {
                     if (m0 + quarter * 32 >= n_active) continue;
                     // (a token outside the vocabulary, however far: in no column)
-                    const int x = in ? (int)min((uint32_t)__ldcg(p.tok + row), 0x7FFFFFFFu) - p.v0 - c0 : -1;
+                    const int x = in ? (int)min((uint32_t)tok, 0x7FFFFFFFu) - p.v0 - c0 : -1;
                     RowStats r;
                     r.clear();
 #pragma unroll
@@ -468,22 +506,20 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                                         if (j < nv) dst[j] = z[g][j];
                                 }
                             }
-                            r.add(z[g], nv, p.c1);
+                            if (nv < 32) r.add_some(z[g], nv, p.c1);
+                            else if (p.entropy) r.add<true>(z[g], p.c1);
+                            else r.add<false>(z[g], p.c1);
                         }
                     }
                     if (in) p.part[(long long)row * p.halves + n0 / w.columns * 2 + half] = make_float4(r.m, r.S, r.T, r.Z);
                 } else {
-                    float4 f = make_float4(0.f, 0.f, 0.f, 0.f), f2 = f;      // HeadCoef
-                    if (in) {
-                        f = __ldcg(reinterpret_cast<const float4*>(p.coef + row));
-                        f2 = __ldcg(reinterpret_cast<const float4*>(p.coef + row) + 1);
-                    }
                     const float lse2 = f.x, A = f.y, B = f.z, C = f.w, E = f2.x;
                     const bool listed = in;
                     in = in && __float_as_int(f2.y) >= 0;    // (rows as they lie: not one that is left out, whose logits may be anything)
                     const int x = in ? __float_as_int(f2.y) - p.v0 - c0 : -1;
-                    const bool rows_kept = p.planes == 1 || m0 + quarter * 32 < kHgPlaneRows;
-                    float lost = 0.f;
+                    const bool all_in = __all_sync(0xFFFFFFFFu, in);
+                    const bool rows_kept = CG == 2 || p.planes == 1 || m0 + quarter * 32 < kHgPlaneRows;
+                    float2 lost = two(0.f);
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         float(&v)[32] = z[g];
@@ -496,28 +532,43 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                             const float u = fmaf(pick(v, x - 32 * g), p.c1, -lse2);
                             at = fmaf(A, expm1f(u * kLn2), A + B) + fmaf(ex2(u) * E, u, C);
                         }
+                        if (all_in && p.V - p.v0 - c0 - 32 * g >= 32) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float u = fmaf(v[j], p.c1, -lse2);
-                            v[j] = j < nv ? fmaf(ex2(u), fmaf(E, u, A), C) : 0.f;
+                            for (int j = 0; j < 16; ++j) {
+                                const float2 u = __ffma2_rn(pair_of(v, j), two(p.c1), two(-lse2)), e = make_float2(ex2(u.x), ex2(u.y));
+                                const float2 y = __ffma2_rn(e, __ffma2_rn(two(E), u, two(A)), two(C));
+                                v[2 * j] = y.x;
+                                v[2 * j + 1] = y.y;
+                            }
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                const float u = fmaf(v[j], p.c1, -lse2);
+                                v[j] = j < nv ? fmaf(ex2(u), fmaf(E, u, A), C) : 0.f;
+                            }
                         }
                         if (any) put_at(v, here ? x - 32 * g : -1, at);
                         if (g & 1) {
                             const int y = m0 + quarter * 32;
                             store64(z[g - 1], v, c0 + 32 * (g - 1), y, rows_kept);
-                            if (p.planes == 2 || p.res) {
+                            if ((CG == 1 && p.planes == 2) || p.res) {
 #pragma unroll
                                 for (int q = g - 1; q <= g; ++q)
 #pragma unroll
-                                    for (int j = 0; j < 32; ++j) {
-                                        z[q][j] -= __uint_as_float(pack_bf16(0.f, z[q][j]) & 0xFFFF0000u);
-                                        lost += z[q][j];
+                                    for (int j = 0; j < 16; ++j) {
+                                        const float2 a = pair_of(z[q], j);
+                                        uint32_t h;                  // (again, instead of kept)
+                                        asm volatile("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(a.y), "f"(a.x));
+                                        const float2 d = __ffma2_rn(make_float2(__uint_as_float(h << 16), __uint_as_float(h & 0xFFFF0000u)), two(-1.f), a);
+                                        z[q][2 * j] = d.x;
+                                        z[q][2 * j + 1] = d.y;
+                                        lost = __fadd2_rn(lost, d);
                                     }
                             }
-                            if (p.planes == 2) store64(z[g - 1], v, c0 + 32 * (g - 1), y + kHgPlaneRows, rows_kept);
+                            if (CG == 1 && p.planes == 2) store64(z[g - 1], v, c0 + 32 * (g - 1), y + kHgPlaneRows, rows_kept);
                         }
                     }
-                    if (listed && p.res && c0 < p.vn) p.res[(long long)row * p.res_halves + (p.v0 + c0) / kHgHalf] = lost;
+                    if (listed && p.res && c0 < p.vn) p.res[(long long)row * p.res_halves + (p.v0 + c0) / kHgHalf] = lost.x + lost.y;
                 }
             } else {
                 const uint32_t acc = next();
