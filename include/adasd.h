@@ -434,7 +434,7 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
  * (ADASD_ERR_DTYPE), and so is a context of fp32 rows.
  *   - hidden_dev: row r at r * hidden_stride (elements), any alignment.  weight_dev: row v at v * weight_stride; it starts at a
  *     multiple of 16 bytes and weight_stride is a multiple of 8 (ADASD_ERR_ALIGN, ADASD_ERR_SHAPE).  dim: a multiple of 8 up to
- *     65536.  n_rows up to 2^22, 0 included.
+ *     65536.  n_rows up to 2^22, 0 included; V up to 2^30.
  *   - Gradients are bf16: grad_hidden_dev as the hidden states, grad_weight_dev as the weight (each nullable, with its stride).  Every element of the
  *     n_rows and of the V rows is written, what lies between rows is left as it was.  A row left out has a gradient of zeros and adds nothing
  *     to the weight's, whatever its hidden states hold (NaN too).  Gradients, inputs and scratch must not overlap (ADASD_ERR_SHAPE).

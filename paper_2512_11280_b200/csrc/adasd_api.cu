@@ -1194,7 +1194,7 @@ static int check_head(const adasd_ctx* ctx, HeadCall& c, int32_t op, const void*
     if (grad_w && (gw_stride < dim || gw_stride > most || gw_stride % 8 != 0)) return ADASD_ERR_SHAPE;
     if (int rc = check_device(ctx)) return rc;
     if (ctx->cfg.dtype != ADASD_BF16 || ctx->cuts_on()) return ADASD_ERR_DTYPE;
-    if (!std::isfinite(kLog2e / ctx->temperature)) return ADASD_ERR_SHAPE;
+    if (!std::isfinite(kLog2e / ctx->temperature) || ctx->cfg.V > kHeadMaxV) return ADASD_ERR_SHAPE;
     const int V = ctx->cfg.V;
     const Extent h = rows_extent(hidden, h_stride, n_rows, dim), w = rows_extent(weight, w_stride, V, dim),
                  gh = rows_extent(grad_h, gh_stride, n_rows, dim), gw = rows_extent(grad_w, gw_stride, V, dim),
@@ -1231,6 +1231,7 @@ static int run_head(const HeadCall& c, cudaStream_t stream) {
 int adasd_head_scratch(adasd_ctx* ctx, int32_t n_rows, int32_t dim, int32_t with_grad, size_t* bytes_out) {
     if (!ctx || !bytes_out) return ADASD_ERR_NULL;
     if (n_rows < 0 || n_rows > (1 << 22) || dim < 8 || dim > 65536 || dim % 8 != 0 || with_grad < 0 || with_grad > 1) return ADASD_ERR_SHAPE;
+    if (ctx->cfg.V > kHeadMaxV) return ADASD_ERR_SHAPE;
     *bytes_out = head_scratch_bytes(n_rows, ctx->cfg.V, dim, with_grad != 0, ctx->sm_count);
     return ADASD_OK;
 }

@@ -9,6 +9,8 @@
 
 namespace adasd {
 
+constexpr int kHeadMaxV = 1 << 30;                   // (columns are counted in 32 bits, tiles beyond the last included)
+
 enum HeadOp : int32_t {
     HEAD_LOGPROB,        // log-probs, entropies
     HEAD_GIVEN,          // gradients of a loss with given dL/dl, dL/dH

@@ -119,6 +119,69 @@ def test_logprob_gradient(torch, n, V, D, entropy):
         assert ctx.status() == 0
 
 
+# rows about 16 (what the products along few rows take at a time), a plane of 64 and a tile of 128; a vocabulary of more than one piece for few rows
+@pytest.mark.parametrize("n,V,D", [(15, 400, 64), (16, 400, 136), (17, 3000, 64), (63, 500, 72), (64, 777, 256), (65, 700, 136), (112, 1500, 64), (127, 257, 520),
+                                   (128, 900, 1032), (129, 255, 72), (256, 600, 200), (257, 513, 64), (3, 1050000, 8), (100, 1049000, 8)])
+def test_few_rows(torch, n, V, D):
+    h, w, tok, g = inputs(torch, n, V, D, n + V, out=0.3)
+    ctx, ref = context(V), Head(h, w, tok)
+    sc, border = scratch_for(torch, ctx, n, D, True)
+    rl, lp, lse, H, total = out(torch, n, 4) + out(torch, 1)
+    gh, gw = torch.full_like(h, 9.0), torch.full_like(w, 9.0)
+    ctx.head_cross_entropy(h, w, tok, rl, sc, label_smoothing=0.05, scale=0.5, loss_out=total, logp_out=lp, grad_hidden_out=gh, grad_weight_out=gw)
+    loss, tol, G, size = ref.cross_entropy(None, 0.05, 0.0, 0.5)
+    assert bool(((rl.double() - loss).abs() <= tol).all())
+    assert abs(float(total) - float(rl.double().sum())) <= 2 * U * float(rl.double().abs().sum())
+    ref.close_logp(lp)
+    ref.close_grads(G, size, gh, gw)
+    # by given dL/dl, from a forward pass in a scratch of its own size
+    sc2, border2 = scratch_for(torch, ctx, n, D, False)
+    ctx.head_logprob(h, w, tok, lp, sc2, H, lse)
+    ref.close_logp(lp)
+    ref.close_lse(lse)
+    dl = torch.randn(n, generator=g, device="cuda")
+    gh.fill_(9.0)
+    gw.fill_(9.0)
+    ctx.head_logprob_grad(h, w, tok, lse, dl, sc, grad_hidden_out=gh, grad_weight_out=gw)
+    G, size = ref.given(dl, None)
+    ref.close_grads(G, size, gh, gw)
+    assert bool((border == 255).all()) and bool((border2 == 255).all()) and ctx.status() == 0
+
+
+def test_captured_ahead_of_any_other_call(torch):
+    """In a process of its own: the first calls of all are captured."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch, paper_2512_11280_b200 as adasd
+torch.manual_seed(0)
+for n in (5, 200):
+    V, D = 1000, 64
+    h, w = torch.randn(n, D, device="cuda").bfloat16(), (torch.randn(V, D, device="cuda") / 8).bfloat16()
+    tok = torch.randint(0, V, (n,), device="cuda").int()
+    ctx = adasd.Context(1, V, 1, list_capacity=1)
+    sc = torch.empty(ctx.head_scratch(n, D, True), dtype=torch.uint8, device="cuda")
+    t = dict(param=w.float(), param_copy=w, grad=torch.empty_like(w), exp_avg=torch.zeros(V, D, device="cuda"), exp_avg_sq=torch.zeros(V, D, device="cuda"))
+    rl, gh = torch.empty(n, device="cuda"), torch.empty_like(h)
+    table = ctx.adamw_table([t])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        ctx.head_cross_entropy(h, w, tok, rl, sc, scale=1.0 / n, grad_hidden_out=gh, grad_weight_out=t["grad"])
+        ctx.adamw_step(table, 1e-2, 1)
+    ref = -torch.log_softmax(h.double() @ w.double().t(), -1).gather(1, tok.long()[:, None])[:, 0] / n
+    g.replay()
+    torch.cuda.synchronize()
+    assert float((rl - ref).abs().max()) < 1e-4, float((rl - ref).abs().max())
+    assert bool((w == t["param"].bfloat16()).all()) and bool(t["grad"].any()) and ctx.status() == 0
+print("fine")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stderr[-2000:]
+
+
 @pytest.mark.parametrize("n,V,D", [(70000, 5000, 64), (20000, 20011, 72)])
 def test_vocabulary_in_pieces(torch, n, V, D):
     """So many rows that the gradient's piece holds a part of the vocabulary; checked on parts of rows."""
