@@ -10,13 +10,13 @@
 namespace adasd {
 namespace {
 
-// What a call keeps in its scratch.  (Statistics of the tiles and a piece of the gradient are never needed at once: they share their place.)
+// What a call keeps in its scratch.  (Of many rows statistics of the tiles and a piece of the gradient are never needed at once: they share their place.)
 struct Layout {
     int n_pad, D8, Dp, tiles;                        // tiles: 256 columns of the vocabulary
     int columns, halves, res_halves;                 // columns of a tile of the statistics; as in HeadTiles
     int piece, splits, planes;                       // columns of a piece; parts that grad_h's sums along them are cut into; planes of G
     long long z_stride;
-    size_t h, index, tok, n_active, ticket, zx, coef, res, z, big, acc, total;
+    size_t h, index, tok, n_active, ticket, zx, coef, res, z, part, big, acc, total;
 };
 
 // Tiles of pairs where the rows fill more than one CTA's.
@@ -97,7 +97,10 @@ Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
         g = (size_t)L.n_pad * L.piece * 2;
         acc = (size_t)L.splits * L.n_pad * L.Dp * 4;
     }
-    L.big = take(std::max(part, g));
+    const bool apart = gradient && n_rows <= kHgM;   // (head_g_kernel reads the one while it writes the other)
+    L.part = take(apart ? part : 0);
+    L.big = take(std::max(apart ? 0 : part, g));
+    if (!apart) L.part = L.big;
     L.acc = take(acc);
     L.total = at;
     return L;
@@ -173,7 +176,7 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     r.n_active = reinterpret_cast<int32_t*>(s + L.n_active);
     r.zx = reinterpret_cast<float*>(s + L.zx);
     r.coef = gradient ? reinterpret_cast<HeadCoef*>(s + L.coef) : nullptr;
-    r.part = reinterpret_cast<const float4*>(s + L.big);
+    r.part = reinterpret_cast<const float4*>(s + L.part);
     r.acc = reinterpret_cast<const float*>(s + L.acc);
     r.acc_slot = (long long)L.n_pad * L.Dp;
     r.Dp = L.Dp;
@@ -212,7 +215,7 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     t.c1 = r.c1;
     t.columns = L.columns;
     t.entropy = c.H != nullptr;
-    t.part = reinterpret_cast<float4*>(s + L.big);
+    t.part = reinterpret_cast<float4*>(s + L.part);
     t.halves = L.halves;
     t.res_halves = L.res_halves;
     t.planes = L.planes;
@@ -242,7 +245,7 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     }
     if (c.op != HEAD_GIVEN)
         if (int rc = launch_tiles<TILE_STATS>(t, pairs, c.sm_count, stream)) return rc;
-    if (c.op != HEAD_GIVEN || as_they_lie)
+    if (!from_logits && (c.op != HEAD_GIVEN || as_they_lie))
         if (int rc = launch_pdl(head_stats_kernel, as_they_lie && gradient ? rows16 : c.n_rows, kHsThreads, 0, 0, stream, r)) return rc;
     if (c.loss && !r.ticket)
         if (int rc = launch_total(c.row_loss, c.n_rows, c.loss, stream)) return rc;
@@ -260,7 +263,8 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
             if (int rc = make_map(&h_grad, r.h, L.n_pad, c.D, L.D8, 64)) return rc;
     }
     if (int rc = make_map(&t.g, g, L.n_pad, L.piece, L.piece, 64)) return rc;
-    if (int rc = make_map(&g_out, g, L.n_pad, L.piece, L.piece, 32)) return rc;
+    if (!from_logits)
+        if (int rc = make_map(&g_out, g, L.n_pad, L.piece, L.piece, 32)) return rc;
     if (c.grad_w)
         if (int rc = make_map(&gw_out, c.grad_w, c.V, c.D, c.gw_stride, 32)) return rc;
     for (int v0 = 0; v0 < c.V; v0 += L.piece) {
@@ -273,8 +277,12 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
         if (from_logits) {
             r.v0 = v0;
             r.vn = t.vn;
-            const int parts = ((t.vn + kHgN - 1) / kHgN * kHgN + kHxColumns - 1) / kHxColumns;
-            if (int rc = launch_pdl(head_g_kernel, rows16 * parts, kHxThreads, 0, 0, stream, r)) return rc;
+            // CTAs: about four for a SM
+            const int width = (t.vn + kHgN - 1) / kHgN * kHgN, most = (width + kHxColumns - 1) / kHxColumns;
+            const int want = std::max(1, std::min(most, (4 * c.sm_count + rows16 - 1) / rows16));
+            r.columns = (most + want - 1) / want * kHxColumns;
+            const int parts = (width + r.columns - 1) / r.columns;
+            if (int rc = launch_pdl(head_g_kernel, rows16 * parts, kHsThreads, 0, 0, stream, r)) return rc;
         } else {
             if (int rc = launch_tiles<TILE_G>(t, pairs, c.sm_count, stream)) return rc;
         }

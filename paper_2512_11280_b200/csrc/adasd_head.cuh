@@ -10,7 +10,8 @@
 // most 256 MB, or 2048 columns) instead of n V values.
 //
 // Precision.  The accumulator in tensor memory is cut, not rounded, to 24 bits with every 16 products: after 4096 of them logits were 9e-6 of their size
-// too small.  Logits are therefore summed from parts of 256 products, the parts added in fp32 by the threads of the epilogue (below 1e-6).
+// too small.  Logits are therefore summed from parts of 512 products (256 where the products are not the bound), the parts added in fp32 by the threads of the
+// epilogue: below 1e-6, for 4 % of the time.
 // G is rounded to bf16, as the products' operands are (2^-8 at most; both gradients are rounded to bf16 once more when they are written).  In grad_h = sum_v g_v w_v
 // the rounding errors e_v do not cancel as the g_v do, which add up to 0 in a row, and what the w_v have in common (a mean, the tokens' frequencies) is
 // multiplied with their sum; so the row's sum of e_v times w_x is taken off again (what is left are errors times differences of w_v): 0.009 -> 0.002 of
@@ -44,7 +45,9 @@ constexpr int kHgOut = 32 * 64 * 2;                          // 32 rows of 64 bf
 constexpr int kHgEpi = 8, kHgFirst = 4, kHgThreads = 32 * (kHgFirst + kHgEpi);
 constexpr int kHgLaunchRegs = 168, kHgFewRegs = 56, kHgManyRegs = 224;
 static_assert(kHgFewRegs * kHgFirst + kHgManyRegs * kHgEpi <= kHgLaunchRegs * (kHgFirst + kHgEpi), "a group that takes more than others gave would wait for good");
-constexpr int kHgPart = 8;                                   // steps along K of a part of the logits' sums
+// Steps along K of a part of the logits' sums: 512 products where the products are the bound, 256 where a CTA on its own waits for memory.
+template <int CG>
+constexpr int kHgPart = CG == 1 ? 4 : 8;
 constexpr int kHgRing = 192 * 1024;                         // 4 stages of 48 KB or 6 of 32
 constexpr int kHgSmem = 1024 + kHgRing + kHgEpi * kHgOut + 256;
 constexpr uint32_t kHgPause = 1u << 16;                       // polls that a copy under way surely ends within
@@ -284,6 +287,12 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
         asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_never) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (threadIdx.x == 32 * kHgFirst) {                      // (the maps are arguments: nobody writes them)
+        tma_prefetch(&p.w);
+        tma_prefetch(&p.h);
+        if (TILE == TILE_GRADS) tma_prefetch(&p.g);
+        if (TILE != TILE_STATS) tma_prefetch(&p.out);
+    }
     if (warp == 1) tensor_alloc<CG>(smem_u32(&s_tmem), 512);
     tensor_fence_before();
     cg::cluster_group cluster = cg::this_cluster();
@@ -372,7 +381,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                 const uint32_t kind = product_kind(kHgM * CG, TILE == TILE_STATS && CG == 1 ? w.columns : kHgN, a_mn, !kParts);
                 int k = t.k0;
                 do {                                         // (a part, or the whole of the tile's sum)
-                    const int end = kParts ? min(k + kHgPart, t.k1) : t.k1;
+                    const int end = kParts ? min(k + kHgPart<CG>, t.k1) : t.k1;
                     const uint32_t buf = n & 1u;
                     ok = wait_or_give_up(acc_empty + 8 * buf, ((n >> 1) & 1u) ^ 1u, &s_gave_up);
                     tensor_fence_after();
@@ -457,7 +466,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                     for (int g = 0; g < 4; ++g) tensor_wait(z[g]);
                     release();
                 }
-                for (int k = k0 + kHgPart; k < k1; k += kHgPart) {
+                for (int k = k0 + kHgPart<CG>; k < k1; k += kHgPart<CG>) {
                     const uint32_t acc = next();
                     if (!ok) break;
 #pragma unroll
@@ -625,7 +634,7 @@ struct HeadRows {
     const float* z;                      // head_g_kernel: the logits
     long long z_stride;
     uint16_t* g;                         // ... and the piece of G
-    int32_t v0, vn, piece;
+    int32_t v0, vn, piece, columns;
     uint16_t* h;                         // [n_pad][D8]: the rows that count, together
     int32_t D8, halves;
     int32_t rows;                        // of a CTA of head_rows_kernel
@@ -753,103 +762,144 @@ __global__ void __launch_bounds__(kHrThreads) head_rows_kernel(const __grid_cons
     }
 }
 
-// A CTA a row: the tiles' statistics joined, the row's outputs, its gradient's constants; the last CTA adds up the losses, in the rows' order.
-// Without an index the rows are taken as they lie, those left out among them; for a gradient a copy of them, with zeros for the latter and up to the next
-// multiple of 16 rows, is what its products read.
+// Of a row by the 128 threads of a CTA: the tiles' statistics joined; by its first thread (returns true there): what the row reports, its gradient's constants.
 constexpr int kHsThreads = 128;
-__global__ void __launch_bounds__(kHsThreads) head_stats_kernel(const __grid_constant__ HeadRows p) {
+struct HeadRow {
+    float logp, H, lse, loss;
+    HeadCoef f;
+};
+__device__ __forceinline__ bool head_join(const HeadRows& p, int row, int r, HeadRow& out) {
     constexpr int kW = kHsThreads / 32;
     __shared__ float s_m[kW], s_S[kW], s_T[kW];
     __shared__ double s_Z[kW];
-    __shared__ uint32_t s_last;
     const HeadCall& c = p.c;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const float4* part = p.part + (long long)row * p.halves;
+    float m = kFloor, S = 0.f, T = 0.f;
+    double Z = 0.0;
+    bool bad = false;
+    auto join = [&](const float4& q) {
+        bad |= !(fabsf(q.w) < INFINITY);                     // (a logit that is not finite shows in their sum)
+        if (q.y == 0.f && q.x == kFloor) return;             // (a half without columns)
+        bad |= !(q.y > 0.f && q.y < INFINITY) || !(fabsf(q.x) < -kFloor);
+        const float m1 = fmaxf(m, q.x), f0 = ex2(m - m1), f1 = ex2(q.x - m1);
+        T = f0 * (T + S * (m - m1)) + f1 * (q.z + q.y * (q.x - m1));
+        S = f0 * S + f1 * q.y;
+        Z += (double)q.w;
+        m = m1;
+    };
+    for (int k = tid; k < p.halves; k += 8 * kHsThreads) {   // (eight loads under way)
+        float4 q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (k + kHsThreads * j < p.halves) q[j] = __ldcg(part + k + kHsThreads * j);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (k + kHsThreads * j < p.halves) join(q[j]);
+    }
+    const float wm = warp_max(m);
+    if (lane == 0) s_m[warp] = wm;
+    bad = __syncthreads_or(bad ? 1 : 0) != 0;
+    float top = s_m[0];
+#pragma unroll
+    for (int k = 1; k < kW; ++k) top = fmaxf(top, s_m[k]);
+    const float f0 = ex2(m - top);
+    T = warp_sum(f0 * (T + S * (m - top)));
+    S = warp_sum(f0 * S);
+    Z = warp_sum_f64(Z);
+    if (lane == 0) {
+        s_S[warp] = S;
+        s_T[warp] = T;
+        s_Z[warp] = Z;
+    }
+    __syncthreads();
+    if (tid != 0) return false;
+#pragma unroll
+    for (int k = 1; k < kW; ++k) {
+        S += s_S[k];
+        T += s_T[k];
+        Z += s_Z[k];
+    }
+    const double ln2 = 0.6931471805599453, lnS = log((double)S);
+    double l = ln2 * (double)fmaf(__ldcg(p.zx + row), p.c1, -top) - lnS, lse = ln2 * (double)top + lnS, H = lnS - ln2 * ((double)T / (double)S);
+    if (bad) {
+        l = lse = H = (double)__int_as_float(0x7FC00000);
+        atomicOr(c.status, ADASD_STATUS_NAN);
+    }
+    out.logp = (float)l;
+    out.H = (float)(H < 0.0 ? 0.0 : H);
+    out.lse = (float)lse;
+    out.loss = 0.f;
+    if (c.op == HEAD_CE) {
+        const double w = (c.row_weight ? (double)c.row_weight[r] : 1.0) * (double)c.scale, e = (double)c.smoothing, zc = (double)c.z_loss;
+        double L = -(1.0 - e) * l + zc * lse * lse;
+        if (e != 0.0) L -= e * (Z * p.inv_T / c.V - lse);
+        out.loss = (float)(w * L);
+        out.f.lse2 = (float)((double)top + lnS * 1.4426950408889634);
+        out.f.A = (float)(w * (1.0 + 2.0 * zc * lse) * p.inv_T);
+        out.f.B = (float)(-w * (1.0 - e) * p.inv_T);
+        out.f.C = (float)(-w * e / c.V * p.inv_T);
+        out.f.E = 0.f;
+        out.f.tok = __ldcg(p.tok + row);
+        out.f.pad[0] = out.f.pad[1] = 0.f;
+    }
+    return true;
+}
+__device__ __forceinline__ void head_report(const HeadCall& c, int r, const HeadRow& o) {
+    if (c.logp) c.logp[r] = o.logp;
+    if (c.H) c.H[r] = o.H;
+    if (c.lse) c.lse[r] = o.lse;
+    if (c.row_loss) c.row_loss[r] = o.loss;
+}
+// A row as it lies (or zeros) to where the gradients' products read it.
+__device__ __forceinline__ void head_keep_row(const HeadRows& p, int row, bool counts) {
+    uint4* dst = reinterpret_cast<uint4*>(p.h + (long long)row * p.D8);
+    if (counts)
+        head_copy(dst, reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.c.hidden) + row * p.c.h_stride), p.D8 / 8, threadIdx.x, kHsThreads);
+    else
+        for (int j = threadIdx.x; j < p.D8 / 8; j += kHsThreads) dst[j] = make_uint4(0u, 0u, 0u, 0u);
+}
+// The last of `of` CTAs to get here adds up the losses, in the rows' order.
+__device__ __forceinline__ void head_total(const HeadRows& p, uint32_t of) {
+    constexpr int kW = kHsThreads / 32;
+    __shared__ double s_sum[kW];
+    __shared__ uint32_t s_last;
+    if (!p.ticket) return;
+    const int tid = threadIdx.x;
+    if (tid == 0) {
+        __threadfence();
+        s_last = atomicAdd(p.ticket, 1u) == of - 1u ? 1u : 0u;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    double sum = 0.0;
+    for (int k = tid; k < p.c.n_rows; k += kHsThreads) sum += (double)__ldcg(p.c.row_loss + k);
+    sum = warp_sum_f64(sum);
+    if ((tid & 31) == 0) s_sum[tid >> 5] = sum;
+    __syncthreads();
+    if (tid == 0) {
+        for (int k = 1; k < kW; ++k) sum += s_sum[k];
+        *p.c.loss = (float)sum;
+    }
+}
+
+// A CTA a row.  Without an index the rows are taken as they lie, those left out among them; for a gradient a copy of them, with zeros for the latter and
+// up to the next multiple of 16 rows, is what its products read.
+__global__ void __launch_bounds__(kHsThreads) head_stats_kernel(const __grid_constant__ HeadRows p) {
+    const HeadCall& c = p.c;
+    const int tid = threadIdx.x, row = blockIdx.x;
     const bool lie = !p.index;
     pdl_wait();
     pdl_trigger();
     const bool listed = row < (lie ? c.n_rows : __ldcg(p.n_active)), counts = listed && (!lie || head_counts(c, row));
-    if (lie && p.coef) {                                     // (n_rows and more: the row's copy)
-        uint4* dst = reinterpret_cast<uint4*>(p.h + (long long)row * p.D8);
-        if (counts)
-            head_copy(dst, reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(c.hidden) + row * c.h_stride), p.D8 / 8, tid, kHsThreads);
-        else
-            for (int j = tid; j < p.D8 / 8; j += kHsThreads) dst[j] = make_uint4(0u, 0u, 0u, 0u);
-    }
+    if (lie && p.coef) head_keep_row(p, row, counts);        // (n_rows and more: zeros)
     if (counts && c.op != HEAD_GIVEN) {
-        const float4* part = p.part + (long long)row * p.halves;
-        float m = kFloor, S = 0.f, T = 0.f;
-        double Z = 0.0;
-        bool bad = false;
-        auto join = [&](const float4& q) {
-            bad |= !(fabsf(q.w) < INFINITY);                 // (a logit that is not finite shows in their sum)
-            if (q.y == 0.f && q.x == kFloor) return;         // (a half without columns)
-            bad |= !(q.y > 0.f && q.y < INFINITY) || !(fabsf(q.x) < -kFloor);
-            const float m1 = fmaxf(m, q.x), f0 = ex2(m - m1), f1 = ex2(q.x - m1);
-            T = f0 * (T + S * (m - m1)) + f1 * (q.z + q.y * (q.x - m1));
-            S = f0 * S + f1 * q.y;
-            Z += (double)q.w;
-            m = m1;
-        };
-        for (int k = tid; k < p.halves; k += 8 * kHsThreads) {       // (eight loads under way)
-            float4 q[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (k + kHsThreads * j < p.halves) q[j] = __ldcg(part + k + kHsThreads * j);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (k + kHsThreads * j < p.halves) join(q[j]);
-        }
-        const float wm = warp_max(m);
-        if (lane == 0) s_m[warp] = wm;
-        bad = __syncthreads_or(bad ? 1 : 0) != 0;
-        float top = s_m[0];
-#pragma unroll
-        for (int k = 1; k < kW; ++k) top = fmaxf(top, s_m[k]);
-        const float f0 = ex2(m - top);
-        T = warp_sum(f0 * (T + S * (m - top)));
-        S = warp_sum(f0 * S);
-        Z = warp_sum_f64(Z);
-        if (lane == 0) {
-            s_S[warp] = S;
-            s_T[warp] = T;
-            s_Z[warp] = Z;
-        }
-        __syncthreads();
-        if (tid == 0) {
-#pragma unroll
-            for (int k = 1; k < kW; ++k) {
-                S += s_S[k];
-                T += s_T[k];
-                Z += s_Z[k];
-            }
-            const int r = lie ? row : __ldcg(p.index + row);
-            const double ln2 = 0.6931471805599453, lnS = log((double)S);
-            const double nan = (double)__int_as_float(0x7FC00000);
-            double l = ln2 * (double)fmaf(__ldcg(p.zx + row), p.c1, -top) - lnS, lse = ln2 * (double)top + lnS, H = lnS - ln2 * ((double)T / (double)S);
-            if (bad) {
-                l = lse = H = nan;
-                atomicOr(c.status, ADASD_STATUS_NAN);
-            }
-            if (c.logp) c.logp[r] = (float)l;
-            if (c.H) c.H[r] = (float)(H < 0.0 ? 0.0 : H);
-            if (c.lse) c.lse[r] = (float)lse;
-            if (c.op == HEAD_CE) {
-                const double w = (c.row_weight ? (double)c.row_weight[r] : 1.0) * (double)c.scale, e = (double)c.smoothing, zc = (double)c.z_loss;
-                double L = -(1.0 - e) * l + zc * lse * lse;
-                if (e != 0.0) L -= e * (Z * p.inv_T / c.V - lse);
-                c.row_loss[r] = (float)(w * L);
-                if (p.coef) {
-                    HeadCoef f;
-                    f.lse2 = (float)((double)top + lnS * 1.4426950408889634);
-                    f.A = (float)(w * (1.0 + 2.0 * zc * lse) * p.inv_T);
-                    f.B = (float)(-w * (1.0 - e) * p.inv_T);
-                    f.C = (float)(-w * e / c.V * p.inv_T);
-                    f.E = 0.f;
-                    f.tok = __ldcg(p.tok + row);
-                    f.pad[0] = f.pad[1] = 0.f;
-                    p.coef[row] = f;
-                }
-            }
+        const int r = lie ? row : __ldcg(p.index + row);
+        HeadRow o;
+        if (head_join(p, row, r, o)) {
+            head_report(c, r, o);
+            if (p.coef) p.coef[row] = o.f;
         }
     } else if (lie && listed && tid == 0) {
         if (counts) {
@@ -864,75 +914,76 @@ __global__ void __launch_bounds__(kHsThreads) head_stats_kernel(const __grid_con
             }
         }
     }
-    if (!p.ticket) return;
-    if (tid == 0) {
-        __threadfence();
-        s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1 ? 1u : 0u;
-    }
-    __syncthreads();
-    if (!s_last) return;
-    __threadfence();
-    double sum = 0.0;
-    for (int k = tid; k < c.n_rows; k += kHsThreads) sum += (double)__ldcg(c.row_loss + k);
-    sum = warp_sum_f64(sum);
-    if (lane == 0) s_Z[warp] = sum;
-    __syncthreads();
-    if (tid == 0) {
-        for (int k = 1; k < kW; ++k) sum += s_Z[k];
-        *c.loss = (float)sum;
-    }
+    head_total(p, gridDim.x);
 }
 
-// G of few rows from their logits, in planes or with what rounding took from it.  A CTA a row and 1024 columns, eight a thread.
-constexpr int kHxThreads = 128, kHxColumns = kHxThreads * 8;
-__global__ void __launch_bounds__(kHxThreads) head_g_kernel(const __grid_constant__ HeadRows p) {
-    const int width = (p.vn + kHgN - 1) / kHgN * kHgN, parts = (width + kHxColumns - 1) / kHxColumns;
-    const int row = blockIdx.x / parts, col = (int)(blockIdx.x - row * parts) * kHxColumns + threadIdx.x * 8;
+// Few rows of a cross entropy, as they lie: their statistics, and G from their logits, in planes or with what rounding took from it.  A CTA a row and a part of
+// the vocabulary (p.columns, a multiple of 1024); every one joins the row's statistics for itself, the first one of a row reports.  (Statistics by a launch of
+// their own: 4 us more, of 27 with 20 rows of 4000.)
+constexpr int kHxColumns = kHsThreads * 8;
+__global__ void __launch_bounds__(kHsThreads) head_g_kernel(const __grid_constant__ HeadRows p) {
+    __shared__ HeadCoef s_f;
+    const HeadCall& c = p.c;
+    const int width = (p.vn + kHgN - 1) / kHgN * kHgN, parts = (width + p.columns - 1) / p.columns;
+    const int tid = threadIdx.x, row = blockIdx.x / parts, part = blockIdx.x - row * parts;
     pdl_wait();
     pdl_trigger();
-    float v[8];
-    float4 f = make_float4(0.f, 0.f, 0.f, 0.f), f2 = make_float4(0.f, __int_as_float(-1), 0.f, 0.f);
-    if (row < p.c.n_rows) {
-        f = __ldcg(reinterpret_cast<const float4*>(p.coef + row));
-        f2 = __ldcg(reinterpret_cast<const float4*>(p.coef + row) + 1);
+    const bool listed = row < c.n_rows, counts = listed && head_counts(c, row), first = part == 0 && p.v0 == 0;
+    if (first) head_keep_row(p, row, counts);
+    if (counts) {
+        HeadRow o;
+        if (head_join(p, row, row, o)) {
+            s_f = o.f;
+            if (first) head_report(c, row, o);
+        }
+    } else if (tid == 0) {
+        s_f.lse2 = s_f.A = s_f.B = s_f.C = s_f.E = 0.f;
+        s_f.tok = -1;
+        if (first && listed) head_left_out(c, row);
     }
-    const float lse2 = f.x, A = f.y, B = f.z, C = f.w, E = f2.x;
-    const int tok = __float_as_int(f2.y), x = tok - p.v0 - col, nv = tok >= 0 ? min(p.vn, p.c.V - p.v0) - col : 0;
-    float lost = 0.f;
-    if (col < width) {
-        const float* z = p.z + row * p.z_stride + p.v0 + col;
+    __syncthreads();
+    const float lse2 = s_f.lse2, A = s_f.A, B = s_f.B, C = s_f.C;            // (a cross entropy has no E)
+    const int tok = s_f.tok, end = min(width, (part + 1) * p.columns);
+    for (int col = part * p.columns + tid * 8; col - tid * 8 < end; col += kHxColumns) {
+        const int x = tok - p.v0 - col, nv = counts ? min(p.vn, c.V - p.v0) - col : 0;
+        float v[8], lost = 0.f;
+        if (col < end) {
+            const float* z = p.z + row * p.z_stride + p.v0 + col;
 #pragma unroll
-        for (int j = 0; j < 8; j += 4) {
-            float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (nv >= j + 4) q = __ldcg(reinterpret_cast<const float4*>(z + j));
-            else if (nv > j) q = make_float4(z[j], nv > j + 1 ? z[j + 1] : 0.f, nv > j + 2 ? z[j + 2] : 0.f, 0.f);
-            v[j] = q.x; v[j + 1] = q.y; v[j + 2] = q.z; v[j + 3] = q.w;
-        }
+            for (int j = 0; j < 8; j += 4) {
+                float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (nv >= j + 4) q = __ldcg(reinterpret_cast<const float4*>(z + j));
+                else if (nv > j) q = make_float4(z[j], nv > j + 1 ? z[j + 1] : 0.f, nv > j + 2 ? z[j + 2] : 0.f, 0.f);
+                v[j] = q.x; v[j + 1] = q.y; v[j + 2] = q.z; v[j + 3] = q.w;
+            }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float u = fmaf(v[j], p.c1, -lse2), e = ex2(u);
-            float y = fmaf(e, fmaf(E, u, A), C);
-            if (x == j) y = fmaf(A, expm1f(u * kLn2), A + B) + fmaf(e * E, u, C);        // (as in a tile)
-            v[j] = j < nv ? y : 0.f;
-        }
-        uint4 w = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-        uint16_t* dst = p.g + (long long)row * p.piece + col;
-        *reinterpret_cast<uint4*>(dst) = w;
-        const uint32_t* u = &w.x;
+            for (int j = 0; j < 8; ++j) {
+                const float u = fmaf(v[j], p.c1, -lse2);
+                float y = fmaf(ex2(u), A, C);
+                if (x == j) y = fmaf(A, expm1f(u * kLn2), A + B) + C;        // (as in a tile)
+                v[j] = j < nv ? y : 0.f;
+            }
+            const uint4 w = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            uint16_t* dst = p.g + (long long)row * p.piece + col;
+            *reinterpret_cast<uint4*>(dst) = w;
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[2 * j] -= __uint_as_float(u[j] << 16);
-            v[2 * j + 1] -= __uint_as_float(u[j] & 0xFFFF0000u);
-            lost += v[2 * j] + v[2 * j + 1];
+            for (int j = 0; j < 4; ++j) {
+                v[2 * j] -= __uint_as_float(u[j] << 16);
+                v[2 * j + 1] -= __uint_as_float(u[j] & 0xFFFF0000u);
+                lost += v[2 * j] + v[2 * j + 1];
+            }
+            if (p.planes == 2)
+                *reinterpret_cast<uint4*>(dst + (long long)kHgPlaneRows * p.piece) =
+                    make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
         }
-        if (p.planes == 2)
-            *reinterpret_cast<uint4*>(dst + (long long)kHgPlaneRows * p.piece) =
-                make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        if (p.res) {
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) lost += __shfl_xor_sync(0xFFFFFFFFu, lost, o);       // (16 threads: 128 columns)
+            if ((tid & 15) == 0 && listed && col < p.vn) const_cast<float*>(p.res)[(long long)row * p.res_halves + (p.v0 + col) / kHgHalf] = lost;
+        }
     }
-    if (!p.res) return;
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) lost += __shfl_xor_sync(0xFFFFFFFFu, lost, o);       // (16 threads: 128 columns)
-    if ((threadIdx.x & 15) == 0 && row < p.c.n_rows && col < p.vn) const_cast<float*>(p.res)[(long long)row * p.res_halves + (p.v0 + col) / kHgHalf] = lost;
+    if (p.v0 == 0) head_total(p, gridDim.x);
 }
 
 // A CTA a part of a row, eight columns a thread; where there are several sums (splits, and both planes of each), groups of threads deal them out among
