@@ -263,6 +263,11 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
             if (int rc = make_map(&h_grad, r.h, L.n_pad, c.D, L.D8, 64)) return rc;
     }
     if (int rc = make_map(&t.g, g, L.n_pad, L.piece, L.piece, 64)) return rc;
+    if (L.planes == 2) {
+        if (!as_they_lie) t.rows16 = kHgPlaneRows;
+        if (int rc = make_map(&t.g_few, g, L.n_pad, L.piece, L.piece, t.rows16)) return rc;
+        if (int rc = make_map(&t.h_few, r.h, L.n_pad, c.D, L.D8, t.rows16)) return rc;
+    }
     if (!from_logits)
         if (int rc = make_map(&g_out, g, L.n_pad, L.piece, L.piece, 32)) return rc;
     if (c.grad_w)

@@ -81,6 +81,7 @@ struct HeadTiles {
     long long z_stride;
     uint32_t* ticket;                    // TILE_STATS: nullable, set to 0
     int32_t rows16;                      // TILE_GRADS: rows as they lie, in sixteens: sums along the rows end there (0: in full steps)
+    CUtensorMap g_few, h_few;            // TILE_GRADS, two planes: boxes of rows16 rows, for the sums along the rows
     float* zx;
     const HeadCoef* coef;                // TILE_G
     float* acc;                          // TILE_GRADS: [splits][rows][Dp]
@@ -319,7 +320,8 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                 const HeadPlace t = w.place(i);
                 const int mc = t.m0 + kHgM * rank, nc = t.n0 + Stage::kColumns * rank;
                 // (every load names its map: a map chosen by a variable costs the issuing thread more than a step's products take)
-                const uint32_t bytes = kParts && CG == 1 ? (p.h_boxes * p.h_box_rows + w.columns) * kHgK * 2 : CG * kHgStageBytes;
+                const bool few_rows = CG == 1 && !kParts && !t.gh && p.planes == 2;
+                const uint32_t bytes = few_rows ? 6 * p.rows16 * 128 : kParts && CG == 1 ? (p.h_boxes * p.h_box_rows + w.columns) * kHgK * 2 : CG * kHgStageBytes;
                 auto steps = [&](auto load) {
                     for (int k = t.k0; k < t.k1; ++k, ++step) {
                         const uint32_t s = step % kHgStages, ph = (step / kHgStages) & 1u;
@@ -354,12 +356,20 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
 #pragma unroll
                         for (int j = 0; j < kB; ++j) tma_load<CG>(b + j * kHgBox, &p.w, nc + 64 * j, p.v0 + k, bar);
                     });
+                } else if (few_rows) {                       // (a step is a plane)
+                    const int box = p.rows16 * 128;
+                    steps([&](uint32_t a, uint32_t b, uint32_t bar, int k) {
+#pragma unroll
+                        for (int j = 0; j < kA; ++j) tma_load<CG>(a + j * box, &p.g_few, mc + 64 * j, k, bar);
+#pragma unroll
+                        for (int j = 0; j < kB; ++j) tma_load<CG>(b + j * box, &p.h_few, nc + 64 * j, 0, bar);
+                    });
                 } else {
                     steps([&](uint32_t a, uint32_t b, uint32_t bar, int k) {
 #pragma unroll
                         for (int j = 0; j < kA; ++j) tma_load<CG>(a + j * kHgBox, &p.g, mc + 64 * j, k, bar);
 #pragma unroll
-                        for (int j = 0; j < kB; ++j) tma_load<CG>(b + j * kHgBox, &p.h, nc + 64 * j, p.planes == 2 ? 0 : k, bar);
+                        for (int j = 0; j < kB; ++j) tma_load<CG>(b + j * kHgBox, &p.h, nc + 64 * j, k, bar);
                     });
                 }
             }
@@ -377,6 +387,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
             bool ok = true;
             for (int i = 0; ok && i < w.count; ++i) {
                 const HeadPlace t = w.place(i);
+                const uint32_t box = CG == 1 && !kParts && !t.gh && p.planes == 2 ? p.rows16 * 128 : kHgBox;
                 const bool a_mn = !kParts && !t.gh;          // G lies along the vocabulary, h and w along dim
                 const uint32_t kind = product_kind(kHgM * CG, TILE == TILE_STATS && CG == 1 ? w.columns : kHgN, a_mn, !kParts);
                 int k = t.k0;
@@ -391,7 +402,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                         if (!ok) break;
                         tensor_fence_after();
                         const uint32_t a = base + s * kHgStageBytes, b = a + kHgABytes;
-                        uint64_t da = a_mn ? operand_mn(a, kHgBox) : operand_k(a), db = kParts ? operand_k(b) : operand_mn(b, kHgBox);
+                        uint64_t da = a_mn ? operand_mn(a, box) : operand_k(a), db = kParts ? operand_k(b) : operand_mn(b, box);
                         const uint64_t na = a_mn ? 2048 >> 4 : 32 >> 4, nb = kParts ? 32 >> 4 : 2048 >> 4;      // 16 of K on
                         int sub = kHgK / 16;                 // (sixteens of this step)
                         if (CG == 1 && !kParts && !t.gh && p.rows16) sub = min(sub, p.rows16 / 16 - (p.planes == 2 ? 0 : sub * k));
@@ -762,17 +773,17 @@ __global__ void __launch_bounds__(kHrThreads) head_rows_kernel(const __grid_cons
     }
 }
 
-// Of a row by the 128 threads of a CTA: the tiles' statistics joined; by its first thread (returns true there): what the row reports, its gradient's constants.
+// Of a row by the 128 threads of a CTA: the tiles' statistics joined; its first thread gets them (and true).
 constexpr int kHsThreads = 128;
-struct HeadRow {
-    float logp, H, lse, loss;
-    HeadCoef f;
+struct HeadJoined {
+    float top, S, T;
+    double Z;
+    bool bad;
 };
-__device__ __forceinline__ bool head_join(const HeadRows& p, int row, int r, HeadRow& out) {
+__device__ __forceinline__ bool head_join(const HeadRows& p, int row, HeadJoined& out) {
     constexpr int kW = kHsThreads / 32;
     __shared__ float s_m[kW], s_S[kW], s_T[kW];
     __shared__ double s_Z[kW];
-    const HeadCall& c = p.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const float4* part = p.part + (long long)row * p.halves;
     float m = kFloor, S = 0.f, T = 0.f;
@@ -820,36 +831,45 @@ __device__ __forceinline__ bool head_join(const HeadRows& p, int row, int r, Hea
         T += s_T[k];
         Z += s_Z[k];
     }
-    const double ln2 = 0.6931471805599453, lnS = log((double)S);
-    double l = ln2 * (double)fmaf(__ldcg(p.zx + row), p.c1, -top) - lnS, lse = ln2 * (double)top + lnS, H = lnS - ln2 * ((double)T / (double)S);
-    if (bad) {
+    out.top = top;
+    out.S = S;
+    out.T = T;
+    out.Z = Z;
+    out.bad = bad;
+    return true;
+}
+// The constants of a cross entropy's gradient.  (32 bits but for the products with weight and 1 / T: every CTA of a row waits for them.)
+__device__ __forceinline__ HeadCoef head_constants(const HeadRows& p, const HeadJoined& j, float weight, int tok) {
+    const HeadCall& c = p.c;
+    HeadCoef f;
+    f.lse2 = j.bad ? __int_as_float(0x7FC00000) : j.top + log2f(j.S);
+    const double w = (double)weight * (double)c.scale * p.inv_T;
+    f.A = (float)(w * (1.0 + 2.0 * (double)(c.z_loss * (f.lse2 * kLn2))));
+    f.B = (float)(-w * (1.0 - (double)c.smoothing));
+    f.C = (float)(-w * (double)c.smoothing / c.V);
+    f.E = 0.f;
+    f.tok = tok;
+    f.pad[0] = f.pad[1] = 0.f;
+    return f;
+}
+// What a row reports, worked out in 64 bits.
+__device__ __forceinline__ void head_report(const HeadRows& p, const HeadJoined& j, int r, float zx, float weight) {
+    const HeadCall& c = p.c;
+    const double ln2 = 0.6931471805599453, lnS = log((double)j.S);
+    double l = ln2 * (double)fmaf(zx, p.c1, -j.top) - lnS, lse = ln2 * (double)j.top + lnS, H = lnS - ln2 * ((double)j.T / (double)j.S);
+    if (j.bad) {
         l = lse = H = (double)__int_as_float(0x7FC00000);
         atomicOr(c.status, ADASD_STATUS_NAN);
     }
-    out.logp = (float)l;
-    out.H = (float)(H < 0.0 ? 0.0 : H);
-    out.lse = (float)lse;
-    out.loss = 0.f;
-    if (c.op == HEAD_CE) {
-        const double w = (c.row_weight ? (double)c.row_weight[r] : 1.0) * (double)c.scale, e = (double)c.smoothing, zc = (double)c.z_loss;
+    if (c.logp) c.logp[r] = (float)l;
+    if (c.H) c.H[r] = (float)(H < 0.0 ? 0.0 : H);
+    if (c.lse) c.lse[r] = (float)lse;
+    if (c.row_loss) {
+        const double e = (double)c.smoothing, zc = (double)c.z_loss;
         double L = -(1.0 - e) * l + zc * lse * lse;
-        if (e != 0.0) L -= e * (Z * p.inv_T / c.V - lse);
-        out.loss = (float)(w * L);
-        out.f.lse2 = (float)((double)top + lnS * 1.4426950408889634);
-        out.f.A = (float)(w * (1.0 + 2.0 * zc * lse) * p.inv_T);
-        out.f.B = (float)(-w * (1.0 - e) * p.inv_T);
-        out.f.C = (float)(-w * e / c.V * p.inv_T);
-        out.f.E = 0.f;
-        out.f.tok = __ldcg(p.tok + row);
-        out.f.pad[0] = out.f.pad[1] = 0.f;
+        if (e != 0.0) L -= e * (j.Z * p.inv_T / c.V - lse);
+        c.row_loss[r] = (float)((double)weight * (double)c.scale * L);
     }
-    return true;
-}
-__device__ __forceinline__ void head_report(const HeadCall& c, int r, const HeadRow& o) {
-    if (c.logp) c.logp[r] = o.logp;
-    if (c.H) c.H[r] = o.H;
-    if (c.lse) c.lse[r] = o.lse;
-    if (c.row_loss) c.row_loss[r] = o.loss;
 }
 // A row as it lies (or zeros) to where the gradients' products read it.
 __device__ __forceinline__ void head_keep_row(const HeadRows& p, int row, bool counts) {
@@ -896,10 +916,11 @@ __global__ void __launch_bounds__(kHsThreads) head_stats_kernel(const __grid_con
     if (lie && p.coef) head_keep_row(p, row, counts);        // (n_rows and more: zeros)
     if (counts && c.op != HEAD_GIVEN) {
         const int r = lie ? row : __ldcg(p.index + row);
-        HeadRow o;
-        if (head_join(p, row, r, o)) {
-            head_report(c, r, o);
-            if (p.coef) p.coef[row] = o.f;
+        const float weight = c.op == HEAD_CE && c.row_weight ? c.row_weight[r] : 1.f, zx = __ldcg(p.zx + row);
+        HeadJoined j;
+        if (head_join(p, row, j)) {
+            if (p.coef) p.coef[row] = head_constants(p, j, weight, __ldcg(p.tok + row));
+            head_report(p, j, r, zx, weight);
         }
     } else if (lie && listed && tid == 0) {
         if (counts) {
@@ -929,13 +950,13 @@ __global__ void __launch_bounds__(kHsThreads) head_g_kernel(const __grid_constan
     pdl_wait();
     pdl_trigger();
     const bool listed = row < c.n_rows, counts = listed && head_counts(c, row), first = part == 0 && p.v0 == 0;
-    if (first) head_keep_row(p, row, counts);
+    const int tok0 = counts ? c.tok[row] : -1;
+    const float weight = counts && c.row_weight ? c.row_weight[row] : 1.f, zx = first && counts ? __ldcg(p.zx + row) : 0.f;
+    HeadJoined joined;
+    bool mine = false;
     if (counts) {
-        HeadRow o;
-        if (head_join(p, row, row, o)) {
-            s_f = o.f;
-            if (first) head_report(c, row, o);
-        }
+        mine = head_join(p, row, joined);
+        if (mine) s_f = head_constants(p, joined, weight, tok0);
     } else if (tid == 0) {
         s_f.lse2 = s_f.A = s_f.B = s_f.C = s_f.E = 0.f;
         s_f.tok = -1;
@@ -982,6 +1003,10 @@ __global__ void __launch_bounds__(kHsThreads) head_g_kernel(const __grid_constan
             for (int o = 8; o > 0; o >>= 1) lost += __shfl_xor_sync(0xFFFFFFFFu, lost, o);       // (16 threads: 128 columns)
             if ((tid & 15) == 0 && listed && col < p.vn) const_cast<float*>(p.res)[(long long)row * p.res_halves + (p.v0 + col) / kHgHalf] = lost;
         }
+    }
+    if (first) {
+        head_keep_row(p, row, counts);
+        if (mine) head_report(p, joined, row, zx, weight);
     }
     if (p.v0 == 0) head_total(p, gridDim.x);
 }
