@@ -57,8 +57,6 @@ int splits_of(int n_rows, int n_pad, int piece, int D, int planes, int m, int sm
     return best;
 }
 
-// Statistics the other way round (head_rows_tile_kernel).
-inline bool in_rows(int n_rows) { return n_rows > kHgM && n_rows <= kHvRows; }
 constexpr size_t kPieceBytes = (size_t)256 << 20;
 
 Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
@@ -69,7 +67,7 @@ Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
     L.Dp = (D + 63) / 64 * 64;
     L.tiles = (V + kHgN - 1) / kHgN;
     L.columns = in_pairs(n_rows) ? kHgN : tile_columns(V, sm_count);
-    L.halves = in_rows(n_rows) ? sm_count / 2 * 8 : (V + L.columns - 1) / L.columns * 2;
+    L.halves = (V + L.columns - 1) / L.columns * 2;
     L.res_halves = (V + kHgHalf - 1) / kHgHalf;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -134,29 +132,21 @@ int make_map(CUtensorMap* map, const void* base, long long rows, long long colum
                : ADASD_ERR_CUDA;
 }
 
-// What a kernel needs once on a device: its shared memory; and, where its warp groups split the registers, as many as the split counts on.
-struct Allowed {
-    std::atomic<bool> on[64];
-    template <typename K>
-    int operator()(K kernel, int smem, bool split) {
-        int dev = 0;
-        CUDA_TRY(cudaGetDevice(&dev));
-        if (dev < 0 || dev >= 64) return ADASD_ERR_CUDA;
-        if (on[dev].load(std::memory_order_acquire)) return ADASD_OK;
-        if (split) {
-            cudaFuncAttributes fa;
-            CUDA_TRY(cudaFuncGetAttributes(&fa, kernel));
-            if (fa.numRegs < kHgLaunchRegs) return ADASD_ERR_CUDA;
-        }
-        CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-        on[dev].store(true, std::memory_order_release);
-        return ADASD_OK;
-    }
-};
 template <int TILE, int CG>
 int launch_tiles(const HeadTiles& p, int sm_count, cudaStream_t stream) {
-    static Allowed allow;
-    if (int rc = allow(head_tile_kernel<TILE, CG>, kHgSmem, TILE != TILE_GRADS)) return rc;
+    static std::atomic<bool> allowed[64];
+    int dev = 0;
+    CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return ADASD_ERR_CUDA;
+    if (!allowed[dev].load(std::memory_order_acquire)) {
+        if (TILE != TILE_GRADS) {          // (the split of the registers counts on them)
+            cudaFuncAttributes fa;
+            CUDA_TRY(cudaFuncGetAttributes(&fa, head_tile_kernel<TILE, CG>));
+            if (fa.numRegs < kHgLaunchRegs) return ADASD_ERR_CUDA;
+        }
+        CUDA_TRY(cudaFuncSetAttribute(head_tile_kernel<TILE, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHgSmem));
+        allowed[dev].store(true, std::memory_order_release);
+    }
     return launch_pdl(head_tile_kernel<TILE, CG>, sm_count / CG * CG, kHgThreads, kHgSmem, CG, stream, p);
 }
 template <int TILE>
@@ -253,18 +243,8 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
             r.piece = L.piece;
         }
     }
-    if (c.op != HEAD_GIVEN) {
-        if (in_rows(c.n_rows)) {
-            HeadTiles u = t;
-            u.block = ((c.n_rows + 1) / 2 + 15) / 16 * 16;
-            if (int rc = make_map(&u.h, r.h, L.n_pad, c.D, L.D8, u.block / 2)) return rc;
-            static Allowed allow;
-            if (int rc = allow(head_rows_tile_kernel, kHvSmem, true)) return rc;
-            if (int rc = launch_pdl(head_rows_tile_kernel, c.sm_count / 2 * 2, kHgThreads, kHvSmem, 2, stream, u)) return rc;
-        } else if (int rc = launch_tiles<TILE_STATS>(t, pairs, c.sm_count, stream)) {
-            return rc;
-        }
-    }
+    if (c.op != HEAD_GIVEN)
+        if (int rc = launch_tiles<TILE_STATS>(t, pairs, c.sm_count, stream)) return rc;
     if (!from_logits && (c.op != HEAD_GIVEN || as_they_lie))
         if (int rc = launch_pdl(head_stats_kernel, as_they_lie && gradient ? rows16 : c.n_rows, kHsThreads, 0, 0, stream, r)) return rc;
     if (c.loss && !r.ticket)

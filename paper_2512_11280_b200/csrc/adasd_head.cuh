@@ -72,7 +72,6 @@ struct HeadTiles {
     const int32_t* tok;
     float c1;                            // log2 e / T
     int32_t columns;                     // TILE_STATS: of a tile
-    int32_t block;                       // head_rows_tile_kernel: rows of a block, a multiple of 16
     int32_t entropy;                     // TILE_STATS: the entropy's sums too
     int32_t h_boxes, h_box_rows;         // one CTA's tiles of logits: its rows come in so many boxes of so many rows (below the last: whatever is there)
     float4* part;                        // TILE_STATS: [row][halves], a tile's first 128 columns and the others
@@ -635,225 +634,6 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
     cluster.sync();                                          // (neither CTA of a pair leaves, or frees its part, while the other is at work)
     tensor_fence_after();
     if (warp == 1) tensor_free<CG>(tmem, 512);
-    if (threadIdx.x == 0 && s_gave_up) atomicOr(p.status, ADASD_STATUS_TIMEOUT);
-}
-
-// ---- the statistics of 129 to 288 rows ------------------------------------------------------------
-// The other way round: a pair's tile is 256 of the vocabulary by all rows, in two blocks of up to 144, so that w crosses from the L2 to the SMs once, and no
-// products are formed of rows that there are not (288 rows as two tiles of 256: 47 % more bytes and 78 % more products; power is the limit of both).
-// Tensor memory holds three sums of a block.  Both blocks' parts are 8 steps long, the second's ends lie half a part behind the first's, and every new part takes
-// the sum that was freed longest ago: the epilogue reads one while the products go on in the other two.  It has a token a lane and the rows in its
-// registers; 32 x 32 values at a time change places through shared memory, and a lane keeps a row's statistics over all the tiles.
-constexpr int kHvBlock = 144, kHvRows = 2 * kHvBlock, kHvStages = 5;
-constexpr int kHvStageBytes = kHgABytes + 18 * 1024;         // (144 rows of 128 bytes)
-constexpr int kHvSum = 160;                                  // columns of tensor memory from one sum to the next
-constexpr int kHvStats = kHgEpi * kHvBlock * 16;             // of a warp's rows
-constexpr int kHvSmem = 1024 + kHvStages * kHvStageBytes + kHgEpi * kHgOut + kHvStats + 256;
-static_assert(kHgOut == 32 * 32 * 4, "a warp's stage holds 32 x 32 numbers");
-
-__global__ void __launch_bounds__(kHgThreads, 1) head_rows_tile_kernel(const __grid_constant__ HeadTiles p) {
-    constexpr int kHalf = kHvBlock / 2;                      // rows of a warp and block, at most
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t out_stage = base + kHvStages * kHvStageBytes, stats = out_stage + kHgEpi * kHgOut, bars = stats + kHvStats;
-    const uint32_t bar_full = bars, bar_empty = bars + 8 * kHvStages, acc_full = bars + 16 * kHvStages, acc_empty = acc_full + 24, bar_drained = acc_empty + 24, bar_never = bar_drained + 8;
-    __shared__ uint32_t s_tmem;
-    __shared__ volatile uint32_t s_gave_up;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-
-    if (threadIdx.x == 0) {
-        s_gave_up = 0u;
-        for (int i = 0; i < kHvStages; ++i) {
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_full + 8 * i) : "memory");
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_empty + 8 * i) : "memory");
-        }
-        for (int i = 0; i < 3; ++i) {
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(acc_full + 8 * i) : "memory");
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(acc_empty + 8 * i), "r"(kHgEpi * 2) : "memory");
-        }
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_drained) : "memory");
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_never) : "memory");
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (threadIdx.x == 32 * kHgFirst) {
-        tma_prefetch(&p.w);
-        tma_prefetch(&p.h);
-    }
-    if (warp == 1) tensor_alloc<2>(smem_u32(&s_tmem), 512);
-    tensor_fence_before();
-    cg::cluster_group cluster = cg::this_cluster();
-    cluster.sync();                                          // (a pair's barriers stand before either uses the other's)
-    tensor_fence_after();
-    const uint32_t rank = cluster.block_rank();
-    const uint32_t lead_full = mapa_u32(smem_raw + (bar_full - smem_u32(smem_raw)), 0);
-    const uint32_t lead_acc_empty = mapa_u32(smem_raw + (acc_empty - smem_u32(smem_raw)), 0);
-    const uint32_t tmem = s_tmem;
-    pdl_wait();
-    pdl_trigger();
-    const int n_active = __ldcg(p.n_active);
-    const int unit = blockIdx.x / 2, units = gridDim.x / 2, tiles = (p.V + 255) / 256, ksteps = (p.D + kHgK - 1) / kHgK;
-    const int block = p.block, half_rows = block / 2;
-    const int starts = 2 + (ksteps - 1) / 4;                 // parts of a tile, the blocks' in turn: at steps 0, 0, 4, 8, 12, ..
-
-    if (warp < kHgFirst) {
-        registers_give<kHgFewRegs>();
-        if (warp == 0) {
-            if (lane == 0) {
-                uint32_t step = 0;
-                bool ok = true;
-                for (int i = unit; ok && i < tiles; i += units) {
-                    const int v0 = i * 256 + kHgM * (int)rank;
-                    for (int k = 0; k < ksteps; ++k, ++step) {
-                        const uint32_t s = step % kHvStages;
-                        ok = wait_or_give_up(bar_empty + 8 * s, ((step / kHvStages) & 1u) ^ 1u, &s_gave_up);
-                        if (!ok) break;
-                        const uint32_t a = base + s * kHvStageBytes, b = a + kHgABytes, bar = lead_full + 8 * s;
-                        if (rank == 0) mbar_expect(bar_full + 8 * s, 2 * (kHgABytes + block * 128));
-                        tma_load<2>(a, &p.w, k * kHgK, v0, bar);
-                        tma_load<2>(a + kHgBox, &p.w, k * kHgK, v0 + 64, bar);
-                        tma_load<2>(b, &p.h, k * kHgK, half_rows * (int)rank, bar);
-                        tma_load<2>(b + half_rows * 128, &p.h, k * kHgK, block + half_rows * (int)rank, bar);
-                    }
-                }
-                // (as in head_tile_kernel)
-                if (rank == 0)
-                    for (uint32_t q = step > kHvStages ? step - kHvStages : 0; q < step; ++q)
-                        mbar_wait_bounded(reinterpret_cast<uint64_t*>(__cvta_shared_to_generic(bar_full + 8 * (q % kHvStages))), (q / kHvStages) & 1u, ok ? kCWaitSpins : kHgPause);
-                else if (!ok)
-                    mbar_wait_bounded(reinterpret_cast<uint64_t*>(__cvta_shared_to_generic(bar_never)), 0, kHgPause);
-            }
-        } else if (warp == 1) {
-            if (lane == 0 && rank == 0) {
-                const uint32_t kind = product_kind(2 * kHgM, block, false, false);
-                uint32_t step = 0, first = 0;                // first: of the tile's parts, counted over all tiles
-                bool ok = true;
-                for (int i = unit; ok && i < tiles; i += units, first += starts) {
-                    uint32_t part[2] = {0u, 1u};
-                    auto begin = [&](uint32_t part) {        // part's sum is free
-                        const uint32_t n = first + part;
-                        ok = ok && wait_or_give_up(acc_empty + 8 * (n % 3), ((n / 3) & 1u) ^ 1u, &s_gave_up);
-                    };
-                    for (int k = 0; ok && k < ksteps; ++k, ++step) {
-                        bool add[2] = {k > 0, k > 0};
-                        if (k == 0) {
-                            begin(0);
-                            begin(1);
-                        } else if ((k & 3) == 0) {
-                            const uint32_t n = k / 4 + 1, b = n & 1u;
-                            product_commit<2>(acc_full + 8 * ((first + n - 2) % 3));
-                            begin(n);
-                            if (b == 0) { part[0] = n; add[0] = false; } else { part[1] = n; add[1] = false; }
-                        }
-                        if (!ok) break;
-                        const uint32_t s = step % kHvStages;
-                        ok = wait_or_give_up(bar_full + 8 * s, (step / kHvStages) & 1u, &s_gave_up);
-                        if (!ok) break;
-                        tensor_fence_after();
-                        const uint32_t a = base + s * kHvStageBytes;
-                        const uint64_t da = operand_k(a);
-#pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            const uint64_t db = operand_k(a + kHgABytes + b * half_rows * 128);
-                            const uint32_t sum = tmem + (first + part[b]) % 3 * kHvSum;
-#pragma unroll
-                            for (int j = 0; j < kHgK / 16; ++j) product<2>(sum, da + j * (32 >> 4), db + j * (32 >> 4), kind, add[b] || j > 0);
-                        }
-                        product_commit<2>(bar_empty + 8 * s);
-                    }
-                    if (ok) {
-                        product_commit<2>(acc_full + 8 * ((first + starts - 2) % 3));
-                        product_commit<2>(acc_full + 8 * ((first + starts - 1) % 3));
-                    }
-                }
-                product_commit_here<2>(bar_drained);
-                mbar_wait_bounded(reinterpret_cast<uint64_t*>(__cvta_shared_to_generic(bar_drained)), 0);
-            }
-        }
-    } else {
-        registers_take<kHgManyRegs>();
-        const int quarter = warp & 3, half = (warp - kHgFirst) >> 2;
-        const uint32_t stage = out_stage + (warp - kHgFirst) * kHgOut;
-        const int r0 = half * half_rows;                     // the warp's first row in a block
-        const uint32_t mine = stats + ((warp - kHgFirst) * kHvBlock + lane) * 16;        // statistics of the lane's rows: of block b and group g at b * kHalf + 32 g
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-            for (int c = lane; c < kHalf; c += 32) st_shared_v4(mine + (b * kHalf + c - lane) * 16, __float_as_uint(kFloor), 0u, 0u, 0u);
-        uint32_t n = 0;
-        bool ok = true;
-        for (int i = unit; ok && i < tiles; i += units) {
-            float z[2][kHalf];                               // of the lane's token: the rows of both blocks
-            auto take = [&](float(&y)[kHalf], bool add) {    // the next part's sums
-                ok = ok && __all_sync(0xFFFFFFFFu, wait_or_give_up(acc_full + 8 * (n % 3), (n / 3) & 1u, &s_gave_up));
-                if (!ok) return;
-                tensor_fence_after();
-                const uint32_t acc = tmem + n % 3 * kHvSum + r0 + ((uint32_t)quarter << 21);
-#pragma unroll
-                for (int c = 0; c < kHalf; c += 8) {         // (columns beyond the block's: of no row)
-                    float v[8];
-                    tensor_load8(acc + c, v);
-                    tensor_wait8(v);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) y[c + j] = add ? y[c + j] + v[j] : v[j];
-                }
-                tensor_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(lead_acc_empty + 8 * (n % 3));
-                ++n;
-            };
-            take(z[0], false);
-            take(z[1], false);
-            for (int part = 2; part < starts; part += 2) {   // (the blocks' parts in turn)
-                take(z[0], true);
-                if (part + 1 < starts) take(z[1], true);
-            }
-            if (!ok) break;
-            const int v0 = i * 256 + kHgM * (int)rank + 32 * quarter, nv = p.V - v0;
-            if (nv <= 0) continue;
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int g = 0; g < 3; ++g) {
-                    if (32 * g >= half_rows) continue;
-                    // value j of lane l to line j, column l ^ j; then line l is the lane's: a row, its columns the tokens
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (32 * g + j < kHalf) asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage + (j * 32 + (lane ^ j)) * 4), "f"(z[b][32 * g + j]) : "memory");
-                    __syncwarp();
-                    float y[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(y[j]) : "r"(stage + (lane * 32 + (lane ^ j)) * 4) : "memory");
-                    __syncwarp();
-                    const int c = 32 * g + lane, row = b * block + r0 + c;
-                    const bool in = c < half_rows && row < n_active;
-                    const int x = in ? __ldcg(p.tok + row) - v0 : -1;
-                    const bool here = x >= 0 && x < 32;
-                    if (__any_sync(0xFFFFFFFFu, here)) {
-                        const float zx = pick(y, x);
-                        if (here) p.zx[row] = zx;
-                    }
-                    if (c >= kHalf) continue;                // (the third group has 8 rows)
-                    RowStats st;
-                    const uint32_t at = mine + (b * kHalf + 32 * g) * 16;
-                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(st.m), "=f"(st.S), "=f"(st.T), "=f"(st.Z) : "r"(at) : "memory");
-                    if (nv < 32) st.add_some(y, nv, p.c1);
-                    else if (p.entropy) st.add<true>(y, p.c1);
-                    else st.add<false>(y, p.c1);
-                    st_shared_v4(at, __float_as_uint(st.m), __float_as_uint(st.S), __float_as_uint(st.T), __float_as_uint(st.Z));
-                }
-        }
-        for (int b = 0; b < 2; ++b)
-            for (int c = lane; c < half_rows; c += 32) {
-                const int row = b * block + r0 + c;
-                float4 q;
-                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "r"(mine + (b * kHalf + c - lane) * 16) : "memory");
-                if (row < n_active) p.part[(long long)row * p.halves + (unit * 2 + (int)rank) * 4 + quarter] = q;
-            }
-    }
-    __syncwarp();
-    tensor_fence_before();
-    cluster.sync();                                          // (neither CTA of a pair leaves, or frees its part, while the other is at work)
-    tensor_fence_after();
-    if (warp == 1) tensor_free<2>(tmem, 512);
     if (threadIdx.x == 0 && s_gave_up) atomicOr(p.status, ADASD_STATUS_TIMEOUT);
 }
 

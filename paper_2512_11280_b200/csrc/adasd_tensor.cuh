@@ -117,18 +117,6 @@ __device__ __forceinline__ void tensor_wait(float (&r)[32]) {
                  : "memory");
 }
 
-// 8 columns.
-__device__ __forceinline__ void tensor_load8(uint32_t addr, float* r) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
-                 : "r"(addr));
-}
-__device__ __forceinline__ void tensor_wait8(float* r) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7])
-                 :
-                 : "memory");
-}
 // Registers of a warp group's threads, by all its warps (a multiple of 8).
 template <int N>
 __device__ __forceinline__ void registers_give() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
