@@ -148,6 +148,28 @@ def test_few_rows(torch, n, V, D):
     assert bool((border == 255).all()) and bool((border2 == 255).all()) and ctx.status() == 0
 
 
+@pytest.mark.parametrize("n", [129, 144, 145, 161, 200, 255, 257, 287, 288, 289])
+@pytest.mark.parametrize("D", [8, 256, 264, 520, 1032])
+def test_rows_of_a_round(torch, n, D):
+    """Rows about one and two tiles of a pair, the last one nearly empty; dims of 1, 4, 5, 9 and 17 steps (sums come in parts of 8)."""
+    for V in (31, 700, 40001):
+        h, w, tok, g = inputs(torch, n, V, D, n + V + D, out=0.2)
+        weight = torch.rand(n, generator=g, device="cuda") + 0.5
+        ctx, ref = context(V, 0.9), Head(h, w, tok, 0.9, weight)
+        sc, border = scratch_for(torch, ctx, n, D, False)
+        rl, lp, lse, H = out(torch, n, 4)
+        ctx.head_cross_entropy(h, w, tok, rl, sc, row_weight=weight, label_smoothing=0.1, z_loss=1e-3, logp_out=lp, lse_out=lse)
+        loss, tol, _, _ = ref.cross_entropy(weight, 0.1, 1e-3, 1.0)
+        assert bool(((rl.double() - loss).abs() <= tol).all())
+        ref.close_logp(lp)
+        ref.close_lse(lse)
+        ref = Head(h, w, tok, 0.9)
+        ctx.head_logprob(h, w, tok, lp, sc, H, lse)
+        ref.close_logp(lp)
+        ref.close_H(H)
+        assert bool((border == 255).all()) and ctx.status() == 0
+
+
 def test_captured_ahead_of_any_other_call(torch):
     """In a process of its own: the first calls of all are captured."""
     import os
