@@ -57,6 +57,11 @@ int splits_of(int n_rows, int n_pad, int piece, int D, int planes, int m, int sm
     return best;
 }
 
+// What a logit loses, in the mean, of its size: see the head of adasd_head.cuh.  part: steps of a part.
+double sum_loss(int D, int part) {
+    const double all = (D + 15) / 16, full = part * (kHgK / 16), parts = std::floor(all / full), rest = all - parts * full;
+    return 1.2e-8 * (parts * full * full + rest * rest) / all;
+}
 constexpr size_t kPieceBytes = (size_t)256 << 20;
 
 Layout layout_of(int n_rows, int V, int D, bool gradient, int sm_count) {
@@ -181,7 +186,9 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     r.acc_slot = (long long)L.n_pad * L.Dp;
     r.Dp = L.Dp;
     r.splits = L.splits;
-    r.c1 = (float)(1.4426950408889634 / (double)c.temperature);
+    const double whole = 1.0 + sum_loss(c.D, in_pairs(c.n_rows) ? kHgPart<2> : kHgPart<1>);
+    r.c1 = (float)(1.4426950408889634 / (double)c.temperature * whole);
+    r.inv_Tz = whole / (double)c.temperature;
     r.inv_T = 1.0 / (double)c.temperature;
     r.rows = c.n_rows <= 2048 ? kHrThreads / 32 : kHrRows;
 

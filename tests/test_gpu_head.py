@@ -170,6 +170,21 @@ def test_rows_of_a_round(torch, n, D):
         assert bool((border == 255).all()) and ctx.status() == 0
 
 
+@pytest.mark.parametrize("n,D", [(4096, 4096), (4096, 520), (128, 4096)])
+def test_logits_lose_nothing_in_the_mean(torch, n, D):
+    """With a vocabulary of one token lse is the logit.  The accumulator is cut with every 16 products; of 4096 logits the errors' regression on the
+    logits is within 1e-7 (it was 3.9e-7 with 512 products to a part; their own spread, 2.5e-7 of the size, leaves 4e-9 of 4096 logits and 2.2e-8 of 128)."""
+    g = torch.Generator(device="cuda").manual_seed(n + D)
+    h, w = torch.randn(n, D, generator=g, device="cuda").bfloat16(), torch.randn(1, D, generator=g, device="cuda").bfloat16()
+    ctx = context(1)
+    sc, _ = scratch_for(torch, ctx, n, D, False)
+    lp, lse = out(torch, n, 2)
+    ctx.head_logprob(h, w, torch.zeros(n, dtype=torch.int32, device="cuda"), lp, sc, lse_out=lse)
+    z = (h.double() @ w.double().t())[:, 0]
+    assert abs(float(((lse.double() - z) * z).sum() / (z * z).sum())) < 1e-7
+    assert float((lse.double() - z).norm() / z.norm()) < 5e-7 and bool((lp.abs() < 1e-5).all())
+
+
 def test_captured_ahead_of_any_other_call(torch):
     """In a process of its own: the first calls of all are captured."""
     import os
