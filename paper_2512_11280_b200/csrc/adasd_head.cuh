@@ -792,12 +792,12 @@ __device__ __forceinline__ bool head_join(const HeadRows& p, int row, HeadJoined
     bool bad = false;
     auto join = [&](const float4& q) {
         bad |= !(fabsf(q.w) < INFINITY);                     // (a logit that is not finite shows in their sum)
-        if (q.y == 0.f && q.x == kFloor) return;             // (a half without columns)
+        Z += (double)q.w;
+        if (q.y == 0.f && q.x == kFloor) return;             // (a half without columns, or with none above the floor)
         bad |= !(q.y > 0.f && q.y < INFINITY) || !(fabsf(q.x) < -kFloor);
         const float m1 = fmaxf(m, q.x), f0 = ex2(m - m1), f1 = ex2(q.x - m1);
         T = f0 * (T + S * (m - m1)) + f1 * (q.z + q.y * (q.x - m1));
         S = f0 * S + f1 * q.y;
-        Z += (double)q.w;
         m = m1;
     };
     for (int k = tid; k < p.halves; k += 8 * kHsThreads) {   // (eight loads under way)
@@ -836,7 +836,7 @@ __device__ __forceinline__ bool head_join(const HeadRows& p, int row, HeadJoined
     out.S = S;
     out.T = T;
     out.Z = Z;
-    out.bad = bad;
+    out.bad = bad || !(S > 0.f);                             // (all below the floor)
     return true;
 }
 // The constants of a cross entropy's gradient.  (32 bits but for the products with weight and 1 / T: every CTA of a row waits for them.)

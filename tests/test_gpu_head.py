@@ -364,6 +364,47 @@ def test_weights_that_are_not_finite(torch, n, value):
         assert bool(torch.isnan(t).all())
 
 
+@pytest.mark.parametrize("n", [6, 200])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_logits_beyond_the_floor(torch, n, sign):
+    """Finite logits of 1e36 in size: where a row has no others it counts as one that is not finite; a few at the lower end have p = 0."""
+    import paper_2512_11280_b200 as adasd
+    V, D = 900, 64
+    h, w, tok, _ = inputs(torch, n, V, D, 8, out=0.0)
+    tok[:] = tok.clamp(0, V - 1)
+    h[:, 5], h[3, 5] = 0.0, 2.0 ** 60
+    w[:, 5] = sign * 2.0 ** 60
+    ctx = context(V)
+    sc, _ = scratch_for(torch, ctx, n, D, True)
+    lp, H, lse, rl = out(torch, n, 4)
+    ctx.head_logprob(h, w, tok, lp, sc, H, lse)
+    assert ctx.status() == adasd.STATUS_NAN and ctx.status() == 0
+    bad = torch.arange(n, device="cuda") == 3
+    for t in (lp, H, lse):
+        assert torch.equal(torch.isnan(t), bad)
+    gh, gw = torch.empty_like(h), torch.empty_like(w)
+    ctx.head_cross_entropy(h, w, tok, rl, sc, lse_out=lse, grad_hidden_out=gh, grad_weight_out=gw)
+    assert ctx.status() == adasd.STATUS_NAN
+    assert torch.equal(torch.isnan(rl), bad) and torch.equal(torch.isnan(lse), bad) and bool(torch.isnan(gw).all())
+    assert bool(torch.isnan(gh[bad]).all()) and bool(torch.isfinite(gh[~bad]).all())
+    if sign > 0:
+        return
+    # 300 of the columns only, two whole tiles' halves among them, in every row: the sum of ln p is theirs
+    h[:, 5], w[:, 5] = 2.0 ** 60, 0.0
+    w[256:556, 5] = -(2.0 ** 60)
+    tok[:] = tok % 256
+    ctx.head_cross_entropy(h, w, tok, rl, sc, label_smoothing=0.5, logp_out=lp, lse_out=lse, grad_hidden_out=gh, grad_weight_out=gw)
+    assert ctx.status() == 0
+    # (those 300 are 2^120 and nothing to 24 bits: their sum is rounded 300 times at the most, the rest of the loss twice)
+    want = 0.5 * 300 / V * 2.0 ** 120
+    assert bool(((rl.double() - want).abs() <= want * 304 * 2.0 ** -24).all())
+    assert bool(torch.isfinite(gh).all())
+    kept = torch.ones(V, dtype=torch.bool, device="cuda")
+    kept[256:556] = False
+    small = Head(torch.where(torch.arange(D, device="cuda") == 5, 0.0, h.float()).bfloat16(), w[kept], tok)
+    assert bool(((lp.double() - small.l).abs() <= small.el + 2.0 ** -24 * small.l.abs()).all())
+
+
 def test_confident_rows(torch):
     """p of the token near 1: p - 1 is not lost; a token of tiny probability."""
     n, V, D = 130, 600, 64
