@@ -1053,8 +1053,11 @@ __global__ void __launch_bounds__(kHrThreads) head_grad_rows_kernel(const __grid
         s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
         s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
     }
-    const int tok = __ldcg(p.tok + row);
-    if (p.res && tok >= 0 && tok < c.V) {                    // (as they lie: a row left out has lost nothing)
+    if (!p.index && !head_counts(c, row)) {                  // (as they lie: zeros, where 0 times a weight is not 0 too)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = 0.f;
+    } else if (p.res) {
+        const int tok = __ldcg(p.tok + row);
         lost = 0.f;
 #pragma unroll
         for (int k = 0; k < kHrThreads / 32; ++k) lost += s_lost[k];

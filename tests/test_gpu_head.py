@@ -364,6 +364,33 @@ def test_weights_that_are_not_finite(torch, n, value):
         assert bool(torch.isnan(t).all())
 
 
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+@pytest.mark.parametrize("n", [6, 100, 200])
+def test_rows_left_out_of_weights_that_are_not_finite(torch, n, value):
+    import paper_2512_11280_b200 as adasd
+    V, D = 900, 64
+    h, w, tok, g = inputs(torch, n, V, D, 8)
+    tok[0], tok[3], tok[4] = 7, -1, 9
+    h[:, 5] = 1.0
+    w[333, 5] = value
+    weight = torch.ones(n, device="cuda")
+    weight[4] = 0.0
+    on = (tok >= 0) & (tok < V)
+    ctx = context(V)
+    sc, _ = scratch_for(torch, ctx, n, D, True)
+    rl, lp, H, lse = out(torch, n, 4)
+    gh, gw = torch.empty_like(h), torch.empty_like(w)
+    ctx.head_cross_entropy(h, w, tok, rl, sc, row_weight=weight, grad_hidden_out=gh, grad_weight_out=gw)
+    assert ctx.status() == adasd.STATUS_NAN
+    counts = on & (weight != 0)
+    assert bool(torch.isnan(gh[counts]).all()) and bool((gh[~counts] == 0).all()) and bool((rl[~counts] == 0).all())
+    ctx.head_logprob(h, w, tok, lp, sc, H, lse)
+    gh.fill_(9.0)
+    ctx.head_logprob_grad(h, w, tok, lse, weight, sc, grad_hidden_out=gh, grad_weight_out=gw)
+    assert ctx.status() == adasd.STATUS_NAN
+    assert bool(torch.isnan(gh[counts]).all()) and bool((gh[~counts] == 0).all())
+
+
 @pytest.mark.parametrize("n", [6, 200])
 @pytest.mark.parametrize("sign", [1.0, -1.0])
 def test_logits_beyond_the_floor(torch, n, sign):
