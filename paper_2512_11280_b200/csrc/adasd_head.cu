@@ -149,10 +149,10 @@ int launch_tiles(const HeadTiles& p, int sm_count, cudaStream_t stream) {
             CUDA_TRY(cudaFuncGetAttributes(&fa, head_tile_kernel<TILE, CG>));
             if (fa.numRegs < kHgLaunchRegs) return ADASD_ERR_CUDA;
         }
-        CUDA_TRY(cudaFuncSetAttribute(head_tile_kernel<TILE, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHgSmem));
+        CUDA_TRY(cudaFuncSetAttribute(head_tile_kernel<TILE, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, HeadStage<TILE, CG>::kAll));
         allowed[dev].store(true, std::memory_order_release);
     }
-    return launch_pdl(head_tile_kernel<TILE, CG>, sm_count / CG * CG, kHgThreads, kHgSmem, CG, stream, p);
+    return launch_pdl(head_tile_kernel<TILE, CG>, sm_count / CG * CG, kHgThreads, HeadStage<TILE, CG>::kAll, CG, stream, p);
 }
 template <int TILE>
 int launch_tiles(const HeadTiles& p, bool pairs, int sm_count, cudaStream_t stream) {

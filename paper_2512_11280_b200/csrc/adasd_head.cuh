@@ -33,11 +33,6 @@ namespace adasd {
 // brings 32 KB to an SM instead of 48 (what the L2 gives, 12 to 15 TB/s, is the bound of the first: 1200 TFLOP/s need 14).
 constexpr int kHgM = 128, kHgN = 256, kHgK = 64;             // rows of a CTA, columns; a step along K
 constexpr int kHgABytes = kHgM * kHgK * 2;
-template <int CG>
-struct HeadStage {
-    static constexpr int kColumns = kHgN / CG;               // of B in a CTA
-    static constexpr int kBytes = kHgABytes + kColumns * kHgK * 2, kCount = CG == 1 ? 4 : 6;
-};
 constexpr int kHgBox = 64 * 64 * 2;
 constexpr int kHgHalf = kHgN / 2;
 constexpr int kHgOut = 32 * 64 * 2;                          // 32 rows of 64 bf16: what a warp stores at a time
@@ -49,12 +44,19 @@ static_assert(kHgFewRegs * kHgFirst + kHgManyRegs * kHgEpi <= kHgLaunchRegs * (k
 // Steps along K of a part of the logits' sums: 512 products where the products are the bound, 256 where a CTA on its own waits for memory.
 template <int CG>
 constexpr int kHgPart = CG == 1 ? 4 : 8;
-constexpr int kHgRing = 192 * 1024;                         // 4 stages of 48 KB or 6 of 32
-constexpr int kHgSmem = 1024 + kHgRing + kHgEpi * kHgOut + 256;
+enum HeadTile : int { TILE_STATS, TILE_G, TILE_GRADS };
+// Shared memory: a ring of steps, and where bf16 is written two places for every warp of the epilogue, one being filled while the other is read (with one
+// place 53 us instead of 47.5 for loss and gradients of 7 rows of 32000 at dim 512; no difference where products are the bound).
+template <int TILE, int CG>
+struct HeadStage {
+    static constexpr int kColumns = kHgN / CG;               // of B in a CTA
+    static constexpr int kBytes = kHgABytes + kColumns * kHgK * 2;
+    static constexpr int kCount = (TILE == TILE_STATS ? 192 : 160) * 1024 / kBytes, kOuts = TILE == TILE_STATS ? 0 : 2;
+    static constexpr int kAll = 1024 + kCount * kBytes + kHgEpi * kOuts * kHgOut + 256;
+    static_assert(kAll <= 227 * 1024, "a CTA's shared memory");
+};
 constexpr uint32_t kHgPause = 1u << 16;                       // polls that a copy under way surely ends within
 constexpr int kHgPlaneRows = 64;                             // rows of a plane of G, where there are two
-
-enum HeadTile : int { TILE_STATS, TILE_G, TILE_GRADS };
 
 // Of a row that counts: g_v = p (A + E u) + C, and at the token B more, where u = log2 p.
 struct __align__(16) HeadCoef {
@@ -262,12 +264,11 @@ __device__ __forceinline__ void stage_bf16(uint32_t stage, int lane, int half, c
 
 template <int TILE, int CG>
 __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_constant__ HeadTiles p) {
-    using Stage = HeadStage<CG>;
+    using Stage = HeadStage<TILE, CG>;
     constexpr int kHgStages = Stage::kCount, kHgStageBytes = Stage::kBytes;
-    static_assert(kHgStages * kHgStageBytes == kHgRing, "the ring's size is one for both");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t out_stage = base + kHgStages * kHgStageBytes, bars = out_stage + kHgEpi * kHgOut;
+    const uint32_t out_stage = base + kHgStages * kHgStageBytes, bars = out_stage + kHgEpi * Stage::kOuts * kHgOut;
     // barriers: full[stage], empty[stage], accumulator full[2], empty[2], drained
     const uint32_t bar_full = bars, bar_empty = bars + 8 * kHgStages, acc_full = bars + 16 * kHgStages, acc_empty = acc_full + 16, bar_drained = acc_empty + 16, bar_never = bar_drained + 8;
     __shared__ uint32_t s_tmem;
@@ -426,7 +427,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
     } else {
         if constexpr (kParts) registers_take<kHgManyRegs>();
         const int quarter = warp & 3, half = (warp - kHgFirst) >> 2;
-        const uint32_t stage = out_stage + (warp - kHgFirst) * kHgOut;
+        uint32_t stage = out_stage + (warp - kHgFirst) * 2 * kHgOut, other = stage + kHgOut;
         uint32_t n = 0;
         bool ok = true;
         for (int i = 0; ok && i < w.count; ++i) {
@@ -445,18 +446,22 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                 if (lane == 0) mbar_arrive(lead_acc_empty + 8 * (n & 1u));
                 ++n;
             };
-            // 64 columns as bf16: into the warp's stage once the store before has read it, and from there to row y on
+            // 64 columns as bf16: into one of the warp's places, once the store before the last has read it, and from there to row y on.  (A store that
+            // is left out counts as one.)
             auto store64 = [&](const float(&a)[32], const float(&b)[32], int x, int y, bool in) {
-                if (lane == 0) bulk_wait_read<0>();
+                if (lane == 0) bulk_wait_read<1>();
                 __syncwarp();
                 stage_bf16(stage, lane, 0, a);
                 stage_bf16(stage, lane, 1, b);
                 fence_async_shared();
                 __syncwarp();
-                if (lane == 0 && in) {
-                    tma_store(&p.out, x, y, stage);
+                if (lane == 0) {
+                    if (in) tma_store(&p.out, x, y, stage);
                     bulk_commit();
                 }
+                const uint32_t s = stage;
+                stage = other;
+                other = s;
             };
             if constexpr (kParts) {
                 bool in = row < n_active;
