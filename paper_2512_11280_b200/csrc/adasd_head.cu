@@ -258,7 +258,7 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
         if (int rc = launch_total(c.row_loss, c.n_rows, c.loss, stream)) return rc;
     if (!gradient) return ADASD_OK;
 
-    CUtensorMap g_out, gw_out;
+    CUtensorMap g_out{}, gw_out{};                   // (zeros where the call has no such product)
     char* g = s + L.big;
     // (G's tiles have 256 columns; the gradients' products take boxes of 64 rows of both)
     CUtensorMap w_tile = t.w, h_tile = t.h, w_grad = t.w, h_grad = t.h;
@@ -283,7 +283,6 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
         t.v0 = v0;
         t.vn = std::min(L.piece, c.V - v0);
         t.first = v0 == 0;
-        t.out = g_out;
         t.w = w_tile;
         t.h = h_tile;
         if (from_logits) {
@@ -296,11 +295,12 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
             const int parts = (width + r.columns - 1) / r.columns;
             if (int rc = launch_pdl(head_g_kernel, rows16 * parts, kHsThreads, 0, 0, stream, r)) return rc;
         } else {
+            t.out = g_out;
             if (int rc = launch_tiles<TILE_G>(t, pairs, c.sm_count, stream)) return rc;
         }
         t.w = w_grad;
         t.h = h_grad;
-        if (c.grad_w) t.out = gw_out;
+        t.out = gw_out;
         if (int rc = launch_tiles<TILE_GRADS>(t, pairs, c.sm_count, stream)) return rc;
     }
     if (!c.grad_h) return ADASD_OK;

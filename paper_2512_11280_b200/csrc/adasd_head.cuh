@@ -68,7 +68,7 @@ struct __align__(16) HeadCoef {
 
 struct HeadTiles {
     CUtensorMap h, w, g;                 // hidden states, weight, the piece of G
-    CUtensorMap out;                     // TILE_G: of G; TILE_GRADS: of grad_w
+    CUtensorMap out;                     // TILE_G: of G; TILE_GRADS: of grad_w, where that is wanted
     int32_t D, V, v0, vn;                // piece of the vocabulary: columns v0 .. v0 + vn - 1
     const int32_t* n_active;             // nullable: n_rows
     int32_t n_rows;
@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
         tma_prefetch(&p.w);
         tma_prefetch(&p.h);
         if (TILE == TILE_GRADS) tma_prefetch(&p.g);
-        if (TILE != TILE_STATS) tma_prefetch(&p.out);
+        if (TILE == TILE_G || (TILE == TILE_GRADS && p.want_w)) tma_prefetch(&p.out);
     }
     if (warp == 1) tensor_alloc<CG>(smem_u32(&s_tmem), 512);
     tensor_fence_before();
