@@ -430,7 +430,7 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
  *
  * The calls above take logits that the caller has made.  These take what the logits are made of: hidden states h [n_rows, dim] ahead of
  * the output projection ("head") and its weight w [V, dim], both bf16, z = h w^T in fp32; log-probs, loss and gradients come
- * out, and more than a piece of an array of n_rows x V is never held.  Tokens, rows left out, T, l and H are as above; top-k and top-p are refused
+ * out, and more than a piece of an array of n_rows x V is not held (of up to 128 rows it is).  Tokens, rows left out, T, l and H are as above; top-k and top-p are refused
  * (ADASD_ERR_DTYPE), and so is a context of fp32 rows.
  *   - hidden_dev: row r at r * hidden_stride (elements), any alignment.  weight_dev: row v at v * weight_stride; it starts at a
  *     multiple of 16 bytes and weight_stride is a multiple of 8 (ADASD_ERR_ALIGN, ADASD_ERR_SHAPE).  dim: a multiple of 8 up to
@@ -441,9 +441,11 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
  *   - A row whose logits are not all finite, or whose largest z / T is 6e29 or more in size, sets ADASD_STATUS_NAN: its outputs, the totals it enters and both its gradient and the
  *     whole of the weight's are NaN.
  *   - scratch_dev: at least the bytes that adasd_head_scratch gives for the call's n_rows and dim, 16-byte aligned, contents of no
- *     meaning between calls.  Two calls that may overlap (streams, captured graphs) need one each.  It grows with n_rows: in the main
- *     2 dim bytes a row and the larger of 16 bytes a row for every 128 of V and, with gradients, a piece of dL/dz (256 MB at the most, or
- *     2048 columns); with gradients 4 dim bytes a row more, and for up to 128 rows their logits.
+ *     meaning between calls.  Two calls that may overlap (streams, captured graphs) need one each.  What it gives for n_rows serves every call of
+ *     fewer rows as well, and what it gives with gradients every call without.  In the main, with rows padded to whole tiles (128, beyond that to 256s): 2 dim
+ *     bytes a row, and the larger of 16 bytes a row for every 128 of V and, with gradients, a piece of dL/dz (2 bytes an element; 256 MB at the most, or 2048
+ *     columns); with gradients the sums of grad_hidden in 32 bits, 4 dim bytes a row or, in parts, up to 64 MB.  Calls of up to 128 rows with gradients hold
+ *     their logits besides (4 bytes an element).
  *   - Sums and statistics are held in 32 bits or more.  z is off by the rounding of an fp32 sum of dim exact products; ln S as above.  A
  *     gradient's p_v comes with (4 |ln p_v| + 2 |lse| + 16) 2^-24 of itself and that; dL/dz is rounded to bf16 (2^-8 of itself at
  *     most) ahead of the products with w and h, which are summed in fp32 and rounded to bf16 once.  Results do not vary from run to run.
@@ -451,7 +453,7 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
  *   - After a wait that expired (ADASD_STATUS_TIMEOUT) the outputs of such a call are not to be used.
  */
 
-/* Bytes of scratch of the calls below for n_rows rows (or fewer) of dim elements; with_grad: 1 for a call with a gradient. */
+/* Bytes of scratch of the calls below for n_rows rows or fewer of dim elements; with_grad: 1 for calls with a gradient. */
 int adasd_head_scratch(adasd_ctx* ctx, int32_t n_rows, int32_t dim, int32_t with_grad, size_t* bytes_out);
 
 /* l, entropy and log-sum-exp (of z / T) of every row; each output [n_rows], entropy and lse nullable. */

@@ -1201,7 +1201,7 @@ static int check_head(const adasd_ctx* ctx, HeadCall& c, int32_t op, const void*
                  s = {reinterpret_cast<uintptr_t>(scratch), reinterpret_cast<uintptr_t>(scratch) + (scratch ? scratch_bytes : 0)};
     if (meet(h, gh) || meet(h, gw) || meet(w, gh) || meet(w, gw) || meet(gh, gw) || meet(s, h) || meet(s, w) || meet(s, gh) || meet(s, gw))
         return ADASD_ERR_SHAPE;
-    if (n_rows > 0 && scratch_bytes < head_scratch_bytes(n_rows, V, dim, grad_h || grad_w, ctx->sm_count)) return ADASD_ERR_CAPACITY;
+    if (n_rows > 0 && scratch_bytes < head_scratch_need(n_rows, V, dim, grad_h || grad_w, ctx->sm_count)) return ADASD_ERR_CAPACITY;
     memset(&c, 0, sizeof(c));
     c.op = op;
     c.n_rows = n_rows;

@@ -160,7 +160,16 @@ int launch_tiles(const HeadTiles& p, bool pairs, int sm_count, cudaStream_t stre
 }
 }  // namespace
 
-size_t head_scratch_bytes(int n_rows, int V, int D, bool gradient, int sm_count) { return layout_of(n_rows, V, D, gradient, sm_count).total; }
+size_t head_scratch_need(int n_rows, int V, int D, bool gradient, int sm_count) { return layout_of(n_rows, V, D, gradient, sm_count).total; }
+
+// A call's need does not grow with its rows throughout: up to a tile of them there are logits and statistics apart, and the parts of grad_h and the piece change
+// with every pair's tile.  Beyond a tile it hangs on the padded rows and the parts, and of counts with the same padded rows the first has the most parts (what a part
+// costs grows with the rows, what it saves does not): one count for each is looked at.
+size_t head_scratch_bytes(int n_rows, int V, int D, bool gradient, int sm_count) {
+    size_t most = 0;
+    for (int n = 0; n <= n_rows; n += n <= kHgM ? 1 : n == kHgM + 1 ? kHgM : 2 * kHgM) most = std::max(most, head_scratch_need(n, V, D, gradient, sm_count));
+    return most;
+}
 
 int launch_head(const HeadCall& c, cudaStream_t stream) {
     const bool gradient = c.gradient();

@@ -46,8 +46,10 @@ struct HeadCall {
     bool gradient() const { return grad_h || grad_w; }
 };
 
-// Bytes of scratch; the launches of a call.  Both return ADASD_OK or a code of the header.
+// Bytes of scratch that a call of n_rows rows needs, and that serve calls of any number up to n_rows.
+size_t head_scratch_need(int n_rows, int V, int D, bool gradient, int sm_count);
 size_t head_scratch_bytes(int n_rows, int V, int D, bool gradient, int sm_count);
+// The launches of a call.  Returns ADASD_OK or a code of the header.
 int launch_head(const HeadCall& c, cudaStream_t stream);
 
 }  // namespace adasd

@@ -1,0 +1,50 @@
+"""Head calls at the edges of what the header allows."""
+import pytest
+
+from tests.head_reference import Head
+from tests.test_gpu_head import context, inputs, out, scratch_for
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    return torch
+
+
+# ---- scratch ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("V,D", [(1, 8), (161, 64), (32000, 512), (32000, 2048), (128256, 2048), (50257, 1000), (300000, 136)])
+def test_scratch_never_falls_with_rows(torch, V, D):
+    ctx = context(V)
+    last = [0, 0]
+    for n in [*range(0, 700), *range(700, 9000, 31), *range(9000, 200000, 4801)]:
+        now = [ctx.head_scratch(n, D, grad) for grad in (False, True)]
+        assert now[0] >= last[0] and now[1] >= last[1] and now[1] >= now[0], n
+        last = now
+
+
+@pytest.mark.parametrize("most", [40, 129, 200, 256, 300, 513])
+@pytest.mark.parametrize("V,D", [(5000, 264), (32000, 64)])
+def test_scratch_made_for_more_rows(torch, most, V, D):
+    """One buffer, made for the largest batch, serves every smaller one and calls without gradients, with the results that a buffer of the call's
+    own gives; nothing behind it is touched."""
+    h, w, tok, _ = inputs(torch, most, V, D, most + V)
+    ctx = context(V)
+    size = ctx.head_scratch(most, D, True)
+    buf = torch.full((size + 4096,), 255, dtype=torch.uint8, device="cuda")
+    shared, border = buf[:size], buf[size:]
+    for n in [k for k in (1, 13, 40, 63, 65, 100, 128, 129, 200, 257, 512, most - 1, most) if k <= most]:
+        got = []
+        for sc in (shared, scratch_for(torch, ctx, n, D, True)[0]):
+            rl, lp, lse = out(torch, n, 3)
+            gh, gw, gh2, gw2 = [torch.full_like(t, 9.0) for t in (h[:n], w, h[:n], w)]
+            ctx.head_cross_entropy(h[:n], w, tok[:n], rl, sc, grad_hidden_out=gh, grad_weight_out=gw)
+            ctx.head_logprob(h[:n], w, tok[:n], lp, sc, lse_out=lse)
+            ctx.head_logprob_grad(h[:n], w, tok[:n], lse, torch.linspace(-1.0, 1.0, n, device="cuda"), sc, grad_hidden_out=gh2, grad_weight_out=gw2)
+            got.append((rl, lp, lse, gh, gw, gh2, gw2))
+        assert all(torch.equal(a, b) for a, b in zip(*got)), n
+        Head(h[:n], w, tok[:n]).close_logp(got[0][1])
+    assert bool((border == 255).all()) and ctx.status() == 0
