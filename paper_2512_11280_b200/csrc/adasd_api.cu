@@ -1177,13 +1177,15 @@ Extent rows_extent(const void* p, int64_t stride, int64_t n, int64_t width) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(p);
     return {a, p && n > 0 ? a + (uintptr_t)(((n - 1) * stride + width) * 2) : a};
 }
+Extent array_extent(const void* p, int64_t n) { return rows_extent(p, 2, n, 2); }          // of 32-bit values
 bool meet(const Extent& a, const Extent& b) { return a.at < b.end && b.at < a.end && a.at != a.end && b.at != b.end; }
 }  // namespace
 
 // Checks what the head calls have in common; fills in what they share.
 static int check_head(const adasd_ctx* ctx, HeadCall& c, int32_t op, const void* hidden, int64_t h_stride, const void* weight, int64_t w_stride,
                       int32_t dim, const int32_t* tokens, int32_t n_rows, void* scratch, size_t scratch_bytes, void* grad_h, int64_t gh_stride,
-                      void* grad_w, int64_t gw_stride) {
+                      void* grad_w, int64_t gw_stride, std::initializer_list<const float*> rows_in, std::initializer_list<float*> rows_out,
+                      float* one_out = nullptr) {
     constexpr int64_t most = (int64_t)1 << 33;
     if (n_rows < 0 || n_rows > (1 << 22) || dim < 8 || dim > 65536 || dim % 8 != 0) return ADASD_ERR_SHAPE;
     if (n_rows > 0 && (!hidden || !weight || !tokens || !scratch)) return ADASD_ERR_NULL;
@@ -1192,15 +1194,23 @@ static int check_head(const adasd_ctx* ctx, HeadCall& c, int32_t op, const void*
     if (h_stride < dim || h_stride > most || w_stride < dim || w_stride > most || w_stride % 8 != 0) return ADASD_ERR_SHAPE;
     if (grad_h && (gh_stride < dim || gh_stride > most)) return ADASD_ERR_SHAPE;
     if (grad_w && (gw_stride < dim || gw_stride > most || gw_stride % 8 != 0)) return ADASD_ERR_SHAPE;
+    const int V = ctx->cfg.V;
+    // What is written (first) meets nothing that is read or written.
+    Extent all[16] = {{reinterpret_cast<uintptr_t>(scratch), reinterpret_cast<uintptr_t>(scratch) + (scratch ? scratch_bytes : 0)},
+                      rows_extent(grad_h, gh_stride, n_rows, dim), rows_extent(grad_w, gw_stride, V, dim), array_extent(one_out, 1)};
+    int n = 4;
+    for (float* p : rows_out) all[n++] = array_extent(p, n_rows);
+    const int written = n;
+    all[n++] = rows_extent(hidden, h_stride, n_rows, dim);
+    all[n++] = rows_extent(weight, w_stride, V, dim);
+    all[n++] = array_extent(tokens, n_rows);
+    for (const float* p : rows_in) all[n++] = array_extent(p, n_rows);
+    for (int i = 0; i < written; ++i)
+        for (int k = i + 1; k < n; ++k)
+            if (meet(all[i], all[k])) return ADASD_ERR_SHAPE;
     if (int rc = check_device(ctx)) return rc;
     if (ctx->cfg.dtype != ADASD_BF16 || ctx->cuts_on()) return ADASD_ERR_DTYPE;
-    if (!std::isfinite(kLog2e / ctx->temperature) || ctx->cfg.V > kHeadMaxV) return ADASD_ERR_SHAPE;
-    const int V = ctx->cfg.V;
-    const Extent h = rows_extent(hidden, h_stride, n_rows, dim), w = rows_extent(weight, w_stride, V, dim),
-                 gh = rows_extent(grad_h, gh_stride, n_rows, dim), gw = rows_extent(grad_w, gw_stride, V, dim),
-                 s = {reinterpret_cast<uintptr_t>(scratch), reinterpret_cast<uintptr_t>(scratch) + (scratch ? scratch_bytes : 0)};
-    if (meet(h, gh) || meet(h, gw) || meet(w, gh) || meet(w, gw) || meet(gh, gw) || meet(s, h) || meet(s, w) || meet(s, gh) || meet(s, gw))
-        return ADASD_ERR_SHAPE;
+    if (!std::isfinite(kLog2e / ctx->temperature) || V > kHeadMaxV) return ADASD_ERR_SHAPE;
     if (n_rows > 0 && scratch_bytes < head_scratch_need(n_rows, V, dim, grad_h || grad_w, ctx->sm_count)) return ADASD_ERR_CAPACITY;
     memset(&c, 0, sizeof(c));
     c.op = op;
@@ -1243,7 +1253,7 @@ int adasd_head_logprob(adasd_ctx* ctx, const void* hidden_dev, int64_t hidden_st
     if (!aligned4({logp_out_dev, entropy_out_dev, lse_out_dev})) return ADASD_ERR_ALIGN;
     HeadCall c;
     if (int rc = check_head(ctx, c, HEAD_LOGPROB, hidden_dev, hidden_stride, weight_dev, weight_stride, dim, tokens_dev, n_rows, scratch_dev,
-                            scratch_bytes, nullptr, 0, nullptr, 0))
+                            scratch_bytes, nullptr, 0, nullptr, 0, {}, {logp_out_dev, entropy_out_dev, lse_out_dev}))
         return rc;
     c.logp = logp_out_dev;
     c.H = entropy_out_dev;
@@ -1260,7 +1270,8 @@ int adasd_head_logprob_grad(adasd_ctx* ctx, const void* hidden_dev, int64_t hidd
     if (!aligned4({lse_dev, entropy_dev, grad_logp_dev, grad_entropy_dev})) return ADASD_ERR_ALIGN;
     HeadCall c;
     if (int rc = check_head(ctx, c, HEAD_GIVEN, hidden_dev, hidden_stride, weight_dev, weight_stride, dim, tokens_dev, n_rows, scratch_dev,
-                            scratch_bytes, grad_hidden_dev, grad_hidden_stride, grad_weight_dev, grad_weight_stride))
+                            scratch_bytes, grad_hidden_dev, grad_hidden_stride, grad_weight_dev, grad_weight_stride,
+                            {lse_dev, entropy_dev, grad_logp_dev, grad_entropy_dev}, {}))
         return rc;
     c.lse_in = lse_dev;
     c.H_in = entropy_dev;
@@ -1281,7 +1292,8 @@ int adasd_head_cross_entropy(adasd_ctx* ctx, const void* hidden_dev, int64_t hid
     if (!aligned4({row_weight_dev, row_loss_out_dev, loss_out_dev, logp_out_dev, lse_out_dev})) return ADASD_ERR_ALIGN;
     HeadCall c;
     if (int rc = check_head(ctx, c, HEAD_CE, hidden_dev, hidden_stride, weight_dev, weight_stride, dim, tokens_dev, n_rows, scratch_dev, scratch_bytes,
-                            grad_hidden_dev, grad_hidden_stride, grad_weight_dev, grad_weight_stride))
+                            grad_hidden_dev, grad_hidden_stride, grad_weight_dev, grad_weight_stride, {row_weight_dev},
+                            {row_loss_out_dev, logp_out_dev, lse_out_dev}, loss_out_dev))
         return rc;
     c.row_weight = row_weight_dev;
     c.smoothing = o.label_smoothing;

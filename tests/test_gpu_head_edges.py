@@ -48,3 +48,24 @@ def test_scratch_made_for_more_rows(torch, most, V, D):
         assert all(torch.equal(a, b) for a, b in zip(*got)), n
         Head(h[:n], w, tok[:n]).close_logp(got[0][1])
     assert bool((border == 255).all()) and ctx.status() == 0
+
+
+# ---- overlaps --------------------------------------------------------------------------------------
+
+def test_overlaps_with_the_weight(torch):
+    import paper_2512_11280_b200 as adasd
+    n, V, D = 10, 300, 64
+    h, w, tok, _ = inputs(torch, n, V, D, 3)
+    ctx = context(V)
+    sc, _ = scratch_for(torch, ctx, n, D, True)
+    rl, lp, total = out(torch, n, 2) + out(torch, 1)
+    inside = w.view(-1).view(torch.float32)                  # the weight's memory as fp32
+    for bad in (dict(grad_hidden_out=w[:n]), dict(grad_weight_out=w), dict(logp_out=inside[5:5 + n]), dict(loss_out=inside[-1:]), dict(logp_out=rl),
+                dict(lse_out=sc[:4 * n].view(torch.float32)), dict(row_weight=rl), dict(row_weight=sc[:4 * n].view(torch.float32))):
+        before = w.clone()
+        with pytest.raises(adasd.AdasdError) as err:
+            ctx.head_cross_entropy(h, w, tok, rl, sc, **bad)
+        assert err.value.code == adasd.ERR_SHAPE, bad.keys()
+        assert torch.equal(before, w)
+    ctx.head_cross_entropy(h, w, tok, rl, sc, loss_out=total, logp_out=lp)
+    assert ctx.status() == 0
