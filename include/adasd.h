@@ -438,7 +438,8 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
  *   - Gradients are bf16: grad_hidden_dev as the hidden states, grad_weight_dev as the weight (each nullable, with its stride).  Every element of the
  *     n_rows and of the V rows is written, what lies between rows is left as it was.  A row left out has a gradient of zeros and adds nothing
  *     to the weight's, whatever its hidden states hold (NaN too).  What a call writes (gradients, outputs, scratch)
- *     must overlap neither with what it reads nor with anything else that it writes (ADASD_ERR_SHAPE).
+ *     must overlap neither with what it reads nor with anything else that it writes (ADASD_ERR_SHAPE; columns of one array, with one
+ *     stride, do not overlap).
  *   - A row whose logits are not all finite, or whose largest z / T is 6e29 or more in size, sets ADASD_STATUS_NAN: its outputs, the totals it enters and both its gradient and the
  *     whole of the weight's are NaN.
  *   - scratch_dev: at least the bytes that adasd_head_scratch gives for the call's n_rows and dim, 16-byte aligned, contents of no

@@ -1171,14 +1171,23 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
 
 namespace {
 struct Extent {
-    uintptr_t at, end;
+    uintptr_t at, end, width, pitch;         // rows of so many bytes, so far apart (pitch 0: one stretch)
 };
 Extent rows_extent(const void* p, int64_t stride, int64_t n, int64_t width) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(p);
-    return {a, p && n > 0 ? a + (uintptr_t)(((n - 1) * stride + width) * 2) : a};
+    return {a, p && n > 0 ? a + (uintptr_t)(((n - 1) * stride + width) * 2) : a, (uintptr_t)width * 2, (uintptr_t)stride * 2};
 }
-Extent array_extent(const void* p, int64_t n) { return rows_extent(p, 2, n, 2); }          // of 32-bit values
-bool meet(const Extent& a, const Extent& b) { return a.at < b.end && b.at < a.end && a.at != a.end && b.at != b.end; }
+Extent array_extent(const void* p, int64_t n) {          // of 32-bit values
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    return {a, p ? a + (uintptr_t)n * 4 : a, 0, 0};
+}
+bool meet(const Extent& a, const Extent& b) {
+    if (!(a.at < b.end && b.at < a.end) || a.at == a.end || b.at == b.end) return false;
+    if (a.pitch == 0 || a.pitch != b.pitch) return true;
+    // rows of one between the rows of the other: columns of one array
+    const uintptr_t d = b.at >= a.at ? (b.at - a.at) % a.pitch : (a.pitch - (a.at - b.at) % a.pitch) % a.pitch;
+    return d < a.width || d + b.width > a.pitch;
+}
 }  // namespace
 
 // Checks what the head calls have in common; fills in what they share.
@@ -1196,7 +1205,7 @@ static int check_head(const adasd_ctx* ctx, HeadCall& c, int32_t op, const void*
     if (grad_w && (gw_stride < dim || gw_stride > most || gw_stride % 8 != 0)) return ADASD_ERR_SHAPE;
     const int V = ctx->cfg.V;
     // What is written (first) meets nothing that is read or written.
-    Extent all[16] = {{reinterpret_cast<uintptr_t>(scratch), reinterpret_cast<uintptr_t>(scratch) + (scratch ? scratch_bytes : 0)},
+    Extent all[16] = {{reinterpret_cast<uintptr_t>(scratch), reinterpret_cast<uintptr_t>(scratch) + (scratch ? scratch_bytes : 0), 0, 0},
                       rows_extent(grad_h, gh_stride, n_rows, dim), rows_extent(grad_w, gw_stride, V, dim), array_extent(one_out, 1)};
     int n = 4;
     for (float* p : rows_out) all[n++] = array_extent(p, n_rows);

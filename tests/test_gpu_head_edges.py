@@ -69,3 +69,21 @@ def test_overlaps_with_the_weight(torch):
         assert torch.equal(before, w)
     ctx.head_cross_entropy(h, w, tok, rl, sc, loss_out=total, logp_out=lp)
     assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("n,pad", [(5, 0), (100, 8), (300, 0), (300, 3)])
+def test_gradients_as_columns_beside_what_they_are_of(torch, n, pad):
+    """Hidden states and their gradient, weight and its gradient, side by side in one array each (pad: columns between the first two)."""
+    V, D = 700, 136
+    h, w, tok, _ = inputs(torch, n, V, D, n)
+    ctx = context(V)
+    sc, _ = scratch_for(torch, ctx, n, D, True)
+    rl, rl2 = out(torch, n, 2)
+    gh, gw = torch.empty_like(h), torch.empty_like(w)
+    ctx.head_cross_entropy(h, w, tok, rl, sc, grad_hidden_out=gh, grad_weight_out=gw)
+    hb, wb = torch.full((n, 2 * D + pad), 9.0, device="cuda").bfloat16(), torch.full((V, 2 * D), 9.0, device="cuda").bfloat16()
+    hb[:, :D], wb[:, D:] = h, w
+    ctx.head_cross_entropy(hb[:, :D], wb[:, D:], tok, rl2, sc, grad_hidden_out=hb[:, D + pad:], grad_weight_out=wb[:, :D])
+    assert torch.equal(rl, rl2) and torch.equal(hb[:, D + pad:], gh) and torch.equal(wb[:, :D], gw)
+    assert torch.equal(hb[:, :D], h) and torch.equal(wb[:, D:], w) and bool((hb[:, D:D + pad] == 9.0).all())
+    assert ctx.status() == 0

@@ -53,3 +53,26 @@ def test_what_is_written_overlaps_with_nothing(call, written, read):
 def test_arrays_that_are_read_may_be_the_same():
     rc = grad({**AT, "entropy": AT["lse"], "dH": AT["dl"]})
     assert rc not in (adasd.ERR_SHAPE, 0)
+
+
+# hidden states and their gradient as columns of one array: offset (elements) of the gradient, stride, and whether that overlaps
+@pytest.mark.parametrize("first,stride,overlap", [(D, 2 * D, False), (D + 8, 2 * D + 8, False), (D - 1, 2 * D, True), (D + 1, 2 * D, True), (-D, 2 * D, False),
+                                                  (-D + 1, 2 * D, True), (5 * 2 * D + D, 2 * D, False), (5 * 2 * D, 2 * D, True), (-7 * 2 * D - D, 2 * D, False),
+                                                  (D, 2 * D - 1, True), (0, 2 * D, True), (N * 2 * D, 2 * D, False)])
+def test_columns_of_one_array(first, stride, overlap):
+    for call in ("grad", "entropy"):
+        a = {**AT, "grad_hidden": AT["hidden"] + 2 * first}
+        if call == "grad":
+            rc = adasd.adasd_head_logprob_grad(CTX, a["hidden"], stride, a["weight"], D, D, a["tok"], N, a["lse"], None, a["dl"], None, a["scratch"], 4096,
+                                               a["grad_hidden"], stride, None, 0, None)
+        else:
+            rc = adasd.adasd_head_cross_entropy(CTX, a["hidden"], stride, a["weight"], D, D, a["tok"], N, None, adasd.CrossEntropyOptions(0.0, 0.0, 1.0),
+                                                a["scratch"], 4096, a["row_loss"], None, None, None, a["grad_hidden"], stride, None, 0, None)
+        assert (rc == adasd.ERR_SHAPE) == overlap, (call, rc)
+
+
+def test_rows_with_other_strides_overlap():
+    a = {**AT, "grad_hidden": AT["hidden"] + 2 * D}
+    rc = adasd.adasd_head_logprob_grad(CTX, a["hidden"], 2 * D, a["weight"], D, D, a["tok"], N, a["lse"], None, a["dl"], None, a["scratch"], 4096,
+                                       a["grad_hidden"], 2 * D + 2, None, 0, None)
+    assert rc == adasd.ERR_SHAPE
