@@ -58,13 +58,19 @@ struct HeadStage {
 constexpr uint32_t kHgPause = 1u << 16;                       // polls that a copy under way surely ends within
 constexpr int kHgPlaneRows = 64;                             // rows of a plane of G, where there are two
 
-// Of a row that counts: g_v = p (A + E u) + C, and at the token B more, where u = log2 p.
+// Of a row that counts: g_v = p (A + E u) + C, and at the token B more, where u = log2 p = z log2 e / T - lse2; at the token u is
+// z log2 e / T - top - log2S.  (lse2 in 32 bits is off by 2^-24 of its size, which may be more than 1 - p is; the exponent less the row's largest is not.)
 struct __align__(16) HeadCoef {
     float lse2, A, B, C;
     float E;
     int32_t tok;
-    float pad[2];
+    float top, log2S;
 };
+// (no p is above 1: p - 1 keeps its sign; a NaN stays)
+__device__ __forceinline__ float head_token_exponent(float z, float c1, float top, float log2S) {
+    const float u = fmaf(z, c1, -top) - log2S;
+    return u > 0.f ? 0.f : u;
+}
 
 struct HeadTiles {
     CUtensorMap h, w, g;                 // hidden states, weight, the piece of G
@@ -555,7 +561,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                         const bool any = __any_sync(0xFFFFFFFFu, here);
                         if (any) {
                             // A p + B as A (p - 1) + (A + B): p - 1 without the difference of two numbers near 1
-                            const float u = fmaf(pick(v, x - 32 * g), p.c1, -lse2);
+                            const float u = head_token_exponent(pick(v, x - 32 * g), p.c1, f2.z, f2.w);
                             at = fmaf(A, expm1f(u * kLn2), A + B) + fmaf(ex2(u) * E, u, C);
                         }
                         if (all_in && p.V - p.v0 - c0 - 32 * g >= 32) {
@@ -697,7 +703,8 @@ __device__ __forceinline__ HeadCoef head_given(const HeadCall& c, int r, double 
     f.C = 0.f;
     f.E = (float)(-(double)dH * 0.6931471805599453 * inv_T);
     f.tok = c.tok[r];
-    f.pad[0] = f.pad[1] = 0.f;
+    f.top = f.lse2;
+    f.log2S = 0.f;
     if (!isfinite(lse)) atomicOr(c.status, ADASD_STATUS_NAN);
     return f;
 }
@@ -848,14 +855,15 @@ __device__ __forceinline__ bool head_join(const HeadRows& p, int row, HeadJoined
 __device__ __forceinline__ HeadCoef head_constants(const HeadRows& p, const HeadJoined& j, float weight, int tok) {
     const HeadCall& c = p.c;
     HeadCoef f;
-    f.lse2 = j.bad ? __int_as_float(0x7FC00000) : j.top + log2f(j.S);
+    f.top = j.bad ? __int_as_float(0x7FC00000) : j.top;
+    f.log2S = log2f(j.S);
+    f.lse2 = f.top + f.log2S;
     const double w = (double)weight * (double)c.scale * p.inv_T;
     f.A = (float)(w * (1.0 + 2.0 * (double)(c.z_loss * (f.lse2 * kLn2))));
     f.B = (float)(-w * (1.0 - (double)c.smoothing));
     f.C = (float)(-w * (double)c.smoothing / c.V);
     f.E = 0.f;
     f.tok = tok;
-    f.pad[0] = f.pad[1] = 0.f;
     return f;
 }
 // What a row reports, worked out in 64 bits.
@@ -935,7 +943,7 @@ __global__ void __launch_bounds__(kHsThreads) head_stats_kernel(const __grid_con
             head_left_out(c, row);
             if (p.coef) {
                 HeadCoef f;
-                f.lse2 = f.A = f.B = f.C = f.E = f.pad[0] = f.pad[1] = 0.f;
+                f.lse2 = f.A = f.B = f.C = f.E = f.top = f.log2S = 0.f;
                 f.tok = -1;
                 p.coef[row] = f;
             }
@@ -964,7 +972,7 @@ __global__ void __launch_bounds__(kHsThreads) head_g_kernel(const __grid_constan
         mine = head_join(p, row, joined);
         if (mine) s_f = head_constants(p, joined, weight, tok0);
     } else if (tid == 0) {
-        s_f.lse2 = s_f.A = s_f.B = s_f.C = s_f.E = 0.f;
+        s_f.lse2 = s_f.A = s_f.B = s_f.C = s_f.E = s_f.top = s_f.log2S = 0.f;
         s_f.tok = -1;
         if (first && listed) head_left_out(c, row);
     }
@@ -987,7 +995,7 @@ __global__ void __launch_bounds__(kHsThreads) head_g_kernel(const __grid_constan
             for (int j = 0; j < 8; ++j) {
                 const float u = fmaf(v[j], p.c1, -lse2);
                 float y = fmaf(ex2(u), A, C);
-                if (x == j) y = fmaf(A, expm1f(u * kLn2), A + B) + C;        // (as in a tile)
+                if (x == j) y = fmaf(A, expm1f(head_token_exponent(v[j], p.c1, s_f.top, s_f.log2S) * kLn2), A + B) + C;      // (as in a tile)
                 v[j] = j < nv ? y : 0.f;
             }
             const uint4 w = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));

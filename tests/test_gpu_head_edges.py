@@ -87,3 +87,34 @@ def test_gradients_as_columns_beside_what_they_are_of(torch, n, pad):
     assert torch.equal(rl, rl2) and torch.equal(hb[:, D + pad:], gh) and torch.equal(wb[:, :D], gw)
     assert torch.equal(hb[:, :D], h) and torch.equal(wb[:, D:], w) and bool((hb[:, D:D + pad] == 9.0).all())
     assert ctx.status() == 0
+
+
+# ---- confident rows --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n,offset", [(7, 0), (7, 1), (100, 0), (200, 0)])
+def test_confident_rows_of_large_logits(torch, n, offset):
+    """Logits of 64 to 519 whose token has 1 - p = 7e-5.  h = (a, 1, 0 ..), w = (1, 0 ..) and at the token (1, 11.5, 0 ..): z is exact, grad_h has the sum of the row's
+    G = dL/dz, which is 0, in column 0, and 11.5 (p - 1) in column 1.  S = 1 + 7e-5 comes from 2^t of the token (2^-22 of itself) and 5 additions, 2^-24 each:
+    p - 1 is off by 9 * 2^-24 for all of it, where lse in 32 bits would take 2^-24 of 519 and more.  The other columns' p, 1e-5 each, add nothing to that."""
+    V, D, U = 8, 8, 2.0 ** -24
+    h = torch.zeros(n * D + offset, device="cuda").bfloat16()[offset:].view(n, D)
+    a = (torch.linspace(64.0, 508.0, n, device="cuda") + 0.37).bfloat16()
+    h[:, 0], h[:, 1] = a, 1.0
+    w = torch.zeros(V, D, device="cuda").bfloat16()
+    w[:, 0], w[3, 1] = 1.0, 11.5
+    tok = torch.full((n,), 3, dtype=torch.int32, device="cuda")
+    z = (h.double() @ w.double().t())
+    p1 = torch.expm1(torch.log_softmax(z, -1)[:, 3])         # (z - a is exact: 0 and 11.5)
+    ctx = context(V)
+    sc, _ = scratch_for(torch, ctx, n, D, True)
+    rl, lp, lse = out(torch, n, 3)
+    gh = torch.full((n, D), 9.0, device="cuda").bfloat16()
+    ctx.head_cross_entropy(h, w, tok, rl, sc, grad_hidden_out=gh)
+    assert bool((gh[:, 0].double().abs() <= 10 * U).all()), float(gh[:, 0].double().abs().max() / U)
+    assert bool(((gh[:, 1].double() - 11.5 * p1).abs() <= 11.5 * 10 * U + 2.0 ** -8 * 11.5 * p1.abs()).all())
+    assert bool((gh[:, 1] < 0).all()) and bool((gh[:, 2:] == 0).all())
+    # from an lse in 32 bits p - 1 is off by as much as that is, but p is not above 1
+    ctx.head_logprob(h, w, tok, lp, sc, lse_out=lse)
+    ctx.head_logprob_grad(h, w, tok, lse, torch.ones(n, device="cuda"), sc, grad_hidden_out=gh)
+    assert bool((gh[:, 1] >= 0).all()), float(gh[:, 1].min())
+    assert ctx.status() == 0
