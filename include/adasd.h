@@ -441,7 +441,8 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
  *     must overlap neither with what it reads nor with anything else that it writes (ADASD_ERR_SHAPE; columns of one array, with one
  *     stride, do not overlap).
  *   - A row whose logits are not all finite, or whose largest z / T is 6e29 or more in size, sets ADASD_STATUS_NAN: its outputs, the totals it enters and both its gradient and the
- *     whole of the weight's are NaN.
+ *     whole of the weight's are NaN.  adasd_head_logprob_grad goes by the lse that it is given: one that is not finite does the same; with a finite one a row
+ *     whose dL/dz is not finite (logits or dL/dl that are not) sets the status, its gradient is not finite, and of the weight's the rows of those logits.
  *   - scratch_dev: at least the bytes that adasd_head_scratch gives for the call's n_rows and dim, 16-byte aligned, contents of no
  *     meaning between calls.  Two calls that may overlap (streams, captured graphs) need one each.  What it gives for n_rows serves every call of
  *     fewer rows as well, and what it gives with gradients every call without.  In the main, with rows padded to whole tiles (128, beyond that to 256s): 2 dim

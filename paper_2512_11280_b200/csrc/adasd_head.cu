@@ -245,6 +245,7 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
     t.splits = r.splits;
     t.want_w = c.grad_w != nullptr;
     t.want_h = c.grad_h != nullptr;
+    t.watch = c.op == HEAD_GIVEN;
     t.status = c.status;
     const bool from_logits = as_they_lie && gradient && c.op == HEAD_CE;
     const int rows16 = (c.n_rows + 15) / 16 * 16;

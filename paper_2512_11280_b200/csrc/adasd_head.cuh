@@ -85,6 +85,7 @@ struct HeadTiles {
     int32_t h_boxes, h_box_rows;         // one CTA's tiles of logits: its rows come in so many boxes of so many rows (below the last: whatever is there)
     float4* part;                        // TILE_STATS: [row][halves], a tile's first 128 columns and the others
     float* res;                          // TILE_G: [row][res_halves], 128 columns each: sums of what rounding took from G; nullable
+    int32_t watch;                       // TILE_G: a row whose G is not finite sets the status (with given lse no forward pass of the call has looked at the logits)
     int32_t halves, res_halves, planes;  // planes of G (1 or 2)
     float* z;                            // TILE_STATS: nullable [row][z_stride] the logits
     long long z_stride;
@@ -596,11 +597,17 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                                         z[q][2 * j + 1] = d.y;
                                         lost = __fadd2_rn(lost, d);
                                     }
+                            } else if (p.watch) {                    // (a sum that shows what is not finite, as that of the differences does)
+#pragma unroll
+                                for (int q = g - 1; q <= g; ++q)
+#pragma unroll
+                                    for (int j = 0; j < 16; ++j) lost = __fadd2_rn(lost, pair_of(z[q], j));
                             }
                             if (CG == 1 && p.planes == 2) store64(z[g - 1], v, c0 + 32 * (g - 1), y + kHgPlaneRows, rows_kept);
                         }
                     }
                     if (listed && p.res && c0 < p.vn) p.res[(long long)row * p.res_halves + (p.v0 + c0) / kHgHalf] = lost.x + lost.y;
+                    if (p.watch && in && !(fabsf(lost.x + lost.y) < INFINITY)) atomicOr(p.status, ADASD_STATUS_NAN);
                 }
             } else {
                 const uint32_t acc = next();

@@ -118,3 +118,41 @@ def test_confident_rows_of_large_logits(torch, n, offset):
     ctx.head_logprob_grad(h, w, tok, lse, torch.ones(n, device="cuda"), sc, grad_hidden_out=gh)
     assert bool((gh[:, 1] >= 0).all()), float(gh[:, 1].min())
     assert ctx.status() == 0
+
+
+# ---- logits that are not finite though the given lse is --------------------------------------------
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("n", [6, 60, 100, 200])
+@pytest.mark.parametrize("which", ["hidden", "weight", "both"])
+def test_logits_that_are_not_finite_with_a_finite_lse(torch, n, value, which):
+    """The weight changed between the forward pass and the backward pass: a row of it is not finite now."""
+    import paper_2512_11280_b200 as adasd
+    V, D = 900, 64
+    h, w, tok, _ = inputs(torch, n, V, D, 8)
+    h[:, 5] = 1.0
+    tok[0], tok[4] = 7, -1
+    on = (tok >= 0) & (tok < V)
+    ctx = context(V)
+    sc, _ = scratch_for(torch, ctx, n, D, True)
+    lp, H, lse = out(torch, n, 3)
+    ctx.head_logprob(h, w, tok, lp, sc, H, lse)
+    dl, dH = torch.linspace(0.5, 1.0, n, device="cuda"), torch.linspace(-1.0, -0.5, n, device="cuda")
+    for ent in (None, H):
+        for broken in (False, True):
+            w2 = w.clone()
+            if broken:
+                w2[333, 5] = value
+            gh, gw = torch.full_like(h, 9.0), torch.full_like(w, 9.0)
+            ctx.head_logprob_grad(h, w2, tok, lse, dl, sc, entropy=ent, grad_entropy=None if ent is None else dH,
+                                  grad_hidden_out=None if which == "weight" else gh, grad_weight_out=None if which == "hidden" else gw)
+            assert ctx.status() == (adasd.STATUS_NAN if broken else 0)
+            if which != "weight":
+                assert bool((torch.isfinite(gh[on]).all(-1) != broken).all()) and bool((gh[~on] == 0).all())
+            if which != "hidden":
+                fine = torch.isfinite(gw).all(-1)
+                assert bool(fine[333]) != broken and int(fine.sum()) == (V - 1 if broken else V)
+    # nobody's row: none is looked at
+    w[333, 5] = value
+    ctx.head_logprob_grad(h, w, torch.full_like(tok, -1), lse, dl, sc, grad_hidden_out=gh, grad_weight_out=gw)
+    assert ctx.status() == 0 and bool((gh == 0).all()) and bool((gw == 0).all())
