@@ -43,13 +43,14 @@ int splits_of(int n_rows, int n_pad, int piece, int D, int planes, int m, int sm
     const double units = sm_count * (double)kHgM / m, steps = piece / (double)kHgK, nt = (D + kHgN - 1) / kHgN, tiles = (double)(n_pad / m) * nt;
     const double w = (piece / (double)m) * nt * ((planes == 2 ? 2 : n_pad / kHgK) + 3);
     const double part = (double)std::max(n_rows, 1) * planes * D * 8.0 / 6.5e6 / 0.3;
-    int best = 1;
+    const int fewest = (piece + kHgVocabPart - 1) / kHgVocabPart;
+    int best = fewest;
     double least = 0.0;
     const int most = (int)std::max<size_t>(1, std::min<size_t>(128, ((size_t)64 << 20) / ((size_t)n_pad * D * 4)));      // (64 MB)
-    for (int s = 1; s <= most && steps / s >= 4; ++s) {
+    for (int s = fewest; s <= most && steps / s >= 4; ++s) {
         const double len = std::ceil(steps / s), alone = std::ceil(tiles * s / units) * len;
         const double t = 0.5 * (alone + std::max((tiles * s * len + w) / units, len)) + s * part;
-        if (s == 1 || t < least) {
+        if (s == fewest || t < least) {
             least = t;
             best = s;
         }
@@ -311,7 +312,7 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
         t.w = w_grad;
         t.h = h_grad;
         t.out = gw_out;
-        if (int rc = launch_tiles<TILE_GRADS>(t, pairs, c.sm_count, stream)) return rc;
+        if (int rc = c.n_rows > kHgRowsPart ? launch_tiles<TILE_LONG, 2>(t, c.sm_count, stream) : launch_tiles<TILE_GRADS>(t, pairs, c.sm_count, stream)) return rc;
     }
     if (!c.grad_h) return ADASD_OK;
     const int columns = kHrThreads / head_groups(r.splits * r.planes) * 8;

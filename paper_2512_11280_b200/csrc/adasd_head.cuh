@@ -44,7 +44,12 @@ static_assert(kHgFewRegs * kHgFirst + kHgManyRegs * kHgEpi <= kHgLaunchRegs * (k
 // Steps along K of a part of the logits' sums: 512 products where the products are the bound, 256 where a CTA on its own waits for memory.
 template <int CG>
 constexpr int kHgPart = CG == 1 ? 4 : 8;
-enum HeadTile : int { TILE_STATS, TILE_G, TILE_GRADS };
+// Products of a part of the gradients' sums: of grad_w's, which run along the rows, and of grad_h's, along the vocabulary.  Each product is cut where it is lined up with the
+// accumulator, 25 places below its first, and the sum of 16 once more at 23: where all have one sign that takes 6e-9 of the sum for every product (8e-4 at 2^17, 6.5e-3
+// at 2^20, measured; at most 2^-27 + 2^-29), and much less where signs vary.  A step of bf16 is 2^-8 and more of the value.
+constexpr int kHgRowsPart = 1 << 15, kHgVocabPart = 1 << 16;
+// TILE_LONG: TILE_GRADS for more than kHgRowsPart rows, with sums in such parts
+enum HeadTile : int { TILE_STATS, TILE_G, TILE_GRADS, TILE_LONG };
 // Shared memory: a ring of steps, and where bf16 is written two places for every warp of the epilogue, one being filled while the other is read (with one
 // place 53 us instead of 47.5 for loss and gradients of 7 rows of 32000 at dim 512; no difference where products are the bound).
 template <int TILE, int CG>
@@ -122,7 +127,7 @@ struct HeadWork {
         unit = blockIdx.x / CG;
         units = gridDim.x / CG;
         columns = TILE == TILE_STATS ? p.columns : kHgN;
-        if (TILE != TILE_GRADS) {
+        if (TILE < TILE_GRADS) {
             mt = (n_active + kM - 1) / kM;
             nt = (p.vn + columns - 1) / columns;
             ksteps = (p.D + kHgK - 1) / kHgK;
@@ -153,7 +158,7 @@ struct HeadWork {
         t.k0 = 0;
         t.k1 = ksteps;
         t.gh = false;
-        if (TILE != TILE_GRADS) {                                   // (the rows of one part of w one after the other)
+        if (TILE < TILE_GRADS) {                                    // (the rows of one part of w one after the other)
             i = unit + i * units;
             t.m0 = i % mt * kM;
             t.n0 = i / mt * columns;
@@ -281,7 +286,8 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_gave_up;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr bool kParts = TILE != TILE_GRADS;              // sums in parts
+    constexpr bool kParts = TILE < TILE_GRADS, kLong = TILE == TILE_LONG;   // logits, whose sums come in parts; gradients in parts
+    constexpr int kPart = kParts ? kHgPart<CG> : kHgRowsPart / kHgK;
 
     if (threadIdx.x == 0) {
         s_gave_up = 0u;
@@ -300,8 +306,8 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
     if (threadIdx.x == 32 * kHgFirst) {                      // (the maps are arguments: nobody writes them)
         tma_prefetch(&p.w);
         tma_prefetch(&p.h);
-        if (TILE == TILE_GRADS) tma_prefetch(&p.g);
-        if (TILE == TILE_G || (TILE == TILE_GRADS && p.want_w)) tma_prefetch(&p.out);
+        if (!kParts) tma_prefetch(&p.g);
+        if (TILE == TILE_G || (!kParts && p.want_w)) tma_prefetch(&p.out);
     }
     if (warp == 1) tensor_alloc<CG>(smem_u32(&s_tmem), 512);
     tensor_fence_before();
@@ -320,7 +326,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
     const HeadWork<TILE, CG> w(p, n_active);
 
     if (warp < kHgFirst) {
-        if constexpr (kParts) registers_give<kHgFewRegs>();
+        if constexpr (kParts || kLong) registers_give<kHgFewRegs>();
     if (warp == 0) {
         if (lane == 0) {
             uint32_t step = 0;
@@ -401,7 +407,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                 const uint32_t kind = product_kind(kHgM * CG, TILE == TILE_STATS && CG == 1 ? w.columns : kHgN, a_mn, !kParts);
                 int k = t.k0;
                 do {                                         // (a part, or the whole of the tile's sum)
-                    const int end = kParts ? min(k + kHgPart<CG>, t.k1) : t.k1;
+                    const int end = kParts || kLong ? min(k + kPart, t.k1) : t.k1;
                     const uint32_t buf = n & 1u;
                     ok = wait_or_give_up(acc_empty + 8 * buf, ((n >> 1) & 1u) ^ 1u, &s_gave_up);
                     tensor_fence_after();
@@ -432,7 +438,7 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
         }
     }
     } else {
-        if constexpr (kParts) registers_take<kHgManyRegs>();
+        if constexpr (kParts || kLong) registers_take<kHgManyRegs>();
         const int quarter = warp & 3, half = (warp - kHgFirst) >> 2;
         uint32_t stage = out_stage + (warp - kHgFirst) * 2 * kHgOut, other = stage + kHgOut;
         uint32_t n = 0;
@@ -470,29 +476,20 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                 stage = other;
                 other = s;
             };
-            if constexpr (kParts) {
-                bool in = row < n_active;
-                int tok = -1;                                // (asked for ahead of the sums)
-                float4 f = make_float4(0.f, 0.f, 0.f, 0.f), f2 = f;          // HeadCoef
-                if (TILE == TILE_STATS) {
-                    if (in) tok = __ldcg(p.tok + row);
-                } else if (in) {
-                    f = __ldcg(reinterpret_cast<const float4*>(p.coef + row));
-                    f2 = __ldcg(reinterpret_cast<const float4*>(p.coef + row) + 1);
-                }
-                float z[4][32];                              // the logits of 128 columns
+            // 128 columns of a tile's sum: its parts added up
+            auto sum_parts = [&](float(&z)[4][32], int k0, int k1) {
                 {
                     const uint32_t acc = next();
-                    if (!ok) break;
+                    if (!ok) return;
 #pragma unroll
                     for (int g = 0; g < 4; ++g) tensor_load(acc + 32 * g, z[g]);
 #pragma unroll
                     for (int g = 0; g < 4; ++g) tensor_wait(z[g]);
                     release();
                 }
-                for (int k = k0 + kHgPart<CG>; k < k1; k += kHgPart<CG>) {
+                for (int k = k0 + kPart; k < k1; k += kPart) {
                     const uint32_t acc = next();
-                    if (!ok) break;
+                    if (!ok) return;
 #pragma unroll
                     for (int g = 0; g < 4; g += 2) {
                         float va[32], vb[32];
@@ -511,6 +508,19 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                         }
                     }
                 }
+            };
+            if constexpr (kParts) {
+                bool in = row < n_active;
+                int tok = -1;                                // (asked for ahead of the sums)
+                float4 f = make_float4(0.f, 0.f, 0.f, 0.f), f2 = f;          // HeadCoef
+                if (TILE == TILE_STATS) {
+                    if (in) tok = __ldcg(p.tok + row);
+                } else if (in) {
+                    f = __ldcg(reinterpret_cast<const float4*>(p.coef + row));
+                    f2 = __ldcg(reinterpret_cast<const float4*>(p.coef + row) + 1);
+                }
+                float z[4][32];                              // the logits of 128 columns
+                sum_parts(z, k0, k1);
                 if (!ok) break;
                 if constexpr (TILE == TILE_STATS) {
                     if (m0 + quarter * 32 >= n_active) continue;
@@ -610,17 +620,8 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                     if (p.watch && in && !(fabsf(lost.x + lost.y) < INFINITY)) atomicOr(p.status, ADASD_STATUS_NAN);
                 }
             } else {
-                const uint32_t acc = next();
-                if (!ok) break;
                 const bool none = k1 <= k0;                  // no product was formed: the sum is 0
-                float va[32], vb[32];
-#pragma unroll 1
-                for (int g = 0; g < 4; g += 2) {
-                    tensor_load(acc + 32 * g, va);
-                    tensor_load(acc + 32 * g + 32, vb);
-                    tensor_wait(va);
-                    tensor_wait(vb);
-                    if (g == 2) release();
+                auto emit = [&](int g, float(&va)[32], float(&vb)[32]) {
                     if (none) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) va[j] = vb[j] = 0.f;
@@ -641,6 +642,26 @@ __global__ void __launch_bounds__(kHgThreads, 1) head_tile_kernel(const __grid_c
                             }
                             d4[j] = s;
                         }
+                    }
+                };
+                if constexpr (kLong) {
+                    float z[4][32];
+                    sum_parts(z, k0, k1);
+                    if (!ok) break;
+                    emit(0, z[0], z[1]);
+                    emit(2, z[2], z[3]);
+                } else {
+                    const uint32_t acc = next();
+                    if (!ok) break;
+                    float va[32], vb[32];
+#pragma unroll 1
+                    for (int g = 0; g < 4; g += 2) {
+                        tensor_load(acc + 32 * g, va);
+                        tensor_load(acc + 32 * g + 32, vb);
+                        tensor_wait(va);
+                        tensor_wait(vb);
+                        if (g == 2) release();
+                        emit(g, va, vb);
                     }
                 }
             }

@@ -156,3 +156,54 @@ def test_logits_that_are_not_finite_with_a_finite_lse(torch, n, value, which):
     w[333, 5] = value
     ctx.head_logprob_grad(h, w, torch.full_like(tok, -1), lse, dl, sc, grad_hidden_out=gh, grad_weight_out=gw)
     assert ctx.status() == 0 and bool((gh == 0).all()) and bool((gw == 0).all())
+
+
+# ---- long sums -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n,masked", [(32768, 0.0), (32769, 0.0), (32833, 0.0), (65537, 0.0), (100001, 0.3), (140001, 0.9)])
+def test_rows_about_the_parts_of_the_weight_gradients_sums(torch, n, masked):
+    V, D = 300, 72
+    h, w, tok, g = inputs(torch, n, V, D, n, out=masked)
+    ctx, ref = context(V), Head(h, w, tok)
+    sc, border = scratch_for(torch, ctx, n, D, True)
+    rl, total = out(torch, n) + out(torch, 1)
+    gh, gw = torch.full_like(h, 9.0), torch.full_like(w, 9.0)
+    ctx.head_cross_entropy(h, w, tok, rl, sc, scale=1.0 / n, loss_out=total, grad_hidden_out=gh, grad_weight_out=gw)
+    loss, tol, G, size = ref.cross_entropy(None, 0.0, 0.0, 1.0 / n)
+    assert bool(((rl.double() - loss).abs() <= tol).all())
+    assert abs(float(total) - float(loss.sum())) <= float(tol.sum()) + 2.0 ** -24 * abs(float(loss.sum()))
+    ref.close_grads(G, size, gh, gw)
+    assert bool((border == 255).all()) and ctx.status() == 0
+
+
+def test_sums_over_many_rows_are_not_cut(torch):
+    """grad_w of 2^20 rows, every product of a sum of one sign.  A product is cut where it is lined up with the accumulator, 25 places below its first: half of 2^-25 of the
+    sum so far, in the mean half of the whole; the sum of 16 products is cut again at 2^-23.  2^-27 + 2^-25 / 16 for every product, at the most, are 3.1e-4 of a part of 2^15
+    products (and 1e-2 of all in one sum).  Roundings to bf16, 2^-9 / sqrt(3) in the mean square and independent (the columns have scales of their own), leave 3e-5
+    of the mean over 1500 elements."""
+    n, V, D = (1 << 20) + 3, 24, 64
+    g = torch.Generator(device="cuda").manual_seed(1)
+    h = (torch.randn(n, D, generator=g, device="cuda").abs() * torch.exp2(torch.rand(D, generator=g, device="cuda"))).bfloat16()
+    w = (torch.randn(V, D, generator=g, device="cuda") / D).bfloat16()
+    tok = torch.zeros(n, dtype=torch.int32, device="cuda")
+    ctx = context(V)
+    sc, _ = scratch_for(torch, ctx, n, D, True)
+    rl, = out(torch, n)
+    gw = torch.full_like(w, 9.0)
+    ctx.head_cross_entropy(h, w, tok, rl, sc, scale=1.0 / n, grad_weight_out=gw)
+    want = torch.zeros(V, D, dtype=torch.float64, device="cuda")
+    for a in range(0, n, 1 << 18):
+        x = h[a:a + (1 << 18)].double()
+        G = torch.softmax(x @ w.double().t(), -1) / n
+        G[:, 0] -= 1.0 / n
+        assert bool((G[:, 0] < 0).all())
+        want += G.t() @ x
+    off = gw.double() / want - 1.0
+    assert abs(float(off.mean())) <= 3.5e-4, float(off.mean())
+    assert bool((off.abs() <= 2.0 ** -8 + 1e-3).all()) and ctx.status() == 0
+
+
+def test_sums_over_a_long_vocabulary_have_parts(torch):
+    """A scratch has room for grad_hidden's sums in parts of at most 2^16 of the vocabulary: here eight, beside the piece of dL/dz."""
+    n, V, D = 129, 1 << 19, 16384
+    assert context(V).head_scratch(n, D, True) >= 256 * V * 2 + 8 * 256 * D * 4
