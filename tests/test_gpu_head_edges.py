@@ -207,3 +207,41 @@ def test_sums_over_a_long_vocabulary_have_parts(torch):
     """A scratch has room for grad_hidden's sums in parts of at most 2^16 of the vocabulary: here eight, beside the piece of dL/dz."""
     n, V, D = 129, 1 << 19, 16384
     assert context(V).head_scratch(n, D, True) >= 256 * V * 2 + 8 * 256 * D * 4
+
+
+# ---- what rounding takes from dL/dz ----------------------------------------------------------------
+
+@pytest.mark.parametrize("n,V,D", [(40, 3000, 64), (70, 3000, 64), (128, 2000, 256), (129, 5000, 136), (300, 5000, 136), (20000, 20011, 72)])
+@pytest.mark.parametrize("given", [False, True])
+def test_weights_with_a_common_direction(torch, n, V, D, given):
+    """w_v = noise - 30 u: what rounding takes from a row's G, summed, would be multiplied with 30 u, which the exact gradient has none of (a row's G adds up to 0).
+    Left in, grad_h is 0.03 off; given back along another row than the token's, 0.0022.  Expected is the final rounding to bf16, 0.43 * 2^-8 in the mean square, and
+    independent of that what is left of G's, the errors times w_v - w_x, worked out in 64 bits (up to 64 rows G has a second plane: nothing); a tenth more for chance."""
+    g = torch.Generator(device="cuda").manual_seed(n + V)
+    u = torch.randn(D, generator=g, device="cuda")
+    u /= u.norm()
+    w = (torch.randn(V, D, generator=g, device="cuda") / D ** 0.5 - 30.0 * u).bfloat16()
+    h = torch.randn(n, D, generator=g, device="cuda")
+    h = ((h - (h @ u)[:, None] * u) * 2.0 + u).bfloat16()
+    rows = min(n, 300)                       # those that are looked at
+    z = h[:rows].double() @ w.double().t()
+    tok = torch.randint(0, V, (n,), generator=g, device="cuda").int()
+    tok[:rows] = torch.multinomial(torch.softmax(z, -1), 1, generator=g)[:, 0].int()
+    ctx = context(V)
+    sc, _ = scratch_for(torch, ctx, n, D, True)
+    rl, lse = out(torch, n, 2)
+    gh = torch.full_like(h, 9.0)
+    if given:
+        ctx.head_logprob(h, w, tok, rl, sc, lse_out=lse)
+        ctx.head_logprob_grad(h, w, tok, lse, torch.full_like(lse, -1.0), sc, grad_hidden_out=gh)
+    else:
+        ctx.head_cross_entropy(h, w, tok, rl, sc, grad_hidden_out=gh)
+    G = torch.softmax(z, -1).scatter_add_(1, tok[:rows].long()[:, None], torch.full((rows, 1), -1.0, dtype=torch.float64, device="cuda"))
+    want = G @ w.double()
+    e = G.float().bfloat16().double() - G
+    left = e @ w.double() - e.sum(-1, keepdim=True) * w[tok[:rows].long()].double()
+    expected = ((0.43 * 2.0 ** -8) ** 2 + (0.0 if n <= 64 else float((left.norm() / want.norm()) ** 2))) ** 0.5
+    assert expected < 0.002
+    off = float((gh[:rows].double() - want).norm() / want.norm())
+    assert off <= 1.1 * expected, (off, expected)
+    assert ctx.status() == 0
