@@ -245,3 +245,51 @@ def test_weights_with_a_common_direction(torch, n, V, D, given):
     off = float((gh[:rows].double() - want).norm() / want.norm())
     assert off <= 1.1 * expected, (off, expected)
     assert ctx.status() == 0
+
+
+# ---- calls that reach branches of their own --------------------------------------------------------
+
+@pytest.mark.parametrize("n", [16384, 16385, 30000])
+@pytest.mark.parametrize("grad", [False, True])
+def test_total_of_many_rows(torch, n, grad):
+    """Up to 16384 rows the last row's CTA adds the losses up, beyond that a launch of its own."""
+    V, D = 130, 64
+    h, w, tok, g = inputs(torch, n, V, D, n, out=0.2)
+    weight = torch.rand(n, generator=g, device="cuda")
+    ctx, ref = context(V), Head(h, w, tok, 1.0, weight)
+    sc, border = scratch_for(torch, ctx, n, D, grad)
+    rl, total = out(torch, n) + out(torch, 1)
+    more = dict(grad_hidden_out=torch.empty_like(h), grad_weight_out=torch.empty_like(w)) if grad else {}
+    for _ in range(2):
+        ctx.head_cross_entropy(h, w, tok, rl, sc, row_weight=weight, z_loss=1e-3, scale=1.0 / n, loss_out=total, **more)
+        loss, tol, G, size = ref.cross_entropy(weight, 0.0, 1e-3, 1.0 / n)
+        assert bool(((rl.double() - loss).abs() <= tol).all())
+        # (added in 64 bits, rounded once)
+        assert abs(float(total) - float(rl.double().sum())) <= 2.0 ** -24 * float(rl.double().sum().abs())
+    if grad:
+        ref.close_grads(G, size, more["grad_hidden_out"], more["grad_weight_out"])
+    assert bool((border == 255).all()) and ctx.status() == 0
+
+
+@pytest.mark.parametrize("n", [2, 33, 64, 65, 100, 128])
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("which", ["hidden", "weight", "both"])
+def test_entropy_gradients_of_few_rows(torch, n, offset, which):
+    """Rows as they lie (offset 0) and put together first; dL/dH alone for one of them."""
+    V, D = 1100, 136
+    hv, w, tok, g = inputs(torch, n, V, D, n, out=0.2)
+    h = torch.empty(n * D + offset, dtype=torch.bfloat16, device="cuda")[offset:].view(n, D)
+    h.copy_(hv)
+    ctx, ref = context(V, 0.9), Head(h, w, tok, 0.9)
+    sc, border = scratch_for(torch, ctx, n, D, True)
+    lp, H, lse = out(torch, n, 3)
+    ctx.head_logprob(h, w, tok, lp, sc, H, lse)
+    ref.close_H(H)
+    dl, dH = torch.randn(n, generator=g, device="cuda"), torch.randn(n, generator=g, device="cuda")
+    dl[0] = 0.0
+    gh, gw = torch.full_like(h, 9.0), torch.full_like(w, 9.0)
+    ctx.head_logprob_grad(h, w, tok, lse, dl, sc, entropy=H, grad_entropy=dH, grad_hidden_out=None if which == "weight" else gh,
+                          grad_weight_out=None if which == "hidden" else gw)
+    G, size = ref.given(dl, dH)
+    ref.close_grads(G, size, None if which == "weight" else gh, None if which == "hidden" else gw)
+    assert bool((border == 255).all()) and ctx.status() == 0
