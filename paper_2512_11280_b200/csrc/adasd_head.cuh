@@ -12,7 +12,9 @@
 // Precision.  The accumulator in tensor memory is cut, not rounded, with every 16 products: after 4096 of them logits were 9e-6 of their size too small.
 // Logits are therefore summed from parts of 512 products (256 where the products are not the bound), the parts added in fp32 by the threads of the
 // epilogue; parts of 384 took up to 7 % longer, none at all 4 % less.  What a part loses of its size was measured: 1.2e-8 for every 16 products where
-// signs are random (3.9e-7 at 512; 8.8e-7 where all products are positive), with 2.4e-7 about it; the first is put back with log2 e / T.
+// signs are random (3.9e-7 at 512), with 2.4e-7 about it; the first is put back with log2 e / T.  What is left hangs on how a sum grows: sums of one sign stay 5e-7 too small, such as
+// a few large channels hold lie between 6.3e-7 too small (these come first) and 4e-7 too large (nothing comes after them).  It is a common factor of
+// a row's logits nearly, so that l and H hardly feel it; lse does.
 // G is rounded to bf16, as the products' operands are (2^-8 at most; both gradients are rounded to bf16 once more when they are written).  In grad_h = sum_v g_v w_v
 // the rounding errors e_v do not cancel as the g_v do, which add up to 0 in a row, and what the w_v have in common (a mean, the tokens' frequencies) is
 // multiplied with their sum; so the row's sum of e_v times w_x is taken off again (what is left are errors times differences of w_v): 0.009 -> 0.002 of

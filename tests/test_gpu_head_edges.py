@@ -293,3 +293,34 @@ def test_entropy_gradients_of_few_rows(torch, n, offset, which):
     G, size = ref.given(dl, dH)
     ref.close_grads(G, size, None if which == "weight" else gh, None if which == "hidden" else gw)
     assert bool((border == 255).all()) and ctx.status() == 0
+
+
+@pytest.mark.parametrize("n,D", [(128, 512), (128, 4096), (4096, 512), (4096, 4096)])
+@pytest.mark.parametrize("kind", ["positive", "few large", "few alone", "log-normal", "large first", "large last"])
+def test_logits_of_channels_of_very_different_size(torch, n, D, kind):
+    """With a vocabulary of one token lse is the logit.  What the accumulator cuts off hangs on how a sum grows, what is put back is the mean for independent products, 3.9e-7 of
+    the logit at the most (and 2^-24 of the constant's own rounding): where few products make the sum, nothing or 31 times (a part's steps after the first) half of 2^-23 of it is cut, 1.85e-6.  Regression of the errors
+    on the logits; the largest, where the large products come first, was -6.3e-7."""
+    g = torch.Generator(device="cuda").manual_seed(n + D)
+    h, w = torch.randn(n, D, generator=g, device="cuda"), torch.randn(1, D, generator=g, device="cuda")
+    few = torch.randperm(D, generator=g, device="cuda")[:4]
+    scale = torch.ones(D, device="cuda")
+    if kind == "positive":
+        h, w = h.abs(), w.abs()
+    elif kind == "few large":
+        scale[few] = 300.0
+    elif kind == "few alone":
+        scale.zero_()[few] = 300.0
+    elif kind == "log-normal":
+        scale = torch.exp(2 * torch.randn(D, generator=g, device="cuda"))
+    else:
+        scale[slice(0, 4) if kind == "large first" else slice(-4, None)] = 3000.0
+    h, w = (h * scale).bfloat16(), w.bfloat16()
+    ctx = context(1)
+    sc, _ = scratch_for(torch, ctx, n, D, False)
+    lp, lse = out(torch, n, 2)
+    ctx.head_logprob(h, w, torch.zeros(n, dtype=torch.int32, device="cuda"), lp, sc, lse_out=lse)
+    z, size = (h.double() @ w.double().t())[:, 0], (h.double().abs() @ w.double().abs().t())[:, 0]
+    off = lse.double() - z
+    assert -1.85e-6 <= float((off * z).sum() / (z * z).sum()) <= 3.9e-7 + 2.0 ** -24
+    assert bool((off.abs() <= (D / 16 + 2) * 2.0 ** -23 * size).all()) and ctx.status() == 0
