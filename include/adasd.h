@@ -447,7 +447,7 @@ int adasd_preference_loss(adasd_ctx* ctx, const void* logits_dev, int64_t row_st
  *     meaning between calls.  Two calls that may overlap (streams, captured graphs) need one each.  What it gives for n_rows serves every call of
  *     fewer rows as well, and what it gives with gradients every call without.  In the main, with rows padded to whole tiles (128, beyond that to 256s): 2 dim
  *     bytes a row, and the larger of 16 bytes a row for every 128 of V and, with gradients, a piece of dL/dz (2 bytes an element; 256 MB at the most, or 2048
- *     columns); with gradients the sums of grad_hidden in 32 bits, 4 dim bytes a row or, in parts, up to 64 MB.  Calls of up to 128 rows with gradients hold
+ *     columns); with gradients the sums of grad_hidden in 32 bits, 4 dim bytes a row for every 2^16 of V or, in more parts, up to 64 MB.  Calls of up to 128 rows with gradients hold
  *     their logits besides (4 bytes an element).
  *   - Sums and statistics are held in 32 bits or more.  z is off by the rounding of an fp32 sum of dim exact products; ln S as above.  A
  *     gradient's p_v comes with (4 |ln p_v| + 2 |lse| + 16) 2^-24 of itself and that (the token's p - 1 in adasd_head_cross_entropy with 16 2^-24
@@ -544,7 +544,8 @@ typedef struct {
 
 /*
  * tensors: host array of n_tensors, read before the call returns.  Arrays are device arrays, aligned to their element type; no two may
- * overlap.  (Arrays that start at multiples of 16 bytes, codes at 8, are faster.)  Only the context's device and status word are
+ * overlap.  (Where one array of a tensor does not start at a multiple of 16 bytes, codes at 8, the tensor takes up to half as long again with states in 8 bits, up to
+ * a sixth with states in 32.)  Only the context's device and status word are
  * used: V and the context's dtype do not matter.  Where grad_scale_dev is given and the product is not finite (a norm that
  * overflowed), nothing is changed and ADASD_STATUS_NAN is set.  A gradient that is not finite makes its parameter and
  * states NaN or infinite as the formulas do, in 8 bits the states of its whole block.

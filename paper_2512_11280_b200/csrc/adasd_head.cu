@@ -312,6 +312,7 @@ int launch_head(const HeadCall& c, cudaStream_t stream) {
         t.w = w_grad;
         t.h = h_grad;
         t.out = gw_out;
+        // (in parts 350 us instead of 341 for 1000 rows of 50257 at dim 1000; no difference from 2048 rows on)
         if (int rc = c.n_rows > kHgRowsPart ? launch_tiles<TILE_LONG, 2>(t, c.sm_count, stream) : launch_tiles<TILE_GRADS>(t, pairs, c.sm_count, stream)) return rc;
     }
     if (!c.grad_h) return ADASD_OK;
