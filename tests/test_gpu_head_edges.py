@@ -324,3 +324,44 @@ def test_logits_of_channels_of_very_different_size(torch, n, D, kind):
     off = lse.double() - z
     assert -1.85e-6 <= float((off * z).sum() / (z * z).sum()) <= 3.9e-7 + 2.0 ** -24
     assert bool((off.abs() <= (D / 16 + 2) * 2.0 ** -23 * size).all()) and ctx.status() == 0
+
+
+# ---- several at once -------------------------------------------------------------------------------
+
+def test_many_rows_captured_beside_few_on_another_stream(torch):
+    """One graph of a call whose sums come in parts, replayed with other masks, while calls of few rows run on a stream of their own: the results are those of each alone."""
+    n, V, D = 40000, 300, 64
+    ctx = context(V)
+    h, w, tok, g = inputs(torch, n, V, D, 31, out=0.1)
+    few = inputs(torch, 60, V, D, 32)
+    big, small = scratch_for(torch, ctx, n, D, True)[0], scratch_for(torch, ctx, 60, D, True)[0]
+    rl, total, gh, gw = out(torch, n) + out(torch, 1) + [torch.empty_like(h), torch.empty_like(w)]
+    rl2, gh2, gw2 = out(torch, 60) + [torch.empty_like(few[0]), torch.empty_like(w)]
+
+    def many():
+        ctx.head_cross_entropy(h, w, tok, rl, big, loss_out=total, grad_hidden_out=gh, grad_weight_out=gw)
+
+    def short():
+        ctx.head_cross_entropy(few[0], few[1], few[2], rl2, small, grad_hidden_out=gh2, grad_weight_out=gw2)
+    short()
+    want2 = [t.clone() for t in (rl2, gh2, gw2)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        many()
+    side = torch.cuda.Stream()
+    for share in (0.1, 1.0, 0.5, 0.0):
+        tok.copy_(inputs(torch, n, V, D, 40 + int(10 * share), out=share)[2])
+        many()
+        want = [t.clone() for t in (rl, total, gh, gw)]
+        Head(h[:4000], w, tok[:4000]).close_logp(-rl[:4000])
+        for t in (rl, total, gh, gw, rl2, gh2, gw2):
+            t.fill_(9.0)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            short()
+        graph.replay()
+        with torch.cuda.stream(side):
+            short()
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(a, b) for a, b in zip(want + want2, (rl, total, gh, gw, rl2, gh2, gw2))), share
+    assert ctx.status() == 0
