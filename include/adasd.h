@@ -529,7 +529,7 @@ typedef struct {
 } adasd_adamw_tensor;
 
 typedef struct {
-    double lr, beta1, beta2; /* betas in [0, 1) */
+    double lr, beta1, beta2; /* betas in [0, 1); lr, eps and grad_scale: finite in 32 bits (ADASD_ERR_SHAPE) */
     double eps;              /* >= 1e-16 */
     double grad_scale;       /* factor of every gradient: 1 / accumulation steps, a clipping factor */
     int32_t step;            /* t, >= 1 */

@@ -1321,8 +1321,9 @@ int adasd_head_cross_entropy(adasd_ctx* ctx, const void* hidden_dev, int64_t hid
 int adasd_adamw_step(adasd_ctx* ctx, const adasd_adamw_tensor* tensors, int32_t n_tensors, const adasd_adamw_options* options, void* stream) {
     if (!ctx || !options || (n_tensors > 0 && !tensors)) return ADASD_ERR_NULL;
     const adasd_adamw_options& o = *options;
-    if (n_tensors < 0 || !std::isfinite(o.lr) || !(o.beta1 >= 0.0) || !(o.beta1 < 1.0) || !(o.beta2 >= 0.0) || !(o.beta2 < 1.0) || !(o.eps >= 1e-16) ||
-        !std::isfinite(o.eps) || !std::isfinite(o.grad_scale) || (o.step < 1 && !o.step_dev))
+    // (the step works in 32 bits: what is not finite there is none either)
+    if (n_tensors < 0 || !std::isfinite((float)o.lr) || !(o.beta1 >= 0.0) || !(o.beta1 < 1.0) || !(o.beta2 >= 0.0) || !(o.beta2 < 1.0) || !(o.eps >= 1e-16) ||
+        !std::isfinite((float)o.eps) || !std::isfinite((float)o.grad_scale) || (o.step < 1 && !o.step_dev))
         return ADASD_ERR_SHAPE;
     if (o.stochastic != 0 && o.stochastic != 1) return ADASD_ERR_DTYPE;
     if (!aligned4({o.lr_dev, o.grad_scale_dev, o.step_dev})) return ADASD_ERR_ALIGN;
